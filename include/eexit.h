@@ -448,6 +448,40 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
                      void* stream);
 
 /*
+ * Cross-entropy of a head over the whole vocabulary and its gradient: the supervised objective L_CE of section 3.3
+ * ("Losses") as a training step of a head needs it.  The M x V logits are never stored: the gradient recomputes them
+ * in pieces of the vocabulary.  With y = bf16(LayerNorm(h)) and z = y W^T as in ee_exit_head:
+ *   lse   fp32 [M]: ln sum_v exp(z[i, v])
+ *   ce    fp32 [M]: lse[i] - z[i, labels[i]]; 0 for a row that is not counted
+ *   loss  fp32 [2]: the mean of ce over the counted rows (0 if there is none), and their number
+ * labels int32 [M]; a row whose label is outside [0, V) is not counted: it adds nothing to the loss or to any
+ * gradient, whatever its hidden state holds (its lse is computed all the same).
+ *
+ * ee_head_ce_grad: gradients of sum_i w_i ce_i, for the same inputs and with lse and loss as ee_head_ce wrote them:
+ *   dce    fp32 [M]: the weights w_i, or NULL: w_i = dloss[0] / loss[1], the gradient of the mean
+ *   dloss  fp32 [1] on the device: incoming gradient of the mean, NULL = 1; must be NULL when dce is given
+ *   dh     bf16 [M, d], row stride ld_dh (ld_dh >= d, ld_dh % 8 == 0), or NULL; rows not counted get zeros
+ *   dW     bf16 [V, d] contiguous, or NULL;   dgamma, dbeta  bf16 [d], both or neither NULL
+ *   accumulate != 0: dW, dgamma and dbeta are added to what the buffers hold (dh is always overwritten)
+ * The rounding of y to bf16 is passed through by the gradient.  All gradients are bf16: the products behind dy and dW
+ * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that.
+ * Sizes, strides and alignment as in ee_exit_head; all gradient buffers 16-byte aligned.  Workspace:
+ * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
+ * initialised once with ee_workspace_init; both 0 if a size is invalid.  W is written by nobody while a call is in
+ * flight (see "Constants of the stream" above: a step that updates W must have completed before the next call is
+ * issued).  M = 0: ee_head_ce writes loss = {0, 0}; ee_head_ce_grad writes zeros (nothing when accumulating).
+ */
+size_t    ee_head_ce_workspace_bytes(int M, int d, int V);
+ee_status ee_head_ce(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W, int M,
+                     int d, int V, const int* labels, float* ce, float* lse, float* loss, void* workspace,
+                     size_t workspace_bytes, void* stream);
+size_t    ee_head_ce_grad_workspace_bytes(int M, int d, int V);
+ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W,
+                          int M, int d, int V, const int* labels, const float* lse, const float* loss, const float* dce,
+                          const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta,
+                          int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Calibration of one head's threshold from a calibration set (section 3.4.1, "Calibration of Confidence
  * Thresholds": Eq. 3 and the two equations that define the index j-hat and tau_k = c_{k, j-hat}), with the
  * entropy as the confidence metric.  Over n calibration tokens:

@@ -479,6 +479,132 @@ def prepare_head_kl(head, teacher, ln_eps, *, labels=None, out=None, workspace=N
     return PreparedCall(_lib.load().ee_head_kl, args, "ee_head_kl", keep, out)
 
 
+def _workspace_of(nbytes: int, where: str, device) -> torch.Tensor:
+    if nbytes == 0:
+        raise EExitError(2, where)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    ee_workspace_init(ws)
+    return ws
+
+
+def _on_current(t: torch.Tensor, name: str) -> torch.Tensor:
+    """The library launches on the current device: a tensor of another one is refused."""
+    _dev(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _buffer(t, name, dtype, shape, device):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype == dtype and t.is_contiguous() and
+            tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t
+
+
+def _scratch(workspace, device):
+    if not (isinstance(workspace, torch.Tensor) and workspace.device == device and workspace.dtype == torch.uint8 and
+            workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+    return workspace
+
+
+def ee_head_ce_workspace_bytes(M: int, d: int, V: int) -> int:
+    return int(_lib.load().ee_head_ce_workspace_bytes(int(M), int(d), int(V)))
+
+
+def ee_head_ce_grad_workspace_bytes(M: int, d: int, V: int) -> int:
+    return int(_lib.load().ee_head_ce_grad_workspace_bytes(int(M), int(d), int(V)))
+
+
+def new_head_ce_workspace(M: int, d: int, V: int, device="cuda") -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace for ee_head_ce at these sizes."""
+    return _workspace_of(ee_head_ce_workspace_bytes(M, d, V), "ee_head_ce_workspace_bytes", device)
+
+
+def new_head_ce_grad_workspace(M: int, d: int, V: int, device="cuda") -> torch.Tensor:
+    """The same for ee_head_ce_grad; it serves ee_head_ce as well."""
+    return _workspace_of(ee_head_ce_grad_workspace_bytes(M, d, V), "ee_head_ce_grad_workspace_bytes", device)
+
+
+def _head_ce_inputs(head, labels):
+    h, W, (M, d, V) = _check_head_tensors(head["h"], head["gamma"], head["beta"], head["W"], None)
+    _on_current(h, "h")
+    _buffer(labels, "labels", torch.int32, (M,), h.device)
+    ld = h.stride(0) if M > 1 else max(h.stride(0), d)
+    return h, W, ld, M, d, V
+
+
+def _head_ce_args(head, labels, ln_eps, out, workspace):
+    h, W, ld, M, d, V = _head_ce_inputs(head, labels)
+    if out is None:
+        out = dict(ce=torch.empty(M, dtype=torch.float32, device=h.device), lse=torch.empty(M, dtype=torch.float32, device=h.device),
+                   loss=torch.empty(2, dtype=torch.float32, device=h.device))
+    for name, shape in (("ce", (M,)), ("lse", (M,)), ("loss", (2,))):
+        _buffer(out.get(name), f"out[{name!r}]", torch.float32, shape, h.device)
+    workspace = new_head_ce_workspace(M, d, V, h.device) if workspace is None else _scratch(workspace, h.device)
+    args = (_ptr(h), ld, _ptr(head["gamma"]), _ptr(head["beta"]), float(ln_eps), _ptr(W), M, d, V, _ptr(labels), _ptr(out["ce"]),
+            _ptr(out["lse"]), _ptr(out["loss"]), _ptr(workspace), workspace.numel(), _stream())
+    return args, out, (h, W, head, labels, out, workspace)
+
+
+def ee_head_ce(head, labels, ln_eps, *, out=None, workspace=None) -> dict:
+    """Cross-entropy of a head (a dict with h, gamma, beta, W) at int32 `labels` [M], without keeping the logits (see
+    include/eexit.h): dict(ce [M], lse [M], loss [2] = mean over the counted rows and their number).  Labels outside
+    [0, V) mark rows that are not counted."""
+    args, out, _ = _head_ce_args(head, labels, ln_eps, out, workspace)
+    _check(_lib.load().ee_head_ce(*args), "ee_head_ce")
+    return out
+
+
+def prepare_head_ce(head, labels, ln_eps, *, out=None, workspace=None) -> PreparedCall:
+    args, out, keep = _head_ce_args(head, labels, ln_eps, out, workspace)
+    return PreparedCall(_lib.load().ee_head_ce, args, "ee_head_ce", keep, out)
+
+
+def _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace):
+    h, W, ld, M, d, V = _head_ce_inputs(head, labels)
+    dev = h.device
+    lse, loss = _buffer(forward["lse"], "lse", torch.float32, (M,), dev), _buffer(forward["loss"], "loss", torch.float32, (2,), dev)
+    if dce is not None:
+        _buffer(dce, "dce", torch.float32, (M,), dev)
+    if dloss is not None and not (isinstance(dloss, torch.Tensor) and dloss.device == dev and dloss.dtype == torch.float32 and dloss.numel() == 1):
+        raise ValueError("dloss must be a float32 CUDA tensor of one element")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the buffers to add to (out)")
+        out = dict(dh=torch.empty((M, d), dtype=torch.bfloat16, device=dev), dW=torch.empty((V, d), dtype=torch.bfloat16, device=dev),
+                   dgamma=torch.empty(d, dtype=torch.bfloat16, device=dev), dbeta=torch.empty(d, dtype=torch.bfloat16, device=dev))
+    dh = out.get("dh")
+    if dh is not None and not (isinstance(dh, torch.Tensor) and dh.device == dev and dh.dtype == torch.bfloat16 and dh.shape == (M, d) and
+                               (M == 0 or dh.stride(1) == 1)):
+        raise ValueError("out['dh'] must be a row-major bfloat16 tensor [M, d] on the device of h")
+    for name, shape in (("dW", (V, d)), ("dgamma", (d,)), ("dbeta", (d,))):
+        if out.get(name) is not None:
+            _buffer(out[name], f"out[{name!r}]", torch.bfloat16, shape, dev)
+    workspace = new_head_ce_grad_workspace(M, d, V, dev) if workspace is None else _scratch(workspace, dev)
+    ld_dh = d if dh is None else (dh.stride(0) if M > 1 else max(dh.stride(0), d))
+    args = (_ptr(h), ld, _ptr(head["gamma"]), _ptr(head["beta"]), float(ln_eps), _ptr(W), M, d, V, _ptr(labels), _ptr(lse), _ptr(loss),
+            _ptr(dce), _ptr(dloss), _ptr(dh), ld_dh, _ptr(out.get("dW")), _ptr(out.get("dgamma")), _ptr(out.get("dbeta")),
+            int(bool(accumulate)), _ptr(workspace), workspace.numel(), _stream())
+    return args, out, (h, W, head, labels, forward, dce, dloss, out, workspace)
+
+
+def ee_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None, accumulate=False, out=None, workspace=None) -> dict:
+    """Gradient of the cross-entropy (see include/eexit.h): dict(dh, dW, dgamma, dbeta), bf16.  `forward` is what
+    ee_head_ce returned for the same inputs (its lse and loss).  By default the gradient of the mean, times the device
+    scalar `dloss` if given; `dce` [M] gives every row's own weight instead.  With `out`, entries left out or None are
+    not computed; accumulate=True adds dW, dgamma and dbeta to the buffers in it."""
+    args, out, _ = _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace)
+    _check(_lib.load().ee_head_ce_grad(*args), "ee_head_ce_grad")
+    return out
+
+
+def prepare_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None, accumulate=False, out=None, workspace=None) -> PreparedCall:
+    args, out, keep = _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace)
+    return PreparedCall(_lib.load().ee_head_ce_grad, args, "ee_head_ce_grad", keep, out)
+
+
 def ee_selftest_wait_timeout(workspace) -> None:
     """Makes one bounded device-side wait give up (see include/eexit.h); ee_query_async_error then reports it."""
     _check(_lib.load().ee_selftest_wait_timeout(_ptr(workspace), workspace.numel(), _stream()), "ee_selftest_wait_timeout")

@@ -610,6 +610,76 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
     return kl_launch(a, t, labels, kl, ce, loss);
 }
 
+size_t ee_head_ce_workspace_bytes(int M, int d, int V) {
+    if (!sizes_ok(M, d, V)) return 0;
+    return ce_workspace_bytes(M, d, V, false);
+}
+
+size_t ee_head_ce_grad_workspace_bytes(int M, int d, int V) {
+    if (!sizes_ok(M, d, V)) return 0;
+    return ce_workspace_bytes(M, d, V, true);
+}
+
+ee_status ee_head_ce(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W, int M,
+                     int d, int V, const int* labels, float* ce, float* lse, float* loss, void* workspace,
+                     size_t workspace_bytes_, void* stream) {
+    if (!sizes_ok(M, d, V)) return EE_ERR_SHAPE;
+    if (!loss) return EE_ERR_NULL;
+    if (M > 0) {
+        if (!h || !gamma || !beta || !W || !labels || !ce || !lse || !workspace) return EE_ERR_NULL;
+        if (ld_h < d || (ld_h % 8) != 0) return EE_ERR_SHAPE;
+        if (!aligned(h, 16) || !aligned(W, 16) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(workspace, 256))
+            return EE_ERR_ALIGN;
+        if (workspace_bytes_ < ce_workspace_bytes(M, d, V, false)) return EE_ERR_WORKSPACE;
+    }
+    CeArgs a{};
+    const ee_status dev = current_device(&a.device, &a.num_sms);
+    if (dev != EE_OK) return dev;
+    a.stream = static_cast<cudaStream_t>(stream);
+    if (M == 0) return cudaMemsetAsync(loss, 0, 8, a.stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    a.h = h; a.ld_h = ld_h; a.gamma = gamma; a.beta = beta; a.ln_eps = ln_eps; a.W = W;
+    a.M = M; a.d = d; a.V = V; a.labels = labels;
+    a.ce = ce; a.lse_out = lse; a.loss_out = loss;
+    a.workspace = workspace;
+    return ce_launch(a);
+}
+
+ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W,
+                          int M, int d, int V, const int* labels, const float* lse, const float* loss, const float* dce,
+                          const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta, int accumulate,
+                          void* workspace, size_t workspace_bytes_, void* stream) {
+    if (!sizes_ok(M, d, V)) return EE_ERR_SHAPE;
+    if ((dgamma != nullptr) != (dbeta != nullptr)) return EE_ERR_NULL;
+    if (dce && dloss) return EE_ERR_SHAPE;                               // the rows' weights and the mean's gradient exclude each other
+    if (!aligned(dh, 16) || !aligned(dW, 16) || !aligned(dgamma, 16) || !aligned(dbeta, 16)) return EE_ERR_ALIGN;
+    if (M > 0) {
+        if (!h || !gamma || !beta || !W || !labels || !lse || !loss || !workspace) return EE_ERR_NULL;
+        if (ld_h < d || (ld_h % 8) != 0 || (dh && (ld_dh < d || (ld_dh % 8) != 0))) return EE_ERR_SHAPE;
+        if (!aligned(h, 16) || !aligned(W, 16) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(workspace, 256))
+            return EE_ERR_ALIGN;
+        if (workspace_bytes_ < ce_workspace_bytes(M, d, V, true)) return EE_ERR_WORKSPACE;
+    }
+    if (!dh && !dW && !dgamma) return EE_OK;
+    CeArgs a{};
+    const ee_status dev = current_device(&a.device, &a.num_sms);
+    if (dev != EE_OK) return dev;
+    a.stream = static_cast<cudaStream_t>(stream);
+    if (M == 0) {
+        if (accumulate) return EE_OK;
+        if ((dW && cudaMemsetAsync(dW, 0, (size_t)V * d * 2, a.stream) != cudaSuccess) ||
+            (dgamma && (cudaMemsetAsync(dgamma, 0, (size_t)d * 2, a.stream) != cudaSuccess ||
+                        cudaMemsetAsync(dbeta, 0, (size_t)d * 2, a.stream) != cudaSuccess)))
+            return EE_ERR_CUDA;
+        return EE_OK;
+    }
+    a.h = h; a.ld_h = ld_h; a.gamma = gamma; a.beta = beta; a.ln_eps = ln_eps; a.W = W;
+    a.M = M; a.d = d; a.V = V; a.labels = labels;
+    a.lse = lse; a.loss = loss; a.dce = dce; a.dloss = dloss;
+    a.dh = dh; a.ld_dh = ld_dh; a.dW = dW; a.dgamma = dgamma; a.dbeta = dbeta; a.accumulate = accumulate ? 1 : 0;
+    a.workspace = workspace;
+    return ce_grad_launch(a);
+}
+
 ee_status ee_selftest_wait_timeout(void* workspace, size_t workspace_bytes_, void* stream) {
     if (!workspace) return EE_ERR_NULL;
     if (!aligned(workspace, 256)) return EE_ERR_ALIGN;

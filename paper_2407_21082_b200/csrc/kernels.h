@@ -93,6 +93,37 @@ ee_status calibrate_launch(const float* entropy, const int* argmax_head, const i
 size_t kl_workspace_bytes(int M, int d, int V);
 ee_status kl_launch(const HeadArgs& head, const HeadArgs& teacher, const int* labels, float* kl, float* ce, float* loss);
 
+// ---- cross-entropy of a head over the whole vocabulary, and its gradient ----
+struct CeArgs {
+    const void* h;
+    long long ld_h;
+    const float* gamma;
+    const float* beta;
+    float ln_eps;
+    const void* W;
+    int M, d, V;
+    const int* labels;
+    float* ce;             // forward outputs
+    float* lse_out;
+    float* loss_out;
+    const float* lse;      // backward: what the forward call wrote
+    const float* loss;
+    const float* dce;
+    const float* dloss;
+    void* dh;
+    long long ld_dh;
+    void* dW;
+    void* dgamma;
+    void* dbeta;
+    int accumulate;
+    void* workspace;
+    cudaStream_t stream;
+    int device, num_sms;
+};
+size_t ce_workspace_bytes(int M, int d, int V, bool grad);
+ee_status ce_launch(const CeArgs& a);
+ee_status ce_grad_launch(const CeArgs& a);
+
 // ---- commit step of a DSSD round (k <= 32) ----
 ee_status dssd_commit_launch(const int* draft_tok, const unsigned char* draft_exit_mask, const int* verify_tok, int S, int k,
                              int kv, int eos, int* out_tok, int cap, int* seq_len, unsigned char* finished, int* draft_len,
