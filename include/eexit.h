@@ -482,6 +482,50 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
                           int accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Heads held in 4 bits.  Drafting (section 4.3.1) evaluates a head for a handful of tokens at a time, which takes the
+ * time of reading its weights; these calls hold them as whole numbers with a scale per row and group of columns:
+ *   s[v, k] = bf16( max |W[v, j]| / 7 ) over the columns j of group k;   q[v, j] = nearest whole number of W[v, j] / s
+ *   (ties to the even one; 0 where s = 0), kept within -8 .. 7;          W4[v, j] = bf16( s q )
+ * W must be finite.  group is 32, 64 or 128; d % group == 0, group <= d <= 8192, V >= 1.  A packed head is
+ * ee_head_q4_bytes(V, d, group) bytes (0 if a size is invalid), 256-byte aligned, in a layout of the library's own;
+ * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous, 16-byte aligned.
+ *
+ * ee_exit_head_q4 is ee_exit_head with W4 for W: same definition, outputs, strides, alignment and rules (the packed
+ * head is a constant of the stream).  Any M; rows beyond those whose LayerNorm output fits shared memory go in further
+ * passes over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
+ * with ee_workspace_init.  M = 0 is a no-op.
+ */
+size_t    ee_head_q4_bytes(int V, int d, int group);
+ee_status ee_head_q4_pack(const void* W, int V, int d, int group, void* q4, size_t q4_bytes, void* stream);
+ee_status ee_head_q4_unpack(const void* q4, size_t q4_bytes, int V, int d, int group, void* W, void* stream);
+size_t    ee_exit_head_q4_workspace_bytes(int M, int d, int V);
+ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* q4,
+                          size_t q4_bytes, int group, int M, int d, int V, const float* tau_per_row, float tau,
+                          int* argmax, float* entropy, float* maxprob, unsigned char* exit_mask, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * The embedding of tokens and its gradient.  A head's weights and the model's embedding may be one table (tied
+ * weights): a training step then adds the lookup's gradient to what ee_head_ce_grad left in dW, and a decoding step
+ * looks up the tokens a round has committed.
+ *   ee_embed:       out[i, :] = bf16( scale * table[tokens[i], :] );  a token outside [0, V) gives a zero row
+ *   ee_embed_grad:  dtable[v, :] = scale * sum of dout[i, :] over the i with tokens[i] = v, summed in fp32 in a fixed order;
+ *                   tokens outside [0, V) are left out.  dtable is bf16 (dtable_fp32 = 0) or fp32; with accumulate != 0
+ *                   the sums are added to what it holds (one rounding), rows of other tokens are not touched;
+ *                   otherwise the whole table is written.
+ * table bf16 [V, d] contiguous; tokens int32 [n]; out, dout bf16 [n, d], row strides ld_* elements (ld_* >= d,
+ * ld_* % 8 == 0); dtable [V, d] contiguous; 16-byte alignment; d % 8 == 0, 8 <= d <= 8192, V >= 1, n >= 0 (n = 0:
+ * ee_embed_grad clears the table unless it accumulates).  Workspace of the gradient:
+ * ee_embed_grad_workspace_bytes(n, d, V) (0 if a size is invalid), 256-byte aligned; needs no initialisation.
+ */
+ee_status ee_embed(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out,
+                   void* stream);
+size_t    ee_embed_grad_workspace_bytes(int n, int d, int V);
+ee_status ee_embed_grad(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale,
+                        void* dtable, int dtable_fp32, int accumulate, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/*
  * Calibration of one head's threshold from a calibration set (section 3.4.1, "Calibration of Confidence
  * Thresholds": Eq. 3 and the two equations that define the index j-hat and tau_k = c_{k, j-hat}), with the
  * entropy as the confidence metric.  Over n calibration tokens:

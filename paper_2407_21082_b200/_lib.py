@@ -90,6 +90,16 @@ PROTOTYPES = {
     "ee_head_ce_grad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_head_ce_grad": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_int, C.c_int, C.c_int, _p, _p, _p, _p, _p,
                                   _p, C.c_longlong, _p, _p, _p, C.c_int, _p, C.c_size_t, _p]),
+    "ee_head_q4_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "ee_head_q4_pack": (C.c_int, [_p, C.c_int, C.c_int, C.c_int, _p, C.c_size_t, _p]),
+    "ee_head_q4_unpack": (C.c_int, [_p, C.c_size_t, C.c_int, C.c_int, C.c_int, _p, _p]),
+    "ee_exit_head_q4_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "ee_exit_head_q4": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_size_t, C.c_int, C.c_int, C.c_int, C.c_int,
+                                  _p, C.c_float, _p, _p, _p, _p, _p, C.c_size_t, _p]),
+    "ee_embed": (C.c_int, [_p, C.c_int, C.c_int, _p, C.c_int, C.c_float, _p, C.c_longlong, _p]),
+    "ee_embed_grad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "ee_embed_grad": (C.c_int, [_p, C.c_longlong, _p, C.c_int, C.c_int, C.c_int, C.c_float, _p, C.c_int, C.c_int,
+                                _p, C.c_size_t, _p]),
     "ee_cascade_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_cascade": (C.c_int, [C.POINTER(EEHead), C.c_int, C.c_float, C.c_int, C.c_int, C.c_int, _p, _p, _p, _p,
                              _p, C.c_size_t, _p]),

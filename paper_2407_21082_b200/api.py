@@ -605,6 +605,179 @@ def prepare_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None,
     return PreparedCall(_lib.load().ee_head_ce_grad, args, "ee_head_ce_grad", keep, out)
 
 
+class Q4Weights:
+    """A head's weights in 4 bits (see include/eexit.h): the packed bytes (a device tensor) and what they are of."""
+    __slots__ = ("data", "V", "d", "group")
+
+    def __init__(self, data: torch.Tensor, V: int, d: int, group: int):
+        need = ee_head_q4_bytes(V, d, group)
+        if need == 0:
+            raise EExitError(2, "ee_head_q4_bytes")
+        if not (isinstance(data, torch.Tensor) and data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous() and data.numel() >= need):
+            raise ValueError(f"data must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+        self.data, self.V, self.d, self.group = data, int(V), int(d), int(group)
+
+
+def ee_head_q4_bytes(V: int, d: int, group: int) -> int:
+    return int(_lib.load().ee_head_q4_bytes(int(V), int(d), int(group)))
+
+
+def ee_head_q4_pack(W, group: int = 64, *, out: Q4Weights | None = None) -> Q4Weights:
+    """Writes a head's weights (bf16 [V, d]) in 4 bits with a scale per row and `group` columns (see include/eexit.h)."""
+    W = _on_current(_bf16(_dev(W, "W")), "W")
+    if W.dim() != 2 or not W.is_contiguous():
+        raise ValueError("W must be contiguous [V, d]")
+    V, d = W.shape
+    if out is None:
+        nbytes = ee_head_q4_bytes(V, d, group)
+        if nbytes == 0:
+            raise EExitError(2, "ee_head_q4_pack")
+        out = Q4Weights(torch.empty(nbytes, dtype=torch.uint8, device=W.device), V, d, group)
+    elif (out.V, out.d, out.group) != (V, d, group) or out.data.device != W.device:
+        raise ValueError("out was made for other weights")
+    _check(_lib.load().ee_head_q4_pack(_ptr(W), V, d, int(group), _ptr(out.data), out.data.numel(), _stream()), "ee_head_q4_pack")
+    return out
+
+
+def ee_head_q4_unpack(q4: Q4Weights, *, out=None) -> torch.Tensor:
+    """What the packed weights stand for, bf16 [V, d]."""
+    _on_current(q4.data, "q4")
+    if out is None:
+        out = torch.empty((q4.V, q4.d), dtype=torch.bfloat16, device=q4.data.device)
+    _buffer(out, "out", torch.bfloat16, (q4.V, q4.d), q4.data.device)
+    _check(_lib.load().ee_head_q4_unpack(_ptr(q4.data), q4.data.numel(), q4.V, q4.d, q4.group, _ptr(out), _stream()), "ee_head_q4_unpack")
+    return out
+
+
+def ee_exit_head_q4_workspace_bytes(M: int, d: int, V: int) -> int:
+    return int(_lib.load().ee_exit_head_q4_workspace_bytes(int(M), int(d), int(V)))
+
+
+def new_exit_head_q4_workspace(M: int, q4: Q4Weights) -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace for ee_exit_head_q4 with these weights."""
+    return _workspace_of(ee_exit_head_q4_workspace_bytes(M, q4.d, q4.V), "ee_exit_head_q4_workspace_bytes", q4.data.device)
+
+
+def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
+    h = _on_current(_bf16(_dev(h, "h")), "h")
+    if h.dim() != 2 or h.shape[1] != q4.d or (h.shape[0] > 0 and h.stride(1) != 1):
+        raise ValueError(f"h must be row-major [M, d = {q4.d}]")
+    M, dev = h.shape[0], h.device
+    if q4.data.device != dev:
+        raise ValueError(f"q4 is on {q4.data.device}, h on {dev}")
+    _buffer(gamma, "gamma", torch.float32, (q4.d,), dev)
+    _buffer(beta, "beta", torch.float32, (q4.d,), dev)
+    if isinstance(tau, torch.Tensor):
+        _buffer(tau, "a per-row tau", torch.float32, (M,), dev)
+    if out is None:
+        out = new_outputs(M, dev)
+    for name, dtype in _OUT_DTYPES.items():
+        t = out.get(name)
+        if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype == dtype and t.is_contiguous() and t.numel() >= M):
+            raise ValueError(f"out[{name!r}] must be a contiguous {dtype} CUDA tensor of at least M = {M} elements")
+    workspace = new_exit_head_q4_workspace(M, q4) if workspace is None else _scratch(workspace, dev)
+    tau_t, tau_f = (tau, 0.0) if isinstance(tau, torch.Tensor) else (None, float(tau))
+    args = (_ptr(h), h.stride(0) if M > 1 else max(h.stride(0), q4.d), _ptr(gamma), _ptr(beta), float(ln_eps), _ptr(q4.data), q4.data.numel(),
+            q4.group, M, q4.d, q4.V, _ptr(tau_t), tau_f, _ptr(out["argmax"]), _ptr(out["entropy"]), _ptr(out["maxprob"]),
+            _ptr(out["exit_mask"]), _ptr(workspace), workspace.numel(), _stream())
+    return args, out, (h, gamma, beta, q4, tau_t, out, workspace)
+
+
+def ee_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> dict:
+    """ee_exit_head with weights held in 4 bits (ee_head_q4_pack); see there for the arguments."""
+    args, out, _ = _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace)
+    _check(_lib.load().ee_exit_head_q4(*args), "ee_exit_head_q4")
+    return out
+
+
+def prepare_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> PreparedCall:
+    args, out, keep = _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace)
+    return PreparedCall(_lib.load().ee_exit_head_q4, args, "ee_exit_head_q4", keep, out)
+
+
+def _rows_of(t, name, n, d, device):
+    if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape == (n, d) and
+            (n == 0 or t.stride(1) == 1)):
+        raise ValueError(f"{name} must be a row-major bfloat16 tensor [{n}, {d}] on {device}")
+    return t.stride(0) if n > 1 else max(t.stride(0), d)
+
+
+def _embed_args(table, tokens, scale, out):
+    table = _on_current(_bf16(_dev(table, "table")), "table")
+    if table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table must be contiguous [V, d]")
+    V, d = table.shape
+    n = tokens.numel()
+    _buffer(tokens, "tokens", torch.int32, (n,), table.device)
+    if out is None:
+        out = torch.empty((n, d), dtype=torch.bfloat16, device=table.device)
+    ld = _rows_of(out, "out", n, d, table.device)
+    args = (_ptr(table), V, d, _ptr(tokens), n, float(scale), _ptr(out), ld, _stream())
+    return args, out, (table, tokens, out)
+
+
+def ee_embed(table, tokens, scale: float = 1.0, *, out=None) -> torch.Tensor:
+    """Rows of `table` (bf16 [V, d]) at int32 `tokens` [n], times `scale`, rounded once; zero rows for tokens outside
+    [0, V)."""
+    args, out, _ = _embed_args(table, tokens, scale, out)
+    _check(_lib.load().ee_embed(*args), "ee_embed")
+    return out
+
+
+def prepare_embed(table, tokens, scale: float = 1.0, *, out=None) -> PreparedCall:
+    args, out, keep = _embed_args(table, tokens, scale, out)
+    return PreparedCall(_lib.load().ee_embed, args, "ee_embed", keep, out)
+
+
+def ee_embed_grad_workspace_bytes(n: int, d: int, V: int) -> int:
+    return int(_lib.load().ee_embed_grad_workspace_bytes(int(n), int(d), int(V)))
+
+
+def new_embed_grad_workspace(n: int, d: int, V: int, device="cuda") -> torch.Tensor:
+    """Allocates (through torch) a workspace for ee_embed_grad at these sizes; it needs no initialisation."""
+    nbytes = ee_embed_grad_workspace_bytes(n, d, V)
+    if nbytes == 0:
+        raise EExitError(2, "ee_embed_grad_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _embed_grad_args(dout, tokens, V, scale, dtype, out, accumulate, workspace):
+    dout = _on_current(_bf16(_dev(dout, "dout")), "dout")
+    if dout.dim() != 2:
+        raise ValueError("dout must be [n, d]")
+    n, d = dout.shape
+    ld = _rows_of(dout, "dout", n, d, dout.device)
+    _buffer(tokens, "tokens", torch.int32, (n,), dout.device)
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("the table's gradient is bfloat16 or float32")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the table to add to (out)")
+        out = torch.empty((V, d), dtype=dtype, device=dout.device)
+    else:
+        dtype = out.dtype
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("the table's gradient is bfloat16 or float32")
+    _buffer(out, "out", dtype, (V, d), dout.device)
+    workspace = new_embed_grad_workspace(n, d, V, dout.device) if workspace is None else _scratch(workspace, dout.device)
+    args = (_ptr(dout), ld, _ptr(tokens), n, int(V), d, float(scale), _ptr(out), int(dtype == torch.float32), int(bool(accumulate)),
+            _ptr(workspace), workspace.numel(), _stream())
+    return args, out, (dout, tokens, out, workspace)
+
+
+def ee_embed_grad(dout, tokens, V: int, scale: float = 1.0, *, dtype=torch.bfloat16, out=None, accumulate=False, workspace=None) -> torch.Tensor:
+    """Gradient of ee_embed's table [V, d]: per token the sum of its rows of `dout` (bf16 [n, d]) times `scale`, in bf16
+    or fp32 (`dtype`, or that of `out`); accumulate=True adds to `out` and touches no other rows."""
+    args, out, _ = _embed_grad_args(dout, tokens, V, scale, dtype, out, accumulate, workspace)
+    _check(_lib.load().ee_embed_grad(*args), "ee_embed_grad")
+    return out
+
+
+def prepare_embed_grad(dout, tokens, V: int, scale: float = 1.0, *, dtype=torch.bfloat16, out=None, accumulate=False, workspace=None) -> PreparedCall:
+    args, out, keep = _embed_grad_args(dout, tokens, V, scale, dtype, out, accumulate, workspace)
+    return PreparedCall(_lib.load().ee_embed_grad, args, "ee_embed_grad", keep, out)
+
+
 def ee_selftest_wait_timeout(workspace) -> None:
     """Makes one bounded device-side wait give up (see include/eexit.h); ee_query_async_error then reports it."""
     _check(_lib.load().ee_selftest_wait_timeout(_ptr(workspace), workspace.numel(), _stream()), "ee_selftest_wait_timeout")

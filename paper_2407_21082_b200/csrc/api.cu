@@ -680,6 +680,106 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
     return ce_grad_launch(a);
 }
 
+namespace {
+bool q4_sizes_ok(int V, int d, int group) {
+    return V >= 1 && (group == 32 || group == 64 || group == 128) && d >= group && d <= 8192 && d % group == 0;
+}
+}  // namespace
+
+size_t ee_head_q4_bytes(int V, int d, int group) {
+    if (!q4_sizes_ok(V, d, group)) return 0;
+    return q4_weight_bytes(V, d, group);
+}
+
+ee_status ee_head_q4_pack(const void* W, int V, int d, int group, void* q4, size_t q4_bytes, void* stream) {
+    if (!q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (!W || !q4) return EE_ERR_NULL;
+    if (!aligned(W, 16) || !aligned(q4, 256)) return EE_ERR_ALIGN;
+    if (q4_bytes < q4_weight_bytes(V, d, group)) return EE_ERR_WORKSPACE;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return q4_pack_launch(W, V, d, group, q4, static_cast<cudaStream_t>(stream));
+}
+
+ee_status ee_head_q4_unpack(const void* q4, size_t q4_bytes, int V, int d, int group, void* W, void* stream) {
+    if (!q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (!W || !q4) return EE_ERR_NULL;
+    if (!aligned(W, 16) || !aligned(q4, 256)) return EE_ERR_ALIGN;
+    if (q4_bytes < q4_weight_bytes(V, d, group)) return EE_ERR_WORKSPACE;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return q4_unpack_launch(q4, V, d, group, W, static_cast<cudaStream_t>(stream));
+}
+
+size_t ee_exit_head_q4_workspace_bytes(int M, int d, int V) {
+    if (!sizes_ok(M, d, V)) return 0;
+    return q4_head_workspace_bytes(M, d);
+}
+
+ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* q4,
+                          size_t q4_bytes, int group, int M, int d, int V, const float* tau_per_row, float tau, int* argmax,
+                          float* entropy, float* maxprob, unsigned char* exit_mask, void* workspace, size_t workspace_bytes_,
+                          void* stream) {
+    if (!sizes_ok(M, d, V) || !q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (M == 0) return EE_OK;
+    if (!h || !gamma || !beta || !q4 || !argmax || !entropy || !maxprob || !exit_mask || !workspace) return EE_ERR_NULL;
+    if (ld_h < d || (ld_h % 8) != 0) return EE_ERR_SHAPE;
+    if (!aligned(h, 16) || !aligned(q4, 256) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(workspace, 256))
+        return EE_ERR_ALIGN;
+    if (q4_bytes < q4_weight_bytes(V, d, group) || workspace_bytes_ < q4_head_workspace_bytes(M, d)) return EE_ERR_WORKSPACE;
+    HeadArgs a{};
+    const ee_status dev = current_device(&a.device, &a.num_sms);
+    if (dev != EE_OK) return dev;
+    a.h = h; a.ld_h = ld_h; a.gamma = gamma; a.beta = beta; a.ln_eps = ln_eps;
+    a.M = M; a.d = d; a.V = V; a.tau_per_row = tau_per_row; a.tau = tau;
+    a.argmax = argmax; a.entropy = entropy; a.maxprob = maxprob; a.exit_mask = exit_mask;
+    a.workspace = workspace; a.workspace_bytes = workspace_bytes_;
+    a.stream = static_cast<cudaStream_t>(stream);
+    return q4_head_launch(a, q4, group);
+}
+
+ee_status ee_embed(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, void* stream) {
+    if (!sizes_ok(n, d, V)) return EE_ERR_SHAPE;
+    if (n == 0) return EE_OK;
+    if (!table || !tokens || !out) return EE_ERR_NULL;
+    if (ld_out < d || (ld_out % 8) != 0) return EE_ERR_SHAPE;
+    if (!aligned(table, 16) || !aligned(out, 16)) return EE_ERR_ALIGN;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return embed_launch(table, V, d, tokens, n, scale, out, ld_out, num_sms, static_cast<cudaStream_t>(stream));
+}
+
+size_t ee_embed_grad_workspace_bytes(int n, int d, int V) {
+    if (!sizes_ok(n, d, V)) return 0;
+    return embed_grad_workspace_bytes(n, d, V);
+}
+
+ee_status ee_embed_grad(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable,
+                        int dtable_fp32, int accumulate, void* workspace, size_t workspace_bytes_, void* stream) {
+    if (!sizes_ok(n, d, V)) return EE_ERR_SHAPE;
+    if (!dtable) return EE_ERR_NULL;
+    if (!aligned(dtable, 16)) return EE_ERR_ALIGN;
+    if (n > 0) {
+        if (!dout || !tokens || !workspace) return EE_ERR_NULL;
+        if (ld_dout < d || (ld_dout % 8) != 0) return EE_ERR_SHAPE;
+        if (!aligned(dout, 16) || !aligned(workspace, 256)) return EE_ERR_ALIGN;
+        if (workspace_bytes_ < embed_grad_workspace_bytes(n, d, V)) return EE_ERR_WORKSPACE;
+    }
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (n == 0) {
+        if (accumulate) return EE_OK;
+        return cudaMemsetAsync(dtable, 0, (size_t)V * d * (dtable_fp32 ? 4 : 2), s) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    }
+    return embed_grad_launch(dout, ld_dout, tokens, n, V, d, scale, dtable, dtable_fp32 ? 1 : 0, accumulate ? 1 : 0, workspace, device,
+                             num_sms, s);
+}
+
 ee_status ee_selftest_wait_timeout(void* workspace, size_t workspace_bytes_, void* stream) {
     if (!workspace) return EE_ERR_NULL;
     if (!aligned(workspace, 256)) return EE_ERR_ALIGN;

@@ -296,6 +296,27 @@ int tiles_of(int n) { return (n + kTile - 1) / kTile; }
 
 }  // namespace
 
+// Digit totals, then the tiles' histograms.
+size_t sort_words_scratch_bytes(int n) { return 1024 + align_up((size_t)kDigits * tiles_of(n) * sizeof(unsigned int), 256); }
+
+ee_status sort_words_launch(u64* a, u64* b, int n, int first_shift, int passes, void* scratch, const u64** sorted, cudaStream_t stream) {
+    unsigned int* digit_total = static_cast<unsigned int*>(scratch);
+    unsigned int* hist = digit_total + kDigits;
+    const int n_tiles = tiles_of(n);
+    u64 *src = a, *dst = b;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = first_shift + 8 * pass;
+        calib_hist_kernel<<<n_tiles, kSortThreads, 0, stream>>>(src, n, shift, hist, n_tiles);
+        calib_scan_kernel<<<kDigits, 1024, 0, stream>>>(hist, n_tiles, digit_total);
+        calib_scatter_kernel<<<n_tiles, kSortThreads, 0, stream>>>(src, dst, n, shift, hist, digit_total, n_tiles);
+        u64* t = src;
+        src = dst;
+        dst = t;
+    }
+    *sorted = src;
+    return cudaGetLastError() == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
 size_t calibrate_workspace_bytes(int n) {
     const int n_tiles = tiles_of(n);
     return kCalibHeader + 2 * words_bytes(n) + align_up((size_t)kDigits * n_tiles * sizeof(unsigned int), 256) +

@@ -796,6 +796,16 @@ CeParams base_params(const CeArgs& a) {
 
 }  // namespace
 
+ee_status layer_norm_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int M, int d,
+                            cudaStream_t stream) {
+    CeLnArgs l{};
+    l.h = static_cast<const __nv_bfloat16*>(h);
+    l.ld_h = ld_h; l.gamma = gamma; l.beta = beta; l.ln_eps = ln_eps;
+    l.y = static_cast<__nv_bfloat16*>(y);
+    l.M = M; l.d = d;
+    return launch_pdl(ce_layer_norm_kernel, dim3((M + 7) / 8), 256, 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
 size_t ce_workspace_bytes(int M, int d, int V, bool grad) { return ce_space(M, d, V, grad).total; }
 
 ee_status ce_launch(const CeArgs& a) {

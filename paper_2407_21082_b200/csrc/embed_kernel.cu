@@ -1,0 +1,366 @@
+// The embedding that shares its table with a head: out[i] = bf16(scale * table[token_i]), and its gradient
+//   dtable[v] = scale * sum over i with token_i = v of dout[i]
+// by sorted tokens, in fp32 and in a fixed order (no floating-point atomics: the same bits from run to run).
+//
+// The gradient is three steps.  (1) The tokens are sorted, stably, by one CTA in shared memory when they fit
+// (n <= 16384 and V < 2^18: 18 bits of token and 14 of position in one word), while the other CTAs clear the table, which takes
+// longer (V d bytes against n words); longer lists go through the library's radix sort.  (2) The sorted list is cut into
+// chunks of equal length, one CTA (per 128 vectors of the width) each: it adds up the rows of every token in it.  A token
+// that lies inside the chunk is finished there; a run that crosses a chunk's border, as frequent tokens' do, leaves
+// fp32 partial sums (one for the run that comes in, one for the run that goes out).  (3) A run's partial sums are
+// joined in order by the chunk it starts in.  So a token that fills the whole batch costs no more than any other batch.
+// Tokens outside [0, V) take no part: they sort behind all others and are skipped.
+#include "common.cuh"
+#include "kernels.h"
+
+namespace ee {
+
+namespace {
+
+typedef unsigned long long u64;
+
+__device__ __forceinline__ void unpack8f(uint4 o, float (&x)[8]) {
+    x[0] = bf16_lo(o.x); x[1] = bf16_hi(o.x); x[2] = bf16_lo(o.y); x[3] = bf16_hi(o.y);
+    x[4] = bf16_lo(o.z); x[5] = bf16_hi(o.z); x[6] = bf16_lo(o.w); x[7] = bf16_hi(o.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// One 16-byte vector per thread and turn.
+__global__ void __launch_bounds__(256) embed_kernel(const __nv_bfloat16* table, int V, int nvec, const int* tokens, int n, float scale,
+                                                    __nv_bfloat16* out, long long ld_out) {
+    launch_dependents();
+    const long long total = (long long)n * nvec, step = (long long)gridDim.x * 256;
+    grid_dependency_wait();
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const int row = (int)(i / nvec), c = (int)(i - (long long)row * nvec);
+        const int token = ld_dep(tokens + row);
+        float x[8] = {};
+        if ((unsigned)token < (unsigned)V) {
+            unpack8f(ld_dep(reinterpret_cast<const uint4*>(table) + (size_t)token * nvec + c), x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] *= scale;
+        }
+        *(reinterpret_cast<uint4*>(out + (size_t)row * ld_out) + c) = pack8(x);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- sorting
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortItems = 16;
+constexpr int kSortMax = kSortThreads * kSortItems;      // tokens one CTA sorts
+constexpr int kSortIndexBits = 14;
+constexpr int kSortMaxV = (1 << (32 - kSortIndexBits)) - 1;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr size_t kSortSmem = (size_t)kSortMax * 4 + kSortWarps * 256 * 4 + 64;
+
+// CTA 0: stable radix sort of (token, position), eight bits a pass; warp w owns a run of consecutive items and walks it 32 at
+// a time, so that (warp, round, lane) is the order in the list.  The other CTAs clear `clear_vecs` vectors at `clear`.
+__global__ void __launch_bounds__(kSortThreads, 1) embed_sort_clear_kernel(const int* tokens, int n, int V, int passes, int2* sorted,
+                                                                           uint4* clear, long long clear_vecs) {
+    launch_dependents();
+    grid_dependency_wait();
+    if (blockIdx.x != 0) {
+        const long long step = (long long)(gridDim.x - 1) * kSortThreads;
+        for (long long i = (long long)(blockIdx.x - 1) * kSortThreads + threadIdx.x; i < clear_vecs; i += step) clear[i] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    extern __shared__ __align__(16) unsigned int sort_smem[];
+    unsigned int* list = sort_smem;                       // [n]
+    unsigned int* cnt = sort_smem + kSortMax;             // [warps][256]
+    unsigned int* warp_part = cnt + kSortWarps * 256;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rounds = (n + kSortThreads - 1) / kSortThreads;
+    const int base = warp * rounds * 32;
+    unsigned int item[kSortItems];
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const int i = base + r * 32 + lane;
+        if (r < rounds && i < n) {
+            const int t = ld_dep(tokens + i);
+            item[r] = ((unsigned int)((unsigned)t < (unsigned)V ? t : V) << kSortIndexBits) | (unsigned int)i;
+        }
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = kSortIndexBits + 8 * pass;
+        for (int i = threadIdx.x; i < kSortWarps * 256; i += kSortThreads) cnt[i] = 0;
+        __syncthreads();
+        unsigned int rank[kSortItems];
+#pragma unroll
+        for (int r = 0; r < kSortItems; ++r) {
+            if (r < rounds) {
+                const bool valid = base + r * 32 + lane < n;
+                const unsigned int digit = valid ? (item[r] >> shift) & 255u : 0xffffffffu;
+                const unsigned int peers = __match_any_sync(0xffffffffu, digit);
+                const int leader = __ffs(peers) - 1;
+                unsigned int before = 0;
+                if (valid && lane == leader) before = atomicAdd(&cnt[warp * 256 + digit], (unsigned int)__popc(peers));
+                before = __shfl_sync(0xffffffffu, before, leader);
+                rank[r] = before + __popc(peers & ((1u << lane) - 1u));
+            }
+        }
+        __syncthreads();
+        unsigned int mine = 0, incl = 0;
+        if (threadIdx.x < 256) {                          // thread = digit
+            for (int w = 0; w < kSortWarps; ++w) mine += cnt[w * 256 + threadIdx.x];
+            incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned int x = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += x;
+            }
+            if (lane == 31) warp_part[warp] = incl;
+        }
+        __syncthreads();
+        if (threadIdx.x < 256) {
+            unsigned int run = incl - mine;
+            for (int w = 0; w < warp; ++w) run += warp_part[w];
+            for (int w = 0; w < kSortWarps; ++w) {
+                const unsigned int k = cnt[w * 256 + threadIdx.x];
+                cnt[w * 256 + threadIdx.x] = run;
+                run += k;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortItems; ++r)
+            if (r < rounds && base + r * 32 + lane < n) list[cnt[warp * 256 + ((item[r] >> shift) & 255u)] + rank[r]] = item[r];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kSortItems; ++r)
+            if (r < rounds && base + r * 32 + lane < n) item[r] = list[base + r * 32 + lane];
+    }
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+        const int i = base + r * 32 + lane;
+        if (r < rounds && i < n) sorted[i] = make_int2((int)(item[r] & ((1u << kSortIndexBits) - 1u)), (int)(item[r] >> kSortIndexBits));
+    }
+}
+
+// (position, token) words for the radix sort over memory, and the clearing of the table.
+__global__ void __launch_bounds__(256) embed_words_kernel(const int* tokens, int n, int V, u64* words, uint4* clear, long long clear_vecs) {
+    const long long step = (long long)gridDim.x * 256, first = (long long)blockIdx.x * 256 + threadIdx.x;
+    for (long long i = first; i < n; i += step) {
+        const int t = ld_dep(tokens + i);
+        words[i] = ((u64)(unsigned int)((unsigned)t < (unsigned)V ? t : V) << 32) | (unsigned int)i;
+    }
+    for (long long i = first; i < clear_vecs; i += step) clear[i] = make_uint4(0, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------------------------------------------- adding up
+
+struct EmbedGrad {
+    const __nv_bfloat16* dout;
+    long long ld_dout;
+    const int2* sorted;            // (position, token) in order of token, then position
+    int n, V, nvec, chunk, n_chunks;
+    float scale;
+    void* dtable;
+    int wide, add;                 // fp32 table; add to what it holds
+    float* parts;                  // [n_chunks][2][8 * nvec]: the run that comes in, the run that goes out
+};
+
+__device__ __forceinline__ void store_row(const EmbedGrad& a, int token, int c, float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+    const size_t at = (size_t)token * a.nvec + c;
+    if (a.wide) {
+        float4* out = reinterpret_cast<float4*>(a.dtable) + 2 * at;
+        if (a.add) {
+            const float4 o0 = ld_dep(out), o1 = ld_dep(out + 1);
+            x[0] += o0.x; x[1] += o0.y; x[2] += o0.z; x[3] += o0.w;
+            x[4] += o1.x; x[5] += o1.y; x[6] += o1.z; x[7] += o1.w;
+        }
+        out[0] = make_float4(x[0], x[1], x[2], x[3]);
+        out[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        uint4* out = reinterpret_cast<uint4*>(a.dtable) + at;
+        if (a.add) {
+            float o[8];
+            unpack8f(ld_dep(out), o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] += o[j];
+        }
+        *out = pack8(x);
+    }
+}
+__device__ __forceinline__ void store_part(const EmbedGrad& a, int chunk, int which, int c, const float (&x)[8]) {
+    float4* out = reinterpret_cast<float4*>(a.parts + ((size_t)chunk * 2 + which) * a.nvec * 8) + 2 * c;
+    out[0] = make_float4(x[0], x[1], x[2], x[3]);
+    out[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+constexpr int kSumThreads = 128;
+constexpr int kSumAhead = 8;                              // rows in flight per thread
+
+__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_constant__ EmbedGrad a) {
+    __shared__ int2 entry[kSumThreads];
+    launch_dependents();
+    grid_dependency_wait();
+    const int p0 = blockIdx.x * a.chunk, p1 = min(a.n, p0 + a.chunk);
+    const int c = blockIdx.y * kSumThreads + threadIdx.x;
+    const bool live = c < a.nvec;
+    const int token_before = p0 > 0 ? ld_dep(a.sorted + p0 - 1).y : -1;
+    const int token_after = p1 < a.n ? ld_dep(a.sorted + p1).y : -1;
+    float acc[8] = {};
+    int token = token_before;                             // token of the run being added up
+    bool comes_in = true;                                 // it started before the chunk
+    bool empty = true;
+    for (int q0 = p0; q0 < p1; q0 += kSumThreads) {
+        __syncthreads();
+        if (q0 + (int)threadIdx.x < p1) entry[threadIdx.x] = ld_dep(a.sorted + q0 + threadIdx.x);
+        __syncthreads();
+        const int count = min(kSumThreads, p1 - q0);
+        for (int k0 = 0; k0 < count; k0 += kSumAhead) {
+            uint4 v[kSumAhead];
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k)
+                if (live && k0 + k < count && entry[k0 + k].y < a.V)
+                    v[k] = ld_dep(reinterpret_cast<const uint4*>(a.dout + (size_t)entry[k0 + k].x * a.ld_dout) + c);
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k) {
+                if (k0 + k >= count) break;
+                const int t = entry[k0 + k].y;
+                if (t >= a.V) break;                      // from here on only tokens that take no part
+                if (t != token) {                         // the run before this token ends here
+                    if (!empty && live) {
+                        if (comes_in) store_part(a, blockIdx.x, 0, c, acc);
+                        else store_row(a, token, c, acc);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+                    token = t;
+                    comes_in = false;
+                }
+                empty = false;
+                float x[8];
+                if (live) {
+                    unpack8f(v[k], x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] += x[j];
+                }
+            }
+        }
+    }
+    if (empty || !live) return;
+    if (comes_in) store_part(a, blockIdx.x, 0, c, acc);
+    else if (token_after == token) store_part(a, blockIdx.x, 1, c, acc);
+    else store_row(a, token, c, acc);
+}
+
+// Joins the partial sums of the run that goes out of chunk blockIdx.x: 16 vectors of the width by 16 groups of chunks.
+__global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedGrad a) {
+    __shared__ float red[16][16][9];
+    launch_dependents();
+    grid_dependency_wait();
+    const int first = blockIdx.x, p0 = first * a.chunk, p1 = p0 + a.chunk;
+    if (p1 >= a.n) return;                                               // nothing goes out of the last chunk
+    const int token = ld_dep(a.sorted + p1 - 1).y;
+    if (token >= a.V || ld_dep(a.sorted + p1).y != token) return;        // no run crosses the border,
+    if (p0 > 0 && ld_dep(a.sorted + p0 - 1).y == token && ld_dep(a.sorted + p0).y == token) return;      // or it started earlier
+    const int v = threadIdx.x & 15, group = threadIdx.x >> 4;
+    const int c = blockIdx.y * 16 + v;
+    float acc[8] = {};
+    if (c < a.nvec) {
+        auto add = [&](int chunk, int which) {
+            const float4* in = reinterpret_cast<const float4*>(a.parts + ((size_t)chunk * 2 + which) * a.nvec * 8) + 2 * c;
+            const float4 x = ld_dep(in), y = ld_dep(in + 1);
+            acc[0] += x.x; acc[1] += x.y; acc[2] += x.z; acc[3] += x.w;
+            acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
+        };
+        if (group == 0) add(first, 1);
+        for (int k = first + 1 + group; k < a.n_chunks && ld_dep(a.sorted + (size_t)k * a.chunk).y == token; k += 16) add(k, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) red[group][v][j] = acc[j];
+    __syncthreads();
+    if (group == 0 && c < a.nvec) {
+        for (int k = 1; k < 16; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += red[k][v][j];
+        store_row(a, token, c, acc);
+    }
+}
+
+// Sorted positions per chunk: at most 1024 chunks (a run over all of them is joined by 16 groups of 64), at least eight
+// positions (a thread's loads in flight).
+int chunk_of(int n) { const int c = (n + 1023) / 1024; return c < 8 ? 8 : c; }
+
+bool sorts_in_one_cta(int n, int V) { return n <= kSortMax && V <= kSortMaxV; }
+
+struct EmbedSpace {
+    size_t a, b, scratch, parts, total;
+};
+EmbedSpace embed_space(int n, int d, int V) {
+    EmbedSpace s;
+    size_t at = 0;
+    auto take = [&](size_t k) { const size_t o = at; at = align_up(at + k, 256); return o; };
+    const bool one = sorts_in_one_cta(n, V);
+    const int chunk = chunk_of(n), n_chunks = (n + chunk - 1) / chunk;
+    s.a = take((size_t)n * 8);
+    s.b = take(one ? 0 : (size_t)n * 8);
+    s.scratch = take(one ? 0 : sort_words_scratch_bytes(n));
+    s.parts = take((size_t)n_chunks * 2 * d * 4);
+    s.total = at > 256 ? at : 256;
+    return s;
+}
+
+}  // namespace
+
+ee_status embed_launch(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, int num_sms,
+                       cudaStream_t stream) {
+    const long long total = (long long)n * (d / 8);
+    const long long want = (total + 255) / 256, most = (long long)num_sms * 8;
+    return launch_pdl(embed_kernel, dim3((unsigned)(want < most ? want : most)), 256, 0, stream, static_cast<const __nv_bfloat16*>(table), V, d / 8,
+                      tokens, n, scale, static_cast<__nv_bfloat16*>(out), ld_out) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+size_t embed_grad_workspace_bytes(int n, int d, int V) { return embed_space(n, d, V).total; }
+
+ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable, int wide,
+                            int accumulate, void* workspace, int device, int num_sms, cudaStream_t stream) {
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    const EmbedSpace s = embed_space(n, d, V);
+    const long long clear_vecs = accumulate ? 0 : (long long)V * d * (wide ? 4 : 2) / 16;
+    int bits = 1;                                                        // tokens 0 .. V (V: takes no part)
+    while (bits < 31 && (V >> bits) != 0) ++bits;
+    const int passes = (bits + 7) / 8;
+    EmbedGrad g;
+    g.dout = static_cast<const __nv_bfloat16*>(dout); g.ld_dout = ld_dout;
+    g.n = n; g.V = V; g.nvec = d / 8;
+    g.chunk = chunk_of(n); g.n_chunks = (n + g.chunk - 1) / g.chunk;
+    g.scale = scale; g.dtable = dtable; g.wide = wide; g.add = accumulate;
+    g.parts = reinterpret_cast<float*>(ws + s.parts);
+    if (sorts_in_one_cta(n, V)) {
+        static bool configured[kMaxDevices] = {};
+        if (!configured[device]) {
+            if (cudaFuncSetAttribute(embed_sort_clear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSortSmem) != cudaSuccess)
+                return EE_ERR_CUDA;
+            configured[device] = true;
+        }
+        const long long others = (clear_vecs + kSortThreads - 1) / kSortThreads;
+        const int grid = 1 + (int)(others < num_sms - 1 ? others : num_sms - 1);
+        int2* sorted = reinterpret_cast<int2*>(ws + s.a);
+        if (launch_pdl(embed_sort_clear_kernel, dim3(grid), kSortThreads, kSortSmem, stream, tokens, n, V, passes, sorted,
+                       static_cast<uint4*>(dtable), clear_vecs) != cudaSuccess)
+            return EE_ERR_CUDA;
+        g.sorted = sorted;
+    } else {
+        u64 *a = reinterpret_cast<u64*>(ws + s.a), *b = reinterpret_cast<u64*>(ws + s.b);
+        embed_words_kernel<<<num_sms * 8, 256, 0, stream>>>(tokens, n, V, a, static_cast<uint4*>(dtable), clear_vecs);
+        if (cudaGetLastError() != cudaSuccess) return EE_ERR_CUDA;
+        const u64* sorted = nullptr;
+        const ee_status st = sort_words_launch(a, b, n, 32, passes, ws + s.scratch, &sorted, stream);
+        if (st != EE_OK) return st;
+        g.sorted = reinterpret_cast<const int2*>(sorted);
+    }
+    const int nvec = d / 8;
+    if (launch_pdl(embed_sum_kernel, dim3(g.n_chunks, (nvec + kSumThreads - 1) / kSumThreads), kSumThreads, 0, stream, g) != cudaSuccess ||
+        launch_pdl(embed_join_kernel, dim3(g.n_chunks, (nvec + 15) / 16), 256, 0, stream, g) != cudaSuccess)
+        return EE_ERR_CUDA;
+    return EE_OK;
+}
+
+}  // namespace ee

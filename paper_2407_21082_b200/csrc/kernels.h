@@ -124,6 +124,29 @@ size_t ce_workspace_bytes(int M, int d, int V, bool grad);
 ee_status ce_launch(const CeArgs& a);
 ee_status ce_grad_launch(const CeArgs& a);
 
+ee_status layer_norm_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int M, int d,
+                            cudaStream_t stream);      // y bf16 [M][d], dense
+
+// ---- heads with weights in 4 bits ----
+size_t q4_weight_bytes(int V, int d, int group);
+ee_status q4_pack_launch(const void* W, int V, int d, int group, void* q4, cudaStream_t stream);
+ee_status q4_unpack_launch(const void* q4, int V, int d, int group, void* W, cudaStream_t stream);
+size_t q4_head_workspace_bytes(int M, int d);
+ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group);      // a.W is not read
+
+// ---- embedding lookup and its gradient ----
+ee_status embed_launch(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, int num_sms,
+                       cudaStream_t stream);
+size_t embed_grad_workspace_bytes(int n, int d, int V);
+ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable, int wide,
+                            int accumulate, void* workspace, int device, int num_sms, cudaStream_t stream);
+
+// ---- stable radix sort of 64-bit words by `passes` digits of eight bits from bit `first_shift` on (calibrate.cu); a holds
+//      the words, *sorted is a or b ----
+size_t sort_words_scratch_bytes(int n);
+ee_status sort_words_launch(unsigned long long* a, unsigned long long* b, int n, int first_shift, int passes, void* scratch,
+                            const unsigned long long** sorted, cudaStream_t stream);
+
 // ---- commit step of a DSSD round (k <= 32) ----
 ee_status dssd_commit_launch(const int* draft_tok, const unsigned char* draft_exit_mask, const int* verify_tok, int S, int k,
                              int kv, int eos, int* out_tok, int cap, int* seq_len, unsigned char* finished, int* draft_len,

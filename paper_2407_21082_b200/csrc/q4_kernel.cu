@@ -1,0 +1,369 @@
+// Exit heads whose weights are held in 4 bits: whole numbers q = -8 .. 7 with one bf16 scale s per row and group of 32, 64
+// or 128 columns.  What they stand for is w = bf16(s q); the head itself is that of ee_exit_head (LayerNorm, projection,
+// entropy, argmax, decision) with these weights.  Drafting reads the whole head for a handful of tokens, so a call's time
+// is the time of that read: 4.25 bits per weight at a group of 64 instead of 16.
+//
+// The product with the scale is rounded to bf16 because the tensor cores take bf16 operands; it is part of the
+// definition (ee_head_q4_unpack returns the same values), so nothing is lost between the two.
+//
+// Layout of a packed head: 16-row tiles; a tile is a sequence of blocks of 64 columns, 512 bytes each; lane (g, c) =
+// (lane / 4, lane % 4) of a warp owns 16 bytes of a block: columns 16c .. 16c + 15 of row g, then of row g + 8.  That is the
+// operand of four m16n8k16 products if the contraction is walked in the order "lane c: columns 16c + 4s .. 16c + 4s + 3 in
+// step s", which costs nothing as long as the other operand is read in the same order: a lane's share of y is then 32
+// consecutive bytes as well.  Inside a 32-bit word (8 columns) column 2i is nibble i and column 2i + 1 nibble i + 4, each as
+// q + 8, so that one shift and one logic operation make the two bf16 numbers 128 + (q + 8) of a register; subtracting
+// 136 is exact.  The scales lie behind the weights: [tile][group][8] words holding rows g and g + 8.  Rows beyond V and
+// columns beyond d are q = 0.
+#include "common.cuh"
+#include "layer_norm.cuh"
+#include "kernels.h"
+
+namespace ee {
+
+namespace {
+
+constexpr int kWarps = 24;                       // 3552 warps on 148 SMs: one 16-row tile each for V = 50304
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxSlabRows = 64;
+constexpr int kUnroll = 4;                       // blocks (512 bytes of a tile) in flight per warp, twice
+constexpr size_t kSmemBudget = 226 * 1024;
+
+struct Q4Layout {
+    int tiles, blocks, groups;                   // 16-row tiles, 64-column blocks, scale groups per row
+};
+__host__ __device__ inline Q4Layout q4_layout(int V, int d, int group) {
+    Q4Layout l;
+    l.tiles = (V + 15) / 16;
+    l.blocks = (d + 63) / 64;
+    l.groups = (l.blocks * 64 + group - 1) / group;
+    return l;
+}
+
+__device__ __forceinline__ uint32_t hsub2_bf16(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t hmul2_bf16(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Columns 2i and 2i + 1 of a word's eight, times the scale (in both halves of s2), as two bf16 numbers.
+__device__ __forceinline__ uint32_t q4_pair(uint32_t word, int i, uint32_t s2) {
+    const uint32_t biased = ((word >> (4 * i)) & 0x000f000fu) | 0x43004300u;      // 128 + (q + 8)
+    return hmul2_bf16(hsub2_bf16(biased, 0x43084308u), s2);                       // the difference is exact, the product rounded once
+}
+__device__ __forceinline__ uint32_t low_twice(uint32_t v) { return __byte_perm(v, 0, 0x1010); }
+__device__ __forceinline__ uint32_t high_twice(uint32_t v) { return __byte_perm(v, 0, 0x3232); }
+
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// ---------------------------------------------------------------------------------------------------- writing and reading
+
+// Eight bf16 (a 16-byte vector) -> a word of nibbles, q = nearest whole number of w / s, ties to the even one.
+__device__ __forceinline__ uint32_t q4_word(uint4 v, float s) {
+    const float x[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int q = s > 0.f ? max(-8, min(7, __float2int_rn(__fdiv_rn(x[j], s)))) : 0;
+        w |= (uint32_t)(q + 8) << (4 * ((j >> 1) + 4 * (j & 1)));
+    }
+    return w;
+}
+__device__ __forceinline__ float amax8(uint4 v) {
+    float m = fmaxf(fabsf(bf16_lo(v.x)), fabsf(bf16_hi(v.x)));
+    m = fmaxf(m, fmaxf(fabsf(bf16_lo(v.y)), fabsf(bf16_hi(v.y))));
+    m = fmaxf(m, fmaxf(fabsf(bf16_lo(v.z)), fabsf(bf16_hi(v.z))));
+    return fmaxf(m, fmaxf(fabsf(bf16_lo(v.w)), fabsf(bf16_hi(v.w))));
+}
+
+// A warp per 16 rows x 128 columns (two blocks, so that a group of 128 lies inside).
+__global__ void __launch_bounds__(256) q4_pack_kernel(const __nv_bfloat16* W, int V, int d, int group, uint4* weights, uint32_t* scales) {
+    launch_dependents();
+    const Q4Layout l = q4_layout(V, d, group);
+    const int pairs = (l.blocks + 1) / 2;
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    if (unit >= (long long)l.tiles * pairs) return;
+    const int tile = (int)(unit / pairs), b0 = 2 * (int)(unit % pairs);
+    uint4 v[2][2][2];                              // [block][row g, row g + 8][first, second eight columns]
+    float m[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int row = tile * 16 + g + 8 * r;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int col = (b0 + b) * 64 + c * 16 + e * 8;
+                v[b][r][e] = (row < V && col < d) ? ld_dep(reinterpret_cast<const uint4*>(W + (size_t)row * d + col)) : make_uint4(0, 0, 0, 0);
+            }
+            m[b][r] = fmaxf(amax8(v[b][r][0]), amax8(v[b][r][1]));
+            m[b][r] = fmaxf(m[b][r], __shfl_xor_sync(0xffffffffu, m[b][r], 1));
+            if (group >= 64) m[b][r] = fmaxf(m[b][r], __shfl_xor_sync(0xffffffffu, m[b][r], 2));
+        }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+        if (group == 128) m[0][r] = m[1][r] = fmaxf(m[0][r], m[1][r]);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+        if (b0 + b >= l.blocks) break;
+        const uint32_t s2 = pack_bf16(__fdiv_rn(m[b][0], 7.f), __fdiv_rn(m[b][1], 7.f));
+        const float s0 = bf16_lo(s2), s1 = bf16_hi(s2);
+        weights[((size_t)tile * l.blocks + b0 + b) * 32 + lane] =
+            make_uint4(q4_word(v[b][0][0], s0), q4_word(v[b][0][1], s0), q4_word(v[b][1][0], s1), q4_word(v[b][1][1], s1));
+        const int col = (b0 + b) * 64 + c * 16;
+        if (col % group == 0) scales[((size_t)tile * l.groups + col / group) * 8 + g] = s2;
+    }
+}
+
+__global__ void __launch_bounds__(256) q4_unpack_kernel(const uint4* weights, const uint32_t* scales, int V, int d, int group, __nv_bfloat16* W) {
+    launch_dependents();
+    const Q4Layout l = q4_layout(V, d, group);
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    grid_dependency_wait();
+    if (unit >= (long long)l.tiles * l.blocks) return;
+    const int tile = (int)(unit / l.blocks), b = (int)(unit % l.blocks);
+    const int col = b * 64 + c * 16;
+    const uint4 w = ld_dep(weights + unit * 32 + lane);
+    const uint32_t s2 = ld_dep(scales + ((size_t)tile * l.groups + col / group) * 8 + g);
+    const uint32_t words[2][2] = {{w.x, w.y}, {w.z, w.w}};
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = tile * 16 + g + 8 * r;
+        const uint32_t s = r ? high_twice(s2) : low_twice(s2);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (row < V && col + e * 8 < d)
+                *reinterpret_cast<uint4*>(W + (size_t)row * d + col + e * 8) =
+                    make_uint4(q4_pair(words[r][e], 0, s), q4_pair(words[r][e], 1, s), q4_pair(words[r][e], 2, s), q4_pair(words[r][e], 3, s));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- the head
+
+struct Q4Params {
+    const uint4* weights;
+    const uint32_t* scales;
+    const __nv_bfloat16* y;        // [M][d]
+    int M, d, V, group;
+    State* parts;                  // [ctas][NT * 8]
+    const float* tau_per_row;
+    float tau;
+    int* argmax;
+    float* entropy;
+    float* maxprob;
+    unsigned char* exit_mask;
+    Control* ctrl;
+};
+
+// Bytes between two rows of y in shared memory: 16 more than a multiple of 128, so that the eight lanes of a 16-byte access
+// (two rows, four columns 32 bytes apart) touch every bank once.
+__host__ __device__ inline int y_row_bytes(int d) { return (d + 63) / 64 * 128 + 16; }
+
+// Up to NT * 8 rows: a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all rows
+// of y (in shared memory); the CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges
+// the CTAs' states and decides.
+template <int NT>
+__global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_constant__ Q4Params p) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int is_last;
+    const Q4Layout l = q4_layout(p.V, p.d, p.group);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int ld = y_row_bytes(p.d);
+    State* states = reinterpret_cast<State*>(smem + NT * 8 * ld);        // [kWarps][NT * 8]
+    launch_dependents();
+
+    uint4 w[kUnroll];
+    uint32_t sc[kUnroll];
+    auto load = [&](int tile, int b0) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (b0 + u < l.blocks) {
+                w[u] = __ldg(p.weights + ((size_t)tile * l.blocks + b0 + u) * 32 + lane);
+                sc[u] = __ldg(p.scales + ((size_t)tile * l.groups + ((b0 + u) * 64 + c * 16) / p.group) * 8 + g);
+            }
+    };
+    int tile = blockIdx.x + gridDim.x * warp;
+    if (tile < l.tiles) load(tile, 0);                                   // weights are constants of the stream
+    grid_dependency_wait();
+    for (int i = threadIdx.x; i < NT * 8 * l.blocks * 8; i += kThreads) {
+        const int row = i / (l.blocks * 8), v = i - row * (l.blocks * 8);
+        const uint4 x = (row < p.M && v * 8 < p.d) ? ld_dep(reinterpret_cast<const uint4*>(p.y + (size_t)row * p.d) + v) : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(smem + row * ld + v * 16) = x;
+    }
+    __syncthreads();
+
+    State* mine = states + warp * (NT * 8);
+    for (int i = lane; i < NT * 8; i += 32) mine[i] = state_empty();
+    __syncwarp();
+    const unsigned char* ybase = smem + g * ld + c * 32;
+    for (; tile < l.tiles; tile += gridDim.x * kWarps) {
+        float acc[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+        for (int b0 = 0; b0 < l.blocks; b0 += kUnroll) {
+            uint4 cur[kUnroll];
+            uint32_t cs[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) { cur[u] = w[u]; cs[u] = sc[u]; }
+            if (b0 + kUnroll < l.blocks) load(tile, b0 + kUnroll);
+            else if (tile + gridDim.x * kWarps < l.tiles) load(tile + gridDim.x * kWarps, 0);
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                if (b0 + u < l.blocks) {
+                    const uint32_t sg = low_twice(cs[u]), sh = high_twice(cs[u]);
+                    const unsigned char* yb = ybase + (b0 + u) * 128;
+                    // a block is summed by itself and added in fp32: the tensor core cuts off, rather than rounds, what falls
+                    // below the last bit of its accumulator, which over a whole row adds up (M = 1, d = 1024: entropy off by 1.4e-5
+                    // of itself when accumulated in one go)
+                    float part[NT][4];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) part[t][0] = part[t][1] = part[t][2] = part[t][3] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {                        // steps 2e and 2e + 1: eight columns of each lane
+                        const uint32_t wg = e ? cur[u].y : cur[u].x, wh = e ? cur[u].w : cur[u].z;
+                        uint32_t a[2][4];
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            a[s][0] = q4_pair(wg, 2 * s, sg);
+                            a[s][1] = q4_pair(wh, 2 * s, sh);
+                            a[s][2] = q4_pair(wg, 2 * s + 1, sg);
+                            a[s][3] = q4_pair(wh, 2 * s + 1, sh);
+                        }
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            const uint4 y = *reinterpret_cast<const uint4*>(yb + t * 8 * ld + e * 16);
+                            mma_16816(part[t], a[0][0], a[0][1], a[0][2], a[0][3], y.x, y.y);
+                            mma_16816(part[t], a[1][0], a[1][1], a[1][2], a[1][3], y.z, y.w);
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[t][j] += part[t][j];
+                }
+            }
+        }
+        const int v = tile * 16 + g;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {                                // token 2c + j of the eight: rows g and g + 8, then over g
+                State s = state_empty();
+                if (v < p.V) state_push(s, acc[t][j], v);
+                if (v + 8 < p.V) state_push(s, acc[t][2 + j], v + 8);
+                s = state_reduce_lanes<4, 16>(s);
+                if (g == 0) {
+                    State o = mine[t * 8 + 2 * c + j];
+                    state_merge(o, s);
+                    mine[t * 8 + 2 * c + j] = o;
+                }
+            }
+    }
+    __syncthreads();
+    for (int tok = threadIdx.x; tok < p.M; tok += kThreads) {
+        State s = states[tok];
+        for (int k = 1; k < kWarps; ++k) state_merge(s, states[k * (NT * 8) + tok]);
+        p.parts[(size_t)blockIdx.x * (NT * 8) + tok] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) is_last = ticket_arrive_is_last(&p.ctrl->head_ticket[0], gridDim.x) ? 1 : 0;
+    __syncthreads();
+    if (!is_last) return;
+    if (gridDim.x <= 160)                                                // one token per warp at a time: registers are short here
+        merge_token_batches<1, 5>(p.parts, false, gridDim.x, NT * 8, p.M, warp, kWarps, lane, p.tau_per_row, p.tau, p.argmax, p.entropy,
+                                  p.maxprob, p.exit_mask);
+    else
+        merge_token_batches<1, 8>(p.parts, false, gridDim.x, NT * 8, p.M, warp, kWarps, lane, p.tau_per_row, p.tau, p.argmax, p.entropy,
+                                  p.maxprob, p.exit_mask);
+    if (threadIdx.x == 0) p.ctrl->head_ticket[0] = 0;                    // ready for the next launch
+}
+
+size_t q4_smem(int nt, int d) { return (size_t)nt * 8 * y_row_bytes(d) + (size_t)kWarps * nt * 8 * sizeof(State); }
+
+// Rows one launch takes: whole tiles of eight tokens in shared memory, at most 64.
+int slab_rows(int d) {
+    int nt = kMaxSlabRows / 8;
+    while (nt > 1 && q4_smem(nt, d) > kSmemBudget) nt = nt > 4 ? 4 : nt / 2;
+    return nt * 8;
+}
+
+template <int NT>
+ee_status launch_head(const Q4Params& p, int num_sms, int device, cudaStream_t stream) {
+    static bool configured[kMaxDevices] = {};
+    if (!configured[device]) {
+        if (cudaFuncSetAttribute(q4_head_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess) return EE_ERR_CUDA;
+        configured[device] = true;
+    }
+    const int tiles = (p.V + 15) / 16;
+    int grid = tiles < num_sms ? tiles : num_sms;
+    if (grid > kStreamMaxCtas) grid = kStreamMaxCtas;
+    return launch_pdl(q4_head_kernel<NT>, dim3(grid), kThreads, q4_smem(NT, p.d), stream, p) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+size_t parts_bytes() { return (size_t)kStreamMaxCtas * kMaxSlabRows * sizeof(State); }
+
+}  // namespace
+
+size_t q4_weight_bytes(int V, int d, int group) {
+    const Q4Layout l = q4_layout(V, d, group);
+    return align_up((size_t)l.tiles * l.blocks * 512, 256) + align_up((size_t)l.tiles * l.groups * 32, 256);
+}
+static const uint32_t* q4_scales(const void* q4, int V, int d, int group) {
+    const Q4Layout l = q4_layout(V, d, group);
+    return reinterpret_cast<const uint32_t*>(static_cast<const unsigned char*>(q4) + align_up((size_t)l.tiles * l.blocks * 512, 256));
+}
+
+ee_status q4_pack_launch(const void* W, int V, int d, int group, void* q4, cudaStream_t stream) {
+    const Q4Layout l = q4_layout(V, d, group);
+    const long long units = (long long)l.tiles * ((l.blocks + 1) / 2);
+    return launch_pdl(q4_pack_kernel, dim3((unsigned)((units + 7) / 8)), 256, 0, stream, static_cast<const __nv_bfloat16*>(W), V, d, group,
+                      static_cast<uint4*>(q4), const_cast<uint32_t*>(q4_scales(q4, V, d, group))) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+ee_status q4_unpack_launch(const void* q4, int V, int d, int group, void* W, cudaStream_t stream) {
+    const Q4Layout l = q4_layout(V, d, group);
+    const long long units = (long long)l.tiles * l.blocks;
+    return launch_pdl(q4_unpack_kernel, dim3((unsigned)((units + 7) / 8)), 256, 0, stream, static_cast<const uint4*>(q4),
+                      q4_scales(q4, V, d, group), V, d, group, static_cast<__nv_bfloat16*>(W)) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+size_t q4_head_workspace_bytes(int M, int d) { return kCtrlBytes + parts_bytes() + align_up((size_t)M * d * 2, 256); }
+
+ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group) {
+    unsigned char* ws = static_cast<unsigned char*>(a.workspace);
+    __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(ws + kCtrlBytes + parts_bytes());
+    const ee_status st = layer_norm_launch(a.h, a.ld_h, a.gamma, a.beta, a.ln_eps, y, a.M, a.d, a.stream);
+    if (st != EE_OK) return st;
+    const int slab = slab_rows(a.d);
+    for (int r0 = 0; r0 < a.M; r0 += slab) {
+        Q4Params p;
+        p.weights = static_cast<const uint4*>(q4);
+        p.scales = q4_scales(q4, a.V, a.d, group);
+        p.y = y + (size_t)r0 * a.d;
+        p.M = a.M - r0 < slab ? a.M - r0 : slab;
+        p.d = a.d; p.V = a.V; p.group = group;
+        p.parts = reinterpret_cast<State*>(ws + kCtrlBytes);
+        p.tau_per_row = a.tau_per_row ? a.tau_per_row + r0 : nullptr;
+        p.tau = a.tau;
+        p.argmax = a.argmax + r0; p.entropy = a.entropy + r0; p.maxprob = a.maxprob + r0; p.exit_mask = a.exit_mask + r0;
+        p.ctrl = reinterpret_cast<Control*>(ws);
+        const int nt = (p.M + 7) / 8;
+        const ee_status s = nt <= 1 ? launch_head<1>(p, a.num_sms, a.device, a.stream) : nt <= 2 ? launch_head<2>(p, a.num_sms, a.device, a.stream)
+                          : nt <= 4 ? launch_head<4>(p, a.num_sms, a.device, a.stream) : launch_head<8>(p, a.num_sms, a.device, a.stream);
+        if (s != EE_OK) return s;
+    }
+    return EE_OK;
+}
+
+}  // namespace ee
