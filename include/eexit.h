@@ -488,7 +488,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
  *   (ties to the even one; 0 where s = 0), kept within -8 .. 7;          W4[v, j] = bf16( s q )
  * W must be finite.  group is 32, 64 or 128; d % group == 0, group <= d <= 8192, V >= 1.  A packed head is
  * ee_head_q4_bytes(V, d, group) bytes (0 if a size is invalid), 256-byte aligned, in a layout of the library's own;
- * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous, 16-byte aligned.
+ * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous.  W and W4 are 32-byte aligned.
  *
  * ee_exit_head_q4 is ee_exit_head with W4 for W: same definition, outputs, strides, alignment and rules (the packed
  * head is a constant of the stream).  Any M; rows beyond those whose LayerNorm output fits shared memory go in further

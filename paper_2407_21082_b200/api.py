@@ -30,7 +30,8 @@ def _ptr(t):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    # torch.cuda.current_stream() builds a Stream object, four to five microseconds a call; this is the handle it would hold
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _bf16(t: torch.Tensor) -> torch.Tensor:
@@ -490,7 +491,7 @@ def _workspace_of(nbytes: int, where: str, device) -> torch.Tensor:
 def _on_current(t: torch.Tensor, name: str) -> torch.Tensor:
     """The library launches on the current device: a tensor of another one is refused."""
     _dev(t, name)
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
     return t
 

@@ -694,7 +694,7 @@ size_t ee_head_q4_bytes(int V, int d, int group) {
 ee_status ee_head_q4_pack(const void* W, int V, int d, int group, void* q4, size_t q4_bytes, void* stream) {
     if (!q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
     if (!W || !q4) return EE_ERR_NULL;
-    if (!aligned(W, 16) || !aligned(q4, 256)) return EE_ERR_ALIGN;
+    if (!aligned(W, 32) || !aligned(q4, 256)) return EE_ERR_ALIGN;
     if (q4_bytes < q4_weight_bytes(V, d, group)) return EE_ERR_WORKSPACE;
     int device, num_sms;
     const ee_status dev = current_device(&device, &num_sms);
@@ -705,7 +705,7 @@ ee_status ee_head_q4_pack(const void* W, int V, int d, int group, void* q4, size
 ee_status ee_head_q4_unpack(const void* q4, size_t q4_bytes, int V, int d, int group, void* W, void* stream) {
     if (!q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
     if (!W || !q4) return EE_ERR_NULL;
-    if (!aligned(W, 16) || !aligned(q4, 256)) return EE_ERR_ALIGN;
+    if (!aligned(W, 32) || !aligned(q4, 256)) return EE_ERR_ALIGN;
     if (q4_bytes < q4_weight_bytes(V, d, group)) return EE_ERR_WORKSPACE;
     int device, num_sms;
     const ee_status dev = current_device(&device, &num_sms);

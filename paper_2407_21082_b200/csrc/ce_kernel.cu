@@ -7,14 +7,15 @@
 //
 // Four matrix products of 2 M V d operations each (the logits twice: they are recomputed in the backward pass), all by
 // one persistent TMA + tcgen05 kernel whose mode decides which operand runs which way and what its epilogue does:
-//   kStats  A = y, B = W (both K-major): per row and 64-column group of the tile the running maximum and sum, and
+//   kStats  A = y, B = W (both K-major): per row and tile the maximum and the sum of exponentials, and
 //           the logit at the label; nothing else leaves the chip
 //   kGrad   the same product for a piece of the vocabulary; the epilogue turns it into G, rounded to bf16
 //   kDy     A = G, B = W with the contraction over the vocabulary: W is read as it lies, as an MN-major operand; fp32
 //           results are stored (first piece) or added (later ones, one launch after the other, so in a fixed order)
 //           into one slab per split of the contraction
 //   kDw     A = G, B = y with the contraction over the rows: both MN-major as they lie
-// The pieces keep G at kGradPieceBytes at most, which the L2 holds in part; all of it is one piece for small batches.
+// The pieces keep G at 128 MB, or a quarter of the whole where that is more: a piece costs three launches and, in kDy, one
+// way of dy to memory and back.  For small batches one piece is all of it.
 // G is rounded to bf16 because the tensor cores take dW and dy from it: each of its elements is off by at most 2^-9
 // of itself, independently, which leaves dy and dW off by about as much as their own rounding to bf16.  G is held
 // without the mean's 1 / n, which is applied to the fp32 results.  Rows whose label is outside [0, V) take no part: their
@@ -32,17 +33,17 @@ namespace {
 
 constexpr int BM = 128;
 constexpr int BK = kRoleBK;
-constexpr int BN = 256;
-constexpr int kThreads = 320;                   // producer warp, MMA warp, eight epilogue warps
+constexpr int BN = 256;                         // widest column tile; dy and dW take 192 or 128 where that wastes less of d
+constexpr int kThreads = 576;                   // producer warp, MMA warp, sixteen epilogue warps
 constexpr int kATileBytes = BM * BK * 2;
-constexpr int kBarBytes = 512;
-constexpr int kStageWarpBytes = 4096;           // an epilogue warp's 32 rows x 128 bytes on their way to memory
+constexpr int kBarBytes = 512 + 8192;             // barriers, then two sets of 4 x 128 partial statistics (kStats)
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kMaxStages = 12;
 constexpr int kAccStride = 256;
 constexpr int kTmemCols = 512;
+constexpr int kMinTile = 64;                    // narrowest tile of the logits
 constexpr int kMaxSplits = 32;
-constexpr size_t kGradPieceBytes = (size_t)128 << 20;
+constexpr size_t kGradPieceBytes = (size_t)128 << 20;      // or a quarter of all of G, whichever is more
 
 enum CeMode { kStats, kGrad, kDy, kDw };
 template <int kMode> struct Layout {
@@ -51,7 +52,7 @@ template <int kMode> struct Layout {
 };
 
 struct CeMaps {
-    CUtensorMap a, b, out;
+    CUtensorMap a, b;
 };
 
 struct CeParams {
@@ -63,17 +64,25 @@ struct CeParams {
     int n_cols;            // columns of the output that exist (vocabulary of the piece, or d)
     int m_rows;            // rows of the output that exist
     int v0;                // first vocabulary row of the piece
+    int bn;                // columns of a tile: a multiple of 16 up to 256 (kStats, kGrad), 256, 192 or 128 (kDy, kDw)
+    int a_rows;            // rows of A a CTA loads: 128, or 64 where no more exist (the products read on into what follows in
+                           // shared memory, which reaches nothing but accumulator rows that nobody reads)
     int n_stages;
+    int kbs;               // k-blocks per ring slot: 2 if the operands' widths allow one request for both, else 1
     int a_3d, b_3d;        // an MN-major operand's 64-wide blocks come with one request
     int add;               // kDy: add into the slab; kDw: add to what dW holds
-    float2* parts;         // kStats: [4 * n_tiles][M] maximum and sum
+    float2* parts;         // kStats: [n_tiles][M] maximum and sum
     float* z_label;        // kStats: [M]
     const int* labels;
     const float* lse;      // kGrad
     const float* dce;      // row weights, or NULL: every counted row 1, and `scale` at the end
     const float* dloss;    // fp32 [1] or NULL (one)
     const float* loss;     // loss[1] = number of counted rows
+    __nv_bfloat16* G;      // kGrad: [M][ld_g]
+    int ld_g;
+    float* dy;             // kDy: [splits][M][d]
     __nv_bfloat16* dW;
+    int sectors;           // kDw: rows of dW begin on 32-byte sectors
     int V;
     Control* ctrl;
 };
@@ -91,28 +100,100 @@ __device__ __forceinline__ float row_weight(const int* labels, const float* dce,
     return dce ? ld_dep(dce + row) : 1.f;
 }
 
-// An operand tile of `rows` elements of its M or N dimension from mn0 on, 64 of the contraction from k0 on.
+// An operand tile: `rows` elements of its M or N dimension from mn0 on, kbs blocks of 64 of the contraction from k0 on.  K-major
+// tiles of two blocks come as [block][row][64], MN-major ones as [64 of the rows][128 of the contraction][64]; both with one
+// request where the maps allow it (three_d).
 template <bool kMn, bool kPair>
-__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* m, int k0, int mn0, int rows, int three_d, uint32_t bar) {
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* m, int k0, int mn0, int rows, int kbs, int three_d, uint32_t bar) {
     if (!kMn) {
-        if (kPair) ptx::tma_load_2d_pair(dst, m, k0, mn0, bar);
-        else ptx::tma_load_2d(dst, m, k0, mn0, bar);
+        if (three_d) {
+            if (kPair) ptx::tma_load_3d_pair(dst, m, 0, mn0, k0 >> 6, bar);
+            else ptx::tma_load_3d(dst, m, 0, mn0, k0 >> 6, bar);
+        } else {
+            for (int b = 0; b < kbs; ++b) {
+                if (kPair) ptx::tma_load_2d_pair(dst + b * rows * 128, m, k0 + b * 64, mn0, bar);
+                else ptx::tma_load_2d(dst + b * rows * 128, m, k0 + b * 64, mn0, bar);
+            }
+        }
     } else if (three_d) {
         if (kPair) ptx::tma_load_3d_pair(dst, m, 0, k0, mn0 >> 6, bar);
         else ptx::tma_load_3d(dst, m, 0, k0, mn0 >> 6, bar);
     } else {
         for (int c = 0; c < rows; c += 64) {
-            if (kPair) ptx::tma_load_2d_pair(dst + c * 128, m, mn0 + c, k0, bar);
-            else ptx::tma_load_2d(dst + c * 128, m, mn0 + c, k0, bar);
+            if (kPair) ptx::tma_load_2d_pair(dst + c * 128 * kbs, m, mn0 + c, k0, bar);
+            else ptx::tma_load_2d(dst + c * 128 * kbs, m, mn0 + c, k0, bar);
         }
+    }
+}
+
+// Maximum and sum of exponentials of 64 logits (the first nvalid real), four chains each.
+template <bool kFull>
+__device__ __forceinline__ void fold_stats(const float (&z)[2][32], int nvalid, float& m, float& s) {
+    float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F}, cs[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 64; ++j)
+        if (kFull || j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[j >> 5][j & 31]);
+    m = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
+#pragma unroll
+    for (int j = 0; j < 64; ++j)
+        if (kFull || j < nvalid) cs[j & 3] += ex2((z[j >> 5][j & 31] - m) * kLog2e);
+    s = (cs[0] + cs[1]) + (cs[2] + cs[3]);
+}
+
+// 32 consecutive values of a row (the first n of them, a multiple of eight) to memory: as bf16 in whole sectors of 32 bytes where
+// rows begin on one, in halves otherwise; as fp32 (rows are multiples of 32 bytes), stored or added.
+__device__ __forceinline__ void store_bf16x32(__nv_bfloat16* out, const float (&z)[32], int n, bool sectors) {
+    uint32_t w[16];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) w[q] = pack_bf16(z[2 * q], z[2 * q + 1]);
+    if (sectors) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (q * 16 < n)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + q * 16), "r"(w[q * 8]), "r"(w[q * 8 + 1]),
+                             "r"(w[q * 8 + 2]), "r"(w[q * 8 + 3]), "r"(w[q * 8 + 4]), "r"(w[q * 8 + 5]), "r"(w[q * 8 + 6]), "r"(w[q * 8 + 7])
+                             : "memory");
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q * 8 < n) *reinterpret_cast<uint4*>(out + q * 8) = make_uint4(w[q * 4], w[q * 4 + 1], w[q * 4 + 2], w[q * 4 + 3]);
+    }
+}
+__device__ __forceinline__ void store_f32x32(float* out, const float (&z)[32], int n, int add) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q * 8 >= n) break;
+        const float* v = z + q * 8;
+        if (add) {
+            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(out + q * 8), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+            asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(out + q * 8 + 4), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+        } else {
+            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + q * 8), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                         "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                         : "memory");
+        }
+    }
+}
+__device__ __forceinline__ void add_bf16x32(const __nv_bfloat16* old, float (&z)[32], int n) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q * 8 >= n) break;
+        const uint4 o = ld_dep(reinterpret_cast<const uint4*>(old + q * 8));
+        z[q * 8 + 0] += bf16_lo(o.x); z[q * 8 + 1] += bf16_hi(o.x);
+        z[q * 8 + 2] += bf16_lo(o.y); z[q * 8 + 3] += bf16_hi(o.y);
+        z[q * 8 + 4] += bf16_lo(o.z); z[q * 8 + 5] += bf16_hi(o.z);
+        z[q * 8 + 6] += bf16_lo(o.w); z[q * 8 + 7] += bf16_hi(o.w);
     }
 }
 
 template <int kMode, bool kPair>
 __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ CeMaps maps, const CeParams p) {
     constexpr bool a_mn = Layout<kMode>::a_mn, b_mn = Layout<kMode>::b_mn;
-    constexpr int b_rows = kPair ? BN / 2 : BN;
-    constexpr int b_tile_bytes = b_rows * BK * 2;
+    const int b_rows = kPair ? p.bn / 2 : p.bn;                          // columns whose operand this CTA stages,
+    const int b_blocks = b_mn ? (b_rows + 63) & ~63 : b_rows;             // whole blocks of 64 of an MN-major one
+    const int kbs = p.kbs;
+    const int a_block = p.a_rows * BK * 2;
+    const int a_stage = a_block * kbs, b_stage = b_blocks * BK * 2 * kbs;
     const int S = p.n_stages;
     const uint32_t rank = kPair ? ptx::cluster_cta_rank() : 0u;
     const int worker = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
@@ -121,9 +202,8 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     unsigned char* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
     const uint32_t a_base = ptx::smem_addr(smem);
-    const uint32_t b_base = a_base + S * kATileBytes;
-    unsigned char* staging = smem + S * (kATileBytes + b_tile_bytes);
-    unsigned char* bar_mem = staging + (kMode == kStats ? 0 : 8 * kStageWarpBytes);
+    const uint32_t b_base = a_base + S * a_stage;
+    unsigned char* bar_mem = smem + S * (a_stage + b_stage);
     const uint32_t bar_base = ptx::smem_addr(bar_mem);
     auto full_bar = [&](int s) { return bar_base + 8u * s; };
     auto empty_bar = [&](int s) { return bar_base + 8u * (S + s); };
@@ -142,14 +222,13 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(tfull_bar(b), 1);
-            ptx::mbar_init(tempty_bar(b), kPair ? 16 : 8);
+            ptx::mbar_init(tempty_bar(b), kPair ? 32 : 16);
         }
         ptx::mbar_init(drain_bar, 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&maps.a);
         ptx::prefetch_tensormap(&maps.b);
-        if (kMode != kStats) ptx::prefetch_tensormap(&maps.out);
     }
     if (warp == 1) {
         if (kPair) {
@@ -177,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         kb1 = (int)((long long)(split + 1) * p.k_blocks / p.splits);
     };
     auto load_full_bar = [&](int s) { return kPair ? ptx::map_to_cta(full_bar(s), 0) : full_bar(s); };
-    constexpr uint32_t arm_bytes = (uint32_t)(kATileBytes + b_tile_bytes) * (kPair ? 2u : 1u);
+    const uint32_t arm_bytes = (uint32_t)(a_stage + b_stage) * (kPair ? 2u : 1u);
     // where the piece of the vocabulary lies in W: rows of B for the logits, the contraction for dy
     const int b_mn_off = (kMode == kStats || kMode == kGrad) ? p.v0 : 0;
     const int b_k_off = kMode == kDy ? p.v0 : 0;
@@ -188,20 +267,37 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             int stage = 0;
             uint32_t phase = 0, armed = 0, armed_parity = 0;
             bool ok = true;
+            int n_pre = 0, issued = 0;
+            if ((kMode == kStats || kMode == kGrad) && worker < total_tiles) {        // W is a constant of the stream: the first
+                int m_tile, n_tile, split, kb0, kb1;                                  // slots' share of it before the wait
+                locate(worker, m_tile, n_tile, split, kb0, kb1);
+                n_pre = min(S, (kb1 - kb0 + kbs - 1) / kbs);
+                for (int s = 0; s < n_pre; ++s) {
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), arm_bytes);
+                    load_operand<b_mn, kPair>(b_base + s * b_stage, &maps.b, s * kbs * BK, b_mn_off + n_tile * p.bn + (int)rank * b_rows, b_rows,
+                                              kbs, p.b_3d, load_full_bar(s));
+                    armed |= 1u << s;
+                }
+            }
             grid_dependency_wait();
             for (int tile = worker; ok && tile < total_tiles; tile += n_workers) {
                 int m_tile, n_tile, split, kb0, kb1;
                 locate(tile, m_tile, n_tile, split, kb0, kb1);
-                for (int kb = kb0; kb < kb1; ++kb) {
+                for (int kb = kb0; kb < kb1; kb += kbs, ++issued) {
+                    if (issued < n_pre) {
+                        load_operand<a_mn, kPair>(a_base + stage * a_stage, &maps.a, kb * BK, m_tile * BM, a_mn ? BM : p.a_rows, kbs, p.a_3d, load_full_bar(stage));
+                        if (++stage == S) { stage = 0; phase ^= 1u; }
+                        continue;
+                    }
                     if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {
                         record_failure(p.ctrl, abort_flag, 1, stage, tile);
                         ok = false;
                         break;
                     }
                     if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), arm_bytes);
-                    load_operand<a_mn, kPair>(a_base + stage * kATileBytes, &maps.a, kb * BK, m_tile * BM, BM, p.a_3d, load_full_bar(stage));
-                    load_operand<b_mn, kPair>(b_base + stage * b_tile_bytes, &maps.b, b_k_off + kb * BK,
-                                              b_mn_off + n_tile * BN + (int)rank * b_rows, b_rows, p.b_3d, load_full_bar(stage));
+                    load_operand<a_mn, kPair>(a_base + stage * a_stage, &maps.a, kb * BK, m_tile * BM, a_mn ? BM : p.a_rows, kbs, p.a_3d, load_full_bar(stage));
+                    load_operand<b_mn, kPair>(b_base + stage * b_stage, &maps.b, b_k_off + kb * BK,
+                                              b_mn_off + n_tile * p.bn + (int)rank * b_rows, b_rows, kbs, p.b_3d, load_full_bar(stage));
                     armed |= 1u << stage;
                     armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
                     if (++stage == S) { stage = 0; phase ^= 1u; }
@@ -212,9 +308,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = ptx::idesc_bf16_f32(kPair ? 2 * BM : BM, BN) | (a_mn ? ptx::kIdescAMnMajor : 0u) |
+            const uint32_t idesc = ptx::idesc_bf16_f32(kPair ? 2 * BM : BM, p.bn) | (a_mn ? ptx::kIdescAMnMajor : 0u) |
                                    (b_mn ? ptx::kIdescBMnMajor : 0u);
             constexpr uint32_t a_step = a_mn ? 2048 >> 4 : 32 >> 4, b_step = b_mn ? 2048 >> 4 : 32 >> 4;   // per K = 16
+            const uint32_t mn_lead = (uint32_t)kbs * 8192u;              // from one block of 64 columns to the next
             int stage = 0;
             uint32_t phase = 0;
             int local = 0;
@@ -232,21 +329,24 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                 }
                 ptx::tc_fence_after_sync();
                 const uint32_t d_tmem = tmem_base + (uint32_t)(buf * kAccStride);
-                for (int kb = kb0; kb < kb1; ++kb) {
+                for (int kb = kb0; kb < kb1; kb += kbs) {
                     if (!ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
                         record_failure(p.ctrl, abort_flag, 2, stage, tile);
                         ok = false;
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t a_addr = a_base + stage * kATileBytes, b_addr = b_base + stage * b_tile_bytes;
-                    const uint64_t adesc = a_mn ? ptx::smem_desc_mn128(a_addr) : ptx::smem_desc_k128(a_addr);
-                    const uint64_t bdesc = b_mn ? ptx::smem_desc_mn128(b_addr) : ptx::smem_desc_k128(b_addr);
+                    const uint32_t a_addr = a_base + stage * a_stage, b_addr = b_base + stage * b_stage;
+                    const int blocks = min(kbs, kb1 - kb);                // the range's last slot may hold one block too many
+                    for (int h = 0; h < blocks; ++h) {
+                        const uint64_t adesc = a_mn ? ptx::smem_desc_mn128(a_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(a_addr + h * a_block);
+                        const uint64_t bdesc = b_mn ? ptx::smem_desc_mn128(b_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(b_addr + h * b_rows * 128);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) {
-                        const uint32_t accumulate = (kb == kb0 && k == 0) ? 0u : 1u;
-                        if (kPair) ptx::mma_bf16_ss_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
-                        else ptx::mma_bf16_ss(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                        for (int k = 0; k < BK / 16; ++k) {
+                            const uint32_t accumulate = (kb == kb0 && h == 0 && k == 0) ? 0u : 1u;
+                            if (kPair) ptx::mma_bf16_ss_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                            else ptx::mma_bf16_ss(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                        }
                     }
                     mma_commit_all<kPair>(empty_bar(stage));
                     if (++stage == S) { stage = 0; phase ^= 1u; }
@@ -256,14 +356,17 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             if (*abort_flag) mma_drain<kPair>(drain_bar);
         }
     } else {
-        // ------------------------------------------------------------------ epilogue (warps 2..9)
+        // ------------------------------------------------------------------ epilogue (warps 2..17)
+        // A warp takes 32 rows x 64 columns of every tile: all of it goes into registers at once, the accumulator is handed back
+        // as soon as it is there, and the arithmetic runs beside the next tile's products.
         const int quarter = warp & 3;
-        const int half = (warp - 2) >> 2;                   // even / odd groups of 64 columns
-        unsigned char* mine = staging + (warp - 2) * kStageWarpBytes;
-        const uint32_t mine_addr = ptx::smem_addr(mine);
+        const int group = (warp - 2) >> 2;                  // 64 columns of the tile
         int local = 0;
         grid_dependency_wait();
         const float scale = kMode == kDw ? grad_scale(p.dce, p.dloss, p.loss) : 1.f;
+        float2* xchg = reinterpret_cast<float2*>(bar_mem + 512);
+        auto epilogue_barrier = [] { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+        bool given_up = false;
         for (int tile = worker; tile < total_tiles; tile += n_workers) {
             int m_tile, n_tile, split, kb0, kb1;
             locate(tile, m_tile, n_tile, split, kb0, kb1);
@@ -273,6 +376,9 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             ++local;
             const int row0 = m_tile * BM + quarter * 32, row = row0 + lane;
             const bool live = row < p.m_rows;
+            const int col0 = n_tile * p.bn + group * 64;
+            const int col1 = min(n_tile * p.bn + p.bn, kMode == kGrad ? (p.n_cols + 63) & ~63 : p.n_cols);     // columns of the tile end here
+            const bool work = row0 < p.m_rows && col0 < col1;            // the same for the whole warp
             float weight = 0.f, lse = 0.f;
             int label = -1;
             if ((kMode == kStats || kMode == kGrad) && live) {
@@ -282,115 +388,19 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                     lse = ld_dep(p.lse + row);
                 }
             }
-            if (!__all_sync(0xffffffffu, ptx::mbar_wait(tfull_bar(buf), acc_phase, abort_flag))) {
-                if (lane == 0) record_failure(p.ctrl, abort_flag, 3, buf, tile);
-                break;
+            if (given_up || !__all_sync(0xffffffffu, ptx::mbar_wait(tfull_bar(buf), acc_phase, abort_flag))) {
+                if (!given_up && lane == 0) record_failure(p.ctrl, abort_flag, 3, buf, tile);
+                given_up = true;
+                if (kMode == kStats) epilogue_barrier();                 // the other warps may still be on their way to it
+                continue;
             }
             ptx::tc_fence_after_sync();
-            const int n0 = n_tile * BN;
-            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kAccStride);
-            if (row0 < p.m_rows) {
-                for (int g = half; g < BN / 64; g += 2) {
-                    const int col0 = n0 + g * 64;
-                    if (col0 >= p.n_cols) break;
-                    if (kMode == kStats) {
-                        float m = -CUDART_INF_F, s = 0.f;
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float z[32];
-                            ptx::tmem_ld_32x32(taddr + g * 64 + c * 32, z);
-                            ptx::tmem_ld_wait();
-                            const int base = col0 + c * 32;
-                            const int nvalid = min(p.n_cols - base, 32);
-                            if (nvalid <= 0) break;
-                            float cm = z[0];
-#pragma unroll
-                            for (int j = 1; j < 32; ++j)
-                                if (j < nvalid) cm = fmaxf(cm, z[j]);
-                            if (cm > m) {
-                                s *= ex2((m - cm) * kLog2e);              // an empty state: 0 times 0
-                                m = cm;
-                            }
-                            float add = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < nvalid) add += ex2((z[j] - m) * kLog2e);
-                            s += add;
-                            if ((unsigned)(label - base) < (unsigned)nvalid) {
-                                float zl = 0.f;
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) zl = (base + j == label) ? z[j] : zl;
-                                p.z_label[row] = zl;
-                            }
-                        }
-                        if (live) p.parts[(size_t)(n_tile * 4 + g) * p.M + row] = make_float2(m, s);
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float z[32];
-                            ptx::tmem_ld_32x32(taddr + g * 64 + c * 32, z);
-                            ptx::tmem_ld_wait();
-                            const int base = col0 + c * 32;
-                            if (kMode == kGrad) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) {
-                                    const float pr = ex2((z[j] - lse) * kLog2e);
-                                    const float gr = weight * ((base + j == label) ? pr - 1.f : pr);
-                                    z[j] = (weight == 0.f || base + j >= p.n_cols) ? 0.f : gr;
-                                }
-                            }
-                            if (kMode == kDw) {
-#pragma unroll
-                                for (int j = 0; j < 32; ++j) z[j] *= scale;
-                                if (p.add && live) {
-                                    const uint4* old = reinterpret_cast<const uint4*>(p.dW + (size_t)(p.v0 + row) * p.d + base);
-#pragma unroll
-                                    for (int q = 0; q < 4; ++q) {
-                                        if (base + q * 8 < p.n_cols) {
-                                            const uint4 o = ld_dep(old + q);
-                                            z[q * 8 + 0] += bf16_lo(o.x); z[q * 8 + 1] += bf16_hi(o.x);
-                                            z[q * 8 + 2] += bf16_lo(o.y); z[q * 8 + 3] += bf16_hi(o.y);
-                                            z[q * 8 + 4] += bf16_lo(o.z); z[q * 8 + 5] += bf16_hi(o.z);
-                                            z[q * 8 + 6] += bf16_lo(o.w); z[q * 8 + 7] += bf16_hi(o.w);
-                                        }
-                                    }
-                                }
-                            }
-                            if (kMode == kDy || c == 0) {                 // the warp's staging area is free again
-                                if (lane == 0) ptx::bulk_wait_read();
-                                __syncwarp();
-                            }
-                            // 128-byte rows in the swizzle the tensor map names: 16-byte piece q of row r lies at q ^ (r & 7)
-                            if (kMode == kDy) {
-#pragma unroll
-                                for (int q = 0; q < 8; ++q)
-                                    *reinterpret_cast<float4*>(mine + lane * 128 + ((q ^ (lane & 7)) << 4)) =
-                                        make_float4(z[q * 4], z[q * 4 + 1], z[q * 4 + 2], z[q * 4 + 3]);
-                            } else {
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    *reinterpret_cast<uint4*>(mine + lane * 128 + (((c * 4 + q) ^ (lane & 7)) << 4)) =
-                                        make_uint4(pack_bf16(z[q * 8], z[q * 8 + 1]), pack_bf16(z[q * 8 + 2], z[q * 8 + 3]),
-                                                   pack_bf16(z[q * 8 + 4], z[q * 8 + 5]), pack_bf16(z[q * 8 + 6], z[q * 8 + 7]));
-                            }
-                            if (kMode == kDy || c == 1) {
-                                ptx::fence_proxy_async();
-                                __syncwarp();
-                                if (lane == 0) {
-                                    if (kMode == kDy) {
-                                        if (base < p.n_cols) {
-                                            if (p.add) ptx::tma_add_3d(&maps.out, mine_addr, base, row0, split);
-                                            else ptx::tma_store_3d(&maps.out, mine_addr, base, row0, split);
-                                        }
-                                    } else {
-                                        ptx::tma_store_2d(&maps.out, mine_addr, col0, (kMode == kDw ? p.v0 : 0) + row0);
-                                    }
-                                    ptx::bulk_commit();
-                                }
-                            }
-                        }
-                    }
-                }
+            float z[2][32];
+            if (work) {
+                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kAccStride + group * 64);
+                ptx::tmem_ld_32x32(taddr, z[0]);
+                ptx::tmem_ld_32x32(taddr + 32, z[1]);
+                ptx::tmem_ld_wait();
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
@@ -398,8 +408,62 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                 if (kPair) ptx::mbar_arrive_remote(ptx::map_to_cta(tempty_bar(buf), 0));
                 else ptx::mbar_arrive(tempty_bar(buf));
             }
+            if (kMode == kStats) {
+                float m = -CUDART_INF_F, s = 0.f;                        // an empty part
+                if (work) {
+                    const int nvalid = col1 - col0;
+                    if (nvalid >= 64) fold_stats<true>(z, 64, m, s);
+                    else fold_stats<false>(z, nvalid, m, s);
+                    if (live && (unsigned)(label - col0) < (unsigned)min(nvalid, 64)) {
+                        float zl = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) zl = (col0 + j == label) ? z[j >> 5][j & 31] : zl;
+                        p.z_label[row] = zl;
+                    }
+                }
+                // the tile's four groups of columns meet in shared memory; two buffers, so that one barrier a tile is enough
+                float2* slot = xchg + (local & 1) * 512 + quarter * 32 + lane;
+                slot[group * 128] = make_float2(m, s);
+                epilogue_barrier();
+                if (group == 0 && live) {
+                    const float2 o1 = slot[128], o2 = slot[256], o3 = slot[384];
+                    const float mm = fmaxf(fmaxf(m, o1.x), fmaxf(o2.x, o3.x));
+                    auto part = [&](float om, float os) { return os == 0.f ? 0.f : os * ex2((om - mm) * kLog2e); };
+                    const float ss = (part(m, s) + part(o1.x, o1.y)) + (part(o2.x, o2.y) + part(o3.x, o3.y));
+                    p.parts[(size_t)n_tile * p.M + row] = make_float2(mm, ss);
+                }
+                continue;
+            }
+            if (!work || !live) continue;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int base = col0 + c * 32;
+                if (kMode == kGrad) {
+                    // G, zeros in the columns that fill up the last block of 64 and in rows that take no part
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[c][j] = weight * ex2((z[c][j] - lse) * kLog2e);
+                    if ((unsigned)(label - base) < 32u) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[c][j] -= (base + j == label) ? weight : 0.f;
+                    }
+                    if (weight == 0.f || base + 32 > p.n_cols) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z[c][j] = (weight == 0.f || base + j >= p.n_cols) ? 0.f : z[c][j];
+                    }
+                    if (base < col1) store_bf16x32(p.G + (size_t)row * p.ld_g + base, z[c], col1 - base, true);
+                } else if (kMode == kDy) {
+                    if (base < p.n_cols) store_f32x32(p.dy + ((size_t)split * p.M + row) * p.d + base, z[c], p.n_cols - base, p.add);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) z[c][j] *= scale;
+                    __nv_bfloat16* out = p.dW + (size_t)(p.v0 + row) * p.d + base;
+                    if (base < p.n_cols) {
+                        if (p.add) add_bf16x32(out, z[c], p.n_cols - base);
+                        store_bf16x32(out, z[c], p.n_cols - base, p.sectors);
+                    }
+                }
+            }
         }
-        if (kMode != kStats && lane == 0) ptx::bulk_wait_all();
     }
 
     ptx::tc_fence_before_sync();
@@ -425,6 +489,7 @@ struct CeLnArgs {
     const float* dce;
     int V;
     __nv_bfloat16* y;
+    int ld_y;              // columns of y from d on are zeros
     float2* stats;
     int M, d;
 };
@@ -435,8 +500,9 @@ __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constan
     const int lane = threadIdx.x & 31;
     if (row >= a.M) return;
     const int nvec = a.d >> 3;
-    uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.d);
+    uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.ld_y);
     grid_dependency_wait();
+    if (nvec + lane < a.ld_y >> 3) yrow[nvec + lane] = make_uint4(0, 0, 0, 0);      // fewer than eight vectors
     if (a.stats && row_weight(a.labels, a.dce, a.V, row) == 0.f) {
         for (int c = lane; c < nvec; c += 32) yrow[c] = make_uint4(0, 0, 0, 0);
         if (lane == 0) a.stats[row] = make_float2(0.f, 0.f);
@@ -448,54 +514,70 @@ __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constan
     if (a.stats && lane == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
 }
 
-// Sum of v over the 256 threads of a CTA, in a fixed order.
+constexpr int kMergeThreads = 1024;
+
+// Sum of v over the threads of a merging CTA, in a fixed order.
 __device__ __forceinline__ double cta_sum_d(double v, double* part) {
-    part[threadIdx.x] = v;
+    v = warp_sum_d(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) part[threadIdx.x] += part[threadIdx.x + o];
-        __syncthreads();
-    }
-    const double r = part[0];
+    const double r = warp_sum_d(part[threadIdx.x & 31]);
     __syncthreads();
     return r;
 }
 
-// 32 rows per CTA, lane = row, the warps stride over the column groups; then the CTA that finishes last adds up the
-// mean over the counted rows, in a fixed order whichever CTA that is.
-__global__ void __launch_bounds__(256) ce_merge_kernel(const float2* parts, int n_parts, const float* z_label, const int* labels, int M,
-                                                       int V, float* ce, float* lse, float* loss, Control* ctrl) {
-    __shared__ float2 part[8][32];
-    __shared__ double sums[256];
+// 32 rows per CTA, lane = row, the 32 warps stride over the parts, four loads in flight (with eight warps and one load this kernel
+// took 25 us of a call); then the CTA that finishes last adds up the mean over the counted rows, in a fixed order whichever
+// CTA that is.
+__global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const float2* parts, int n_parts, const float* z_label, const int* labels, int M,
+                                                                 int V, float* ce, float* lse, float* loss, Control* ctrl) {
+    constexpr int kWarps = kMergeThreads / 32, kAhead = 4;
+    __shared__ float2 part[kWarps][33];
+    __shared__ double sums[kWarps];
     __shared__ int is_last;
     launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + lane;
     grid_dependency_wait();
     float m = -CUDART_INF_F, s = 0.f;
-    auto fold = [&](float2 o) {
-        const float nm = fmaxf(m, o.x);
-        s = (s == 0.f ? 0.f : s * ex2((m - nm) * kLog2e)) + (o.y == 0.f ? 0.f : o.y * ex2((o.x - nm) * kLog2e));
+    auto fold = [&](float om, float os) {
+        const float nm = fmaxf(m, om);
+        s = (s == 0.f ? 0.f : s * ex2((m - nm) * kLog2e)) + (os == 0.f ? 0.f : os * ex2((om - nm) * kLog2e));
         m = nm;
     };
     if (row < M)
-        for (int n = warp; n < n_parts; n += 8) fold(__ldcg(parts + (size_t)n * M + row));
+        for (int n0 = warp; n0 < n_parts; n0 += kWarps * kAhead) {
+            float2 o[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int n = n0 + i * kWarps;
+                o[i] = n < n_parts ? __ldcg(parts + (size_t)n * M + row) : make_float2(-CUDART_INF_F, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) fold(o[i].x, o[i].y);
+        }
     part[warp][lane] = make_float2(m, s);
     __syncthreads();
-    if (warp == 0 && row < M) {
+    {   // one row per warp: its 32 parts, one per lane, by shuffles
+        const float2 o = part[lane][warp];
+        const int r = blockIdx.x * 32 + warp;
+        float mm = o.x;
 #pragma unroll
-        for (int w = 1; w < 8; ++w) fold(part[w][lane]);
-        const float l = m + logf(s);
-        lse[row] = l;
-        const bool counted = (unsigned)ld_dep(labels + row) < (unsigned)V;
-        ce[row] = counted ? l - ld_dep(z_label + row) : 0.f;
+        for (int k = 16; k > 0; k >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, k));
+        const float ss = warp_sum(o.y == 0.f ? 0.f : o.y * ex2((o.x - mm) * kLog2e));
+        if (lane == 0 && r < M) {
+            const float l = mm + logf(ss);
+            lse[r] = l;
+            const bool counted = (unsigned)ld_dep(labels + r) < (unsigned)V;
+            ce[r] = counted ? l - ld_dep(z_label + r) : 0.f;
+        }
     }
     __syncthreads();
     if (threadIdx.x == 0) is_last = ticket_arrive_is_last(&ctrl->head_ticket[0], gridDim.x) ? 1 : 0;
     __syncthreads();
     if (!is_last) return;
     double total = 0.0, n = 0.0;
-    for (int i = threadIdx.x; i < M; i += 256)
+    for (int i = threadIdx.x; i < M; i += kMergeThreads)
         if ((unsigned)ld_dep(labels + i) < (unsigned)V) {
             total += (double)ld_dep(ce + i);
             n += 1.0;
@@ -509,22 +591,28 @@ __global__ void __launch_bounds__(256) ce_merge_kernel(const float2* parts, int 
     }
 }
 
-// dy (the sum of its slabs) back through the LayerNorm, a warp per row; the summed dy is left in the first slab.
+// dy (the sum of its slabs) back through the LayerNorm, and the column sums behind dgamma and dbeta, in one pass over dy and h.
+// A thread owns eight columns and walks a strip of rows, kBackRows at a time (their loads are in flight together, their two
+// row sums are reduced together); the columns' threads are one of `groups` groups of a CTA that take alternate batches.
+// Four rows take 96 registers (d <= 5120: 640 threads; two CTAs of 320 threads on an SM at d = 2560); above that it is one row.
 struct CeBackArgs {
     const __nv_bfloat16* h;
     long long ld_h;
     const float* gamma;
     const float2* stats;
-    float* dy;             // [splits][M][d]
+    const float* dy;       // [splits][M][d]
     int splits;
     const float* dce;
     const float* dloss;
     const float* loss;
     __nv_bfloat16* dh;     // or NULL
     long long ld_dh;
+    float* cols;           // [CTAs][groups][2][d] sums of dy xhat and of dy, or NULL
     int M, d;
+    int warps;             // warps of a group
+    int groups;
+    int strip;             // rows per CTA
 };
-
 __device__ __forceinline__ void add8(float (&v)[8], const float* p) {
     const float4 a = __ldcg(reinterpret_cast<const float4*>(p)), b = __ldcg(reinterpret_cast<const float4*>(p) + 1);
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
@@ -535,98 +623,118 @@ __device__ __forceinline__ void unpack8(uint4 o, float (&x)[8]) {
     x[4] = bf16_lo(o.z); x[5] = bf16_hi(o.z); x[6] = bf16_lo(o.w); x[7] = bf16_hi(o.w);
 }
 
-__global__ void __launch_bounds__(256) ce_dh_kernel(const __grid_constant__ CeBackArgs a) {
+template <int kBackRows, int kMostThreads>
+__global__ void __launch_bounds__(kMostThreads) ce_back_kernel(const __grid_constant__ CeBackArgs a) {
+    __shared__ float2 red[2][kBackRows][32];
     launch_dependents();
-    const int row = blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int group = warp / a.warps, gwarp = warp - group * a.warps;
+    const int c = gwarp * 32 + lane;                                     // the thread's vector of eight columns
+    const bool on = c * 8 < a.d;
+    float gamma[8] = {};
+    if (on) {
+        const float4 g0 = ld_param4(a.gamma + c * 8), g1 = ld_param4(a.gamma + c * 8 + 4);
+        gamma[0] = g0.x; gamma[1] = g0.y; gamma[2] = g0.z; gamma[3] = g0.w;
+        gamma[4] = g1.x; gamma[5] = g1.y; gamma[6] = g1.z; gamma[7] = g1.w;
+    }
     grid_dependency_wait();
-    if (row >= a.M) return;
-    const int nvec = a.d >> 3;
-    const float2 st = __ldcg(a.stats + row);
-    float* dyrow = a.dy + (size_t)row * a.d;
-    const uint4* hrow = reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h);
-    const bool dead = st.y == 0.f;                                       // takes no part
-    float sum = 0.f, dot = 0.f;
-    for (int c = lane; c < nvec; c += 32) {
-        float v[8] = {};
-        for (int k = 0; k < a.splits; ++k) add8(v, dyrow + (size_t)k * a.M * a.d + c * 8);
-        if (a.splits > 1) {
-            reinterpret_cast<float4*>(dyrow + c * 8)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(dyrow + c * 8)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        }
-        if (!a.dh || dead) continue;
-        float x[8];
-        unpack8(ld_dep(hrow + c), x);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float t = v[j] * __ldg(a.gamma + c * 8 + j);
-            sum += t;
-            dot = fmaf(t, (x[j] - st.x) * st.y, dot);
-        }
-    }
-    if (!a.dh) return;
-    uint4* out = reinterpret_cast<uint4*>(a.dh + (size_t)row * a.ld_dh);
-    if (dead) {
-        for (int c = lane; c < nvec; c += 32) out[c] = make_uint4(0, 0, 0, 0);
-        return;
-    }
+    const float scale = grad_scale(a.dce, a.dloss, a.loss);
     const float inv_d = 1.f / (float)a.d;
-    const float c1 = warp_sum(sum) * inv_d, c2 = warp_sum(dot) * inv_d;
-    const float scale = grad_scale(a.dce, a.dloss, a.loss) * st.y;
-    for (int c = lane; c < nvec; c += 32) {
-        float v[8] = {}, x[8];
-        add8(v, dyrow + c * 8);                                          // this lane's own store when there were several slabs
-        unpack8(ld_dep(hrow + c), x);
+    float dg[8] = {}, db[8] = {};
+    const int r0 = blockIdx.x * a.strip, r1 = min(a.M, r0 + a.strip);
+    const int step = kBackRows * a.groups;
+    int turn = 0;
+    for (int base = r0; base < r1; base += step, turn ^= 1) {
+        float v[kBackRows][8];
+        uint4 xw[kBackRows];                                             // h as it lies, unpacked where it is used: registers are short
+        float2 st[kBackRows];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            v[j] = scale * (v[j] * __ldg(a.gamma + c * 8 + j) - c1 - (x[j] - st.x) * st.y * c2);
-        out[c] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        for (int k = 0; k < kBackRows; ++k) {
+            const int row = base + group * kBackRows + k;
+            st[k] = make_float2(0.f, 0.f);
+            xw[k] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = 0.f;
+            if (row < r1) st[k] = __ldcg(a.stats + row);
+            if (on && row < r1) {
+                xw[k] = ld_dep(reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h) + c);
+                for (int s = 0; s < a.splits; ++s) add8(v[k], a.dy + ((size_t)s * a.M + row) * a.d + c * 8);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kBackRows; ++k) {
+            float sum = 0.f, dot = 0.f, x[8];
+            unpack8(xw[k], x);
+            const bool dead = st[k].y == 0.f;                            // takes no part, whatever it holds
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xhat = dead ? 0.f : (x[j] - st[k].x) * st[k].y;
+                if (dead) v[k][j] = 0.f;
+                dg[j] = fmaf(v[k][j], xhat, dg[j]);
+                db[j] += v[k][j];
+                const float t = v[k][j] * gamma[j];
+                sum += t;
+                dot = fmaf(t, xhat, dot);
+            }
+            sum = warp_sum(sum);
+            dot = warp_sum(dot);
+            if (lane == 0) red[turn][k][warp] = make_float2(sum, dot);
+        }
+        if (!a.dh) continue;
+        __syncthreads();                                                 // `red` of two turns ago is read before anyone writes it again
+#pragma unroll
+        for (int k = 0; k < kBackRows; ++k) {
+            const int row = base + group * kBackRows + k;
+            float c1 = 0.f, c2 = 0.f;
+            for (int w = 0; w < a.warps; ++w) {
+                const float2 o = red[turn][k][group * a.warps + w];
+                c1 += o.x;
+                c2 += o.y;
+            }
+            c1 *= inv_d;
+            c2 *= inv_d;
+            const float f = scale * st[k].y;
+            if (on && row < r1) {
+                float x[8];
+                unpack8(xw[k], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float xhat = st[k].y != 0.f ? (x[j] - st[k].x) * st[k].y : 0.f;
+                    v[k][j] = f * (v[k][j] * gamma[j] - c1 - xhat * c2);
+                }
+                *(reinterpret_cast<uint4*>(a.dh + (size_t)row * a.ld_dh) + c) =
+                    make_uint4(pack_bf16(v[k][0], v[k][1]), pack_bf16(v[k][2], v[k][3]), pack_bf16(v[k][4], v[k][5]), pack_bf16(v[k][6], v[k][7]));
+            }
+        }
+    }
+    if (a.cols && on) {
+        float4* out = reinterpret_cast<float4*>(a.cols + ((size_t)blockIdx.x * a.groups + group) * 2 * a.d + c * 8);
+        out[0] = make_float4(dg[0], dg[1], dg[2], dg[3]);
+        out[1] = make_float4(dg[4], dg[5], dg[6], dg[7]);
+        out = reinterpret_cast<float4*>(a.cols + (((size_t)blockIdx.x * a.groups + group) * 2 + 1) * a.d + c * 8);
+        out[0] = make_float4(db[0], db[1], db[2], db[3]);
+        out[1] = make_float4(db[4], db[5], db[6], db[7]);
     }
 }
 
-// Column sums of dy xhat and of dy over a strip of rows: 64 columns per CTA, two per thread, eight rows at a time.
-constexpr int kStripRows = 128;
-__global__ void __launch_bounds__(256) ce_colsum_kernel(const float* dy, const __nv_bfloat16* h, long long ld_h, const float2* stats,
-                                                        int M, int d, float* part) {
-    __shared__ float4 red[256];
+// The strips' column sums: 32 columns per CTA, 32 groups of strips, joined in order.
+__global__ void __launch_bounds__(1024) ce_colsum_kernel(const float* part, int strips, int d, const float* dce, const float* dloss,
+                                                        const float* loss, int add, __nv_bfloat16* dgamma, __nv_bfloat16* dbeta) {
+    __shared__ float red[32][32];
     launch_dependents();
-    const int col = blockIdx.x * 64 + (threadIdx.x & 31) * 2, group = threadIdx.x >> 5;
-    const int r0 = blockIdx.y * kStripRows, r1 = min(M, r0 + kStripRows);
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int i = blockIdx.x * 32 + lane;
     grid_dependency_wait();
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);                        // dgamma of two columns, dbeta of two columns
-    if (col < d) {
-        for (int r = r0 + group; r < r1; r += 8) {
-            const float2 st = __ldcg(stats + r);
-            if (st.y == 0.f) continue;
-            const float2 g = __ldcg(reinterpret_cast<const float2*>(dy + (size_t)r * d + col));
-            const uint32_t x = ld_dep(reinterpret_cast<const uint32_t*>(h + (size_t)r * ld_h + col));
-            acc.x = fmaf(g.x, (bf16_lo(x) - st.x) * st.y, acc.x);
-            acc.y = fmaf(g.y, (bf16_hi(x) - st.x) * st.y, acc.y);
-            acc.z += g.x;
-            acc.w += g.y;
-        }
-    }
-    red[threadIdx.x] = acc;
-    __syncthreads();
-    if (group == 0 && col < d) {
-        for (int k = 1; k < 8; ++k) {
-            const float4 o = red[threadIdx.x + 32 * k];
-            acc.x += o.x; acc.y += o.y; acc.z += o.z; acc.w += o.w;
-        }
-        float* mine = part + (size_t)blockIdx.y * 2 * d;
-        *reinterpret_cast<float2*>(mine + col) = make_float2(acc.x, acc.y);
-        *reinterpret_cast<float2*>(mine + d + col) = make_float2(acc.z, acc.w);
-    }
-}
-
-__global__ void __launch_bounds__(256) ce_colsum_final_kernel(const float* part, int strips, int d, const float* dce, const float* dloss,
-                                                              const float* loss, int add, __nv_bfloat16* dgamma, __nv_bfloat16* dbeta) {
-    launch_dependents();
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    grid_dependency_wait();
-    if (i >= 2 * d) return;
     float s = 0.f;
-    for (int k = 0; k < strips; ++k) s += ld_dep(part + (size_t)k * 2 * d + i);
+    if (i < 2 * d) {
+#pragma unroll 8
+        for (int k = group; k < strips; k += 32) s += ld_dep(part + (size_t)k * 2 * d + i);
+    }
+    red[group][lane] = s;
+    __syncthreads();
+    if (group != 0 || i >= 2 * d) return;
+#pragma unroll 8
+    for (int k = 1; k < 32; ++k) s += red[k][lane];
     __nv_bfloat16* out = i < d ? dgamma + i : dbeta + (i - d);
     s *= grad_scale(dce, dloss, loss);
     if (add) s += __bfloat162float(*out);
@@ -635,58 +743,92 @@ __global__ void __launch_bounds__(256) ce_colsum_final_kernel(const float* part,
 
 // ---------------------------------------------------------------------------------------------------- host
 
-bool make_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+bool make_map(CUtensorMap* map, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
               const cuuint32_t* box, CUtensorMapL2promotion promo = CU_TENSOR_MAP_L2_PROMOTION_L2_128B) {
     EncodeTiledFn fn = encode_tiled_fn();
     const cuuint32_t estr[3] = {1, 1, 1};
-    return fn && fn(map, type, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                     CU_TENSOR_MAP_SWIZZLE_128B, promo, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // bf16 [rows, cols] with row stride ld, boxes of box_rows x 64 columns.
 bool map_2d(CUtensorMap* map, const void* base, int rows, int cols, int ld, int box_rows) {
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
     const cuuint32_t box[2] = {64u, (cuuint32_t)box_rows};
-    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box);
+    return make_map(map, 2, base, dims, strides, box);
 }
-// An MN-major operand: bf16 [rows (contraction), cols] with row stride ld, read as blocks of 64 x 64; `blocks` of them with
-// one request where the columns are whole blocks.
-bool map_mn(CUtensorMap* map, int* three_d, const void* base, int rows, int cols, int ld, int blocks) {
-    *three_d = cols % 64 == 0;
-    if (!*three_d) return map_2d(map, base, rows, cols, ld, 64);
+// The same as blocks of 64 columns (whole ones: cols % 64 == 0), box_rows x box_blocks of them with one request.
+bool map_blocks(CUtensorMap* map, const void* base, int rows, int cols, int ld, int box_rows, int box_blocks) {
     const cuuint64_t dims[3] = {64u, (cuuint64_t)rows, (cuuint64_t)(cols / 64)}, strides[2] = {(cuuint64_t)ld * 2, 128u};
-    const cuuint32_t box[3] = {64u, 64u, (cuuint32_t)blocks};
-    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box);
+    const cuuint32_t box[3] = {64u, (cuuint32_t)box_rows, (cuuint32_t)box_blocks};
+    return make_map(map, 3, base, dims, strides, box);
+}
+// A K-major operand: `rows` of it, kbs k-blocks at a time; two with one request where the columns are whole blocks.
+bool map_k(CUtensorMap* map, int* three_d, const void* base, int rows, int cols, int ld, int box_rows, int kbs) {
+    *three_d = kbs == 2 && cols % 64 == 0;
+    return *three_d ? map_blocks(map, base, rows, cols, ld, box_rows, 2) : map_2d(map, base, rows, cols, ld, box_rows);
+}
+// An MN-major operand: bf16 [rows (contraction), cols], `width` columns of it and kbs blocks of 64 rows at a time; with one
+// request where the columns and the width are whole blocks.
+bool map_mn(CUtensorMap* map, int* three_d, const void* base, int rows, int cols, int ld, int width, int kbs) {
+    *three_d = cols % 64 == 0 && width % 64 == 0;
+    return *three_d ? map_blocks(map, base, rows, cols, ld, 64 * kbs, width / 64) : map_2d(map, base, rows, cols, ld, 64 * kbs);
 }
 
 int tiles(int n, int t) { return (n + t - 1) / t; }
 
-// Piece of the vocabulary and splits of dy's contraction for a batch (fixed by the sizes alone: the workspace is sized
-// with them).
+// Piece of the vocabulary, splits of dy's contraction, tile width of dy and dW, and the layout of the last step (fixed by the
+// sizes alone: the workspace is sized with them).
+int back_rows(int d) { return d <= 5120 ? 4 : 1; }
 struct CePlan {
-    int piece, n_pieces, splits, strips;
+    int piece, n_pieces, splits, bn;
+    int back_warps, back_groups, back_strip, back_ctas;
 };
 CePlan ce_plan(int M, int d, int V) {
     CePlan c;
-    long long most = (long long)(kGradPieceBytes / 2) / (M > 0 ? M : 1) / BN * BN;
-    if (most < BN) most = BN;
-    if (most > V) most = (V + BN - 1LL) / BN * BN;
-    c.n_pieces = (int)((V + most - 1) / most);
-    c.piece = (int)((((long long)V + c.n_pieces - 1) / c.n_pieces + BN - 1) / BN * BN);
-    c.n_pieces = tiles(V, c.piece);
-    // as many splits as make the workers' rounds shortest; a split costs its slab's way to memory and back
+    const int rows = M > 0 ? M : 1;
+    // the width that computes the fewest columns beyond d; a tile costs about 32 columns more than its own (loads, hand-over)
+    c.bn = 256;
+    for (int w = 192; w >= 128; w -= 64)
+        if (tiles(d, w) * (w + 32) < tiles(d, c.bn) * (c.bn + 32)) c.bn = w;
     const bool pair = M > BM;
-    const long long workers = pair ? 74 : 148, t = (long long)(pair ? tiles(M, 2 * BM) : 1) * tiles(d, BN);
-    const int k_blocks = tiles(c.piece < V ? c.piece : V, BK);
+    const int m_units = pair ? tiles(M, 2 * BM) : 1, n_tiles = tiles(d, c.bn), vocab_units = tiles(V, 2 * BM);
+    const long long workers = pair ? 74 : 148;
+    auto rounds = [](long long n, long long w) { return (n + w - 1) / w; };
+    // Splits of dy's contraction over `units` blocks of 256: rounds of tiles over the workers, in k-blocks, and a slab's way to memory
+    // and back (5 TB/s against 22 TFLOP/s of a pair of SMs on 256 x bn x 64: some 0.0042 k-blocks per row and column / 256).
+    const double slab = (double)rows * d * 8.0 / 5e12 / ((pair ? 256.0 : 128.0) * c.bn * 2.0 * BK / (pair ? 22e12 : 11e12));
+    auto dy_cost = [&](int units, int s) { return (double)rounds((long long)m_units * n_tiles * s, workers) / s * (units * 4.0) + s * slab; };
+    // Pieces of the vocabulary in units of 256 columns, from the most that G may take down to half of that: the ones whose tiles come out
+    // at whole rounds over the SMs, counted in k-blocks of a 256-wide tile; a launch costs about 20 of them.
+    long long most = (long long)(kGradPieceBytes / 2) / rows / (2 * BM);
+    if (most < vocab_units / 4) most = vocab_units / 4;
+    if (most < 1) most = 1;
+    if (most > vocab_units) most = vocab_units;
     double best = 0;
-    c.splits = 1;
-    for (int s = 1; s <= kMaxSplits && s * 4 <= k_blocks; ++s) {
-        const double cost = (double)((t * s + workers - 1) / workers) / s + 0.004 * s;
-        if (s == 1 || cost < best) {
+    int best_units = 0;
+    const int step = most > 256 ? (int)(most / 128) : 1;
+    for (int units = (int)most; units >= 1 && (units * 2 > most || best_units == 0); units -= step) {
+        const int full = vocab_units / units, rest = vocab_units - full * units;
+        auto piece_cost = [&](int u) {
+            return u == 0 ? 0.0 : 60.0 + (double)rounds((long long)m_units * u, workers) * tiles(d, BK) +
+                                  (double)rounds((long long)u * n_tiles, 74) * tiles(rows, BK) * (c.bn / 256.0) + dy_cost(u, 1) * (c.bn / 256.0);
+        };
+        const double cost = full * piece_cost(units) + piece_cost(rest);
+        if (best_units == 0 || cost < best) {
             best = cost;
-            c.splits = s;
+            best_units = units;
         }
     }
-    c.strips = tiles(M, kStripRows);
+    c.piece = best_units * 2 * BM;
+    c.n_pieces = tiles(V, c.piece);
+    c.splits = 1;
+    for (int s = 2; s <= kMaxSplits && s <= best_units && s * 4 <= tiles(c.piece < V ? c.piece : V, BK); ++s)
+        if (dy_cost(best_units, s) < dy_cost(best_units, c.splits)) c.splits = s;
+    c.back_warps = tiles(d / 8, 32);
+    c.back_groups = c.back_warps >= 8 ? 1 : 8 / c.back_warps;
+    const int batch = back_rows(d) * c.back_groups;
+    c.back_strip = tiles(tiles(rows, batch), 296) * batch;                // two CTAs per SM, whole batches
+    c.back_ctas = tiles(rows, c.back_strip);
     return c;
 }
 
@@ -697,31 +839,52 @@ CeSpace ce_space(int M, int d, int V, bool grad) {
     CeSpace s;
     size_t at = kCtrlBytes;
     auto take = [&](size_t n) { const size_t o = at; at = align_up(at + n, 256); return o; };
-    s.y = take((size_t)M * d * 2);
+    s.y = take((size_t)M * tiles(d, 64) * 128);
     s.stats = take((size_t)M * 8);
-    s.parts = take((size_t)4 * tiles(V, BN) * M * 8);
+    s.parts = take((size_t)tiles(V, kMinTile) * M * 8);
     s.z_label = take((size_t)M * 4);
     s.g = s.dy = s.cols = at;
     if (grad) {
         const CePlan c = ce_plan(M, d, V);
         s.g = take((size_t)M * c.piece * 2);
         s.dy = take((size_t)c.splits * M * d * 4);
-        s.cols = take((size_t)c.strips * 2 * d * 4);
+        s.cols = take((size_t)c.back_ctas * c.back_groups * 2 * d * 4);
     }
     s.total = at;
     return s;
 }
 
-template <int kMode, bool kPair>
-constexpr int ring_stages() {
-    const size_t stage = kATileBytes + (size_t)(kPair ? BN / 2 : BN) * BK * 2;
-    const size_t n = (kSmemBudget - 1024 - kBarBytes - (kMode == kStats ? 0 : 8 * kStageWarpBytes)) / stage;
+// Bytes of one k-block of both operands, and the ring slots that fit.
+size_t slot_bytes(int kMode, bool pair, int bn, int a_rows) {
+    const int b_rows = pair ? bn / 2 : bn;
+    return (size_t)a_rows * BK * 2 + (size_t)((kMode == kDy || kMode == kDw) ? (b_rows + 63) / 64 * 64 : b_rows) * BK * 2;
+}
+constexpr size_t kFixedSmem = kBarBytes + 1024;
+int ring_stages(int kMode, bool pair, int bn, int a_rows, int kbs) {
+    const size_t n = (kSmemBudget - kFixedSmem) / (slot_bytes(kMode, pair, bn, a_rows) * kbs);
     return (int)(n < (size_t)kMaxStages ? n : (size_t)kMaxStages);
 }
-template <int kMode, bool kPair>
-constexpr size_t ring_smem() {
-    return (size_t)ring_stages<kMode, kPair>() * (kATileBytes + (size_t)(kPair ? BN / 2 : BN) * BK * 2) +
-           (kMode == kStats ? 0 : 8 * kStageWarpBytes) + kBarBytes + 1024;
+// Two k-blocks per slot -- one request per operand where its columns are whole blocks of 64 -- if three such slots fit (tiles of 256 by
+// pairs: they do).  EE_GEMM_K2=0 keeps one.
+int blocks_per_slot(int kMode, bool pair, int bn, int a_rows) {
+    static const bool on = !(getenv("EE_GEMM_K2") && getenv("EE_GEMM_K2")[0] == '0');
+    return on && ring_stages(kMode, pair, bn, a_rows, 2) >= 3 ? 2 : 1;
+}
+
+// Width of the logits' tiles: 256 for many rows, else the multiple of 16 from kMinTile on that makes rounds x (width + 16) smallest
+// (the CTAs take whole rounds of tiles: 197 tiles of 256 on 148 SMs are two rounds, as are 286 of 176).
+int logit_tile(int m_units, int V, int workers) {
+    if (m_units > 4) return BN;
+    int best = BN;
+    long long best_cost = -1;
+    for (int bn = kMinTile; bn <= BN; bn += 16) {
+        const long long cost = (((long long)m_units * tiles(V, bn) + workers - 1) / workers) * (bn + 16);
+        if (best_cost < 0 || cost <= best_cost) {
+            best = bn;
+            best_cost = cost;
+        }
+    }
+    return best;
 }
 
 // Two-CTA clusters the device runs at once; 0 if the query fails or EE_GEMM_PAIRS=0 switches pairs off.
@@ -751,16 +914,16 @@ template <int kMode, bool kPair>
 ee_status launch_mode(const CeMaps& maps, CeParams p, int workers, int device, cudaStream_t stream) {
     static bool configured[kMaxDevices] = {};
     if (!configured[device]) {
-        if (cudaFuncSetAttribute(ce_gemm_kernel<kMode, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)ring_smem<kMode, kPair>()) != cudaSuccess)
+        if (cudaFuncSetAttribute(ce_gemm_kernel<kMode, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess)
             return EE_ERR_CUDA;
         configured[device] = true;
     }
-    p.n_stages = ring_stages<kMode, kPair>();
+    p.n_stages = ring_stages(kMode, kPair, p.bn, p.a_rows, p.kbs);
+    const size_t smem = p.n_stages * p.kbs * slot_bytes(kMode, kPair, p.bn, p.a_rows) + kFixedSmem;
     const long long total = (long long)(kPair ? (p.m_tiles + 1) / 2 : p.m_tiles) * p.n_tiles * p.splits;
     const int grid = (int)(total < workers ? total : workers);
-    const cudaError_t e = kPair ? launch_pdl_pairs(ce_gemm_kernel<kMode, kPair>, 2 * grid, kThreads, ring_smem<kMode, kPair>(), stream, maps, p)
-                                : launch_pdl(ce_gemm_kernel<kMode, kPair>, grid, kThreads, ring_smem<kMode, kPair>(), stream, maps, p);
+    const cudaError_t e = kPair ? launch_pdl_pairs(ce_gemm_kernel<kMode, kPair>, 2 * grid, kThreads, smem, stream, maps, p)
+                                : launch_pdl(ce_gemm_kernel<kMode, kPair>, grid, kThreads, smem, stream, maps, p);
     return e == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
@@ -779,6 +942,7 @@ CeLnArgs ln_args(const CeArgs& a, const CeSpace& s, bool grad) {
     l.ld_h = a.ld_h; l.gamma = a.gamma; l.beta = a.beta; l.ln_eps = a.ln_eps;
     l.labels = a.labels; l.dce = a.dce; l.V = a.V;
     l.y = reinterpret_cast<__nv_bfloat16*>(ws + s.y);
+    l.ld_y = tiles(a.d, 64) * 64;
     l.stats = grad ? reinterpret_cast<float2*>(ws + s.stats) : nullptr;
     l.M = a.M; l.d = a.d;
     return l;
@@ -788,6 +952,8 @@ CeParams base_params(const CeArgs& a) {
     CeParams p{};
     p.M = a.M; p.d = a.d; p.V = a.V;
     p.splits = 1;
+    p.bn = BN;
+    p.a_rows = BM;
     p.labels = a.labels; p.lse = a.lse; p.dce = a.dce; p.dloss = a.dloss; p.loss = a.loss;
     p.dW = static_cast<__nv_bfloat16*>(a.dW);
     p.ctrl = reinterpret_cast<Control*>(a.workspace);
@@ -802,6 +968,7 @@ ee_status layer_norm_launch(const void* h, long long ld_h, const float* gamma, c
     l.h = static_cast<const __nv_bfloat16*>(h);
     l.ld_h = ld_h; l.gamma = gamma; l.beta = beta; l.ln_eps = ln_eps;
     l.y = static_cast<__nv_bfloat16*>(y);
+    l.ld_y = d;
     l.M = M; l.d = d;
     return launch_pdl(ce_layer_norm_kernel, dim3((M + 7) / 8), 256, 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
@@ -815,11 +982,13 @@ ee_status ce_launch(const CeArgs& a) {
     if (launch_pdl(ce_layer_norm_kernel, dim3((a.M + 7) / 8), 256, 0, a.stream, l) != cudaSuccess) return EE_ERR_CUDA;
     const bool pair = use_pairs(a.M, a.device);
     CeMaps maps;
-    if (!map_2d(&maps.a, l.y, a.M, a.d, a.d, BM) || !map_2d(&maps.b, a.W, a.V, a.d, a.d, pair ? BN / 2 : BN)) return EE_ERR_CUDA;
-    maps.out = maps.a;                                                   // not used
     CeParams p = base_params(a);
+    p.bn = logit_tile(pair ? tiles(a.M, 2 * BM) : 1, a.V, pair ? resident_pairs(a.device) : a.num_sms);
+    p.a_rows = a.M <= 64 ? 64 : BM;
+    p.kbs = blocks_per_slot(kStats, pair, p.bn, p.a_rows);
+    if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs)) return EE_ERR_CUDA;
     p.m_tiles = tiles(a.M, BM);
-    p.n_tiles = tiles(a.V, BN);
+    p.n_tiles = tiles(a.V, p.bn);
     p.k_blocks = tiles(a.d, BK);
     p.n_cols = a.V;
     p.m_rows = a.M;
@@ -827,9 +996,8 @@ ee_status ce_launch(const CeArgs& a) {
     p.z_label = reinterpret_cast<float*>(ws + s.z_label);
     const ee_status st = launch_product<kStats>(maps, p, pair, a);
     if (st != EE_OK) return st;
-    // the last tile's groups of 64 columns beyond the vocabulary are not written
-    const int n_parts = tiles(a.V, 64);
-    if (launch_pdl(ce_merge_kernel, (a.M + 31) / 32, 256, 0, a.stream, (const float2*)p.parts, n_parts, (const float*)p.z_label, a.labels,
+    const int n_parts = p.n_tiles;
+    if (launch_pdl(ce_merge_kernel, (a.M + 31) / 32, kMergeThreads, 0, a.stream, (const float2*)p.parts, n_parts, (const float*)p.z_label, a.labels,
                    a.M, a.V, a.ce, a.lse_out, a.loss_out, p.ctrl) != cudaSuccess)
         return EE_ERR_CUDA;
     return EE_OK;
@@ -854,23 +1022,25 @@ ee_status ce_grad_launch(const CeArgs& a) {
         CeParams p = base_params(a);
         p.v0 = v0;
         {
-            if (!map_2d(&maps.a, l.y, a.M, a.d, a.d, BM) || !map_2d(&maps.b, a.W, a.V, a.d, a.d, pair ? BN / 2 : BN) ||
-                !map_2d(&maps.out, G, a.M, nv_pad, ld_g, 32))
+            p.bn = logit_tile(pair ? tiles(a.M, 2 * BM) : 1, nv, pair ? resident_pairs(a.device) : a.num_sms);
+            p.a_rows = a.M <= 64 ? 64 : BM;
+            p.kbs = blocks_per_slot(kGrad, pair, p.bn, p.a_rows);
+            if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs))
                 return EE_ERR_CUDA;
-            p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv, BN); p.k_blocks = tiles(a.d, BK);
+            p.G = G; p.ld_g = ld_g;
+            p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv, p.bn); p.k_blocks = tiles(a.d, BK);
             p.n_cols = nv; p.m_rows = a.M;
             const ee_status st = launch_product<kGrad>(maps, p, pair, a);
             if (st != EE_OK) return st;
         }
         if (need_dy) {
             CeParams q = p;
-            const cuuint64_t dims[3] = {(cuuint64_t)a.d, (cuuint64_t)a.M, (cuuint64_t)c.splits};
-            const cuuint64_t strides[2] = {(cuuint64_t)a.d * 4, (cuuint64_t)a.M * a.d * 4};
-            const cuuint32_t box[3] = {32u, 32u, 1u};
-            if (!map_2d(&maps.a, G, a.M, nv_pad, ld_g, BM) || !map_mn(&maps.b, &q.b_3d, a.W, a.V, a.d, a.d, (pair ? BN / 2 : BN) / 64) ||
-                !make_map(&maps.out, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, dy, dims, strides, box))
+            q.bn = c.bn;
+            q.kbs = blocks_per_slot(kDy, pair, q.bn, q.a_rows);
+            if (!map_k(&maps.a, &q.a_3d, G, a.M, nv_pad, ld_g, q.a_rows, q.kbs) || !map_mn(&maps.b, &q.b_3d, a.W, a.V, a.d, a.d, pair ? q.bn / 2 : q.bn, q.kbs))
                 return EE_ERR_CUDA;
-            q.m_tiles = tiles(a.M, BM); q.n_tiles = tiles(a.d, BN); q.k_blocks = tiles(nv, BK);
+            q.dy = dy;
+            q.m_tiles = tiles(a.M, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = tiles(nv, BK);
             q.splits = c.splits;
             q.n_cols = a.d; q.m_rows = a.M;
             q.add = i > 0;
@@ -880,10 +1050,14 @@ ee_status ce_grad_launch(const CeArgs& a) {
         if (a.dW) {
             CeParams q = p;
             const bool pair_w = use_pairs(nv, a.device);
-            if (!map_mn(&maps.a, &q.a_3d, G, a.M, nv_pad, ld_g, BM / 64) ||
-                !map_mn(&maps.b, &q.b_3d, l.y, a.M, a.d, a.d, (pair_w ? BN / 2 : BN) / 64) || !map_2d(&maps.out, a.dW, a.V, a.d, a.d, 32))
+            q.bn = c.bn;
+            q.a_rows = BM;
+            q.kbs = blocks_per_slot(kDw, pair_w, q.bn, BM);
+            if (!map_mn(&maps.a, &q.a_3d, G, a.M, nv_pad, ld_g, BM, q.kbs) ||
+                !map_mn(&maps.b, &q.b_3d, l.y, a.M, l.ld_y, l.ld_y, pair_w ? q.bn / 2 : q.bn, q.kbs))
                 return EE_ERR_CUDA;
-            q.m_tiles = tiles(nv, BM); q.n_tiles = tiles(a.d, BN); q.k_blocks = tiles(a.M, BK);
+            q.sectors = a.d % 16 == 0 && reinterpret_cast<uintptr_t>(a.dW) % 32 == 0;
+            q.m_tiles = tiles(nv, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = tiles(a.M, BK);
             q.n_cols = a.d; q.m_rows = nv;
             q.add = a.accumulate;
             const ee_status st = launch_product<kDw>(maps, q, pair_w, a);
@@ -897,15 +1071,15 @@ ee_status ce_grad_launch(const CeArgs& a) {
     b.dce = a.dce; b.dloss = a.dloss; b.loss = a.loss;
     b.dh = static_cast<__nv_bfloat16*>(a.dh); b.ld_dh = a.ld_dh;
     b.M = a.M; b.d = a.d;
-    if (launch_pdl(ce_dh_kernel, dim3((a.M + 7) / 8), 256, 0, a.stream, b) != cudaSuccess) return EE_ERR_CUDA;
-    if (a.dgamma) {
-        float* part = reinterpret_cast<float*>(ws + s.cols);
-        if (launch_pdl(ce_colsum_kernel, dim3(tiles(a.d, 64), c.strips), 256, 0, a.stream, (const float*)dy, l.h, a.ld_h,
-                       (const float2*)l.stats, a.M, a.d, part) != cudaSuccess ||
-            launch_pdl(ce_colsum_final_kernel, dim3(tiles(2 * a.d, 256)), 256, 0, a.stream, (const float*)part, c.strips, a.d, a.dce, a.dloss,
-                       a.loss, a.accumulate, static_cast<__nv_bfloat16*>(a.dgamma), static_cast<__nv_bfloat16*>(a.dbeta)) != cudaSuccess)
-            return EE_ERR_CUDA;
-    }
+    b.cols = a.dgamma ? reinterpret_cast<float*>(ws + s.cols) : nullptr;
+    b.warps = c.back_warps; b.groups = c.back_groups; b.strip = c.back_strip;
+    if (launch_pdl(back_rows(a.d) == 4 ? ce_back_kernel<4, 640> : ce_back_kernel<1, 1024>, dim3(c.back_ctas), 32 * c.back_warps * c.back_groups, 0,
+                   a.stream, b) != cudaSuccess)
+        return EE_ERR_CUDA;
+    if (a.dgamma &&
+        launch_pdl(ce_colsum_kernel, dim3(tiles(2 * a.d, 32)), 1024, 0, a.stream, (const float*)b.cols, c.back_ctas * c.back_groups, a.d, a.dce,
+                   a.dloss, a.loss, a.accumulate, static_cast<__nv_bfloat16*>(a.dgamma), static_cast<__nv_bfloat16*>(a.dbeta)) != cudaSuccess)
+        return EE_ERR_CUDA;
     return EE_OK;
 }
 

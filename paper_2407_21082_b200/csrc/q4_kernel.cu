@@ -66,47 +66,76 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a
 
 // ---------------------------------------------------------------------------------------------------- writing and reading
 
-// Eight bf16 (a 16-byte vector) -> a word of nibbles, q = nearest whole number of w / s, ties to the even one.
-__device__ __forceinline__ uint32_t q4_word(uint4 v, float s) {
-    const float x[8] = {bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y), bf16_lo(v.z), bf16_hi(v.z), bf16_lo(v.w), bf16_hi(v.w)};
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int q = s > 0.f ? max(-8, min(7, __float2int_rn(__fdiv_rn(x[j], s)))) : 0;
-        w |= (uint32_t)(q + 8) << (4 * ((j >> 1) + 4 * (j & 1)));
-    }
-    return w;
+// 32 bytes with one access: the 16 columns a lane owns are a whole sector, where two 16-byte accesses would each move half of
+// every sector they touch (packing + unpacking at d = 2048, V = 50304: 242 us with two, PACK_US with one).
+struct Sector { uint32_t w[8]; };
+__device__ __forceinline__ Sector ld_sector(const void* p) {
+    Sector s;
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(s.w[0]), "=r"(s.w[1]), "=r"(s.w[2]), "=r"(s.w[3]), "=r"(s.w[4]), "=r"(s.w[5]), "=r"(s.w[6]), "=r"(s.w[7]) : "l"(p));
+    return s;
 }
-__device__ __forceinline__ float amax8(uint4 v) {
-    float m = fmaxf(fabsf(bf16_lo(v.x)), fabsf(bf16_hi(v.x)));
-    m = fmaxf(m, fmaxf(fabsf(bf16_lo(v.y)), fabsf(bf16_hi(v.y))));
-    m = fmaxf(m, fmaxf(fabsf(bf16_lo(v.z)), fabsf(bf16_hi(v.z))));
-    return fmaxf(m, fmaxf(fabsf(bf16_lo(v.w)), fabsf(bf16_hi(v.w))));
+__device__ __forceinline__ void st_sector(void* p, const Sector& s) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(s.w[0]), "r"(s.w[1]), "r"(s.w[2]), "r"(s.w[3]), "r"(s.w[4]), "r"(s.w[5]), "r"(s.w[6]), "r"(s.w[7]) : "memory");
 }
 
-// A warp per 16 rows x 128 columns (two blocks, so that a group of 128 lies inside).
+__device__ __forceinline__ float amax16(const Sector& v) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fmaxf(fabsf(bf16_lo(v.w[i])), fabsf(bf16_hi(v.w[i]))));
+    return m;
+}
+
+// q + 8 of one weight, q = nearest whole number of x / s, ties to the even one; r = 1 / s.  A quotient of two numbers of eight
+// significant bits and at most 8 in magnitude is either exactly a whole number and a half or at least 2^-11 away from one,
+// while x r is off by less than 2^-20: rounded to the grid of 2^-13 first, it is a tie exactly where the quotient is.
+__device__ __forceinline__ uint32_t q4_fast(float x, float r) {
+    const float snapped = __fadd_rn(__fadd_rn(__fmul_rn(x, r), 1536.f), -1536.f);
+    return __float_as_uint(__fadd_rn(snapped, 12582912.f + 8.f)) & 15u;          // 1.5 * 2^23: the low bits are the whole number
+}
+__device__ __forceinline__ uint32_t q4_slow(float x, float s) {                    // scales next to or below the smallest normal number
+    return (uint32_t)(max(-8, min(7, __float2int_rn(__fdiv_rn(x, s)))) + 8);
+}
+// Words [i] = columns 8i .. 8i + 7 of the lane's sixteen.
+__device__ __forceinline__ uint2 q4_words(const Sector& v, float s) {
+    if (!(s > 0.f)) return make_uint2(0x88888888u, 0x88888888u);
+    uint32_t w[2] = {0, 0};
+    if (s >= 1e-30f) {
+        const float r = __frcp_rn(s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= (q4_fast(bf16_lo(v.w[i]), r) << (4 * (i & 3))) | (q4_fast(bf16_hi(v.w[i]), r) << (4 * (i & 3) + 16));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= (q4_slow(bf16_lo(v.w[i]), s) << (4 * (i & 3))) | (q4_slow(bf16_hi(v.w[i]), s) << (4 * (i & 3) + 16));
+    }
+    return make_uint2(w[0], w[1]);
+}
+
+// A warp per 16 rows x 128 columns (two blocks, so that a group of 128 lies inside).  An ordinary launch, here and below: the
+// weights may just have been written, and 32-byte loads take the L1.
 __global__ void __launch_bounds__(256) q4_pack_kernel(const __nv_bfloat16* W, int V, int d, int group, uint4* weights, uint32_t* scales) {
-    launch_dependents();
     const Q4Layout l = q4_layout(V, d, group);
     const int pairs = (l.blocks + 1) / 2;
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    grid_dependency_wait();
     if (unit >= (long long)l.tiles * pairs) return;
     const int tile = (int)(unit / pairs), b0 = 2 * (int)(unit % pairs);
-    uint4 v[2][2][2];                              // [block][row g, row g + 8][first, second eight columns]
+    Sector v[2][2];                                // [block][row g, row g + 8]
     float m[2][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int row = tile * 16 + g + 8 * r;
+            const int row = tile * 16 + g + 8 * r, col = (b0 + b) * 64 + c * 16;
+            v[b][r] = Sector{};
+            if (row < V && col < d) v[b][r] = ld_sector(W + (size_t)row * d + col);      // d is a multiple of 32: a whole sector
+        }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int col = (b0 + b) * 64 + c * 16 + e * 8;
-                v[b][r][e] = (row < V && col < d) ? ld_dep(reinterpret_cast<const uint4*>(W + (size_t)row * d + col)) : make_uint4(0, 0, 0, 0);
-            }
-            m[b][r] = fmaxf(amax8(v[b][r][0]), amax8(v[b][r][1]));
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            m[b][r] = amax16(v[b][r]);
             m[b][r] = fmaxf(m[b][r], __shfl_xor_sync(0xffffffffu, m[b][r], 1));
             if (group >= 64) m[b][r] = fmaxf(m[b][r], __shfl_xor_sync(0xffffffffu, m[b][r], 2));
         }
@@ -117,35 +146,32 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const __nv_bfloat16* W, in
     for (int b = 0; b < 2; ++b) {
         if (b0 + b >= l.blocks) break;
         const uint32_t s2 = pack_bf16(__fdiv_rn(m[b][0], 7.f), __fdiv_rn(m[b][1], 7.f));
-        const float s0 = bf16_lo(s2), s1 = bf16_hi(s2);
-        weights[((size_t)tile * l.blocks + b0 + b) * 32 + lane] =
-            make_uint4(q4_word(v[b][0][0], s0), q4_word(v[b][0][1], s0), q4_word(v[b][1][0], s1), q4_word(v[b][1][1], s1));
+        const uint2 wg = q4_words(v[b][0], bf16_lo(s2)), wh = q4_words(v[b][1], bf16_hi(s2));
+        weights[((size_t)tile * l.blocks + b0 + b) * 32 + lane] = make_uint4(wg.x, wg.y, wh.x, wh.y);
         const int col = (b0 + b) * 64 + c * 16;
         if (col % group == 0) scales[((size_t)tile * l.groups + col / group) * 8 + g] = s2;
     }
 }
 
+// A warp per 16 rows x 64 columns.
 __global__ void __launch_bounds__(256) q4_unpack_kernel(const uint4* weights, const uint32_t* scales, int V, int d, int group, __nv_bfloat16* W) {
-    launch_dependents();
     const Q4Layout l = q4_layout(V, d, group);
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const long long unit = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    grid_dependency_wait();
     if (unit >= (long long)l.tiles * l.blocks) return;
     const int tile = (int)(unit / l.blocks), b = (int)(unit % l.blocks);
     const int col = b * 64 + c * 16;
-    const uint4 w = ld_dep(weights + unit * 32 + lane);
-    const uint32_t s2 = ld_dep(scales + ((size_t)tile * l.groups + col / group) * 8 + g);
+    const uint4 w = weights[unit * 32 + lane];
+    const uint32_t s2 = scales[((size_t)tile * l.groups + col / group) * 8 + g];
     const uint32_t words[2][2] = {{w.x, w.y}, {w.z, w.w}};
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int row = tile * 16 + g + 8 * r;
         const uint32_t s = r ? high_twice(s2) : low_twice(s2);
+        Sector o;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (row < V && col + e * 8 < d)
-                *reinterpret_cast<uint4*>(W + (size_t)row * d + col + e * 8) =
-                    make_uint4(q4_pair(words[r][e], 0, s), q4_pair(words[r][e], 1, s), q4_pair(words[r][e], 2, s), q4_pair(words[r][e], 3, s));
+        for (int i = 0; i < 8; ++i) o.w[i] = q4_pair(words[r][i >> 2], i & 3, s);
+        if (row < V && col < d) st_sector(W + (size_t)row * d + col, o);
     }
 }
 
@@ -327,15 +353,17 @@ static const uint32_t* q4_scales(const void* q4, int V, int d, int group) {
 ee_status q4_pack_launch(const void* W, int V, int d, int group, void* q4, cudaStream_t stream) {
     const Q4Layout l = q4_layout(V, d, group);
     const long long units = (long long)l.tiles * ((l.blocks + 1) / 2);
-    return launch_pdl(q4_pack_kernel, dim3((unsigned)((units + 7) / 8)), 256, 0, stream, static_cast<const __nv_bfloat16*>(W), V, d, group,
-                      static_cast<uint4*>(q4), const_cast<uint32_t*>(q4_scales(q4, V, d, group))) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    q4_pack_kernel<<<(unsigned)((units + 7) / 8), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(W), V, d, group, static_cast<uint4*>(q4),
+                                                                    const_cast<uint32_t*>(q4_scales(q4, V, d, group)));
+    return cudaGetLastError() == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 ee_status q4_unpack_launch(const void* q4, int V, int d, int group, void* W, cudaStream_t stream) {
     const Q4Layout l = q4_layout(V, d, group);
     const long long units = (long long)l.tiles * l.blocks;
-    return launch_pdl(q4_unpack_kernel, dim3((unsigned)((units + 7) / 8)), 256, 0, stream, static_cast<const uint4*>(q4),
-                      q4_scales(q4, V, d, group), V, d, group, static_cast<__nv_bfloat16*>(W)) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    q4_unpack_kernel<<<(unsigned)((units + 7) / 8), 256, 0, stream>>>(static_cast<const uint4*>(q4), q4_scales(q4, V, d, group), V, d, group,
+                                                                      static_cast<__nv_bfloat16*>(W));
+    return cudaGetLastError() == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 size_t q4_head_workspace_bytes(int M, int d) { return kCtrlBytes + parts_bytes() + align_up((size_t)M * d * 2, 256); }

@@ -73,27 +73,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* m, 
         : "memory");
 }
 
-// Tile stores shared -> global (the parts of a box outside the tensor are not written), and the same adding into
-// global memory; completion is tracked per thread in bulk groups.
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, uint32_t src, int c0, int c1) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap* m, uint32_t src, int c0, int c1, int c2) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1), "r"(c2)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_add_3d(const CUtensorMap* m, uint32_t src, int c0, int c1, int c2) {
-    asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1), "r"(c2)
-                 : "memory");
-}
-__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }   // sources free
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }         // written
-
 // ---------------------------------------------------------------- tensor memory
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {      // whole warp
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols)
@@ -235,14 +214,13 @@ __device__ __forceinline__ uint64_t smem_desc_k128(uint32_t saddr) {
     return d;
 }
 
-// The same for an MN-major bf16 operand (the contraction runs over the rows in memory): blocks of 64 k-rows of 128
-// bytes (64 elements of the M or N dimension), one block of 8192 bytes per 64 elements.  Eight k-rows make a swizzle
-// group of 1024 bytes (stride byte offset); the leading byte offset leads to the next 64 elements.  A step of K = 16
-// is two groups, 2048 bytes.
-__device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr) {
+// The same for an MN-major bf16 operand (the contraction runs over the rows in memory): blocks of k-rows of 128 bytes (64
+// elements of the M or N dimension) each, `lead` bytes from one block to the next 64 elements (leading byte offset).
+// Eight k-rows make a swizzle group of 1024 bytes (stride byte offset); a step of K = 16 is two groups, 2048 bytes.
+__device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr, uint32_t lead) {
     uint64_t d = 0;
     d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
-    d |= (uint64_t)(8192 >> 4) << 16;
+    d |= (uint64_t)(lead >> 4) << 16;
     d |= (uint64_t)(1024 >> 4) << 32;
     d |= (uint64_t)1 << 46;
     d |= (uint64_t)2 << 61;

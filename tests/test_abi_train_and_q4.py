@@ -37,6 +37,8 @@ def test_argument_errors_of_the_4_bit_heads(lib):
     # half a byte per weight and two per group, rounded up to tiles
     assert f(16, 64, 64) == 512 + 256 and f(50304, 1024, 64) == 50304 * 512 + 50304 * 16 * 2
     assert lib.ee_head_q4_pack(p, 5, 96, 64, p, 1 << 20, N) == 2 and lib.ee_head_q4_pack(N, 5, 64, 64, p, 1 << 20, N) == 1
+    assert lib.ee_head_q4_pack(ctypes.c_void_p(4112), 5, 64, 64, p, 1 << 20, N) == 3                     # 32 bytes, not 16
+    assert lib.ee_head_q4_unpack(p, 1 << 20, 5, 64, 64, ctypes.c_void_p(4112), N) == 3
     assert lib.ee_head_q4_pack(off, 5, 64, 64, p, 1 << 20, N) == 3 and lib.ee_head_q4_pack(p, 5, 64, 64, off, 1 << 20, N) == 3
     assert lib.ee_head_q4_pack(p, 5, 64, 64, p, 512, N) == 4 and lib.ee_head_q4_unpack(p, 512, 5, 64, 64, p, N) == 4
     assert lib.ee_head_q4_unpack(p, 1 << 20, 5, 64, 64, N, N) == 1
