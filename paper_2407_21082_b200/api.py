@@ -488,25 +488,49 @@ def _workspace_of(nbytes: int, where: str, device) -> torch.Tensor:
     return ws
 
 
-def _on_current(t: torch.Tensor, name: str) -> torch.Tensor:
-    """The library launches on the current device: a tensor of another one is refused."""
-    _dev(t, name)
-    if t.get_device() != torch._C._cuda_getDevice():
+# The checks of the calls below are a few attribute reads per tensor: these calls take ten to twenty microseconds on the device, and
+# a wrapper that takes as long sets the pace of a decoding loop that does not prepare its calls.
+def _device_of(t, name: str) -> int:
+    """Ordinal of the CUDA device t is on.  The library launches on the current device: a tensor of another one is refused."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a CUDA tensor")
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _vector(t, name: str, dtype, n: int, dev: int):
+    """t, a contiguous tensor of n elements on device `dev`."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on cuda:{dev}")
     return t
 
 
-def _buffer(t, name, dtype, shape, device):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype == dtype and t.is_contiguous() and
-            tuple(t.shape) == tuple(shape)):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _matrix(t, name: str, dtype, rows: int, cols: int, dev: int):
+    """t, a contiguous tensor [rows, cols] on device `dev`."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor [{rows}, {cols}] on cuda:{dev}")
     return t
 
 
-def _scratch(workspace, device):
-    if not (isinstance(workspace, torch.Tensor) and workspace.device == device and workspace.dtype == torch.uint8 and
-            workspace.is_contiguous()):
-        raise ValueError(f"workspace must be a contiguous uint8 tensor on {device}")
+def _row_stride(t, name: str, rows: int, cols: int, dev: int) -> int:
+    """Row stride of t, a row-major bf16 matrix [rows, cols] on device `dev`."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or t.get_device() != dev or t.shape != (rows, cols):
+        raise ValueError(f"{name} must be a bfloat16 tensor [{rows}, {cols}] on cuda:{dev}")
+    if rows == 0:
+        return cols
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name} must be row-major")
+    return ld if rows > 1 else max(ld, cols)
+
+
+def _scratch(workspace, dev: int):
+    if not isinstance(workspace, torch.Tensor) or workspace.dtype is not torch.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{dev}")
     return workspace
 
 
@@ -529,23 +553,32 @@ def new_head_ce_grad_workspace(M: int, d: int, V: int, device="cuda") -> torch.T
 
 
 def _head_ce_inputs(head, labels):
-    h, W, (M, d, V) = _check_head_tensors(head["h"], head["gamma"], head["beta"], head["W"], None)
-    _on_current(h, "h")
-    _buffer(labels, "labels", torch.int32, (M,), h.device)
-    ld = h.stride(0) if M > 1 else max(h.stride(0), d)
-    return h, W, ld, M, d, V
+    h, W = _bf16(head["h"]), _bf16(head["W"])
+    dev = _device_of(h, "h")
+    if h.dim() != 2 or W.dim() != 2:
+        raise ValueError("h must be [M, d] and W [V, d]")
+    M, d = h.shape
+    V = W.shape[0]
+    ld = _row_stride(h, "h", M, d, dev)
+    _matrix(W, "W", torch.bfloat16, V, d, dev)
+    _vector(head["gamma"], "gamma", torch.float32, d, dev)
+    _vector(head["beta"], "beta", torch.float32, d, dev)
+    _vector(labels, "labels", torch.int32, M, dev)
+    return h, W, ld, M, d, V, dev
 
 
 def _head_ce_args(head, labels, ln_eps, out, workspace):
-    h, W, ld, M, d, V = _head_ce_inputs(head, labels)
+    h, W, ld, M, d, V, dev = _head_ce_inputs(head, labels)
     if out is None:
-        out = dict(ce=torch.empty(M, dtype=torch.float32, device=h.device), lse=torch.empty(M, dtype=torch.float32, device=h.device),
-                   loss=torch.empty(2, dtype=torch.float32, device=h.device))
-    for name, shape in (("ce", (M,)), ("lse", (M,)), ("loss", (2,))):
-        _buffer(out.get(name), f"out[{name!r}]", torch.float32, shape, h.device)
-    workspace = new_head_ce_workspace(M, d, V, h.device) if workspace is None else _scratch(workspace, h.device)
-    args = (_ptr(h), ld, _ptr(head["gamma"]), _ptr(head["beta"]), float(ln_eps), _ptr(W), M, d, V, _ptr(labels), _ptr(out["ce"]),
-            _ptr(out["lse"]), _ptr(out["loss"]), _ptr(workspace), workspace.numel(), _stream())
+        f32 = torch.float32
+        out = dict(ce=torch.empty(M, dtype=f32, device=h.device), lse=torch.empty(M, dtype=f32, device=h.device),
+                   loss=torch.empty(2, dtype=f32, device=h.device))
+    else:
+        for name, n in (("ce", M), ("lse", M), ("loss", 2)):
+            _vector(out.get(name), f"out[{name!r}]", torch.float32, n, dev)
+    workspace = new_head_ce_workspace(M, d, V, h.device) if workspace is None else _scratch(workspace, dev)
+    args = (h.data_ptr(), ld, head["gamma"].data_ptr(), head["beta"].data_ptr(), ln_eps, W.data_ptr(), M, d, V, labels.data_ptr(),
+            out["ce"].data_ptr(), out["lse"].data_ptr(), out["loss"].data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
     return args, out, (h, W, head, labels, out, workspace)
 
 
@@ -564,30 +597,31 @@ def prepare_head_ce(head, labels, ln_eps, *, out=None, workspace=None) -> Prepar
 
 
 def _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace):
-    h, W, ld, M, d, V = _head_ce_inputs(head, labels)
-    dev = h.device
-    lse, loss = _buffer(forward["lse"], "lse", torch.float32, (M,), dev), _buffer(forward["loss"], "loss", torch.float32, (2,), dev)
+    h, W, ld, M, d, V, dev = _head_ce_inputs(head, labels)
+    lse, loss = _vector(forward["lse"], "lse", torch.float32, M, dev), _vector(forward["loss"], "loss", torch.float32, 2, dev)
     if dce is not None:
-        _buffer(dce, "dce", torch.float32, (M,), dev)
-    if dloss is not None and not (isinstance(dloss, torch.Tensor) and dloss.device == dev and dloss.dtype == torch.float32 and dloss.numel() == 1):
-        raise ValueError("dloss must be a float32 CUDA tensor of one element")
+        _vector(dce, "dce", torch.float32, M, dev)
+    if dloss is not None:
+        _vector(dloss, "dloss", torch.float32, 1, dev)
+    bf16 = torch.bfloat16
+    ld_dh = d
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the buffers to add to (out)")
-        out = dict(dh=torch.empty((M, d), dtype=torch.bfloat16, device=dev), dW=torch.empty((V, d), dtype=torch.bfloat16, device=dev),
-                   dgamma=torch.empty(d, dtype=torch.bfloat16, device=dev), dbeta=torch.empty(d, dtype=torch.bfloat16, device=dev))
-    dh = out.get("dh")
-    if dh is not None and not (isinstance(dh, torch.Tensor) and dh.device == dev and dh.dtype == torch.bfloat16 and dh.shape == (M, d) and
-                               (M == 0 or dh.stride(1) == 1)):
-        raise ValueError("out['dh'] must be a row-major bfloat16 tensor [M, d] on the device of h")
-    for name, shape in (("dW", (V, d)), ("dgamma", (d,)), ("dbeta", (d,))):
-        if out.get(name) is not None:
-            _buffer(out[name], f"out[{name!r}]", torch.bfloat16, shape, dev)
-    workspace = new_head_ce_grad_workspace(M, d, V, dev) if workspace is None else _scratch(workspace, dev)
-    ld_dh = d if dh is None else (dh.stride(0) if M > 1 else max(dh.stride(0), d))
-    args = (_ptr(h), ld, _ptr(head["gamma"]), _ptr(head["beta"]), float(ln_eps), _ptr(W), M, d, V, _ptr(labels), _ptr(lse), _ptr(loss),
-            _ptr(dce), _ptr(dloss), _ptr(dh), ld_dh, _ptr(out.get("dW")), _ptr(out.get("dgamma")), _ptr(out.get("dbeta")),
-            int(bool(accumulate)), _ptr(workspace), workspace.numel(), _stream())
+        out = dict(dh=torch.empty((M, d), dtype=bf16, device=h.device), dW=torch.empty((V, d), dtype=bf16, device=h.device),
+                   dgamma=torch.empty(d, dtype=bf16, device=h.device), dbeta=torch.empty(d, dtype=bf16, device=h.device))
+    else:
+        if out.get("dh") is not None:
+            ld_dh = _row_stride(out["dh"], "out['dh']", M, d, dev)
+        if out.get("dW") is not None:
+            _matrix(out["dW"], "out['dW']", bf16, V, d, dev)
+        for name in ("dgamma", "dbeta"):
+            if out.get(name) is not None:
+                _vector(out[name], f"out[{name!r}]", bf16, d, dev)
+    workspace = new_head_ce_grad_workspace(M, d, V, h.device) if workspace is None else _scratch(workspace, dev)
+    args = (h.data_ptr(), ld, head["gamma"].data_ptr(), head["beta"].data_ptr(), ln_eps, W.data_ptr(), M, d, V, labels.data_ptr(),
+            lse.data_ptr(), loss.data_ptr(), _ptr(dce), _ptr(dloss), _ptr(out.get("dh")), ld_dh, _ptr(out.get("dW")), _ptr(out.get("dgamma")),
+            _ptr(out.get("dbeta")), int(bool(accumulate)), workspace.data_ptr(), workspace.numel(), _stream())
     return args, out, (h, W, head, labels, forward, dce, dloss, out, workspace)
 
 
@@ -625,7 +659,8 @@ def ee_head_q4_bytes(V: int, d: int, group: int) -> int:
 
 def ee_head_q4_pack(W, group: int = 64, *, out: Q4Weights | None = None) -> Q4Weights:
     """Writes a head's weights (bf16 [V, d]) in 4 bits with a scale per row and `group` columns (see include/eexit.h)."""
-    W = _on_current(_bf16(_dev(W, "W")), "W")
+    W = _bf16(W)
+    dev = _device_of(W, "W")
     if W.dim() != 2 or not W.is_contiguous():
         raise ValueError("W must be contiguous [V, d]")
     V, d = W.shape
@@ -634,19 +669,21 @@ def ee_head_q4_pack(W, group: int = 64, *, out: Q4Weights | None = None) -> Q4We
         if nbytes == 0:
             raise EExitError(2, "ee_head_q4_pack")
         out = Q4Weights(torch.empty(nbytes, dtype=torch.uint8, device=W.device), V, d, group)
-    elif (out.V, out.d, out.group) != (V, d, group) or out.data.device != W.device:
+    elif (out.V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
         raise ValueError("out was made for other weights")
-    _check(_lib.load().ee_head_q4_pack(_ptr(W), V, d, int(group), _ptr(out.data), out.data.numel(), _stream()), "ee_head_q4_pack")
+    _check(_lib.load().ee_head_q4_pack(W.data_ptr(), V, d, int(group), out.data.data_ptr(), out.data.numel(), _stream()), "ee_head_q4_pack")
     return out
 
 
 def ee_head_q4_unpack(q4: Q4Weights, *, out=None) -> torch.Tensor:
     """What the packed weights stand for, bf16 [V, d]."""
-    _on_current(q4.data, "q4")
+    dev = _device_of(q4.data, "q4")
     if out is None:
         out = torch.empty((q4.V, q4.d), dtype=torch.bfloat16, device=q4.data.device)
-    _buffer(out, "out", torch.bfloat16, (q4.V, q4.d), q4.data.device)
-    _check(_lib.load().ee_head_q4_unpack(_ptr(q4.data), q4.data.numel(), q4.V, q4.d, q4.group, _ptr(out), _stream()), "ee_head_q4_unpack")
+    else:
+        _matrix(out, "out", torch.bfloat16, q4.V, q4.d, dev)
+    _check(_lib.load().ee_head_q4_unpack(q4.data.data_ptr(), q4.data.numel(), q4.V, q4.d, q4.group, out.data_ptr(), _stream()),
+           "ee_head_q4_unpack")
     return out
 
 
@@ -660,27 +697,33 @@ def new_exit_head_q4_workspace(M: int, q4: Q4Weights) -> torch.Tensor:
 
 
 def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
-    h = _on_current(_bf16(_dev(h, "h")), "h")
-    if h.dim() != 2 or h.shape[1] != q4.d or (h.shape[0] > 0 and h.stride(1) != 1):
-        raise ValueError(f"h must be row-major [M, d = {q4.d}]")
-    M, dev = h.shape[0], h.device
-    if q4.data.device != dev:
-        raise ValueError(f"q4 is on {q4.data.device}, h on {dev}")
-    _buffer(gamma, "gamma", torch.float32, (q4.d,), dev)
-    _buffer(beta, "beta", torch.float32, (q4.d,), dev)
+    h = _bf16(h)
+    dev = _device_of(h, "h")
+    d = q4.d
+    if h.dim() != 2:
+        raise ValueError(f"h must be row-major [M, d = {d}]")
+    M = h.shape[0]
+    ld = _row_stride(h, "h", M, d, dev)
+    data = q4.data
+    if data.get_device() != dev:
+        raise ValueError(f"q4 is on {data.device}, h on {h.device}")
+    _vector(gamma, "gamma", torch.float32, d, dev)
+    _vector(beta, "beta", torch.float32, d, dev)
+    tau_t = tau_ptr = None
     if isinstance(tau, torch.Tensor):
-        _buffer(tau, "a per-row tau", torch.float32, (M,), dev)
+        tau_t, tau = _vector(tau, "a per-row tau", torch.float32, M, dev), 0.0
+        tau_ptr = tau_t.data_ptr()
     if out is None:
-        out = new_outputs(M, dev)
-    for name, dtype in _OUT_DTYPES.items():
-        t = out.get(name)
-        if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype == dtype and t.is_contiguous() and t.numel() >= M):
-            raise ValueError(f"out[{name!r}] must be a contiguous {dtype} CUDA tensor of at least M = {M} elements")
+        out = new_outputs(M, h.device)
+    else:
+        for name, dtype in _OUT_DTYPES.items():
+            t = out.get(name)
+            if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < M:
+                raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of at least M = {M} elements on cuda:{dev}")
     workspace = new_exit_head_q4_workspace(M, q4) if workspace is None else _scratch(workspace, dev)
-    tau_t, tau_f = (tau, 0.0) if isinstance(tau, torch.Tensor) else (None, float(tau))
-    args = (_ptr(h), h.stride(0) if M > 1 else max(h.stride(0), q4.d), _ptr(gamma), _ptr(beta), float(ln_eps), _ptr(q4.data), q4.data.numel(),
-            q4.group, M, q4.d, q4.V, _ptr(tau_t), tau_f, _ptr(out["argmax"]), _ptr(out["entropy"]), _ptr(out["maxprob"]),
-            _ptr(out["exit_mask"]), _ptr(workspace), workspace.numel(), _stream())
+    args = (h.data_ptr(), ld, gamma.data_ptr(), beta.data_ptr(), ln_eps, data.data_ptr(), data.numel(), q4.group, M, d, q4.V, tau_ptr, tau,
+            out["argmax"].data_ptr(), out["entropy"].data_ptr(), out["maxprob"].data_ptr(), out["exit_mask"].data_ptr(),
+            workspace.data_ptr(), workspace.numel(), _stream())
     return args, out, (h, gamma, beta, q4, tau_t, out, workspace)
 
 
@@ -696,24 +739,19 @@ def prepare_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None
     return PreparedCall(_lib.load().ee_exit_head_q4, args, "ee_exit_head_q4", keep, out)
 
 
-def _rows_of(t, name, n, d, device):
-    if not (isinstance(t, torch.Tensor) and t.device == device and t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape == (n, d) and
-            (n == 0 or t.stride(1) == 1)):
-        raise ValueError(f"{name} must be a row-major bfloat16 tensor [{n}, {d}] on {device}")
-    return t.stride(0) if n > 1 else max(t.stride(0), d)
-
-
 def _embed_args(table, tokens, scale, out):
-    table = _on_current(_bf16(_dev(table, "table")), "table")
+    table = _bf16(table)
+    dev = _device_of(table, "table")
     if table.dim() != 2 or not table.is_contiguous():
         raise ValueError("table must be contiguous [V, d]")
     V, d = table.shape
     n = tokens.numel()
-    _buffer(tokens, "tokens", torch.int32, (n,), table.device)
+    _vector(tokens, "tokens", torch.int32, n, dev)
     if out is None:
-        out = torch.empty((n, d), dtype=torch.bfloat16, device=table.device)
-    ld = _rows_of(out, "out", n, d, table.device)
-    args = (_ptr(table), V, d, _ptr(tokens), n, float(scale), _ptr(out), ld, _stream())
+        out, ld = table.new_empty((n, d)), d
+    else:
+        ld = _row_stride(out, "out", n, d, dev)
+    args = (table.data_ptr(), V, d, tokens.data_ptr(), n, scale, out.data_ptr(), ld, _stream())
     return args, out, (table, tokens, out)
 
 
@@ -743,26 +781,26 @@ def new_embed_grad_workspace(n: int, d: int, V: int, device="cuda") -> torch.Ten
 
 
 def _embed_grad_args(dout, tokens, V, scale, dtype, out, accumulate, workspace):
-    dout = _on_current(_bf16(_dev(dout, "dout")), "dout")
+    dout = _bf16(dout)
+    dev = _device_of(dout, "dout")
     if dout.dim() != 2:
         raise ValueError("dout must be [n, d]")
     n, d = dout.shape
-    ld = _rows_of(dout, "dout", n, d, dout.device)
-    _buffer(tokens, "tokens", torch.int32, (n,), dout.device)
-    if dtype not in (torch.bfloat16, torch.float32):
+    ld = _row_stride(dout, "dout", n, d, dev)
+    _vector(tokens, "tokens", torch.int32, n, dev)
+    if out is not None:
+        dtype = out.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
         raise ValueError("the table's gradient is bfloat16 or float32")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the table to add to (out)")
         out = torch.empty((V, d), dtype=dtype, device=dout.device)
     else:
-        dtype = out.dtype
-        if dtype not in (torch.bfloat16, torch.float32):
-            raise ValueError("the table's gradient is bfloat16 or float32")
-    _buffer(out, "out", dtype, (V, d), dout.device)
-    workspace = new_embed_grad_workspace(n, d, V, dout.device) if workspace is None else _scratch(workspace, dout.device)
-    args = (_ptr(dout), ld, _ptr(tokens), n, int(V), d, float(scale), _ptr(out), int(dtype == torch.float32), int(bool(accumulate)),
-            _ptr(workspace), workspace.numel(), _stream())
+        _matrix(out, "out", dtype, V, d, dev)
+    workspace = new_embed_grad_workspace(n, d, V, dout.device) if workspace is None else _scratch(workspace, dev)
+    args = (dout.data_ptr(), ld, tokens.data_ptr(), n, V, d, scale, out.data_ptr(), 1 if dtype is torch.float32 else 0, 1 if accumulate else 0,
+            workspace.data_ptr(), workspace.numel(), _stream())
     return args, out, (dout, tokens, out, workspace)
 
 

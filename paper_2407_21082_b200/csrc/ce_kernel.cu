@@ -477,6 +477,18 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     }
 }
 
+// Vector c (columns 8c .. 8c + 7) of a row of y.  Permuted, column 16m + 4j + i of every 64 (m, j, i < 4) lies at 16j + 4m + i.
+__device__ __forceinline__ void put_vec8(uint4* yrow, int c, uint4 v, int permuted) {
+    if (!permuted) {
+        yrow[c] = v;
+        return;
+    }
+    uint2* block = reinterpret_cast<uint2*>(yrow + (c & ~7));            // pieces of four columns
+    const int m = (c & 7) >> 1, j = 2 * (c & 1);
+    block[4 * j + m] = make_uint2(v.x, v.y);
+    block[4 * (j + 1) + m] = make_uint2(v.z, v.w);
+}
+
 // LayerNorm of the rows into y, a warp per row.  In the backward pass (`stats` given) it also leaves each row's mean
 // and 1/sigma for the way back, and a row that takes no part in the gradient becomes zeros with 1/sigma = 0.
 struct CeLnArgs {
@@ -490,6 +502,7 @@ struct CeLnArgs {
     int V;
     __nv_bfloat16* y;
     int ld_y;              // columns of y from d on are zeros
+    int permuted;          // y in the column order of the 4-bit heads (q4_gemm.cu)
     float2* stats;
     int M, d;
 };
@@ -502,7 +515,7 @@ __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constan
     const int nvec = a.d >> 3;
     uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.ld_y);
     grid_dependency_wait();
-    if (nvec + lane < a.ld_y >> 3) yrow[nvec + lane] = make_uint4(0, 0, 0, 0);      // fewer than eight vectors
+    if (nvec + lane < a.ld_y >> 3) put_vec8(yrow, nvec + lane, make_uint4(0, 0, 0, 0), a.permuted);      // fewer than eight vectors
     if (a.stats && row_weight(a.labels, a.dce, a.V, row) == 0.f) {
         for (int c = lane; c < nvec; c += 32) yrow[c] = make_uint4(0, 0, 0, 0);
         if (lane == 0) a.stats[row] = make_float2(0.f, 0.f);
@@ -510,11 +523,75 @@ __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constan
     }
     const uint4* hrow = reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h);
     const RowStats st = row_stats_strided([&](int c) { return ld_dep(hrow + c); }, nvec, a.ln_eps, lane);
-    for (int c = lane; c < nvec; c += 32) yrow[c] = layer_norm_vec8(ld_dep(hrow + c), st, a.gamma, a.beta, c);
+    for (int c = lane; c < nvec; c += 32) put_vec8(yrow, c, layer_norm_vec8(ld_dep(hrow + c), st, a.gamma, a.beta, c), a.permuted);
     if (a.stats && lane == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
 }
 
 constexpr int kMergeThreads = 1024;
+
+// The same with a CTA per row, for batches that do not fill the SMs with a warp per row: every step of the chain -- the loads,
+// the sums, the normalisation -- is one vector per thread (up to four at d = 8192) instead of d / 256.
+constexpr int kLnCtaThreads = 256;
+__global__ void __launch_bounds__(kLnCtaThreads) ce_layer_norm_cta_kernel(const __grid_constant__ CeLnArgs a) {
+    __shared__ double sums[2][kLnCtaThreads / 32];
+    launch_dependents();
+    const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int nvec = a.d >> 3, warps = blockDim.x >> 5;
+    float4 g[2], b[2];
+    const bool first = (int)threadIdx.x < nvec;
+    if (first) {                                                         // the first vector's parameters before the wait
+        g[0] = ld_param4(a.gamma + 8 * threadIdx.x); g[1] = ld_param4(a.gamma + 8 * threadIdx.x + 4);
+        b[0] = ld_param4(a.beta + 8 * threadIdx.x); b[1] = ld_param4(a.beta + 8 * threadIdx.x + 4);
+    }
+    uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.ld_y);
+    grid_dependency_wait();
+    for (int c = nvec + threadIdx.x; c < a.ld_y >> 3; c += blockDim.x) put_vec8(yrow, c, make_uint4(0, 0, 0, 0), a.permuted);
+    if (a.stats && row_weight(a.labels, a.dce, a.V, row) == 0.f) {
+        for (int c = threadIdx.x; c < nvec; c += blockDim.x) yrow[c] = make_uint4(0, 0, 0, 0);
+        if (threadIdx.x == 0) a.stats[row] = make_float2(0.f, 0.f);
+        return;
+    }
+    const uint4* hrow = reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h);
+    uint4 x[4];
+    Moments m;
+    m.clear();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int c = threadIdx.x + k * blockDim.x;
+        if (c < nvec) x[k] = ld_dep(hrow + c);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if ((int)(threadIdx.x + k * blockDim.x) < nvec) m.add(x[k], k);
+    auto cta_sums = [&](double& s, double& q) {                          // in a fixed order, the same bits in every thread
+        warp_sum2_d(s, q);
+        if (lane == 0) { sums[0][warp] = s; sums[1][warp] = q; }
+        __syncthreads();
+        s = q = 0.0;
+        for (int w = 0; w < warps; ++w) { s += sums[0][w]; q += sums[1][w]; }
+        __syncthreads();
+    };
+    const double d = (double)a.d, inv_d = 1.0 / d;
+    double s = m.sum(), q = m.sum_sq(), mu, var;
+    cta_sums(s, q);
+    if (!row_variance_one_pass(s, q, d, inv_d, mu, var)) {
+        double q0 = 0.0, q1 = 0.0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if ((int)(threadIdx.x + k * blockDim.x) < nvec) vec8_sqdev_d(x[k], mu, q0, q1);
+        double v = q0 + q1, none = 0.0;
+        cta_sums(v, none);
+        var = v * inv_d;
+    }
+    const RowStats st = row_stats(mu, var, a.ln_eps);
+    if (first) put_vec8(yrow, threadIdx.x, layer_norm_vec8(x[0], st, g[0], g[1], b[0], b[1]), a.permuted);
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+        const int c = threadIdx.x + k * blockDim.x;
+        if (c < nvec) put_vec8(yrow, c, layer_norm_vec8(x[k], st, a.gamma, a.beta, c), a.permuted);
+    }
+    if (a.stats && threadIdx.x == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
+}
 
 // Sum of v over the threads of a merging CTA, in a fixed order.
 __device__ __forceinline__ double cta_sum_d(double v, double* part) {
@@ -943,6 +1020,7 @@ CeLnArgs ln_args(const CeArgs& a, const CeSpace& s, bool grad) {
     l.labels = a.labels; l.dce = a.dce; l.V = a.V;
     l.y = reinterpret_cast<__nv_bfloat16*>(ws + s.y);
     l.ld_y = tiles(a.d, 64) * 64;
+    l.permuted = 0;
     l.stats = grad ? reinterpret_cast<float2*>(ws + s.stats) : nullptr;
     l.M = a.M; l.d = a.d;
     return l;
@@ -962,15 +1040,26 @@ CeParams base_params(const CeArgs& a) {
 
 }  // namespace
 
-ee_status layer_norm_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int M, int d,
-                            cudaStream_t stream) {
+// A CTA per row up to kLnCtaRows rows, above that a warp per row.
+constexpr int kLnCtaRows = 1024;
+static ee_status ln_launch(const CeLnArgs& l, cudaStream_t stream) {
+    if (l.M <= kLnCtaRows) {
+        const int warps = (l.d / 8 + 31) / 32;
+        return launch_pdl(ce_layer_norm_cta_kernel, dim3(l.M), 32 * (warps < 8 ? warps : 8), 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    }
+    return launch_pdl(ce_layer_norm_kernel, dim3((l.M + 7) / 8), 256, 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+ee_status layer_norm_permuted_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int ld_y,
+                                     int M, int d, cudaStream_t stream) {
     CeLnArgs l{};
     l.h = static_cast<const __nv_bfloat16*>(h);
     l.ld_h = ld_h; l.gamma = gamma; l.beta = beta; l.ln_eps = ln_eps;
     l.y = static_cast<__nv_bfloat16*>(y);
-    l.ld_y = d;
+    l.ld_y = ld_y;
+    l.permuted = 1;
     l.M = M; l.d = d;
-    return launch_pdl(ce_layer_norm_kernel, dim3((M + 7) / 8), 256, 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    return ln_launch(l, stream);
 }
 
 size_t ce_workspace_bytes(int M, int d, int V, bool grad) { return ce_space(M, d, V, grad).total; }
@@ -979,7 +1068,8 @@ ee_status ce_launch(const CeArgs& a) {
     unsigned char* ws = static_cast<unsigned char*>(a.workspace);
     const CeSpace s = ce_space(a.M, a.d, a.V, false);
     const CeLnArgs l = ln_args(a, s, false);
-    if (launch_pdl(ce_layer_norm_kernel, dim3((a.M + 7) / 8), 256, 0, a.stream, l) != cudaSuccess) return EE_ERR_CUDA;
+    const ee_status ln = ln_launch(l, a.stream);
+    if (ln != EE_OK) return ln;
     const bool pair = use_pairs(a.M, a.device);
     CeMaps maps;
     CeParams p = base_params(a);
@@ -1008,7 +1098,8 @@ ee_status ce_grad_launch(const CeArgs& a) {
     const CeSpace s = ce_space(a.M, a.d, a.V, true);
     const CePlan c = ce_plan(a.M, a.d, a.V);
     const CeLnArgs l = ln_args(a, s, true);
-    if (launch_pdl(ce_layer_norm_kernel, dim3((a.M + 7) / 8), 256, 0, a.stream, l) != cudaSuccess) return EE_ERR_CUDA;
+    const ee_status ln = ln_launch(l, a.stream);
+    if (ln != EE_OK) return ln;
     const bool pair = use_pairs(a.M, a.device);
     const bool need_dy = a.dh || a.dgamma;
     const int ld_g = c.piece;

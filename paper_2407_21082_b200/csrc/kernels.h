@@ -124,8 +124,9 @@ size_t ce_workspace_bytes(int M, int d, int V, bool grad);
 ee_status ce_launch(const CeArgs& a);
 ee_status ce_grad_launch(const CeArgs& a);
 
-ee_status layer_norm_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int M, int d,
-                            cudaStream_t stream);      // y bf16 [M][d], dense
+// y bf16 [M][ld_y] in the column order of the 4-bit heads, ld_y = d rounded up to 64
+ee_status layer_norm_permuted_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int ld_y,
+                                     int M, int d, cudaStream_t stream);
 
 // ---- heads with weights in 4 bits ----
 size_t q4_weight_bytes(int V, int d, int group);

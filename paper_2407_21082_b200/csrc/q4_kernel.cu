@@ -6,15 +6,10 @@
 // The product with the scale is rounded to bf16 because the tensor cores take bf16 operands; it is part of the
 // definition (ee_head_q4_unpack returns the same values), so nothing is lost between the two.
 //
-// Layout of a packed head: 16-row tiles; a tile is a sequence of blocks of 64 columns, 512 bytes each; lane (g, c) =
-// (lane / 4, lane % 4) of a warp owns 16 bytes of a block: columns 16c .. 16c + 15 of row g, then of row g + 8.  That is the
-// operand of four m16n8k16 products if the contraction is walked in the order "lane c: columns 16c + 4s .. 16c + 4s + 3 in
-// step s", which costs nothing as long as the other operand is read in the same order: a lane's share of y is then 32
-// consecutive bytes as well.  Inside a 32-bit word (8 columns) column 2i is nibble i and column 2i + 1 nibble i + 4, each as
-// q + 8, so that one shift and one logic operation make the two bf16 numbers 128 + (q + 8) of a register; subtracting
-// 136 is exact.  The scales lie behind the weights: [tile][group][8] words holding rows g and g + 8.  Rows beyond V and
-// columns beyond d are q = 0.
-#include "common.cuh"
+// The packed layout (q4_common.cuh) is the operand of four m16n8k16 products per block of 64 columns if the contraction is walked
+// in the order "lane c: columns 16c + 4s .. 16c + 4s + 3 in step s", which costs nothing as long as the other operand is read
+// in the same order: a lane's share of y is then 32 consecutive bytes as well.
+#include "q4_common.cuh"
 #include "layer_norm.cuh"
 #include "kernels.h"
 
@@ -24,38 +19,9 @@ namespace {
 
 constexpr int kWarps = 24;                       // 3552 warps on 148 SMs: one 16-row tile each for V = 50304
 constexpr int kThreads = kWarps * 32;
-constexpr int kMaxSlabRows = 64;
-constexpr int kUnroll = 4;                       // blocks (512 bytes of a tile) in flight per warp, twice
+constexpr int kMaxSlabRows = 16;               // rows per launch: above that the tensor-core kernel takes over
+constexpr int kUnroll = 2;                       // blocks (512 bytes of a tile) in flight per warp, twice
 constexpr size_t kSmemBudget = 226 * 1024;
-
-struct Q4Layout {
-    int tiles, blocks, groups;                   // 16-row tiles, 64-column blocks, scale groups per row
-};
-__host__ __device__ inline Q4Layout q4_layout(int V, int d, int group) {
-    Q4Layout l;
-    l.tiles = (V + 15) / 16;
-    l.blocks = (d + 63) / 64;
-    l.groups = (l.blocks * 64 + group - 1) / group;
-    return l;
-}
-
-__device__ __forceinline__ uint32_t hsub2_bf16(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ uint32_t hmul2_bf16(uint32_t a, uint32_t b) {
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-// Columns 2i and 2i + 1 of a word's eight, times the scale (in both halves of s2), as two bf16 numbers.
-__device__ __forceinline__ uint32_t q4_pair(uint32_t word, int i, uint32_t s2) {
-    const uint32_t biased = ((word >> (4 * i)) & 0x000f000fu) | 0x43004300u;      // 128 + (q + 8)
-    return hmul2_bf16(hsub2_bf16(biased, 0x43084308u), s2);                       // the difference is exact, the product rounded once
-}
-__device__ __forceinline__ uint32_t low_twice(uint32_t v) { return __byte_perm(v, 0, 0x1010); }
-__device__ __forceinline__ uint32_t high_twice(uint32_t v) { return __byte_perm(v, 0, 0x3232); }
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -177,28 +143,14 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const uint4* weights, co
 
 // ---------------------------------------------------------------------------------------------------- the head
 
-struct Q4Params {
-    const uint4* weights;
-    const uint32_t* scales;
-    const __nv_bfloat16* y;        // [M][d]
-    int M, d, V, group;
-    State* parts;                  // [ctas][NT * 8]
-    const float* tau_per_row;
-    float tau;
-    int* argmax;
-    float* entropy;
-    float* maxprob;
-    unsigned char* exit_mask;
-    Control* ctrl;
-};
-
 // Bytes between two rows of y in shared memory: 16 more than a multiple of 128, so that the eight lanes of a 16-byte access
 // (two rows, four columns 32 bytes apart) touch every bank once.
 __host__ __device__ inline int y_row_bytes(int d) { return (d + 63) / 64 * 128 + 16; }
 
-// Up to NT * 8 rows: a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all rows
-// of y (in shared memory); the CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges
-// the CTAs' states and decides.
+// Up to NT * 8 rows, one launch: the rows are normalised by every CTA into its shared memory (a warp per row) while the first
+// weights are on their way; a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all
+// rows of y; the CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges the CTAs'
+// states and decides.
 template <int NT>
 __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_constant__ Q4Params p) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -206,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
     const Q4Layout l = q4_layout(p.V, p.d, p.group);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int ld = y_row_bytes(p.d);
-    State* states = reinterpret_cast<State*>(smem + NT * 8 * ld);        // [kWarps][NT * 8]
+    State* states = reinterpret_cast<State*>(smem + NT * 8 * ld);        // [kWarps][max(NT * 8, 32)]: per warp, then scratch of the merge
     launch_dependents();
 
     uint4 w[kUnroll];
@@ -222,21 +174,26 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
     int tile = blockIdx.x + gridDim.x * warp;
     if (tile < l.tiles) load(tile, 0);                                   // weights are constants of the stream
     grid_dependency_wait();
-    for (int i = threadIdx.x; i < NT * 8 * l.blocks * 8; i += kThreads) {
-        const int row = i / (l.blocks * 8), v = i - row * (l.blocks * 8);
-        const uint4 x = (row < p.M && v * 8 < p.d) ? ld_dep(reinterpret_cast<const uint4*>(p.y + (size_t)row * p.d) + v) : make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(smem + row * ld + v * 16) = x;
+    for (int row = warp; row < NT * 8; row += kWarps) {
+        uint4* yrow = reinterpret_cast<uint4*>(smem + row * ld);
+        const int nvec = p.d >> 3;
+        if (row < p.M) {
+            const uint4* hrow = reinterpret_cast<const uint4*>(p.h + (size_t)row * p.ld_h);
+            const RowStats st = row_stats_strided([&](int k) { return ld_dep(hrow + k); }, nvec, p.ln_eps, lane);
+            for (int k = lane; k < nvec; k += 32) yrow[k] = layer_norm_vec8(ld_dep(hrow + k), st, p.gamma, p.beta, k);
+        }
+        for (int k = (row < p.M ? nvec : 0) + lane; k < l.blocks * 8; k += 32) yrow[k] = make_uint4(0, 0, 0, 0);
     }
-    __syncthreads();
-
     State* mine = states + warp * (NT * 8);
     for (int i = lane; i < NT * 8; i += 32) mine[i] = state_empty();
-    __syncwarp();
+    __syncthreads();
+
     const unsigned char* ybase = smem + g * ld + c * 32;
     for (; tile < l.tiles; tile += gridDim.x * kWarps) {
         float acc[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.f;
+#pragma unroll 1
         for (int b0 = 0; b0 < l.blocks; b0 += kUnroll) {
             uint4 cur[kUnroll];
             uint32_t cs[kUnroll];
@@ -297,32 +254,29 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
             }
     }
     __syncthreads();
-    for (int tok = threadIdx.x; tok < p.M; tok += kThreads) {
-        State s = states[tok];
-        for (int k = 1; k < kWarps; ++k) state_merge(s, states[k * (NT * 8) + tok]);
-        p.parts[(size_t)blockIdx.x * (NT * 8) + tok] = s;
+    for (int tok = warp; tok < p.M; tok += kWarps) {                      // the warps' states of a row, one per lane
+        const State s = state_reduce_lanes<1, 16>(lane < kWarps ? states[lane * (NT * 8) + tok] : state_empty());
+        if (lane == 0) p.parts[(size_t)blockIdx.x * (NT * 8) + tok] = s;
     }
     __syncthreads();
     if (threadIdx.x == 0) is_last = ticket_arrive_is_last(&p.ctrl->head_ticket[0], gridDim.x) ? 1 : 0;
     __syncthreads();
     if (!is_last) return;
-    if (gridDim.x <= 160)                                                // one token per warp at a time: registers are short here
-        merge_token_batches<1, 5>(p.parts, false, gridDim.x, NT * 8, p.M, warp, kWarps, lane, p.tau_per_row, p.tau, p.argmax, p.entropy,
-                                  p.maxprob, p.exit_mask);
-    else
-        merge_token_batches<1, 8>(p.parts, false, gridDim.x, NT * 8, p.M, warp, kWarps, lane, p.tau_per_row, p.tau, p.argmax, p.entropy,
-                                  p.maxprob, p.exit_mask);
+    for (int tok = warp; tok < p.M; tok += kWarps) {                      // the CTAs' states, up to eight per lane
+        State v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            v[i] = lane + 32 * i < (int)gridDim.x ? state_load_cg(p.parts + (size_t)(lane + 32 * i) * (NT * 8) + tok) : state_empty();
+        const State s = state_reduce_lanes<1, 16>(state_combine<8>(v));
+        if (lane == 0) state_finish(s, p.tau_per_row ? ld_dep(p.tau_per_row + tok) : p.tau, p.argmax, p.entropy, p.maxprob, p.exit_mask, tok);
+    }
     if (threadIdx.x == 0) p.ctrl->head_ticket[0] = 0;                    // ready for the next launch
 }
 
-size_t q4_smem(int nt, int d) { return (size_t)nt * 8 * y_row_bytes(d) + (size_t)kWarps * nt * 8 * sizeof(State); }
+size_t q4_smem(int nt, int d) { return (size_t)nt * 8 * y_row_bytes(d) + (size_t)kWarps * (nt * 8 > 32 ? nt * 8 : 32) * sizeof(State); }
 
-// Rows one launch takes: whole tiles of eight tokens in shared memory, at most 64.
-int slab_rows(int d) {
-    int nt = kMaxSlabRows / 8;
-    while (nt > 1 && q4_smem(nt, d) > kSmemBudget) nt = nt > 4 ? 4 : nt / 2;
-    return nt * 8;
-}
+// Rows one launch takes: sixteen, or eight where sixteen do not fit shared memory.
+int slab_rows(int d) { return q4_smem(2, d) <= kSmemBudget ? 16 : 8; }
 
 template <int NT>
 ee_status launch_head(const Q4Params& p, int num_sms, int device, cudaStream_t stream) {
@@ -337,7 +291,8 @@ ee_status launch_head(const Q4Params& p, int num_sms, int device, cudaStream_t s
     return launch_pdl(q4_head_kernel<NT>, dim3(grid), kThreads, q4_smem(NT, p.d), stream, p) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
-size_t parts_bytes() { return (size_t)kStreamMaxCtas * kMaxSlabRows * sizeof(State); }
+size_t parts_bytes() { return (size_t)kStreamMaxCtas * kQ4GemmRows * sizeof(State); }
+
 
 }  // namespace
 
@@ -366,19 +321,27 @@ ee_status q4_unpack_launch(const void* q4, int V, int d, int group, void* W, cud
     return cudaGetLastError() == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
-size_t q4_head_workspace_bytes(int M, int d) { return kCtrlBytes + parts_bytes() + align_up((size_t)M * d * 2, 256); }
+size_t q4_head_workspace_bytes(int M, int d) { return kCtrlBytes + parts_bytes() + align_up((size_t)M * ((d + 63) / 64) * 128, 256); }
 
 ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group) {
     unsigned char* ws = static_cast<unsigned char*>(a.workspace);
     __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(ws + kCtrlBytes + parts_bytes());
-    const ee_status st = layer_norm_launch(a.h, a.ld_h, a.gamma, a.beta, a.ln_eps, y, a.M, a.d, a.stream);
-    if (st != EE_OK) return st;
-    const int slab = slab_rows(a.d);
+    // EE_Q4_KERNEL=stream | gemm forces one of the two kernels (for tests and comparisons)
+    const char* force = getenv("EE_Q4_KERNEL");
+    const bool gemm = force && force[0] == 'g' ? true : force && force[0] == 's' ? false : a.M > kMaxSlabRows;
+    const int slab = gemm ? kQ4GemmRows : slab_rows(a.d);
+    const int ld_y = (a.d + 63) / 64 * 64;
+    if (gemm) {
+        const ee_status st = layer_norm_permuted_launch(a.h, a.ld_h, a.gamma, a.beta, a.ln_eps, y, ld_y, a.M, a.d, a.stream);
+        if (st != EE_OK) return st;
+    }
     for (int r0 = 0; r0 < a.M; r0 += slab) {
         Q4Params p;
         p.weights = static_cast<const uint4*>(q4);
         p.scales = q4_scales(q4, a.V, a.d, group);
-        p.y = y + (size_t)r0 * a.d;
+        p.y = y + (size_t)r0 * ld_y;
+        p.h = static_cast<const __nv_bfloat16*>(a.h) + (size_t)r0 * a.ld_h;
+        p.ld_h = a.ld_h; p.gamma = a.gamma; p.beta = a.beta; p.ln_eps = a.ln_eps;
         p.M = a.M - r0 < slab ? a.M - r0 : slab;
         p.d = a.d; p.V = a.V; p.group = group;
         p.parts = reinterpret_cast<State*>(ws + kCtrlBytes);
@@ -387,8 +350,8 @@ ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group) {
         p.argmax = a.argmax + r0; p.entropy = a.entropy + r0; p.maxprob = a.maxprob + r0; p.exit_mask = a.exit_mask + r0;
         p.ctrl = reinterpret_cast<Control*>(ws);
         const int nt = (p.M + 7) / 8;
-        const ee_status s = nt <= 1 ? launch_head<1>(p, a.num_sms, a.device, a.stream) : nt <= 2 ? launch_head<2>(p, a.num_sms, a.device, a.stream)
-                          : nt <= 4 ? launch_head<4>(p, a.num_sms, a.device, a.stream) : launch_head<8>(p, a.num_sms, a.device, a.stream);
+        const ee_status s = gemm ? q4_gemm_launch(p, a.num_sms, a.device, a.stream)
+                          : nt <= 1 ? launch_head<1>(p, a.num_sms, a.device, a.stream) : launch_head<2>(p, a.num_sms, a.device, a.stream);
         if (s != EE_OK) return s;
     }
     return EE_OK;
