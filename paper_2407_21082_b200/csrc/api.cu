@@ -776,7 +776,7 @@ ee_status ee_embed_grad(const void* dout, long long ld_dout, const int* tokens, 
         if (accumulate) return EE_OK;
         return cudaMemsetAsync(dtable, 0, (size_t)V * d * (dtable_fp32 ? 4 : 2), s) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
     }
-    return embed_grad_launch(dout, ld_dout, tokens, n, V, d, scale, dtable, dtable_fp32 ? 1 : 0, accumulate ? 1 : 0, workspace, device,
+    return embed_grad_launch(dout, ld_dout, tokens, n, V, d, scale, dtable, dtable_fp32 ? 1 : 0, accumulate ? 1 : 0, workspace,
                              num_sms, s);
 }
 

@@ -2,9 +2,9 @@
 //   dtable[v] = scale * sum over i with token_i = v of dout[i]
 // by sorted tokens, in fp32 and in a fixed order (no floating-point atomics: the same bits from run to run).
 //
-// The gradient is three steps.  (1) The tokens are sorted, stably, by one CTA in shared memory when they fit
-// (n <= 16384 and V < 2^18: 18 bits of token and 14 of position in one word), while the other CTAs clear the table, which takes
-// longer (V d bytes against n words); longer lists go through the library's radix sort.  (2) The sorted list is cut into
+// The gradient is three steps.  (1) The tokens are sorted, stably, by one cluster of CTAs in its shared memory when they fit
+// (n <= 16384 and V < 2^18: 18 bits of token and 14 of position in one word), while the rest of the device clears the table, which
+// takes longer (V d bytes against n words); longer lists go through the library's radix sort.  (2) The sorted list is cut into
 // chunks of equal length, one CTA (per 128 vectors of the width) each: it adds up the rows of every token in it.  A token
 // that lies inside the chunk is finished there; a run that crosses a chunk's border, as frequent tokens' do, leaves
 // fp32 partial sums (one for the run that comes in, one for the run that goes out).  (3) A run's partial sums are
@@ -12,6 +12,7 @@
 // Tokens outside [0, V) take no part: they sort behind all others and are skipped.
 #include "common.cuh"
 #include "kernels.h"
+#include "sm100_ptx.cuh"
 
 namespace ee {
 
@@ -48,64 +49,113 @@ __global__ void __launch_bounds__(256) embed_kernel(const __nv_bfloat16* table, 
 
 // ---------------------------------------------------------------------------------------------------- sorting
 
+constexpr int kSortCtas = 8;                             // one cluster
 constexpr int kSortThreads = 1024;
-constexpr int kSortItems = 16;
-constexpr int kSortMax = kSortThreads * kSortItems;      // tokens one CTA sorts
+constexpr int kSortItems = 2;                            // per thread
+constexpr int kSortCtaItems = kSortThreads * kSortItems;
+constexpr int kSortMax = kSortCtas * kSortCtaItems;      // 16384 tokens one cluster sorts
 constexpr int kSortIndexBits = 14;
 constexpr int kSortMaxV = (1 << (32 - kSortIndexBits)) - 1;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr size_t kSortSmem = (size_t)kSortMax * 4 + kSortWarps * 256 * 4 + 64;
 
-// CTA 0: stable radix sort of (token, position), eight bits a pass; warp w owns a run of consecutive items and walks it 32 at
-// a time, so that (warp, round, lane) is the order in the list.  The other CTAs clear `clear_vecs` vectors at `clear`.
-__global__ void __launch_bounds__(kSortThreads, 1) embed_sort_clear_kernel(const int* tokens, int n, int V, int passes, int2* sorted,
-                                                                           uint4* clear, long long clear_vecs) {
+__device__ __forceinline__ unsigned int ld_cluster(uint32_t addr) {
+    unsigned int v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, unsigned int v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+// Clears `vecs` vectors: bulk copies out of zeros in shared memory, all of a CTA's issued by one thread.  The kernel that sorts the
+// tokens lets this one start after its own wait for the stream's earlier work, so that clearing (V d bytes) runs beside sorting
+// (n words) and needs no wait before it writes; it waits before it ends, so that its own end means that of both.
+constexpr unsigned int kClearBytes = 16384;
+__global__ void __launch_bounds__(128) embed_clear_kernel(uint4* clear, long long vecs) {
+    __shared__ __align__(128) uint4 zeros[kClearBytes / 16];
     launch_dependents();
-    grid_dependency_wait();
-    if (blockIdx.x != 0) {
-        const long long step = (long long)(gridDim.x - 1) * kSortThreads;
-        for (long long i = (long long)(blockIdx.x - 1) * kSortThreads + threadIdx.x; i < clear_vecs; i += step) clear[i] = make_uint4(0, 0, 0, 0);
-        return;
+    for (int i = threadIdx.x; i < (int)(kClearBytes / 16); i += 128) zeros[i] = make_uint4(0, 0, 0, 0);
+    ptx::fence_proxy_async();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t src = ptx::smem_addr(zeros);
+        const long long total = vecs * 16;
+        unsigned char* out = reinterpret_cast<unsigned char*>(clear);
+        for (long long at = (long long)blockIdx.x * kClearBytes; at < total; at += (long long)gridDim.x * kClearBytes) {
+            const uint32_t size = (uint32_t)(total - at < kClearBytes ? total - at : kClearBytes);
+            asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(out + at), "r"(src), "r"(size) : "memory");
+        }
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // written, and the zeros are read
     }
-    extern __shared__ __align__(16) unsigned int sort_smem[];
-    unsigned int* list = sort_smem;                       // [n]
-    unsigned int* cnt = sort_smem + kSortMax;             // [warps][256]
-    unsigned int* warp_part = cnt + kSortWarps * 256;
+    grid_dependency_wait();
+}
+
+// One cluster: stable radix sort of (token, position), eight bits a pass, items in registers and the sorted list spread over the
+// CTAs' shared memory.  A CTA owns 2048 consecutive items, a warp 64 of them in two rounds, so that (CTA, warp, round, lane) is
+// the order in the list; the CTAs exchange their digit counts and scatter into one another's memory.  (One CTA alone took
+// 35 us for 16384 tokens, twice the clearing of the table beside it.)
+__global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const int* tokens, int n, int V, int passes, int2* sorted) {
+    __shared__ unsigned int list[kSortCtaItems];
+    __shared__ unsigned int cnt[kSortWarps][256];
+    __shared__ unsigned int total[256];                   // this CTA's items of each digit, read by the others
+    __shared__ unsigned int start[256];                   // where this CTA's run of a digit begins
+    __shared__ unsigned int warp_part[8];
+    grid_dependency_wait();
+    launch_dependents();                                  // after the wait: see embed_clear_kernel
+    const int rank = (int)ptx::cluster_cta_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rounds = (n + kSortThreads - 1) / kSortThreads;
-    const int base = warp * rounds * 32;
+    const int local0 = warp * 64 + lane, base = rank * kSortCtaItems;
     unsigned int item[kSortItems];
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int i = base + r * 32 + lane;
-        if (r < rounds && i < n) {
+        const int i = base + local0 + r * 32;
+        item[r] = 0;
+        if (i < n) {
             const int t = ld_dep(tokens + i);
             item[r] = ((unsigned int)((unsigned)t < (unsigned)V ? t : V) << kSortIndexBits) | (unsigned int)i;
         }
     }
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = kSortIndexBits + 8 * pass;
-        for (int i = threadIdx.x; i < kSortWarps * 256; i += kSortThreads) cnt[i] = 0;
+        for (int i = threadIdx.x; i < kSortWarps * 256; i += kSortThreads) (&cnt[0][0])[i] = 0;
         __syncthreads();
-        unsigned int rank[kSortItems];
+        unsigned int place[kSortItems];
 #pragma unroll
         for (int r = 0; r < kSortItems; ++r) {
-            if (r < rounds) {
-                const bool valid = base + r * 32 + lane < n;
-                const unsigned int digit = valid ? (item[r] >> shift) & 255u : 0xffffffffu;
-                const unsigned int peers = __match_any_sync(0xffffffffu, digit);
-                const int leader = __ffs(peers) - 1;
-                unsigned int before = 0;
-                if (valid && lane == leader) before = atomicAdd(&cnt[warp * 256 + digit], (unsigned int)__popc(peers));
-                before = __shfl_sync(0xffffffffu, before, leader);
-                rank[r] = before + __popc(peers & ((1u << lane) - 1u));
-            }
+            const bool valid = base + local0 + r * 32 < n;
+            const unsigned int digit = valid ? (item[r] >> shift) & 255u : 0xffffffffu;
+            const unsigned int peers = __match_any_sync(0xffffffffu, digit);
+            const int leader = __ffs(peers) - 1;
+            unsigned int before = 0;
+            if (valid && lane == leader) before = atomicAdd(&cnt[warp][digit], (unsigned int)__popc(peers));
+            before = __shfl_sync(0xffffffffu, before, leader);
+            place[r] = before + __popc(peers & ((1u << lane) - 1u));
         }
         __syncthreads();
-        unsigned int mine = 0, incl = 0;
-        if (threadIdx.x < 256) {                          // thread = digit
-            for (int w = 0; w < kSortWarps; ++w) mine += cnt[w * 256 + threadIdx.x];
-            incl = mine;
+        if (threadIdx.x < 256) {                          // thread = digit: the warps' starts inside the CTA's run
+            unsigned int run = 0;
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; ++w) {
+                const unsigned int k = cnt[w][threadIdx.x];
+                cnt[w][threadIdx.x] = run;
+                run += k;
+            }
+            total[threadIdx.x] = run;
+        }
+        ptx::cluster_sync_all();
+        unsigned int all = 0, before = 0, incl = 0;
+        if (threadIdx.x < 256) {
+            const uint32_t mine = ptx::smem_addr(&total[threadIdx.x]);
+            unsigned int k[kSortCtas];
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) k[c] = ld_cluster(ptx::map_to_cta(mine, c));
+#pragma unroll
+            for (int c = 0; c < kSortCtas; ++c) {
+                all += k[c];
+                before += c < rank ? k[c] : 0u;
+            }
+            incl = all;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const unsigned int x = __shfl_up_sync(0xffffffffu, incl, o);
@@ -115,38 +165,36 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_clear_kernel(const
         }
         __syncthreads();
         if (threadIdx.x < 256) {
-            unsigned int run = incl - mine;
-            for (int w = 0; w < warp; ++w) run += warp_part[w];
-            for (int w = 0; w < kSortWarps; ++w) {
-                const unsigned int k = cnt[w * 256 + threadIdx.x];
-                cnt[w * 256 + threadIdx.x] = run;
-                run += k;
-            }
+            unsigned int digits_before = 0;
+            for (int w = 0; w < warp; ++w) digits_before += warp_part[w];
+            start[threadIdx.x] = digits_before + incl - all + before;
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < kSortItems; ++r)
-            if (r < rounds && base + r * 32 + lane < n) list[cnt[warp * 256 + ((item[r] >> shift) & 255u)] + rank[r]] = item[r];
-        __syncthreads();
-#pragma unroll
+            if (base + local0 + r * 32 < n) {
+                const unsigned int digit = (item[r] >> shift) & 255u;
+                const unsigned int to = start[digit] + cnt[warp][digit] + place[r];
+                st_cluster(ptx::map_to_cta(ptx::smem_addr(&list[to % kSortCtaItems]), to / kSortCtaItems), item[r]);
+            }
+        ptx::cluster_sync_all();                          // the list is whole; and nobody scatters again before everyone has read it,
+#pragma unroll                                            // the next pass's first meeting being in between
         for (int r = 0; r < kSortItems; ++r)
-            if (r < rounds && base + r * 32 + lane < n) item[r] = list[base + r * 32 + lane];
+            if (base + local0 + r * 32 < n) item[r] = list[local0 + r * 32];
     }
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-        const int i = base + r * 32 + lane;
-        if (r < rounds && i < n) sorted[i] = make_int2((int)(item[r] & ((1u << kSortIndexBits) - 1u)), (int)(item[r] >> kSortIndexBits));
+        const int i = base + local0 + r * 32;
+        if (i < n) sorted[i] = make_int2((int)(item[r] & ((1u << kSortIndexBits) - 1u)), (int)(item[r] >> kSortIndexBits));
     }
 }
 
-// (position, token) words for the radix sort over memory, and the clearing of the table.
-__global__ void __launch_bounds__(256) embed_words_kernel(const int* tokens, int n, int V, u64* words, uint4* clear, long long clear_vecs) {
-    const long long step = (long long)gridDim.x * 256, first = (long long)blockIdx.x * 256 + threadIdx.x;
-    for (long long i = first; i < n; i += step) {
-        const int t = ld_dep(tokens + i);
-        words[i] = ((u64)(unsigned int)((unsigned)t < (unsigned)V ? t : V) << 32) | (unsigned int)i;
-    }
-    for (long long i = first; i < clear_vecs; i += step) clear[i] = make_uint4(0, 0, 0, 0);
+// (position, token) words for the radix sort over memory.
+__global__ void __launch_bounds__(256) embed_words_kernel(const int* tokens, int n, int V, u64* words) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int t = ld_dep(tokens + i);
+    words[i] = ((u64)(unsigned int)((unsigned)t < (unsigned)V ? t : V) << 32) | (unsigned int)i;
 }
 
 // ---------------------------------------------------------------------------------------------------- adding up
@@ -193,7 +241,7 @@ __device__ __forceinline__ void store_part(const EmbedGrad& a, int chunk, int wh
 }
 
 constexpr int kSumThreads = 128;
-constexpr int kSumAhead = 8;                              // rows in flight per thread
+constexpr int kSumAhead = 8;                              // rows in flight per thread (16: 96 registers, 12 -> 15.6 us at n = 16384)
 
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_constant__ EmbedGrad a) {
     __shared__ int2 entry[kSumThreads];
@@ -250,18 +298,28 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(const __grid_con
     else store_row(a, token, c, acc);
 }
 
-// Joins the partial sums of the run that goes out of chunk blockIdx.x: 16 vectors of the width by 16 groups of chunks.
-__global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedGrad a) {
-    __shared__ float red[16][16][9];
+// Joins the partial sums of the run that goes out of chunk blockIdx.x, if one starts there: 128 vectors of the width by four
+// groups of the chunks it goes through, whose number the CTA counts first, so that the loads do not wait for one another.
+constexpr int kJoinThreads = 512;
+constexpr int kJoinGroups = kJoinThreads / 128;
+__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_constant__ EmbedGrad a) {
+    __shared__ float red[kJoinGroups - 1][8][128];
     launch_dependents();
     grid_dependency_wait();
     const int first = blockIdx.x, p0 = first * a.chunk, p1 = p0 + a.chunk;
     if (p1 >= a.n) return;                                               // nothing goes out of the last chunk
-    const int token = ld_dep(a.sorted + p1 - 1).y;
-    if (token >= a.V || ld_dep(a.sorted + p1).y != token) return;        // no run crosses the border,
-    if (p0 > 0 && ld_dep(a.sorted + p0 - 1).y == token && ld_dep(a.sorted + p0).y == token) return;      // or it started earlier
-    const int v = threadIdx.x & 15, group = threadIdx.x >> 4;
-    const int c = blockIdx.y * 16 + v;
+    const int token = ld_dep(a.sorted + p1 - 1).y, next = ld_dep(a.sorted + p1).y;
+    const int here = ld_dep(a.sorted + p0).y, before = p0 > 0 ? ld_dep(a.sorted + p0 - 1).y : -1;
+    if (token != next || token >= a.V || (here == token && before == token)) return;       // no run crosses the border, or it started earlier
+    int through = 0;                                                     // chunks after this one that begin with the token
+    for (;;) {
+        const int k = first + 1 + through + (int)threadIdx.x;
+        const int more = __syncthreads_count(k < a.n_chunks && ld_dep(a.sorted + (size_t)(k < a.n_chunks ? k : first) * a.chunk).y == token);
+        through += more;
+        if (more < kJoinThreads) break;
+    }
+    const int v = threadIdx.x & 127, group = threadIdx.x >> 7;
+    const int c = blockIdx.y * 128 + v;
     float acc[8] = {};
     if (c < a.nvec) {
         auto add = [&](int chunk, int which) {
@@ -271,24 +329,28 @@ __global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__
             acc[4] += y.x; acc[5] += y.y; acc[6] += y.z; acc[7] += y.w;
         };
         if (group == 0) add(first, 1);
-        for (int k = first + 1 + group; k < a.n_chunks && ld_dep(a.sorted + (size_t)k * a.chunk).y == token; k += 16) add(k, 0);
+#pragma unroll 8
+        for (int k = 1 + group; k <= through; k += kJoinGroups) add(first + k, 0);
     }
+    if (group > 0) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) red[group][v][j] = acc[j];
+        for (int j = 0; j < 8; ++j) red[group - 1][j][v] = acc[j];
+    }
     __syncthreads();
     if (group == 0 && c < a.nvec) {
-        for (int k = 1; k < 16; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += red[k][v][j];
+        for (int k = 0; k < kJoinGroups - 1; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += red[k][j][v];
         store_row(a, token, c, acc);
     }
 }
 
-// Sorted positions per chunk: at most 1024 chunks (a run over all of them is joined by 16 groups of 64), at least eight
+// Sorted positions per chunk: at most 1024 chunks (a run over all of them is joined by four groups of 256), at least eight
 // positions (a thread's loads in flight).
 int chunk_of(int n) { const int c = (n + 1023) / 1024; return c < 8 ? 8 : c; }
 
-bool sorts_in_one_cta(int n, int V) { return n <= kSortMax && V <= kSortMaxV; }
+bool sorts_in_one_cluster(int n, int V) { return n <= kSortMax && V <= kSortMaxV; }
 
 struct EmbedSpace {
     size_t a, b, scratch, parts, total;
@@ -297,7 +359,7 @@ EmbedSpace embed_space(int n, int d, int V) {
     EmbedSpace s;
     size_t at = 0;
     auto take = [&](size_t k) { const size_t o = at; at = align_up(at + k, 256); return o; };
-    const bool one = sorts_in_one_cta(n, V);
+    const bool one = sorts_in_one_cluster(n, V);
     const int chunk = chunk_of(n), n_chunks = (n + chunk - 1) / chunk;
     s.a = take((size_t)n * 8);
     s.b = take(one ? 0 : (size_t)n * 8);
@@ -320,7 +382,7 @@ ee_status embed_launch(const void* table, int V, int d, const int* tokens, int n
 size_t embed_grad_workspace_bytes(int n, int d, int V) { return embed_space(n, d, V).total; }
 
 ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable, int wide,
-                            int accumulate, void* workspace, int device, int num_sms, cudaStream_t stream) {
+                            int accumulate, void* workspace, int num_sms, cudaStream_t stream) {
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const EmbedSpace s = embed_space(n, d, V);
     const long long clear_vecs = accumulate ? 0 : (long long)V * d * (wide ? 4 : 2) / 16;
@@ -333,23 +395,24 @@ ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* toke
     g.chunk = chunk_of(n); g.n_chunks = (n + g.chunk - 1) / g.chunk;
     g.scale = scale; g.dtable = dtable; g.wide = wide; g.add = accumulate;
     g.parts = reinterpret_cast<float*>(ws + s.parts);
-    if (sorts_in_one_cta(n, V)) {
-        static bool configured[kMaxDevices] = {};
-        if (!configured[device]) {
-            if (cudaFuncSetAttribute(embed_sort_clear_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSortSmem) != cudaSuccess)
-                return EE_ERR_CUDA;
-            configured[device] = true;
-        }
-        const long long others = (clear_vecs + kSortThreads - 1) / kSortThreads;
-        const int grid = 1 + (int)(others < num_sms - 1 ? others : num_sms - 1);
+    if (sorts_in_one_cluster(n, V)) {
         int2* sorted = reinterpret_cast<int2*>(ws + s.a);
-        if (launch_pdl(embed_sort_clear_kernel, dim3(grid), kSortThreads, kSortSmem, stream, tokens, n, V, passes, sorted,
-                       static_cast<uint4*>(dtable), clear_vecs) != cudaSuccess)
-            return EE_ERR_CUDA;
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        pair_launch_config(cfg, attr, dim3(kSortCtas), kSortThreads, 0, stream);
+        attr[1].val.clusterDim.x = kSortCtas;
+        if (cudaLaunchKernelEx(&cfg, embed_sort_kernel, tokens, n, V, passes, sorted) != cudaSuccess) return EE_ERR_CUDA;
+        if (clear_vecs) {
+            const long long copies = (clear_vecs * 16 + kClearBytes - 1) / kClearBytes, most = 4LL * num_sms;
+            if (launch_pdl(embed_clear_kernel, dim3((unsigned)(copies < most ? copies : most)), 128, 0, stream, static_cast<uint4*>(dtable), clear_vecs) !=
+                cudaSuccess)
+                return EE_ERR_CUDA;
+        }
         g.sorted = sorted;
     } else {
         u64 *a = reinterpret_cast<u64*>(ws + s.a), *b = reinterpret_cast<u64*>(ws + s.b);
-        embed_words_kernel<<<num_sms * 8, 256, 0, stream>>>(tokens, n, V, a, static_cast<uint4*>(dtable), clear_vecs);
+        if (clear_vecs && cudaMemsetAsync(dtable, 0, (size_t)clear_vecs * 16, stream) != cudaSuccess) return EE_ERR_CUDA;
+        embed_words_kernel<<<(n + 255) / 256, 256, 0, stream>>>(tokens, n, V, a);
         if (cudaGetLastError() != cudaSuccess) return EE_ERR_CUDA;
         const u64* sorted = nullptr;
         const ee_status st = sort_words_launch(a, b, n, 32, passes, ws + s.scratch, &sorted, stream);
@@ -358,7 +421,7 @@ ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* toke
     }
     const int nvec = d / 8;
     if (launch_pdl(embed_sum_kernel, dim3(g.n_chunks, (nvec + kSumThreads - 1) / kSumThreads), kSumThreads, 0, stream, g) != cudaSuccess ||
-        launch_pdl(embed_join_kernel, dim3(g.n_chunks, (nvec + 15) / 16), 256, 0, stream, g) != cudaSuccess)
+        launch_pdl(embed_join_kernel, dim3(g.n_chunks, (nvec + 127) / 128), kJoinThreads, 0, stream, g) != cudaSuccess)
         return EE_ERR_CUDA;
     return EE_OK;
 }

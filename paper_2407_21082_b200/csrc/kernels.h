@@ -140,7 +140,7 @@ ee_status embed_launch(const void* table, int V, int d, const int* tokens, int n
                        cudaStream_t stream);
 size_t embed_grad_workspace_bytes(int n, int d, int V);
 ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable, int wide,
-                            int accumulate, void* workspace, int device, int num_sms, cudaStream_t stream);
+                            int accumulate, void* workspace, int num_sms, cudaStream_t stream);
 
 // ---- stable radix sort of 64-bit words by `passes` digits of eight bits from bit `first_shift` on (calibrate.cu); a holds
 //      the words, *sorted is a or b ----
