@@ -1108,7 +1108,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
 
     for (int i = 0; i < c.n_pieces; ++i) {
         const int v0 = i * c.piece, nv = a.V - v0 < c.piece ? a.V - v0 : c.piece;
-        const int nv_pad = (nv + 63) / 64 * 64;                          // the columns of G that are written (zeros beyond nv)
+        const int nv_pad = (nv + 63) / 64 * 64;                          // the columns of G that are written, tiles enough for all (zeros beyond nv)
         CeMaps maps;
         CeParams p = base_params(a);
         p.v0 = v0;
@@ -1119,7 +1119,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
             if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs))
                 return EE_ERR_CUDA;
             p.G = G; p.ld_g = ld_g;
-            p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv, p.bn); p.k_blocks = tiles(a.d, BK);
+            p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv_pad, p.bn); p.k_blocks = tiles(a.d, BK);
             p.n_cols = nv; p.m_rows = a.M;
             const ee_status st = launch_product<kGrad>(maps, p, pair, a);
             if (st != EE_OK) return st;

@@ -230,6 +230,22 @@ def test_a_captured_step_replays_on_another_stream_beside_an_eager_one(ee):
     assert ee.ee_query_async_error(ws) == 0 and ee.ee_query_async_error(ws2) == 0
 
 
+@pytest.mark.parametrize("M,d,V", [(1, 8, 1), (64, 72, 300), (130, 64, 900), (648, 128, 13018), (1000, 64, 13018), (500, 1216, 3546), (2100, 8, 40000)])
+def test_what_the_workspace_held_does_not_matter(ee, M, d, V):
+    """13018 = 73 tiles of 176 columns and 170 more, 38 short of a whole block of 64: every column that the products read is written."""
+    cfg, labels = make(M, d, V)
+    head, lab = device_head(cfg), dev(labels)
+    ws = ee.new_head_ce_grad_workspace(M, d, V)
+    results = []
+    for junk in (0.0, float("nan")):
+        ws[256:256 + (ws.numel() - 256) // 4 * 4].view(torch.float32).fill_(junk)
+        fwd = ee.ee_head_ce(head, lab, 1e-5, workspace=ws)
+        ws[256:256 + (ws.numel() - 256) // 4 * 4].view(torch.float32).fill_(junk)
+        results.append(dict(fwd, **ee.ee_head_ce_grad(head, lab, 1e-5, fwd, workspace=ws)))
+    for k in results[0]:
+        assert torch.isfinite(results[1][k].float()).all() and torch.equal(results[0][k], results[1][k]), k
+
+
 def test_no_rows(ee):
     head = dict(h=torch.empty((0, 64), dtype=torch.bfloat16, device="cuda"), gamma=torch.ones(64, device="cuda"),
                 beta=torch.zeros(64, device="cuda"), W=torch.ones((50, 64), dtype=torch.bfloat16, device="cuda"))

@@ -145,6 +145,18 @@ def test_captured_beside_an_eager_call(ee, n):
     assert torch.equal(call.out, want) and torch.equal(eager, want)
 
 
+@pytest.mark.parametrize("n,d,V,kind", [(1, 8, 1, "one"), (300, 64, 50, "zipf"), (5000, 24, 900, "two"), (17000, 64, 900, "mixed")])
+def test_what_the_workspace_held_does_not_matter(ee, n, d, V, kind):
+    rng = np.random.default_rng(n)
+    dout, tokens = dev_bf16(_rand_bits(rng, n, d)), dev(_tokens(rng, kind, n, V))
+    ws = ee.new_embed_grad_workspace(n, d, V)
+    results = []
+    for junk in (0, 255):
+        ws.fill_(junk)
+        results.append(ee.ee_embed_grad(dout, tokens, V, workspace=ws, out=torch.full((V, d), float("nan"), device="cuda")))
+    assert torch.isfinite(results[1]).all() and torch.equal(results[0], results[1])
+
+
 def test_nothing_to_look_up(ee):
     table = torch.ones((5, 16), dtype=torch.bfloat16, device="cuda")
     none = torch.empty(0, dtype=torch.int32, device="cuda")

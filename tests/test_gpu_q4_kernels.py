@@ -52,3 +52,20 @@ def test_not_a_number_stays_in_its_row(ee, monkeypatch, kernel):
     for k in want:
         assert torch.equal(got[k][keep], want[k][keep]), k
     assert torch.isnan(got["entropy"][~keep]).all() and not got["exit_mask"][~keep].any()
+
+
+@pytest.mark.parametrize("kernel", ["stream", "gemm"])
+@pytest.mark.parametrize("M,d,V,group", [(1, 32, 5, 32), (5, 96, 700, 32), (33, 640, 2500, 128), (100, 64, 60000, 64)])
+def test_what_the_workspace_held_does_not_matter(ee, monkeypatch, kernel, M, d, V, group):
+    monkeypatch.setenv("EE_Q4_KERNEL", kernel)
+    cfg = gen.make_config("c1", seed=8, planted=True, M=M, d=d, V=V, heads=1)
+    hd, h = head_to_dev(cfg["heads"][0]), dev_bf16(cfg["h"])
+    q4 = ee.ee_head_q4_pack(hd["W"], group)
+    ws = ee.new_exit_head_q4_workspace(M, q4)
+    results = []
+    for junk in (0, 255):
+        ws[256:].fill_(junk)
+        results.append({k: v.clone() for k, v in ee.ee_exit_head_q4(h, hd["gamma"], hd["beta"], 1e-5, q4, 1.0, workspace=ws).items()})
+    for k in results[0]:
+        assert torch.equal(results[0][k], results[1][k]), k
+    assert torch.isfinite(results[1]["entropy"]).all()
