@@ -450,7 +450,8 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
 /*
  * Cross-entropy of a head over the whole vocabulary and its gradient: the supervised objective L_CE of section 3.3
  * ("Losses") as a training step of a head needs it.  The M x V logits are never stored: the gradient recomputes them
- * in pieces of the vocabulary.  With y = bf16(LayerNorm(h)) and z = y W^T as in ee_exit_head:
+ * in pieces of the vocabulary.  With z = y W^T and y = bf16(fp32(LayerNorm(h))) -- rounded as the cast of a LayerNorm that
+ * returns fp32 is, which differs from ee_exit_head's y in about one element of 10^5, by one step --:
  *   lse   fp32 [M]: ln sum_v exp(z[i, v])
  *   ce    fp32 [M]: lse[i] - z[i, labels[i]]; 0 for a row that is not counted
  *   loss  fp32 [2]: the mean of ce over the counted rows (0 if there is none), and their number
@@ -490,8 +491,8 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
  * ee_head_q4_bytes(V, d, group) bytes (0 if a size is invalid), 256-byte aligned, in a layout of the library's own;
  * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous.  W and W4 are 32-byte aligned.
  *
- * ee_exit_head_q4 is ee_exit_head with W4 for W: same definition, outputs, strides, alignment and rules (the packed
- * head is a constant of the stream).  Any M; rows beyond those whose LayerNorm output fits shared memory go in further
+ * ee_exit_head_q4 is ee_exit_head with W4 for W and the y of ee_head_ce: same definition otherwise, same outputs, strides,
+ * alignment and rules (the packed head is a constant of the stream).  Any M; rows beyond those whose LayerNorm output fits shared memory go in further
  * passes over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
  * with ee_workspace_init.  M = 0 is a no-op.
  */

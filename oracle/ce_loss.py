@@ -2,7 +2,7 @@
 
 TEST INFRASTRUCTURE ONLY (see oracle/exit_head.py).  Shares no code with the CUDA sources.
 
-Per token: y = LayerNorm(h) rounded to bf16, z = W y, lse = ln sum exp z, ce = lse - z[label].  Rows whose label is
+Per token: y = LayerNorm(h) rounded to fp32 and then to bf16, z = W y, lse = ln sum exp z, ce = lse - z[label].  Rows whose label is
 outside [0, V) are not counted.  Gradient of sum_i w_i ce_i, the rounding of y passed through:
     g = w (softmax(z) - onehot(label)),  dy = g W,  dW = g^T y,
     t = dy * gamma,  dh = rstd (t - mean t - xhat mean(t xhat)),  dgamma = sum dy xhat,  dbeta = sum dy.
@@ -14,6 +14,11 @@ from __future__ import annotations
 import numpy as np
 
 from .exit_head import bf16_decode, bf16_rne
+
+
+def bf16_by_f32(x):
+    """fp64 -> fp32 -> bf16, each to nearest: what casting a LayerNorm that returns fp32 gives."""
+    return bf16_rne(np.asarray(x, dtype=np.float64).astype(np.float32).astype(np.float64))
 
 
 def _rows(h_bits, head):
@@ -34,7 +39,7 @@ def cross_entropy(h_bits, head, labels, weights=None, round_y: bool = True) -> d
     counted = (labels >= 0) & (labels < V)
     xhat, rstd, y = _rows(h_bits, head)
     if round_y:
-        y = bf16_rne(y)
+        y = bf16_by_f32(y)
     z = y @ W.T
     top = z.max(axis=1, keepdims=True)
     P = np.exp(z - top)

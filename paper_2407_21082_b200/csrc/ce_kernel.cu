@@ -489,7 +489,7 @@ __device__ __forceinline__ void put_vec8(uint4* yrow, int c, uint4 v, int permut
     block[4 * (j + 1) + m] = make_uint2(v.z, v.w);
 }
 
-// LayerNorm of the rows into y, a warp per row.  In the backward pass (`stats` given) it also leaves each row's mean
+// LayerNorm of the rows into y (rounded to fp32 and then to bf16, see layer_norm.cuh), a warp per row.  In the backward pass (`stats` given) it also leaves each row's mean
 // and 1/sigma for the way back, and a row that takes no part in the gradient becomes zeros with 1/sigma = 0.
 struct CeLnArgs {
     const __nv_bfloat16* h;
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constan
     }
     const uint4* hrow = reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h);
     const RowStats st = row_stats_strided([&](int c) { return ld_dep(hrow + c); }, nvec, a.ln_eps, lane);
-    for (int c = lane; c < nvec; c += 32) put_vec8(yrow, c, layer_norm_vec8(ld_dep(hrow + c), st, a.gamma, a.beta, c), a.permuted);
+    for (int c = lane; c < nvec; c += 32) put_vec8(yrow, c, layer_norm_vec8<true>(ld_dep(hrow + c), st, a.gamma, a.beta, c), a.permuted);
     if (a.stats && lane == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
 }
 
@@ -584,11 +584,11 @@ __global__ void __launch_bounds__(kLnCtaThreads) ce_layer_norm_cta_kernel(const 
         var = v * inv_d;
     }
     const RowStats st = row_stats(mu, var, a.ln_eps);
-    if (first) put_vec8(yrow, threadIdx.x, layer_norm_vec8(x[0], st, g[0], g[1], b[0], b[1]), a.permuted);
+    if (first) put_vec8(yrow, threadIdx.x, layer_norm_vec8<true>(x[0], st, g[0], g[1], b[0], b[1]), a.permuted);
 #pragma unroll
     for (int k = 1; k < 4; ++k) {
         const int c = threadIdx.x + k * blockDim.x;
-        if (c < nvec) put_vec8(yrow, c, layer_norm_vec8(x[k], st, a.gamma, a.beta, c), a.permuted);
+        if (c < nvec) put_vec8(yrow, c, layer_norm_vec8<true>(x[k], st, a.gamma, a.beta, c), a.permuted);
     }
     if (a.stats && threadIdx.x == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
 }

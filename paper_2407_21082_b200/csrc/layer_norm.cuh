@@ -130,6 +130,13 @@ __device__ __forceinline__ uint32_t bf16_from_double(double v) {
     return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f));
 }
 
+// The same in two steps, fp64 -> fp32 -> bf16, each to nearest: what casting a LayerNorm that returns fp32 gives.  It differs from the
+// single rounding where the fp32 value lies on a bf16 midpoint, about one element in 10^5.
+template <bool kTwice>
+__device__ __forceinline__ uint32_t bf16_of_exact(double v) {
+    return kTwice ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(__double2float_rn(v))) : bf16_from_double(v);
+}
+
 // One element on the fp32 path: y, and whether the exact value may round to another bf16 value than y does
 // (`doubt`): that is the case when the bf16 midpoint nearest to y -- y's bits with the low half replaced by 0x8000 --
 // lies within B of y (y - mid is exact in fp32: the two share their upper sixteen bits).
@@ -159,6 +166,7 @@ __device__ __forceinline__ uint4 layer_norm_vec8_fast(uint4 v, const RowStats& s
 }
 
 // The elements of a vector named in `doubts` (about one element in two thousand), decided in fp64 and put into y.
+template <bool kTwice = false>
 __device__ __forceinline__ uint4 layer_norm_vec8_redo_inline(uint4 v, uint4 y, double mu, double rstd, float4 g0, float4 g1,
                                                              float4 b0, float4 b1, uint32_t doubts) {
     const uint32_t xw[4] = {v.x, v.y, v.z, v.w};
@@ -169,7 +177,7 @@ __device__ __forceinline__ uint4 layer_norm_vec8_redo_inline(uint4 v, uint4 y, d
     for (int e = 0; e < 8; ++e) {
         if ((doubts >> e) & 1u) {
             const float x = (e & 1) ? bf16_hi(xw[e >> 1]) : bf16_lo(xw[e >> 1]);
-            const uint32_t r = bf16_from_double(fma(((double)x - mu) * rstd, (double)g[e], (double)b[e]));
+            const uint32_t r = bf16_of_exact<kTwice>(fma(((double)x - mu) * rstd, (double)g[e], (double)b[e]));
             yw[e >> 1] = (e & 1) ? ((yw[e >> 1] & 0x0000ffffu) | (r << 16)) : ((yw[e >> 1] & 0xffff0000u) | r);
         }
     }
@@ -177,26 +185,30 @@ __device__ __forceinline__ uint4 layer_norm_vec8_redo_inline(uint4 v, uint4 y, d
 }
 // Out of line, for loops that are not unrolled over a row's vectors: it runs rarely and would otherwise be
 // replicated, with its registers, at every call site.
+template <bool kTwice = false>
 static __device__ __noinline__ uint4 layer_norm_vec8_redo(uint4 v, uint4 y, double mu, double rstd, float4 g0, float4 g1, float4 b0,
                                                           float4 b1, uint32_t doubts) {
-    return layer_norm_vec8_redo_inline(v, y, mu, rstd, g0, g1, b0, b1, doubts);
+    return layer_norm_vec8_redo_inline<kTwice>(v, y, mu, rstd, g0, g1, b0, b1, doubts);
 }
 
-// Eight consecutive elements -> eight correctly rounded bf16, given the gammas / betas of these columns.
+// Eight consecutive elements -> eight correctly rounded bf16, given the gammas / betas of these columns (kTwice: rounded by way of
+// fp32; the fp32 path decides alike for both, its bound being wider than the rounding to fp32).
+template <bool kTwice = false>
 __device__ __forceinline__ uint4 layer_norm_vec8(uint4 v, const RowStats& st, float4 g0, float4 g1, float4 b0, float4 b1) {
     uint32_t doubts;
     uint4 o = layer_norm_vec8_fast(v, st, g0, g1, b0, b1, doubts);
-    if (doubts) o = layer_norm_vec8_redo(v, o, st.mu, st.rstd, g0, g1, b0, b1, doubts);
+    if (doubts) o = layer_norm_vec8_redo<kTwice>(v, o, st.mu, st.rstd, g0, g1, b0, b1, doubts);
     return o;
 }
 
 // Same, reading gamma and beta of vector c (columns 8c .. 8c+7) from global memory (weights: read-only path).
+template <bool kTwice = false>
 __device__ __forceinline__ uint4 layer_norm_vec8(uint4 v, const RowStats& st, const float* gamma, const float* beta, int c) {
     const float4 g0 = ld_param4(gamma + 8 * c);
     const float4 g1 = ld_param4(gamma + 8 * c + 4);
     const float4 b0 = ld_param4(beta + 8 * c);
     const float4 b1 = ld_param4(beta + 8 * c + 4);
-    return layer_norm_vec8(v, st, g0, g1, b0, b1);
+    return layer_norm_vec8<kTwice>(v, st, g0, g1, b0, b1);
 }
 
 // For a caller that keeps a row's vectors in registers: the fp32 path alone, with the doubts handed back, so that

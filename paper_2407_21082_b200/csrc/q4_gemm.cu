@@ -1,16 +1,17 @@
 // A head in 4 bits on the 5th-generation tensor cores.
 //
 // One CTA per SM takes an equal share of W's 16-row tiles -- at V = 50304 on 148 SMs 21 or 22 of them -- and walks the width
-// once, 64 columns at a time.  The weights are the M operand, in tensor memory: 24 warps unpack one tile each, from registers
-// straight into the rows of three 128-row operands (tcgen05.st in the order of a matrix fragment, which is the order the
-// packed form is laid out in), so unpacked weights touch neither shared memory nor its bandwidth.  The tokens are the N
-// operand, in shared memory (TMA, up to 64 rows; a stage is read by three products).  (With the tokens as M and the weights
-// written to shared memory as N, a stage of 64 columns took 0.89 us: the products read 78 KB of shared memory for it and waited
-// for that, not for the tensor cores.)  The fragment order permutes the columns of every 64; y is written in the same order.
+// once, 64 columns at a time.  The weights are the M operand, in tensor memory: 24 warps unpack one tile each, straight into the
+// rows of three 128-row operands (tcgen05.st in the order of a matrix fragment, which is the order the packed form is laid out
+// in), so unpacked weights touch neither shared memory nor its bandwidth.  The tokens are the N operand, in shared memory (TMA,
+// up to 64 rows; a stage is read by three products).  (With the tokens as M and the weights written to shared memory as N, the
+// products read 78 KB of shared memory per 64 columns and waited for that.)  The fragment order permutes the columns of every 64; y
+// is written in the same order.  The packed blocks come in bulk copies, four at a time per warp, into a ring of its own.
 //
-// Accumulators: three operands x N tokens (16, 32 or 64), in as many sets as 192 columns hold; k-block b goes to set b mod
-// sets, and the sets are added up in fp32.  The tensor core truncates rather than rounds what falls below the last bit of its
-// accumulator, which adds up over a row; with four sets (up to 16 tokens) a quarter as much.
+// The tensor core truncates rather than rounds what falls below the last bit of its accumulator, which adds up over a row: summed
+// in one go over d = 2176 an entropy was off by 3e-5 of itself where fp32 is off by 3e-7.  So an accumulator holds 256 columns at a
+// time, and the unpacking warps add it to fp32 sums in their registers, two blocks after its last one was unpacked, when its products
+// have long ended.
 //
 // Then the CTA's logits go through shared memory, so that a thread has one token and some of the rows, and its states to the
 // CTA that finishes last.  A share of more than 24 tiles goes in several passes; more than 64 tokens in several launches.
@@ -24,29 +25,40 @@ namespace ee {
 
 namespace {
 
-constexpr int kUnpackWarps = 24;                 // warp w: rows 16 (w / 4 % 2) + 32 (w % 4) of operand w / 8
+constexpr int kUnpackWarps = 24;                 // warp w unpacks rows 16 (w / 4 % 2) + 32 (w % 4) of operand w / 8
 constexpr int kOperands = 3;                     // of 128 rows, each with eight unpacking warps and a product warp
 constexpr int kTmaWarp = kUnpackWarps, kProductWarp = kUnpackWarps + 1;
 constexpr int kThreads = (kUnpackWarps + 1 + kOperands) * 32;
 constexpr int kWorkers = kUnpackWarps * 32;      // threads of the softmax
-constexpr int kAhead = 4;                        // packed blocks in flight per warp
 constexpr int kMaxTiles = 24;
 constexpr int kWStages = 3;                      // of 3 x 32 columns of tensor memory
 constexpr int kYStages = 8;                      // of N x 128 bytes of shared memory
+constexpr int kSegment = 4;                      // blocks of 64 columns an accumulator sums
+constexpr int kLag = 2;                          // blocks unpacked between a segment's last one and its reading: fewer than kWStages, or nobody moves
+constexpr int kRawBlocks = 4;                    // packed blocks per bulk copy
+constexpr int kRawBytes = kRawBlocks * 512 + 256;      // ... and their scales, up to eight groups
 constexpr int kAccCols = 192;
 constexpr int kTmemCols = 512;
-constexpr int kBarBytes = 512;
 constexpr size_t kSmemBudget = 226 * 1024;
 
 struct GemmParams {
     Q4Params q;
     int passes;                                  // of every CTA
-    int n;                                       // tokens, padded: 16, 32 or 64
-    int sets;                                    // of accumulators
     int group_shift;                             // log2 of the scales' group
 };
 
-size_t z_bytes(int n) { return (size_t)kMaxTiles * 16 * (n + 4) * sizeof(float); }
+// Barriers: per operand the ring of unpacked weights and the accumulators, the ring of y, per unpacking warp the ring of packed blocks.
+constexpr int kWBars = kOperands * kWStages, kAccBars = kOperands * 4, kRawBars = kUnpackWarps * 2;
+constexpr int kBarBytes = 8 * (2 * kWBars + 2 * kAccBars + 2 * kYStages + kRawBars + kOperands) + 64;
+size_t big_bytes(int n) {                         // the rings of packed blocks, and afterwards the logits
+    const size_t z = (size_t)kMaxTiles * 16 * (n + 4) * sizeof(float), raw = (size_t)kUnpackWarps * 2 * kRawBytes;
+    return ((z > raw ? z : raw) + 127) / 128 * 128;
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 
 // n states of a token, `stride` apart in shared memory: the maximum first, then the sums, so that no step waits for the one before.
 __device__ __forceinline__ State combine_column(const State* s, int n, int stride) {
@@ -65,63 +77,48 @@ __device__ __forceinline__ State combine_column(const State* s, int n, int strid
     return r;
 }
 
-__global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
+template <int N>                                  // tokens, padded: 16, 32 or 64
+__global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_constant__ CUtensorMap map_y, const GemmParams p, const int big) {
+    constexpr int kSets = kAccCols / (kOperands * N);                    // accumulators: 4, 2 or 1
+    constexpr int y_bytes = N * 128;
     const Q4Params& q = p.q;
     const Q4Layout l = q4_layout(q.V, q.d, q.group);
     const int t_begin = (int)((long long)blockIdx.x * l.tiles / gridDim.x), t_end = (int)((long long)(blockIdx.x + 1) * l.tiles / gridDim.x);
     const int nt = (t_end - t_begin + p.passes - 1) / p.passes;          // tiles of a pass (the last of several may have fewer)
     const int operands = (nt + 7) / 8;
-    const int N = p.n, y_bytes = N * 128;
+    const int segments = (l.blocks + kSegment - 1) / kSegment;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     unsigned char* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
     const uint32_t y_base = ptx::smem_addr(smem);
-    float* z_mem = reinterpret_cast<float*>(smem + kYStages * y_bytes);  // [rows][N + 4]
-    State* states = reinterpret_cast<State*>(smem + kYStages * y_bytes + (size_t)kMaxTiles * 16 * (N + 4) * sizeof(float));   // [kWorkers / N][N]
+    unsigned char* big_mem = smem + kYStages * y_bytes;
+    float* z_mem = reinterpret_cast<float*>(big_mem);                    // [rows][N + 4]
+    State* states = reinterpret_cast<State*>(big_mem + big);             // [kWorkers / N][N]
     unsigned char* bar_mem = reinterpret_cast<unsigned char*>(states + kWorkers);
     const uint32_t bar_base = ptx::smem_addr(bar_mem);
-    constexpr int kWBars = kOperands * kWStages;
     auto wfull_bar = [&](int o, int s) { return bar_base + 8u * (o * kWStages + s); };
     auto wempty_bar = [&](int o, int s) { return bar_base + 8u * (kWBars + o * kWStages + s); };
-    auto yfull_bar = [&](int s) { return bar_base + 8u * (2 * kWBars + s); };
-    auto yempty_bar = [&](int s) { return bar_base + 8u * (2 * kWBars + kYStages + s); };
-    const uint32_t tfull_bar = bar_base + 8u * (2 * kWBars + 2 * kYStages);
-    auto drain_bar = [&](int o) { return tfull_bar + 8u * (1 + o); };
-    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + 8 * (2 * kWBars + 2 * kYStages + 1 + kOperands));
+    auto accfull_bar = [&](int o, int s) { return bar_base + 8u * (2 * kWBars + o * 4 + s); };
+    auto accfree_bar = [&](int o, int s) { return bar_base + 8u * (2 * kWBars + kAccBars + o * 4 + s); };
+    const uint32_t y_bars = bar_base + 8u * (2 * kWBars + 2 * kAccBars);
+    auto yfull_bar = [&](int s) { return y_bars + 8u * s; };
+    auto yempty_bar = [&](int s) { return y_bars + 8u * (kYStages + s); };
+    auto raw_bar = [&](int w, int s) { return y_bars + 8u * (2 * kYStages + 2 * w + s); };
+    auto drain_bar = [&](int o) { return y_bars + 8u * (2 * kYStages + kRawBars + o); };
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + kBarBytes - 64);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
     volatile int* is_last = abort_flag + 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     launch_dependents();
-
-    // An unpacking warp keeps its tile of a pass from k-block to k-block; the first blocks are requested here, weights being
-    // constants of the stream.
-    const int quarter = warp & 3;
-    const int slot = warp < kUnpackWarps ? (warp >> 3) * 8 + 2 * quarter + ((warp >> 2) & 1) : kMaxTiles;       // which of the pass's tiles
-    const bool unpacks = slot < nt;
-    const int g = lane >> 2, c = lane & 3;
-    uint4 wq[kAhead];
-    uint32_t sc[kAhead];
-    const uint4* my_weights = nullptr;
-    const uint32_t* my_scales = nullptr;
-    auto fetch = [&](int i, int kb) {
-        if (kb < l.blocks) {
-            wq[i] = __ldg(my_weights + kb * 32);
-            sc[i] = __ldg(my_scales + ((kb * 64 + c * 16) >> p.group_shift) * 8);
-        }
-    };
-    auto begin_pass = [&](int pass) {
-        const int tile = min(t_begin + pass * nt + slot, t_end - 1);
-        my_weights = q.weights + (size_t)tile * l.blocks * 32 + lane;
-        my_scales = q.scales + (size_t)tile * l.groups * 8 + g;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) fetch(i, i);
-    };
-    if (unpacks) begin_pass(0);
     if (threadIdx.x == 0) {
         for (int o = 0; o < kOperands; ++o) {
             for (int s = 0; s < kWStages; ++s) {
                 ptx::mbar_init(wfull_bar(o, s), max(1, min(8, nt - 8 * o)));
                 ptx::mbar_init(wempty_bar(o, s), 1);
+            }
+            for (int s = 0; s < 4; ++s) {
+                ptx::mbar_init(accfull_bar(o, s), 1);
+                ptx::mbar_init(accfree_bar(o, s), 8);
             }
             ptx::mbar_init(drain_bar(o), 1);
         }
@@ -129,7 +126,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
             ptx::mbar_init(yfull_bar(s), 1);
             ptx::mbar_init(yempty_bar(s), operands);
         }
-        ptx::mbar_init(tfull_bar, operands);
+        for (int w = 0; w < kUnpackWarps; ++w)
+            for (int s = 0; s < 2; ++s) ptx::mbar_init(raw_bar(w, s), 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tensormap(&map_y);
@@ -143,14 +141,39 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_holder, ring = tmem_base + kAccCols;
 
+    // unpacking: a warp keeps its tile of a pass from block to block
+    const int quarter = warp & 3;
+    const int slot = warp < kUnpackWarps ? (warp >> 3) * 8 + 2 * quarter + ((warp >> 2) & 1) : kMaxTiles;       // which of the pass's tiles
+    const bool unpacks = slot < nt;
+    const int g = lane >> 2, c = lane & 3;
+    unsigned char* raw_mem = big_mem + warp * 2 * kRawBytes;             // this warp's two slots
+    // four blocks of the warp's tile and their scales from block kb0 on (one lane)
+    auto fetch = [&](int tile, int kb0, int s) {
+        const int n = min(kRawBlocks, l.blocks - kb0);
+        const int g0 = (kb0 * 64) >> p.group_shift, g1 = ((kb0 + n) * 64 - 1) >> p.group_shift;
+        const uint32_t dst = ptx::smem_addr(raw_mem + s * kRawBytes), scale_bytes = (uint32_t)(g1 - g0 + 1) * 32u;
+        ptx::mbar_arrive_expect_tx(raw_bar(warp, s), n * 512u + scale_bytes);
+        bulk_load(dst, q.weights + ((size_t)tile * l.blocks + kb0) * 32, n * 512u, raw_bar(warp, s));
+        bulk_load(dst + kRawBlocks * 512, q.scales + ((size_t)tile * l.groups + g0) * 8, scale_bytes, raw_bar(warp, s));
+    };
+    // sums: warp = 32 rows of operand (w / 4) % 3, half (w / 12) of the tokens
+    const int my_op = (warp >> 2) % 3, my_half = warp / 12;
+    const bool sums = warp < kUnpackWarps && my_op < operands;
+    const uint32_t acc_from = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(my_op * N + my_half * (N / 2));
+
     // softmax: thread = one token and every `shares`-th row
-    const int tok = threadIdx.x & (N - 1), share = threadIdx.x / N, shares = kWorkers / N;
+    constexpr int shares = kWorkers / N;
+    const int tok = threadIdx.x & (N - 1), share = threadIdx.x / N;
     State st = state_empty();
     bool ok = true;                                                      // of this warp's role
     int ws = 0, ys = 0;                                                  // ring positions
-    uint32_t wp = 0, yp = 0;
+    uint32_t wp = 0, yp = 0, rp = 0;
     uint32_t armed = 0, armed_parity = 0;
     for (int pass = 0; pass < p.passes; ++pass) {
+        const int seg0 = pass * segments;                                // segments before this pass, for the accumulators' parities
+        float z[N / 2];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) z[j] = 0.f;
         if (warp == kTmaWarp) {
             // ---------------------------------------------------------------- y
             if (lane == 0) {
@@ -172,51 +195,84 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
             __syncwarp();
         } else if (warp >= kProductWarp) {
             // ---------------------------------------------------------------- products: a warp per operand (one thread issues a product in
-            // about 75 cycles, whatever its size; twelve of them a stage by one thread were what the kernel waited for)
+            // about 75 cycles, whatever its size; twelve of them a block by one thread were what the kernel waited for)
             const int o = warp - kProductWarp;
             if (lane == 0 && o < operands) {
-                const uint32_t idesc = ptx::idesc_bf16_f32(128, N);
-                int set = 0;
-                for (int kb = 0; ok && kb < l.blocks; ++kb) {
-                    if (!ptx::mbar_wait(yfull_bar(ys), yp, abort_flag) || !ptx::mbar_wait(wfull_bar(o, ws), wp, abort_flag)) {
-                        record_failure(q.ctrl, abort_flag, 2, ws, kb);
+                constexpr uint32_t idesc = ptx::idesc_bf16_f32(128, N);
+                for (int seg = 0; ok && seg < segments; ++seg) {
+                    const int set = (seg0 + seg) % kSets, use = (seg0 + seg) / kSets;
+                    if (use > 0 && !ptx::mbar_wait(accfree_bar(o, set), (uint32_t)(use - 1) & 1u, abort_flag)) {
+                        record_failure(q.ctrl, abort_flag, 2, 0x80 | set, seg);
                         ok = false;
                         break;
                     }
-                    ptx::tc_fence_after_sync();
-                    const uint64_t bdesc = ptx::smem_desc_k128(y_base + ys * y_bytes);
-                    const uint32_t acc = tmem_base + (set * 3 + o) * N, a = ring + ws * 96 + o * 32;
+                    const uint32_t acc = tmem_base + (set * kOperands + o) * N;
+                    for (int kb = seg * kSegment; kb < min(l.blocks, (seg + 1) * kSegment); ++kb) {
+                        if (!ptx::mbar_wait(yfull_bar(ys), yp, abort_flag) || !ptx::mbar_wait(wfull_bar(o, ws), wp, abort_flag)) {
+                            record_failure(q.ctrl, abort_flag, 2, ws, kb);
+                            ok = false;
+                            break;
+                        }
+                        ptx::tc_fence_after_sync();
+                        const uint64_t bdesc = ptx::smem_desc_k128(y_base + ys * y_bytes);
+                        const uint32_t a = ring + ws * 96 + o * 32;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) ptx::mma_bf16_ts(acc, a + k * 8, bdesc + 2u * k, idesc, (kb >= p.sets || k > 0) ? 1u : 0u);
-                    ptx::mma_commit(wempty_bar(o, ws));
-                    ptx::mma_commit(yempty_bar(ys));
-                    if (++ws == kWStages) { ws = 0; wp ^= 1u; }
-                    if (++ys == kYStages) { ys = 0; yp ^= 1u; }
-                    if (++set == p.sets) set = 0;
+                        for (int k = 0; k < 4; ++k) ptx::mma_bf16_ts(acc, a + k * 8, bdesc + 2u * k, idesc, (kb > seg * kSegment || k > 0) ? 1u : 0u);
+                        ptx::mma_commit(wempty_bar(o, ws));
+                        ptx::mma_commit(yempty_bar(ys));
+                        if (++ws == kWStages) { ws = 0; wp ^= 1u; }
+                        if (++ys == kYStages) { ys = 0; yp ^= 1u; }
+                    }
+                    if (ok) ptx::mma_commit(accfull_bar(o, set));
                 }
-                if (ok) ptx::mma_commit(tfull_bar);
                 if (*abort_flag) mma_drain<false>(drain_bar(o));
             }
             __syncwarp();
-        } else if (unpacks) {
-            // ---------------------------------------------------------------- unpacking
-            if (pass > 0) begin_pass(pass);
+        } else {
+            // ---------------------------------------------------------------- unpacking and sums
             const int o = warp >> 3;
             const uint32_t to = ring + (uint32_t)o * 32u + ((uint32_t)(quarter * 32 + ((warp >> 2) & 1) * 16) << 16);
-            for (int kb0 = 0; ok && kb0 < l.blocks; kb0 += kAhead) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    if (kb0 + i >= l.blocks) break;
-                    const uint32_t sl = low_twice(sc[i]), sh = high_twice(sc[i]);
+            const int tile = min(t_begin + pass * nt + slot, t_end - 1);
+            int fetched = 0;                                             // copies issued, four blocks each
+            if (unpacks && lane == 0) {
+                if (pass > 0) ptx::fence_proxy_async();                  // the logits of the pass before lay here
+                fetch(tile, 0, 0);
+                if (kRawBlocks < l.blocks) fetch(tile, kRawBlocks, 1);
+            }
+            if (unpacks) fetched = kRawBlocks < l.blocks ? 2 : 1;
+            const uint32_t rp0 = rp;
+            int next = 0;                                                // segment to add next
+            // blocks, and then as many turns as the last segments lag behind
+            for (int kb = 0; ok && (kb < l.blocks || next < segments); ++kb) {
+                if (unpacks && kb < l.blocks) {
+                    const int s = (kb / kRawBlocks) & 1, i = kb % kRawBlocks;
+                    if (i == 0 && !__all_sync(0xffffffffu, ptx::mbar_wait(raw_bar(warp, s), (rp >> s) & 1u, abort_flag))) {
+                        if (lane == 0) record_failure(q.ctrl, abort_flag, 4, s, kb);
+                        ok = false;
+                        break;
+                    }
+                    const unsigned char* raw = raw_mem + s * kRawBytes;
+                    const uint4 w = *reinterpret_cast<const uint4*>(raw + i * 512 + lane * 16);
+                    const int group = ((kb * 64 + c * 16) >> p.group_shift) - (((kb - i) * 64) >> p.group_shift);
+                    const uint32_t s2 = *reinterpret_cast<const uint32_t*>(raw + kRawBlocks * 512 + group * 32 + g * 4);
+                    const uint32_t sl = low_twice(s2), sh = high_twice(s2);
                     uint32_t v[16];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {                        // pair k of the lane's eight, rows g and g + 8
-                        v[(k >> 1) * 4 + (k & 1)] = q4_pair(k < 4 ? wq[i].x : wq[i].y, k & 3, sl);
-                        v[(k >> 1) * 4 + 2 + (k & 1)] = q4_pair(k < 4 ? wq[i].z : wq[i].w, k & 3, sh);
+                        v[(k >> 1) * 4 + (k & 1)] = q4_pair(k < 4 ? w.x : w.y, k & 3, sl);
+                        v[(k >> 1) * 4 + 2 + (k & 1)] = q4_pair(k < 4 ? w.z : w.w, k & 3, sh);
                     }
-                    fetch(i, kb0 + i + kAhead);
+                    if (i == kRawBlocks - 1) {                           // the slot is read: the blocks after the next four
+                        rp ^= 1u << s;
+                        __syncwarp();
+                        const int kb0 = kb + 1 + kRawBlocks;
+                        if (kb0 < l.blocks) {
+                            if (lane == 0) fetch(tile, kb0, s);
+                            ++fetched;
+                        }
+                    }
                     if (!__all_sync(0xffffffffu, ptx::mbar_wait(wempty_bar(o, ws), wp ^ 1u, abort_flag))) {
-                        if (lane == 0) record_failure(q.ctrl, abort_flag, 4, ws, kb0 + i);
+                        if (lane == 0) record_failure(q.ctrl, abort_flag, 4, 0x40 | ws, kb);
                         ok = false;
                         break;
                     }
@@ -228,41 +284,55 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
                     if (lane == 0) ptx::mbar_arrive(wfull_bar(o, ws));
                     if (++ws == kWStages) { ws = 0; wp ^= 1u; }
                 }
+                if (next < segments && kb + 1 >= min(l.blocks, (next + 1) * kSegment) + kLag) {
+                    if (sums) {
+                        const int set = (seg0 + next) % kSets, use = (seg0 + next) / kSets;
+                        if (!__all_sync(0xffffffffu, ptx::mbar_wait(accfull_bar(my_op, set), (uint32_t)use & 1u, abort_flag))) {
+                            if (lane == 0) record_failure(q.ctrl, abort_flag, 3, set, next);
+                            ok = false;
+                            break;
+                        }
+                        ptx::tc_fence_after_sync();
+#pragma unroll
+                        for (int b = 0; b < N / 2; b += 8) {
+                            float x[8];
+                            ptx::tmem_ld_32x8(acc_from + set * kOperands * N + b, x);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) z[b + j] += x[j];
+                        }
+                        ptx::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(accfree_bar(my_op, set));
+                    }
+                    ++next;
+                }
+            }
+            if (unpacks && ok && l.blocks % kRawBlocks != 0) rp ^= 1u << ((l.blocks / kRawBlocks) & 1);      // the last slot, partly filled
+            if (unpacks && !ok && lane == 0) {                           // let the copies in flight land before the CTA ends
+                uint32_t par = rp0;
+                for (int k = 0; k < fetched; ++k) {
+                    const int s = k & 1;
+                    if (k + 2 >= fetched)
+                        for (uint32_t i = 0; i < (1u << 16) && !ptx::mbar_try_wait(raw_bar(warp, s), (par >> s) & 1u); ++i) __nanosleep(100);
+                    par ^= 1u << s;
+                }
             }
         }
         // -------------------------------------------------------------------- logits to shared memory: rows x tokens
         if (pass == 0 && warp != kTmaWarp) grid_dependency_wait();
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(tfull_bar, (uint32_t)pass & 1u, abort_flag))) {
-            if (lane == 0) record_failure(q.ctrl, abort_flag, 3, 0, pass);
-            ok = false;
-        }
-        ptx::tc_fence_after_sync();
+        __syncthreads();                                                 // the packed blocks, which lay here, are all read
         const int first = t_begin + pass * nt;
         const int rows = min(min(nt, t_end - first) * 16, q.V - first * 16);      // of this pass that exist
-        if (warp < kUnpackWarps && ok) {
-            // warp = a quarter of the lanes, operand (warp / 4) % 3, half (warp / 12) of the tokens
-            const int o = (warp >> 2) % 3, half = warp / 12, r0 = o * 128 + quarter * 32;
-            const int sets = min(p.sets, l.blocks);
+        if (sums) {
+            const int r0 = my_op * 128 + quarter * 32;
+            float* out = z_mem + (size_t)(r0 + lane) * (N + 4) + my_half * (N / 2);
             if (r0 < rows) {
-                const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(o * N + half * (N / 2));
-                float* to = z_mem + (size_t)(r0 + lane) * (N + 4) + half * (N / 2);
-                for (int b = 0; b < N / 2; b += 8) {
-                    float z[8] = {};
-                    for (int s = 0; s < sets; ++s) {
-                        float x[8];
-                        ptx::tmem_ld_32x8(from + s * 3 * N + b, x);
-                        ptx::tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) z[j] += x[j];
-                    }
-                    *reinterpret_cast<float4*>(to + b) = make_float4(z[0], z[1], z[2], z[3]);
-                    *reinterpret_cast<float4*>(to + b + 4) = make_float4(z[4], z[5], z[6], z[7]);
-                }
+                for (int b = 0; b < N / 2; b += 4) *reinterpret_cast<float4*>(out + b) = make_float4(z[b], z[b + 1], z[b + 2], z[b + 3]);
             }
         }
-        ptx::tc_fence_before_sync();
         __syncthreads();
-        ptx::tc_fence_after_sync();
         if (threadIdx.x < kWorkers && tok < q.M && share < rows) {
             const float* z = z_mem + tok;
             float m = -CUDART_INF_F;
@@ -283,6 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     }
 
     if (threadIdx.x < kWorkers) states[share * N + tok] = st;
+    ptx::tc_fence_before_sync();
     __syncthreads();
     if (warp == kProductWarp) {
         ptx::tc_fence_after_sync();
@@ -315,12 +386,11 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     if (threadIdx.x == 0) q.ctrl->head_ticket[0] = 0;                    // ready for the next launch
 }
 
-}  // namespace
-
-ee_status q4_gemm_launch(const Q4Params& q, int num_sms, int device, cudaStream_t stream) {
+template <int N>
+ee_status launch_tokens(const Q4Params& q, int num_sms, int device, cudaStream_t stream) {
     static bool configured[kMaxDevices] = {};
     if (!configured[device]) {
-        if (cudaFuncSetAttribute(q4_gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess) return EE_ERR_CUDA;
+        if (cudaFuncSetAttribute(q4_gemm_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess) return EE_ERR_CUDA;
         configured[device] = true;
     }
     const Q4Layout l = q4_layout(q.V, q.d, q.group);
@@ -330,13 +400,18 @@ ee_status q4_gemm_launch(const Q4Params& q, int num_sms, int device, cudaStream_
     if (grid > kStreamMaxCtas) grid = kStreamMaxCtas;
     const int most = (l.tiles + grid - 1) / grid;                        // tiles of the largest share
     p.passes = (most + kMaxTiles - 1) / kMaxTiles;
-    p.n = q.M <= 16 ? 16 : q.M <= 32 ? 32 : 64;
-    p.sets = kAccCols / (3 * p.n);
     p.group_shift = q.group == 32 ? 5 : q.group == 64 ? 6 : 7;
-    const size_t smem = (size_t)kYStages * p.n * 128 + z_bytes(p.n) + kWorkers * sizeof(State) + kBarBytes + 1024;
+    const size_t smem = (size_t)kYStages * N * 128 + big_bytes(N) + kWorkers * sizeof(State) + kBarBytes + 1024;
     CUtensorMap map;
-    if (!make_tile_map(&map, q.y, q.M, l.blocks * 64, p.n)) return EE_ERR_CUDA;
-    return launch_pdl(q4_gemm_kernel, dim3(grid), kThreads, smem, stream, map, p) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    if (!make_tile_map(&map, q.y, q.M, l.blocks * 64, N)) return EE_ERR_CUDA;
+    return launch_pdl(q4_gemm_kernel<N>, dim3(grid), kThreads, smem, stream, map, p, (int)big_bytes(N)) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+}  // namespace
+
+ee_status q4_gemm_launch(const Q4Params& q, int num_sms, int device, cudaStream_t stream) {
+    return q.M <= 16 ? launch_tokens<16>(q, num_sms, device, stream) : q.M <= 32 ? launch_tokens<32>(q, num_sms, device, stream)
+                                                                                 : launch_tokens<64>(q, num_sms, device, stream);
 }
 
 }  // namespace ee

@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
         if (row < p.M) {
             const uint4* hrow = reinterpret_cast<const uint4*>(p.h + (size_t)row * p.ld_h);
             const RowStats st = row_stats_strided([&](int k) { return ld_dep(hrow + k); }, nvec, p.ln_eps, lane);
-            for (int k = lane; k < nvec; k += 32) yrow[k] = layer_norm_vec8(ld_dep(hrow + k), st, p.gamma, p.beta, k);
+            for (int k = lane; k < nvec; k += 32) yrow[k] = layer_norm_vec8<true>(ld_dep(hrow + k), st, p.gamma, p.beta, k);
         }
         for (int k = (row < p.M ? nvec : 0) + lane; k < l.blocks * 8; k += 32) yrow[k] = make_uint4(0, 0, 0, 0);
     }
