@@ -126,17 +126,41 @@ __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* m,
     }
 }
 
-// Maximum and sum of exponentials of 64 logits (the first nvalid real), four chains each.
+// exp(z - shift) of two logits: the difference and its product with log2 e are rounded one after the other, two to an instruction.
+__device__ __forceinline__ float2 exp_pair(float z0, float z1, unsigned long long minus_shift) {
+    const unsigned long long x = ptx::mul_f32x2(ptx::add_f32x2(ptx::pack_f32x2(z0, z1), minus_shift), ptx::pack_f32x2(kLog2e, kLog2e));
+    const float2 v = ptx::unpack_f32x2(x);
+    return make_float2(ex2(v.x), ex2(v.y));
+}
+
+// Maximum and sum of exponentials of 64 logits (the first nvalid real).  Whole tiles take 1.5 issue slots an element besides
+// the exponential, so that for short rows, whose products do not hide it, the epilogue comes near the exponentials' own rate.
 template <bool kFull>
 __device__ __forceinline__ void fold_stats(const float (&z)[2][32], int nvalid, float& m, float& s) {
-    float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F}, cs[4] = {0.f, 0.f, 0.f, 0.f};
+    float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+    if (kFull) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) cm[j & 3] = ptx::max3(cm[j & 3], z[0][j], z[1][j]);
+        m = ptx::max3(fmaxf(cm[0], cm[1]), cm[2], cm[3]);
+        const unsigned long long minus_m = ptx::pack_f32x2(-m, -m);
+        unsigned long long cs[2] = {ptx::pack_f32x2(0.f, 0.f), ptx::pack_f32x2(0.f, 0.f)};
+#pragma unroll
+        for (int j = 0; j < 64; j += 2) {
+            const float2 e = exp_pair(z[j >> 5][j & 31], z[j >> 5][(j & 31) + 1], minus_m);
+            cs[(j >> 1) & 1] = ptx::add_f32x2(cs[(j >> 1) & 1], ptx::pack_f32x2(e.x, e.y));
+        }
+        const float2 sum = ptx::unpack_f32x2(ptx::add_f32x2(cs[0], cs[1]));
+        s = sum.x + sum.y;
+        return;
+    }
+    float cs[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 64; ++j)
-        if (kFull || j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[j >> 5][j & 31]);
+        if (j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[j >> 5][j & 31]);
     m = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
 #pragma unroll
     for (int j = 0; j < 64; ++j)
-        if (kFull || j < nvalid) cs[j & 3] += ex2((z[j >> 5][j & 31] - m) * kLog2e);
+        if (j < nvalid) cs[j & 3] += ex2((z[j >> 5][j & 31] - m) * kLog2e);
     s = (cs[0] + cs[1]) + (cs[2] + cs[3]);
 }
 
@@ -222,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         }
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(tfull_bar(b), 1);
-            ptx::mbar_init(tempty_bar(b), kPair ? 32 : 16);
+            ptx::mbar_init(tempty_bar(b), kPair && rank == 0 ? 17 : 16);           // a CTA's epilogue warps, and the partner's word for its own
         }
         ptx::mbar_init(drain_bar, 1);
         *abort_flag = 0;
@@ -249,11 +273,17 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
     const int total_tiles = mn_tiles * p.splits;
     // tile -> row tile of this CTA, column tile, range of k-blocks (empty for a split that has nothing to do)
     auto locate = [&](int tile, int& m_tile, int& n_tile, int& split, int& kb0, int& kb1) {
-        split = tile / mn_tiles;
+        // one part is the rule; the general quotients, a few hundred cycles, would lie between any two tiles of every role
+        split = 0;
+        kb0 = 0;
+        kb1 = p.k_blocks;
+        if (p.splits > 1) {                                              // splits x k_blocks is below 2^31, see dy_cost
+            split = tile / mn_tiles;
+            kb0 = split * p.k_blocks / p.splits;
+            kb1 = (split + 1) * p.k_blocks / p.splits;
+        }
         tile_coords(tile - split * mn_tiles, m_units, p.n_tiles, m_tile, n_tile);
         if (kPair) m_tile = 2 * m_tile + (int)rank;
-        kb0 = (int)((long long)split * p.k_blocks / p.splits);
-        kb1 = (int)((long long)(split + 1) * p.k_blocks / p.splits);
     };
     auto load_full_bar = [&](int s) { return kPair ? ptx::map_to_cta(full_bar(s), 0) : full_bar(s); };
     const uint32_t arm_bytes = (uint32_t)(a_stage + b_stage) * (kPair ? 2u : 1u);
@@ -354,6 +384,23 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                 if (ok) mma_commit_all<kPair>(tfull_bar(buf));
             }
             if (*abort_flag) mma_drain<kPair>(drain_bar);
+        } else if (lane == 0 && kPair) {
+            // The second CTA's thread, which has no products to issue, passes its epilogue's hand-over on: an arrival at the
+            // partner waits some 600 cycles for its release, which each of the sixteen warps would otherwise spend at every tile.
+            int local = 0;
+            for (int tile = worker; tile < total_tiles; tile += n_workers) {
+                int m_tile, n_tile, split, kb0, kb1;
+                locate(tile, m_tile, n_tile, split, kb0, kb1);
+                if (kb0 == kb1) continue;
+                const int buf = local & 1;
+                const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
+                ++local;
+                if (!ptx::mbar_wait(tempty_bar(buf), acc_phase, abort_flag)) {
+                    record_failure(p.ctrl, abort_flag, 2, 0xc0 | buf, tile);
+                    break;
+                }
+                ptx::mbar_arrive_remote(ptx::map_to_cta(tempty_bar(buf), 0));
+            }
         }
     } else {
         // ------------------------------------------------------------------ epilogue (warps 2..17)
@@ -405,8 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             ptx::tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) {
-                if (kPair) ptx::mbar_arrive_remote(ptx::map_to_cta(tempty_bar(buf), 0));
-                else ptx::mbar_arrive(tempty_bar(buf));
+                ptx::mbar_arrive(tempty_bar(buf));
             }
             if (kMode == kStats) {
                 float m = -CUDART_INF_F, s = 0.f;                        // an empty part
@@ -441,7 +487,12 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                 if (kMode == kGrad) {
                     // G, zeros in the columns that fill up the last block of 64 and in rows that take no part
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) z[c][j] = weight * ex2((z[c][j] - lse) * kLog2e);
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 e = exp_pair(z[c][j], z[c][j + 1], ptx::pack_f32x2(-lse, -lse));
+                        const float2 g = ptx::unpack_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(e.x, e.y), ptx::pack_f32x2(weight, weight)));
+                        z[c][j] = g.x;
+                        z[c][j + 1] = g.y;
+                    }
                     if ((unsigned)(label - base) < 32u) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) z[c][j] -= (base + j == label) ? weight : 0.f;
