@@ -60,23 +60,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// n states of a token, `stride` apart in shared memory: the maximum first, then the sums, so that no step waits for the one before.
-__device__ __forceinline__ State combine_column(const State* s, int n, int stride) {
-    float m = -CUDART_INF_F;
-    for (int k = 0; k < n; ++k) m = fmaxf(m, s[k * stride].m);
-    State r{m, 0.f, 0.f, 0x7fffffff};
-    for (int k = 0; k < n; ++k) {
-        const State o = s[k * stride];
-        const bool live = !(o.s == 0.f);
-        const float dl = o.m - m, al = live ? ex2(dl * kLog2e) : 0.f;
-        r.s += live ? al * o.s : 0.f;
-        r.t += live ? al * fmaf(dl, o.s, o.t) : 0.f;
-        r.idx = (live && o.m == m) ? min(r.idx, o.idx) : r.idx;
-    }
-    if (r.s == 0.f) r.m = -CUDART_INF_F;
-    return r;
-}
-
 template <int N>                                  // tokens, padded: 16, 32 or 64
 __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_constant__ CUtensorMap map_y, const GemmParams p, const int big) {
     constexpr int kSets = kAccCols / (kOperands * N);                    // accumulators: 4, 2 or 1
@@ -93,7 +76,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     const uint32_t y_base = ptx::smem_addr(smem);
     unsigned char* big_mem = smem + kYStages * y_bytes;
     float* z_mem = reinterpret_cast<float*>(big_mem);                    // [rows][N + 4]
-    State* states = reinterpret_cast<State*>(big_mem + big);             // [kWorkers / N][N]
+    RestState* states = reinterpret_cast<RestState*>(big_mem + big);             // [kWorkers / N][N]
     unsigned char* bar_mem = reinterpret_cast<unsigned char*>(states + kWorkers);
     const uint32_t bar_base = ptx::smem_addr(bar_mem);
     auto wfull_bar = [&](int o, int s) { return bar_base + 8u * (o * kWStages + s); };
@@ -164,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     // softmax: thread = one token and every `shares`-th row
     constexpr int shares = kWorkers / N;
     const int tok = threadIdx.x & (N - 1), share = threadIdx.x / N;
-    State st = state_empty();
+    RestState st = rest_empty();
     bool ok = true;                                                      // of this warp's role
     int ws = 0, ys = 0;                                                  // ring positions
     uint32_t wp = 0, yp = 0, rp = 0;
@@ -343,15 +326,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
 #pragma unroll 8
             for (int r = share; r < rows; r += shares) {
                 const float x = z[(size_t)r * (N + 4)], dz = x - m, e = ex2(dz * kLog2e);
-                s += e;
+                const bool top = x == m && idx == 0x7fffffff;            // the largest term stays out of the sum
+                s += top ? 0.f : e;
                 t = fmaf(e, dz, t);
-                idx = (x == m && idx == 0x7fffffff) ? r : idx;
+                idx = top ? r : idx;
             }
-            state_merge(st, State{m, s, t, first * 16 + idx});
+            rest_merge(st, RestState{m, s, t, idx == 0x7fffffff ? idx : first * 16 + idx});
         }
         if (pass + 1 < p.passes) __syncthreads();                        // z is read before the next pass writes it
     }
 
+    auto column = [&](int token) { return rest_combine(shares, [&](int k) -> const RestState& { return states[k * N + token]; }); };
     if (threadIdx.x < kWorkers) states[share * N + tok] = st;
     ptx::tc_fence_before_sync();
     __syncthreads();
@@ -359,30 +344,29 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(tmem_base, kTmemCols);
     }
-    if ((int)threadIdx.x < q.M) q.parts[(size_t)blockIdx.x * N + threadIdx.x] = combine_column(states + threadIdx.x, shares, N);
+    if ((int)threadIdx.x < q.M) q.parts[(size_t)blockIdx.x * N + threadIdx.x] = column(threadIdx.x);
     __syncthreads();
     if (threadIdx.x == 0) *is_last = ticket_arrive_is_last(&q.ctrl->head_ticket[0], gridDim.x) ? 1 : 0;
     __syncthreads();
     if (!*is_last) return;
     // the CTAs' states: lane = token, eight CTAs at a time in flight per thread, then as above
     if (threadIdx.x < kWorkers) {
-        State s = state_empty();
+        RestState s = rest_empty();
         if (tok < q.M)
             for (int b0 = share; b0 < (int)gridDim.x; b0 += 8 * shares) {
-                State v[8];
+                RestState v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int b = b0 + i * shares;
-                    v[i] = b < (int)gridDim.x ? state_load_cg(q.parts + (size_t)b * N + tok) : state_empty();
+                    v[i] = b < (int)gridDim.x ? rest_load_cg(q.parts + (size_t)b * N + tok) : rest_empty();
                 }
-                state_merge(s, state_combine<8>(v));
+                rest_merge(s, rest_combine(8, [&](int k) -> const RestState& { return v[k]; }));
             }
         states[share * N + tok] = s;
     }
     __syncthreads();
     if ((int)threadIdx.x < q.M)
-        state_finish(combine_column(states + threadIdx.x, shares, N), q.tau_per_row ? ld_dep(q.tau_per_row + threadIdx.x) : q.tau, q.argmax,
-                     q.entropy, q.maxprob, q.exit_mask, threadIdx.x);
+        rest_finish(column(threadIdx.x), q, threadIdx.x);
     if (threadIdx.x == 0) q.ctrl->head_ticket[0] = 0;                    // ready for the next launch
 }
 
@@ -401,7 +385,7 @@ ee_status launch_tokens(const Q4Params& q, int num_sms, int device, cudaStream_t
     const int most = (l.tiles + grid - 1) / grid;                        // tiles of the largest share
     p.passes = (most + kMaxTiles - 1) / kMaxTiles;
     p.group_shift = q.group == 32 ? 5 : q.group == 64 ? 6 : 7;
-    const size_t smem = (size_t)kYStages * N * 128 + big_bytes(N) + kWorkers * sizeof(State) + kBarBytes + 1024;
+    const size_t smem = (size_t)kYStages * N * 128 + big_bytes(N) + kWorkers * sizeof(RestState) + kBarBytes + 1024;
     CUtensorMap map;
     if (!make_tile_map(&map, q.y, q.M, l.blocks * 64, N)) return EE_ERR_CUDA;
     return launch_pdl(q4_gemm_kernel<N>, dim3(grid), kThreads, smem, stream, map, p, (int)big_bytes(N)) == cudaSuccess ? EE_OK : EE_ERR_CUDA;

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
     const Q4Layout l = q4_layout(p.V, p.d, p.group);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int ld = y_row_bytes(p.d);
-    State* states = reinterpret_cast<State*>(smem + NT * 8 * ld);        // [kWarps][max(NT * 8, 32)]: per warp, then scratch of the merge
+    RestState* states = reinterpret_cast<RestState*>(smem + NT * 8 * ld);        // [kWarps][max(NT * 8, 32)]: per warp, then scratch of the merge
     launch_dependents();
 
     uint4 w[kUnroll];
@@ -184,8 +184,8 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
         }
         for (int k = (row < p.M ? nvec : 0) + lane; k < l.blocks * 8; k += 32) yrow[k] = make_uint4(0, 0, 0, 0);
     }
-    State* mine = states + warp * (NT * 8);
-    for (int i = lane; i < NT * 8; i += 32) mine[i] = state_empty();
+    RestState* mine = states + warp * (NT * 8);
+    for (int i = lane; i < NT * 8; i += 32) mine[i] = rest_empty();
     __syncthreads();
 
     const unsigned char* ybase = smem + g * ld + c * 32;
@@ -242,20 +242,20 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {                                // token 2c + j of the eight: rows g and g + 8, then over g
-                State s = state_empty();
-                if (v < p.V) state_push(s, acc[t][j], v);
-                if (v + 8 < p.V) state_push(s, acc[t][2 + j], v + 8);
-                s = state_reduce_lanes<4, 16>(s);
+                RestState s = rest_empty();
+                if (v < p.V) rest_push(s, acc[t][j], v);
+                if (v + 8 < p.V) rest_push(s, acc[t][2 + j], v + 8);
+                s = rest_reduce_lanes<4>(s);
                 if (g == 0) {
-                    State o = mine[t * 8 + 2 * c + j];
-                    state_merge(o, s);
+                    RestState o = mine[t * 8 + 2 * c + j];
+                    rest_merge(o, s);
                     mine[t * 8 + 2 * c + j] = o;
                 }
             }
     }
     __syncthreads();
     for (int tok = warp; tok < p.M; tok += kWarps) {                      // the warps' states of a row, one per lane
-        const State s = state_reduce_lanes<1, 16>(lane < kWarps ? states[lane * (NT * 8) + tok] : state_empty());
+        const RestState s = rest_reduce_lanes<1>(lane < kWarps ? states[lane * (NT * 8) + tok] : rest_empty());
         if (lane == 0) p.parts[(size_t)blockIdx.x * (NT * 8) + tok] = s;
     }
     __syncthreads();
@@ -263,17 +263,17 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
     __syncthreads();
     if (!is_last) return;
     for (int tok = warp; tok < p.M; tok += kWarps) {                      // the CTAs' states, up to eight per lane
-        State v[8];
+        RestState v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            v[i] = lane + 32 * i < (int)gridDim.x ? state_load_cg(p.parts + (size_t)(lane + 32 * i) * (NT * 8) + tok) : state_empty();
-        const State s = state_reduce_lanes<1, 16>(state_combine<8>(v));
-        if (lane == 0) state_finish(s, p.tau_per_row ? ld_dep(p.tau_per_row + tok) : p.tau, p.argmax, p.entropy, p.maxprob, p.exit_mask, tok);
+            v[i] = lane + 32 * i < (int)gridDim.x ? rest_load_cg(p.parts + (size_t)(lane + 32 * i) * (NT * 8) + tok) : rest_empty();
+        const RestState s = rest_reduce_lanes<1>(rest_combine(8, [&](int k) -> const RestState& { return v[k]; }));
+        if (lane == 0) rest_finish(s, p, tok);
     }
     if (threadIdx.x == 0) p.ctrl->head_ticket[0] = 0;                    // ready for the next launch
 }
 
-size_t q4_smem(int nt, int d) { return (size_t)nt * 8 * y_row_bytes(d) + (size_t)kWarps * (nt * 8 > 32 ? nt * 8 : 32) * sizeof(State); }
+size_t q4_smem(int nt, int d) { return (size_t)nt * 8 * y_row_bytes(d) + (size_t)kWarps * (nt * 8 > 32 ? nt * 8 : 32) * sizeof(RestState); }
 
 // Rows one launch takes: sixteen, or eight where sixteen do not fit shared memory.
 int slab_rows(int d) { return q4_smem(2, d) <= kSmemBudget ? 16 : 8; }
@@ -291,7 +291,7 @@ ee_status launch_head(const Q4Params& p, int num_sms, int device, cudaStream_t s
     return launch_pdl(q4_head_kernel<NT>, dim3(grid), kThreads, q4_smem(NT, p.d), stream, p) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
-size_t parts_bytes() { return (size_t)kStreamMaxCtas * kQ4GemmRows * sizeof(State); }
+size_t parts_bytes() { return (size_t)kStreamMaxCtas * kQ4GemmRows * sizeof(RestState); }
 
 
 }  // namespace
@@ -344,7 +344,7 @@ ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group) {
         p.ld_h = a.ld_h; p.gamma = a.gamma; p.beta = a.beta; p.ln_eps = a.ln_eps;
         p.M = a.M - r0 < slab ? a.M - r0 : slab;
         p.d = a.d; p.V = a.V; p.group = group;
-        p.parts = reinterpret_cast<State*>(ws + kCtrlBytes);
+        p.parts = reinterpret_cast<RestState*>(ws + kCtrlBytes);
         p.tau_per_row = a.tau_per_row ? a.tau_per_row + r0 : nullptr;
         p.tau = a.tau;
         p.argmax = a.argmax + r0; p.entropy = a.entropy + r0; p.maxprob = a.maxprob + r0; p.exit_mask = a.exit_mask + r0;
