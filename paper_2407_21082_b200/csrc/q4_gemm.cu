@@ -36,6 +36,7 @@ constexpr int kYStages = 8;                      // of N x 128 bytes of shared m
 constexpr int kSegment = 4;                      // blocks of 64 columns an accumulator sums
 constexpr int kLag = 2;                          // blocks unpacked between a segment's last one and its reading: fewer than kWStages, or nobody moves
 constexpr int kRawBlocks = 4;                    // packed blocks per bulk copy
+static_assert(kRawBlocks == kSegment, "a copy is a segment");
 constexpr int kRawBytes = kRawBlocks * 512 + 256;      // ... and their scales, up to eight groups
 constexpr int kAccCols = 192;
 constexpr int kTmemCols = 512;
@@ -147,19 +148,19 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
     // softmax: thread = one token and every `shares`-th row
     constexpr int shares = kWorkers / N;
     const int tok = threadIdx.x & (N - 1), share = threadIdx.x / N;
-    RestState st = rest_empty();
+    if (threadIdx.x < kWorkers) states[share * N + tok] = rest_empty();          // in shared memory: the loop needs its registers
     bool ok = true;                                                      // of this warp's role
-    int ws = 0, ys = 0;                                                  // ring positions
-    uint32_t wp = 0, yp = 0, rp = 0;
-    uint32_t armed = 0, armed_parity = 0;
     for (int pass = 0; pass < p.passes; ++pass) {
         const int seg0 = pass * segments;                                // segments before this pass, for the accumulators' parities
+        int ws = pass * l.blocks % kWStages, ys = pass * l.blocks % kYStages;              // ring positions and their parities
+        uint32_t wp = pass * l.blocks / kWStages & 1, yp = pass * l.blocks / kYStages & 1;
         float z[N / 2];
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) z[j] = 0.f;
         if (warp == kTmaWarp) {
             // ---------------------------------------------------------------- y
             if (lane == 0) {
+                uint32_t armed = 0, armed_parity = 0;                    // of this pass: the loads of the one before were all waited for
                 if (pass == 0) grid_dependency_wait();
                 for (int kb = 0; ok && kb < l.blocks; ++kb) {
                     if (!ptx::mbar_wait(yempty_bar(ys), yp ^ 1u, abort_flag)) {
@@ -217,61 +218,61 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
             const uint32_t to = ring + (uint32_t)o * 32u + ((uint32_t)(quarter * 32 + ((warp >> 2) & 1) * 16) << 16);
             const int tile = min(t_begin + pass * nt + slot, t_end - 1);
             int fetched = 0;                                             // copies issued, four blocks each
-            if (unpacks && lane == 0) {
+            if (unpacks && ok && lane == 0) {
                 if (pass > 0) ptx::fence_proxy_async();                  // the logits of the pass before lay here
                 fetch(tile, 0, 0);
                 if (kRawBlocks < l.blocks) fetch(tile, kRawBlocks, 1);
             }
-            if (unpacks) fetched = kRawBlocks < l.blocks ? 2 : 1;
-            const uint32_t rp0 = rp;
-            int next = 0;                                                // segment to add next
-            // blocks, and then as many turns as the last segments lag behind
-            for (int kb = 0; ok && (kb < l.blocks || next < segments); ++kb) {
-                if (unpacks && kb < l.blocks) {
-                    const int s = (kb / kRawBlocks) & 1, i = kb % kRawBlocks;
-                    if (i == 0 && !__all_sync(0xffffffffu, ptx::mbar_wait(raw_bar(warp, s), (rp >> s) & 1u, abort_flag))) {
-                        if (lane == 0) record_failure(q.ctrl, abort_flag, 4, s, kb);
-                        ok = false;
-                        break;
-                    }
-                    const unsigned char* raw = raw_mem + s * kRawBytes;
-                    const uint4 w = *reinterpret_cast<const uint4*>(raw + i * 512 + lane * 16);
-                    const int group = ((kb * 64 + c * 16) >> p.group_shift) - (((kb - i) * 64) >> p.group_shift);
-                    const uint32_t s2 = *reinterpret_cast<const uint32_t*>(raw + kRawBlocks * 512 + group * 32 + g * 4);
-                    const uint32_t sl = low_twice(s2), sh = high_twice(s2);
-                    uint32_t v[16];
+            if (unpacks && ok) fetched = kRawBlocks < l.blocks ? 2 : 1;
+            const uint32_t raw0 = (uint32_t)(pass * ((segments + 1) >> 1)), raw1 = (uint32_t)(pass * (segments >> 1));     // copies before, by slot
+            // segments, and one turn more for adding the last; unrolled, so that what depends on a block's place in its segment is constant
+            for (int seg = 0; ok && seg <= segments; ++seg) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {                        // pair k of the lane's eight, rows g and g + 8
-                        v[(k >> 1) * 4 + (k & 1)] = q4_pair(k < 4 ? w.x : w.y, k & 3, sl);
-                        v[(k >> 1) * 4 + 2 + (k & 1)] = q4_pair(k < 4 ? w.z : w.w, k & 3, sh);
-                    }
-                    if (i == kRawBlocks - 1) {                           // the slot is read: the blocks after the next four
-                        rp ^= 1u << s;
-                        __syncwarp();
-                        const int kb0 = kb + 1 + kRawBlocks;
-                        if (kb0 < l.blocks) {
-                            if (lane == 0) fetch(tile, kb0, s);
-                            ++fetched;
+                for (int i = 0; i < kSegment; ++i) {
+                    const int kb = seg * kSegment + i;
+                    if (unpacks && kb < l.blocks) {
+                        const int s = seg & 1;
+                        if (i == 0 && !__all_sync(0xffffffffu, ptx::mbar_wait(raw_bar(warp, s), ((s ? raw1 : raw0) + (uint32_t)(seg >> 1)) & 1u, abort_flag))) {
+                            if (lane == 0) record_failure(q.ctrl, abort_flag, 4, s, kb);
+                            ok = false;
+                            break;
                         }
+                        const unsigned char* raw = raw_mem + s * kRawBytes;
+                        const uint4 w = *reinterpret_cast<const uint4*>(raw + i * 512 + lane * 16);
+                        const int group = (i * 64 + c * 16) >> p.group_shift;                // a copy begins with a group: 256 columns
+                        const uint32_t s2 = *reinterpret_cast<const uint32_t*>(raw + kRawBlocks * 512 + group * 32 + g * 4);
+                        const uint32_t sl = low_twice(s2), sh = high_twice(s2);
+                        uint32_t v[16];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {                        // pair k of the lane's eight, rows g and g + 8
+                            v[(k >> 1) * 4 + (k & 1)] = q4_pair(k < 4 ? w.x : w.y, k & 3, sl);
+                            v[(k >> 1) * 4 + 2 + (k & 1)] = q4_pair(k < 4 ? w.z : w.w, k & 3, sh);
+                        }
+                        if (i == kRawBlocks - 1) {                           // the slot is read: the blocks after the next four
+                            __syncwarp();
+                            const int kb0 = kb + 1 + kRawBlocks;
+                            if (kb0 < l.blocks) {
+                                if (lane == 0) fetch(tile, kb0, s);
+                                ++fetched;
+                            }
+                        }
+                        if (!__all_sync(0xffffffffu, ptx::mbar_wait(wempty_bar(o, ws), wp ^ 1u, abort_flag))) {
+                            if (lane == 0) record_failure(q.ctrl, abort_flag, 4, 0x40 | ws, kb);
+                            ok = false;
+                            break;
+                        }
+                        ptx::tc_fence_after_sync();
+                        ptx::tmem_st_16x64bf16(to + ws * 96, v);
+                        ptx::tmem_st_wait();
+                        ptx::tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(wfull_bar(o, ws));
+                        if (++ws == kWStages) { ws = 0; wp ^= 1u; }
                     }
-                    if (!__all_sync(0xffffffffu, ptx::mbar_wait(wempty_bar(o, ws), wp ^ 1u, abort_flag))) {
-                        if (lane == 0) record_failure(q.ctrl, abort_flag, 4, 0x40 | ws, kb);
-                        ok = false;
-                        break;
-                    }
-                    ptx::tc_fence_after_sync();
-                    ptx::tmem_st_16x64bf16(to + ws * 96, v);
-                    ptx::tmem_st_wait();
-                    ptx::tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(wfull_bar(o, ws));
-                    if (++ws == kWStages) { ws = 0; wp ^= 1u; }
-                }
-                if (next < segments && kb + 1 >= min(l.blocks, (next + 1) * kSegment) + kLag) {
-                    if (sums) {
-                        const int set = (seg0 + next) % kSets, use = (seg0 + next) / kSets;
+                    if (i == kLag - 1 && seg > 0 && sums) {                  // the segment before
+                        const int set = (seg0 + seg - 1) % kSets, use = (seg0 + seg - 1) / kSets;
                         if (!__all_sync(0xffffffffu, ptx::mbar_wait(accfull_bar(my_op, set), (uint32_t)use & 1u, abort_flag))) {
-                            if (lane == 0) record_failure(q.ctrl, abort_flag, 3, set, next);
+                            if (lane == 0) record_failure(q.ctrl, abort_flag, 3, set, seg - 1);
                             ok = false;
                             break;
                         }
@@ -282,24 +283,22 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
                             ptx::tmem_ld_32x8(acc_from + set * kOperands * N + b, x);
                             ptx::tmem_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) z[b + j] += x[j];
+                            for (int j = 0; j < 8; j += 2) {
+                                const float2 sum = ptx::unpack_f32x2(ptx::add_f32x2(ptx::pack_f32x2(z[b + j], z[b + j + 1]), ptx::pack_f32x2(x[j], x[j + 1])));
+                                z[b + j] = sum.x;
+                                z[b + j + 1] = sum.y;
+                            }
                         }
                         ptx::tc_fence_before_sync();
                         __syncwarp();
                         if (lane == 0) ptx::mbar_arrive(accfree_bar(my_op, set));
                     }
-                    ++next;
                 }
             }
-            if (unpacks && ok && l.blocks % kRawBlocks != 0) rp ^= 1u << ((l.blocks / kRawBlocks) & 1);      // the last slot, partly filled
             if (unpacks && !ok && lane == 0) {                           // let the copies in flight land before the CTA ends
-                uint32_t par = rp0;
-                for (int k = 0; k < fetched; ++k) {
-                    const int s = k & 1;
-                    if (k + 2 >= fetched)
-                        for (uint32_t i = 0; i < (1u << 16) && !ptx::mbar_try_wait(raw_bar(warp, s), (par >> s) & 1u); ++i) __nanosleep(100);
-                    par ^= 1u << s;
-                }
+                for (int k = max(0, fetched - 2); k < fetched; ++k)
+                    for (uint32_t i = 0; i < (1u << 16) && !ptx::mbar_try_wait(raw_bar(warp, k & 1), ((k & 1 ? raw1 : raw0) + (uint32_t)(k >> 1)) & 1u); ++i)
+                        __nanosleep(100);
             }
         }
         // -------------------------------------------------------------------- logits to shared memory: rows x tokens
@@ -331,13 +330,14 @@ __global__ void __launch_bounds__(kThreads, 1) q4_gemm_kernel(const __grid_const
                 t = fmaf(e, dz, t);
                 idx = top ? r : idx;
             }
+            RestState st = states[share * N + tok];
             rest_merge(st, RestState{m, s, t, idx == 0x7fffffff ? idx : first * 16 + idx});
+            states[share * N + tok] = st;
         }
         if (pass + 1 < p.passes) __syncthreads();                        // z is read before the next pass writes it
     }
 
     auto column = [&](int token) { return rest_combine(shares, [&](int k) -> const RestState& { return states[k * N + token]; }); };
-    if (threadIdx.x < kWorkers) states[share * N + tok] = st;
     ptx::tc_fence_before_sync();
     __syncthreads();
     if (warp == kProductWarp) {
