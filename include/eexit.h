@@ -21,7 +21,8 @@
  * EE_GEMM_PAIRS=0 keeps every CTA on its own 128-row tiles and EE_GEMM_K2=0 keeps one k-block per ring slot
  * (both read once per process); EE_MERGE_LOOKS=n sets how often a row group's owner looks for the launch's
  * other CTAs before it hands its rows over (read when a call is planned); EE_CASCADE_ALL_ROWS_MAX=m moves
- * the batch size at which ee_cascade changes path (read once).  They change which kernel or tile width runs, so
+ * the batch size at which ee_cascade changes path (read once); EE_Q4_KERNEL=stream|gemm forces the kernel of
+ * ee_exit_head_q4 (read per call).  They change which kernel or tile width runs, so
  * entropy and max-probability may differ in their last bits (sums taken in another order); decisions away from
  * the tolerance band do not change.
  *
@@ -466,7 +467,7 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  *   accumulate != 0: dW, dgamma and dbeta are added to what the buffers hold (dh is always overwritten)
  * The rounding of y to bf16 is passed through by the gradient.  All gradients are bf16: the products behind dy and dW
  * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that.
- * Sizes, strides and alignment as in ee_exit_head; all gradient buffers 16-byte aligned.  Workspace:
+ * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
  * initialised once with ee_workspace_init; both 0 if a size is invalid.  W is written by nobody while a call is in
  * flight (see "Constants of the stream" above: a step that updates W must have completed before the next call is
@@ -487,13 +488,13 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
  * time of reading its weights; these calls hold them as whole numbers with a scale per row and group of columns:
  *   s[v, k] = bf16( max |W[v, j]| / 7 ) over the columns j of group k;   q[v, j] = nearest whole number of W[v, j] / s
  *   (ties to the even one; 0 where s = 0), kept within -8 .. 7;          W4[v, j] = bf16( s q )
- * W must be finite.  group is 32, 64 or 128; d % group == 0, group <= d <= 8192, V >= 1.  A packed head is
+ * W must be finite.  group is 32, 64 or 128; d % group == 0, group <= d <= 8192, 1 <= V <= 2^30.  A packed head is
  * ee_head_q4_bytes(V, d, group) bytes (0 if a size is invalid), 256-byte aligned, in a layout of the library's own;
  * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous.  W and W4 are 32-byte aligned.
  *
  * ee_exit_head_q4 is ee_exit_head with W4 for W and the y of ee_head_ce: same definition otherwise, same outputs, strides,
- * alignment and rules (the packed head is a constant of the stream).  Any M; rows beyond those whose LayerNorm output fits shared memory go in further
- * passes over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
+ * alignment and rules (the packed head is a constant of the stream).  M up to 2^30; up to 16 rows (8 where d is large), and above
+ * that every 64 rows, are one pass over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
  * with ee_workspace_init.  M = 0 is a no-op.
  */
 size_t    ee_head_q4_bytes(int V, int d, int group);
@@ -515,7 +516,7 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
  *                   the sums are added to what it holds (one rounding), rows of other tokens are not touched;
  *                   otherwise the whole table is written.
  * table bf16 [V, d] contiguous; tokens int32 [n]; out, dout bf16 [n, d], row strides ld_* elements (ld_* >= d,
- * ld_* % 8 == 0); dtable [V, d] contiguous; 16-byte alignment; d % 8 == 0, 8 <= d <= 8192, V >= 1, n >= 0 (n = 0:
+ * ld_* % 8 == 0); dtable [V, d] contiguous; 16-byte alignment; d % 8 == 0, 8 <= d <= 8192, 1 <= V <= 2^30, 0 <= n <= 2^30 (n = 0:
  * ee_embed_grad clears the table unless it accumulates).  Workspace of the gradient:
  * ee_embed_grad_workspace_bytes(n, d, V) (0 if a size is invalid), 256-byte aligned; needs no initialisation.
  */

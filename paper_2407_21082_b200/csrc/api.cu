@@ -40,6 +40,10 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 
 bool sizes_ok(int M, int d, int V) { return M >= 0 && V >= 1 && d >= 8 && d <= 8192 && (d % 8) == 0; }
 
+// Rows and vocabularies that a multiple of a tile's size still fits 32 bits beside.
+constexpr int kMaxCount = 1 << 30;
+bool train_sizes_ok(int M, int d, int V) { return sizes_ok(M, d, V) && M <= kMaxCount && V <= kMaxCount; }
+
 // Kernel used when the caller does not choose: the tensor-core path for every size.  (Measured per head call,
 // d = 512..2560, V = 50304: it is ahead of the streaming kernel from M = 1 on, 16.3 against 17.4 us at
 // d = 512 M = 1 and 41.8 against 56.7 us at d = 2048 M = 16; the other two kernels stay selectable.)
@@ -611,19 +615,19 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
 }
 
 size_t ee_head_ce_workspace_bytes(int M, int d, int V) {
-    if (!sizes_ok(M, d, V)) return 0;
+    if (!train_sizes_ok(M, d, V)) return 0;
     return ce_workspace_bytes(M, d, V, false);
 }
 
 size_t ee_head_ce_grad_workspace_bytes(int M, int d, int V) {
-    if (!sizes_ok(M, d, V)) return 0;
+    if (!train_sizes_ok(M, d, V)) return 0;
     return ce_workspace_bytes(M, d, V, true);
 }
 
 ee_status ee_head_ce(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W, int M,
                      int d, int V, const int* labels, float* ce, float* lse, float* loss, void* workspace,
                      size_t workspace_bytes_, void* stream) {
-    if (!sizes_ok(M, d, V)) return EE_ERR_SHAPE;
+    if (!train_sizes_ok(M, d, V)) return EE_ERR_SHAPE;
     if (!loss) return EE_ERR_NULL;
     if (M > 0) {
         if (!h || !gamma || !beta || !W || !labels || !ce || !lse || !workspace) return EE_ERR_NULL;
@@ -648,7 +652,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
                           int M, int d, int V, const int* labels, const float* lse, const float* loss, const float* dce,
                           const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta, int accumulate,
                           void* workspace, size_t workspace_bytes_, void* stream) {
-    if (!sizes_ok(M, d, V)) return EE_ERR_SHAPE;
+    if (!train_sizes_ok(M, d, V)) return EE_ERR_SHAPE;
     if ((dgamma != nullptr) != (dbeta != nullptr)) return EE_ERR_NULL;
     if (dce && dloss) return EE_ERR_SHAPE;                               // the rows' weights and the mean's gradient exclude each other
     if (!aligned(dh, 16) || !aligned(dW, 16) || !aligned(dgamma, 16) || !aligned(dbeta, 16)) return EE_ERR_ALIGN;
@@ -682,7 +686,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
 
 namespace {
 bool q4_sizes_ok(int V, int d, int group) {
-    return V >= 1 && (group == 32 || group == 64 || group == 128) && d >= group && d <= 8192 && d % group == 0;
+    return V >= 1 && V <= kMaxCount && (group == 32 || group == 64 || group == 128) && d >= group && d <= 8192 && d % group == 0;
 }
 }  // namespace
 
@@ -714,7 +718,7 @@ ee_status ee_head_q4_unpack(const void* q4, size_t q4_bytes, int V, int d, int g
 }
 
 size_t ee_exit_head_q4_workspace_bytes(int M, int d, int V) {
-    if (!sizes_ok(M, d, V)) return 0;
+    if (!train_sizes_ok(M, d, V)) return 0;
     return q4_head_workspace_bytes(M, d);
 }
 
@@ -722,7 +726,7 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
                           size_t q4_bytes, int group, int M, int d, int V, const float* tau_per_row, float tau, int* argmax,
                           float* entropy, float* maxprob, unsigned char* exit_mask, void* workspace, size_t workspace_bytes_,
                           void* stream) {
-    if (!sizes_ok(M, d, V) || !q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (!train_sizes_ok(M, d, V) || !q4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
     if (M == 0) return EE_OK;
     if (!h || !gamma || !beta || !q4 || !argmax || !entropy || !maxprob || !exit_mask || !workspace) return EE_ERR_NULL;
     if (ld_h < d || (ld_h % 8) != 0) return EE_ERR_SHAPE;
@@ -741,7 +745,7 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
 }
 
 ee_status ee_embed(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, void* stream) {
-    if (!sizes_ok(n, d, V)) return EE_ERR_SHAPE;
+    if (!train_sizes_ok(n, d, V)) return EE_ERR_SHAPE;
     if (n == 0) return EE_OK;
     if (!table || !tokens || !out) return EE_ERR_NULL;
     if (ld_out < d || (ld_out % 8) != 0) return EE_ERR_SHAPE;
@@ -753,13 +757,13 @@ ee_status ee_embed(const void* table, int V, int d, const int* tokens, int n, fl
 }
 
 size_t ee_embed_grad_workspace_bytes(int n, int d, int V) {
-    if (!sizes_ok(n, d, V)) return 0;
+    if (!train_sizes_ok(n, d, V)) return 0;
     return embed_grad_workspace_bytes(n, d, V);
 }
 
 ee_status ee_embed_grad(const void* dout, long long ld_dout, const int* tokens, int n, int V, int d, float scale, void* dtable,
                         int dtable_fp32, int accumulate, void* workspace, size_t workspace_bytes_, void* stream) {
-    if (!sizes_ok(n, d, V)) return EE_ERR_SHAPE;
+    if (!train_sizes_ok(n, d, V)) return EE_ERR_SHAPE;
     if (!dtable) return EE_ERR_NULL;
     if (!aligned(dtable, 16)) return EE_ERR_ALIGN;
     if (n > 0) {

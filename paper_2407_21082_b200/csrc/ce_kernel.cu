@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         split = 0;
         kb0 = 0;
         kb1 = p.k_blocks;
-        if (p.splits > 1) {                                              // splits x k_blocks is below 2^31, see dy_cost
+        if (p.splits > 1) {                                              // at most 32 parts of at most 2^24 blocks
             split = tile / mn_tiles;
             kb0 = split * p.k_blocks / p.splits;
             kb1 = (split + 1) * p.k_blocks / p.splits;
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             float weight = 0.f, lse = 0.f;
             int label = -1;
             if ((kMode == kStats || kMode == kGrad) && live) {
-                label = p.labels ? ld_dep(p.labels + row) - p.v0 : -1;
+                label = p.labels ? (int)((unsigned)ld_dep(p.labels + row) - (unsigned)p.v0) : -1;      // any label, INT_MIN too
                 if (kMode == kGrad) {
                     weight = row_weight(p.labels, p.dce, p.V, row);
                     lse = ld_dep(p.lse + row);

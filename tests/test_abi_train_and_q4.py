@@ -69,3 +69,17 @@ def test_argument_errors_of_the_embedding(lib):
     assert lib.ee_embed_grad(p, 16, p, 3, 5, 16, 1.0, N, 0, 0, p, big, N) == 1
     assert lib.ee_embed_grad(p, 16, p, 3, 5, 16, 1.0, off, 0, 0, p, big, N) == 3
     assert lib.ee_embed_grad(p, 16, p, 3, 5, 16, 1.0, p, 0, 0, p, 64, N) == 4
+
+
+def test_rows_and_vocabularies_beyond_32_bits_of_tiles_are_refused(lib):
+    N, p, big, over = None, ctypes.c_void_p(4096), 1 << 40, (1 << 30) + 1
+    for f in (lib.ee_head_ce_workspace_bytes, lib.ee_head_ce_grad_workspace_bytes, lib.ee_exit_head_q4_workspace_bytes, lib.ee_embed_grad_workspace_bytes):
+        assert f(over, 8, 10) == 0 and f(1, 8, over) == 0 and f(1, 8, 2 ** 31 - 1) == 0 and f(1, 8, 1 << 30) > 0
+    assert lib.ee_head_q4_bytes(over, 32, 32) == 0 and lib.ee_head_q4_bytes(1 << 30, 32, 32) == (1 << 26) * (512 + 2 * 32)          # 64 columns, two groups
+    for M, V in [(over, 10), (4, over), (4, 2 ** 31 - 1)]:
+        assert lib.ee_head_ce(p, 8, p, p, 1e-5, p, M, 8, V, p, p, p, p, p, big, N) == 2
+        assert lib.ee_head_ce_grad(p, 8, p, p, 1e-5, p, M, 8, V, p, p, p, N, N, p, 8, p, p, p, 0, p, big, N) == 2
+        assert lib.ee_exit_head_q4(p, 32, p, p, 1e-5, p, big, 32, M, 32, V, N, 1.0, p, p, p, p, p, big, N) == 2
+        assert lib.ee_embed(p, V, 8, p, M, 1.0, p, 8, N) == 2
+        assert lib.ee_embed_grad(p, 8, p, M, V, 8, 1.0, p, 0, 0, p, big, N) == 2
+    assert lib.ee_head_q4_pack(p, over, 32, 32, p, big, N) == 2 and lib.ee_head_q4_unpack(p, big, over, 32, 32, p, N) == 2

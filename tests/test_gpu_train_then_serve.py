@@ -143,3 +143,21 @@ def test_entropies_of_nearly_certain_rows_keep_their_digits(ee, M):
     assert H.max() < 0.05 and H.min() < 1e-4                             # what the test is about
     assert (np.abs(_np(got["entropy"]) - H) <= bound).all()
     assert got["exit_mask"].all()
+
+
+def test_any_label_outside_the_vocabulary_marks_a_row(ee):
+    """The extreme ones too, in every piece of the vocabulary."""
+    M, d, V = 600, 8, 140000                                             # G is more than one piece holds
+    rng = np.random.default_rng(2)
+    head = dict(h=dev_bf16(gen.bf16_bits_from_f32(rng.normal(0, 1, (M, d)).astype(np.float32))), gamma=torch.ones(d, device="cuda"),
+                beta=torch.zeros(d, device="cuda"), W=dev_bf16(gen.bf16_bits_from_f32(rng.normal(0, 0.3, (V, d)).astype(np.float32))))
+    labels = rng.integers(0, V, M).astype(np.int32)
+    labels[::3] = -1
+    extreme = labels.copy()
+    extreme[::3] = rng.choice([-2 ** 31, -2 ** 31 + 1, 2 ** 31 - 1, V, -V, -1], len(labels[::3]))
+    got = []
+    for lab in (labels, extreme):
+        fwd = ee.ee_head_ce(head, dev(lab), 1e-5)
+        got.append({**fwd, **ee.ee_head_ce_grad(head, dev(lab), 1e-5, fwd)})
+    for k in got[0]:
+        assert torch.equal(got[0][k], got[1][k]), k
