@@ -30,7 +30,7 @@
 #include "common.cuh"
 #include "layer_norm.cuh"
 #include "kernels.h"
-#include "sm100_ptx.cuh"
+#include "sm100_operands.cuh"
 #include "gemm_roles.cuh"
 #include "tensor_map.h"
 

@@ -147,15 +147,24 @@ __global__ void __launch_bounds__(256) q4_unpack_kernel(const uint4* weights, co
 // (two rows, four columns 32 bytes apart) touch every bank once.
 __host__ __device__ inline int y_row_bytes(int d) { return (d + 63) / 64 * 128 + 16; }
 
-// Up to NT * 8 rows, one launch: the rows are normalised by every CTA into its shared memory (a warp per row) while the first
-// weights are on their way; a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all
-// rows of y; the CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges the CTAs'
-// states and decides.
+// Up to NT * 8 rows, one launch: the rows are normalised by every CTA into its shared memory while the first weights are on
+// their way; a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all rows of y; the
+// CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges the CTAs' states and decides.
+//
+// V = 50304, group 64, one call after the other: 16.3 us for 1 row of 1024 (27 MB of weights), 17.5 for 8, 21.6 for 16; 11.8 for 8
+// rows of 512; 28 for 1 and 31.5 for 8 of 2560 (2.2 TB/s).  Unpacking bounds it: a 64-column block takes a warp some 110
+// instructions, half of them in the pipe that issues every other cycle, 150 cycles of its scheduler; start, LayerNorm and merge are
+// 8 us beside that.  A ring of eight blocks per warp in shared memory, filled by asynchronous copies, was no faster (31.7 us
+// for 8 rows of 2560, 13.0 for 8 of 512): what is in flight is not what it waits for.
+// Up to 16 rows this kernel, above that the tensor-core one: 16 rows of 1024 take 21.6 us here and 25.5 there, 17 rows (two
+// passes here) 38 and 26.7; at d = 2560 42 and 46, then 77 and 48.5.
 template <int NT>
 __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_constant__ Q4Params p) {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int is_last;
+    __shared__ double2 sums[kWarps];
     const Q4Layout l = q4_layout(p.V, p.d, p.group);
+    const int group_shift = 31 - __clz(p.group);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int ld = y_row_bytes(p.d);
     RestState* states = reinterpret_cast<RestState*>(smem + NT * 8 * ld);        // [kWarps][max(NT * 8, 32)]: per warp, then scratch of the merge
@@ -168,21 +177,56 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
         for (int u = 0; u < kUnroll; ++u)
             if (b0 + u < l.blocks) {
                 w[u] = __ldg(p.weights + ((size_t)tile * l.blocks + b0 + u) * 32 + lane);
-                sc[u] = __ldg(p.scales + ((size_t)tile * l.groups + ((b0 + u) * 64 + c * 16) / p.group) * 8 + g);
+                sc[u] = __ldg(p.scales + ((size_t)tile * l.groups + (((b0 + u) * 64 + c * 16) >> group_shift)) * 8 + g);
             }
     };
     int tile = blockIdx.x + gridDim.x * warp;
     if (tile < l.tiles) load(tile, 0);                                   // weights are constants of the stream
     grid_dependency_wait();
-    for (int row = warp; row < NT * 8; row += kWarps) {
-        uint4* yrow = reinterpret_cast<uint4*>(smem + row * ld);
-        const int nvec = p.d >> 3;
-        if (row < p.M) {
-            const uint4* hrow = reinterpret_cast<const uint4*>(p.h + (size_t)row * p.ld_h);
-            const RowStats st = row_stats_strided([&](int k) { return ld_dep(hrow + k); }, nvec, p.ln_eps, lane);
-            for (int k = lane; k < nvec; k += 32) yrow[k] = layer_norm_vec8<true>(ld_dep(hrow + k), st, p.gamma, p.beta, k);
+    {
+        // the LayerNorm, above 1024 columns with every warp taking part, kWarps / M of them to a row (M <= 16): 8 rows of 2560 take
+        // 31.5 us instead of 35; up to 1024 a warp per row, without the barriers: 8 rows of 512 take 11.8 us instead of 13.4
+        const int nvec = p.d >> 3, width = l.blocks * 8, per_row = nvec > 128 ? kWarps / p.M : 1;
+        const int row = warp / per_row, first = (warp - row * per_row) * 32 + lane, step = per_row * 32;
+        const bool live = row < p.M;
+        const uint4* hrow = reinterpret_cast<const uint4*>(p.h + (size_t)(live ? row : 0) * p.ld_h);
+        const double d = (double)p.d, inv_d = 1.0 / d;
+        auto row_sum2 = [&](double& s, double& q) {                      // in a fixed order, the same bits in every warp of the row
+            warp_sum2_d(s, q);
+            if (per_row == 1) return;
+            if (lane == 0) sums[warp] = make_double2(s, q);
+            __syncthreads();
+            s = q = 0.0;
+            if (live)
+                for (int i = 0; i < per_row; ++i) {
+                    const double2 o = sums[row * per_row + i];
+                    s += o.x;
+                    q += o.y;
+                }
+        };
+        Moments m;
+        m.clear();
+        if (live)
+            for (int k = first, j = 0; k < nvec; k += step, ++j) m.add(ld_dep(hrow + k), j);
+        double s = m.sum(), q = m.sum_sq(), mu = 0.0, var = 0.0;
+        row_sum2(s, q);
+        const bool again = live && !row_variance_one_pass(s, q, d, inv_d, mu, var);
+        if (per_row == 1 ? again : __syncthreads_or(again)) {
+            double v0 = 0.0, v1 = 0.0;
+            if (again)
+                for (int k = first; k < nvec; k += step) vec8_sqdev_d(ld_dep(hrow + k), mu, v0, v1);
+            double v = v0 + v1, none = 0.0;
+            row_sum2(v, none);
+            if (again) var = v * inv_d;
         }
-        for (int k = (row < p.M ? nvec : 0) + lane; k < l.blocks * 8; k += 32) yrow[k] = make_uint4(0, 0, 0, 0);
+        if (live) {
+            uint4* yrow = reinterpret_cast<uint4*>(smem + row * ld);
+            const RowStats st = row_stats(mu, var, p.ln_eps);
+            for (int k = first; k < nvec; k += step) yrow[k] = layer_norm_vec8<true>(ld_dep(hrow + k), st, p.gamma, p.beta, k);
+            for (int k = nvec + first; k < width; k += step) yrow[k] = make_uint4(0, 0, 0, 0);
+        }
+        for (int r = p.M + warp; r < NT * 8; r += kWarps)
+            for (int k = lane; k < width; k += 32) reinterpret_cast<uint4*>(smem + r * ld)[k] = make_uint4(0, 0, 0, 0);
     }
     RestState* mine = states + warp * (NT * 8);
     for (int i = lane; i < NT * 8; i += 32) mine[i] = rest_empty();

@@ -174,3 +174,17 @@ def test_refusals(ee):
     assert e.value.code == 4
     empty = ee.ee_exit_head_q4(h[:0], gamma, beta, 1e-5, q4, 1.0)
     assert empty["argmax"].numel() == 0
+
+
+@pytest.mark.parametrize("M,d", [(1, 96), (2, 2560), (3, 1056), (9, 1024), (16, 2048), (20, 1536)])
+def test_rows_far_from_zero_need_their_squared_deviations(ee, M, d):
+    """Half of the rows are 100 plus 0 or 1/2: mean of squares minus square of the mean keeps too few bits there, in some warps only."""
+    rng = np.random.default_rng(d)
+    cfg = gen.make_config("c1", seed=7, planted=True, M=M, d=d, V=333, heads=1)
+    h = gen.f32_from_bf16_bits(cfg["h"])
+    h[::2] = 100 + 0.5 * rng.integers(0, 2, h[::2].shape)
+    bits = gen.bf16_bits_from_f32(h.astype(np.float32))
+    head = cfg["heads"][0]
+    hd = head_to_dev(head)
+    out = ee.ee_exit_head_q4(dev_bf16(bits), hd["gamma"], hd["beta"], 1e-5, ee.ee_head_q4_pack(hd["W"], 32), 1.0)
+    assert_head_matches(out, oracle_head(bits, dict(head, W=oracle.q4_values(head["W"], 32)), 1.0), label=f"{M} {d}")
