@@ -20,7 +20,8 @@
 // each other.  Issue slots bound it: two thirds of all cycles issue an instruction, half of those to unpack (four per two weights), the
 // others to hand blocks from one role to the next and to add the segments.  Timed in copies with a part left out, a block of
 // 64 columns took 0.73 us without the unpacking arithmetic, 0.82 without the sums, 0.83 with a quarter of the products, 0.56 without
-// all three, of 0.9.
+// all three, of 0.9.  Handing two blocks over at a time changed nothing (28.4 us), nor did handing over after the next block's arithmetic (30.9
+// where 30.1 was the rule).
 #include "q4_common.cuh"
 #include "kernels.h"
 #include "sm100_operands.cuh"
