@@ -666,7 +666,7 @@ __device__ __forceinline__ double cta_sum_d(double v, double* part) {
 // CTA that is.
 __global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const float2* parts, int n_parts, const float* z_label, const int* labels, int M,
                                                                  int V, float* ce, float* lse, float* loss, Control* ctrl) {
-    constexpr int kWarps = kMergeThreads / 32, kAhead = 4;
+    constexpr int kWarps = kMergeThreads / 32, kAhead = 9;
     __shared__ float2 part[kWarps][33];
     __shared__ double sums[kWarps];
     __shared__ int is_last;

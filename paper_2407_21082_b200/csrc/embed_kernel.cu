@@ -2,7 +2,8 @@
 //   dtable[v] = scale * sum over i with token_i = v of dout[i]
 // by sorted tokens, in fp32 and in a fixed order (no floating-point atomics: the same bits from run to run).
 //
-// The gradient is three steps.  (1) The tokens are sorted, stably, by one cluster of CTAs in its shared memory when they fit
+// For up to 512 tokens every position looks for its token in the list (embed_short_kernel).  For longer lists the gradient is
+// three steps.  (1) The tokens are sorted, stably, by one cluster of CTAs in its shared memory when they fit
 // (n <= 16384 and V < 2^18: 18 bits of token and 14 of position in one word), while the rest of the device clears the table, which
 // takes longer (V d bytes against n words); longer lists go through the library's radix sort.  (2) The sorted list is cut into
 // chunks of equal length, one CTA (per 128 vectors of the width) each: it adds up the rows of every token in it.  A token
@@ -13,7 +14,7 @@
 //
 // 16384 tokens, d = 1024, V = 50304, bf16: 37 to 40 us (floor 21: 34 MB of rows, 103 MB of table), of which 16 clear the table (6.4 TB/s)
 // beside the sort's 13, 12 add up and 9 join; 16385 tokens through the radix sort 59 us; 257 tokens x 520 into 32003 rows of
-// fp32 18 us, four launches in a row.  The lookup of 32 tokens takes 1.5 us on the device.
+// fp32 11.5 us.  The lookup of 32 tokens takes 1.5 us on the device.
 #include "common.cuh"
 #include "kernels.h"
 #include "sm100_ptx.cuh"
@@ -73,7 +74,10 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, unsigned int v) {
 
 // Clears `vecs` vectors: bulk copies out of zeros in shared memory, all of a CTA's issued by one thread.  The kernel that sorts the
 // tokens lets this one start after its own wait for the stream's earlier work, so that clearing (V d bytes) runs beside sorting
-// (n words) and needs no wait before it writes; it waits before it ends, so that its own end means that of both.
+// (n words) and needs no wait before it writes; it waits before it ends, so that its own end means that of both.  For short lists it
+// comes first itself, as an ordinary launch, and lets what adds up the rows start beside it.  (Its CTAs have to find the SMs evenly
+// free: started early, among the CTAs of a kernel that is still there, they crowd on some of them, and clearing 208 MB took 92 us
+// instead of 35.)
 constexpr unsigned int kClearBytes = 16384;
 __global__ void __launch_bounds__(128) embed_clear_kernel(uint4* clear, long long vecs) {
     __shared__ __align__(128) uint4 zeros[kClearBytes / 16];
@@ -350,6 +354,72 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const __grid_c
     }
 }
 
+// Lists of up to kShortMax tokens are not sorted: the CTA of position i (per 128 vectors of the width) finds out whether its token came
+// earlier in the list, and if not adds up the rows of all positions that have it, four groups of threads taking every fourth of
+// them and joining in order.  Two launches instead of four; where the table is cleared, all but the last stores run beside that.
+// 257 tokens x 520 into 32003 rows of fp32: 11.5 us instead of 18 (floor 10.3), added to what is there 3.3; 512 tokens x 1024 4.9 us and
+// 14.5 if they are all the same one, where sorting takes 13.4 and 14.4 for 513.  It lets nothing start early, for the clearing's sake.
+constexpr int kShortMax = 512;
+constexpr int kShortThreads = 512, kShortGroups = kShortThreads / 128;
+__global__ void __launch_bounds__(kShortThreads) embed_short_kernel(const __grid_constant__ EmbedGrad a, const int* tokens, int beside_clear) {
+    __shared__ float red[kShortGroups - 1][8][128];
+    __shared__ int list[kShortMax];
+    __shared__ int counts[kShortThreads / 32];
+    if (!beside_clear) grid_dependency_wait();                           // beside it: the clearing kernel has waited
+    const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
+    const int token = ld_dep(tokens + blockIdx.x);
+    const bool same = i < a.n && ld_dep(tokens + i) == token;
+    const unsigned ballot = __ballot_sync(0xffffffffu, same);
+    if (lane == 0) counts[warp] = __popc(ballot);
+    if (__syncthreads_or((same && i < (int)blockIdx.x) || (unsigned)token >= (unsigned)a.V)) {
+        if (beside_clear) grid_dependency_wait();                        // the kernel's end is that of the clearing too
+        return;
+    }
+    int at = __popc(ballot & ((1u << lane) - 1u)), count = 0;
+    for (int w = 0; w < kShortThreads / 32; ++w) {
+        at += w < warp ? counts[w] : 0;
+        count += counts[w];
+    }
+    if (same) list[at] = i;
+    __syncthreads();
+    const int v = i & 127, group = i >> 7, c = blockIdx.y * 128 + v;
+    const bool live = c < a.nvec;
+    float acc[8] = {};
+    if (live) {
+#pragma unroll 1
+        for (int k0 = group; k0 < count; k0 += kShortGroups * kSumAhead) {
+            uint4 x[kSumAhead];
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k)
+                if (k0 + k * kShortGroups < count)
+                    x[k] = ld_dep(reinterpret_cast<const uint4*>(a.dout + (size_t)list[k0 + k * kShortGroups] * a.ld_dout) + c);
+#pragma unroll
+            for (int k = 0; k < kSumAhead; ++k) {
+                if (k0 + k * kShortGroups >= count) break;
+                float f[8];
+                unpack8f(x[k], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += f[j];
+            }
+        }
+    }
+    if (count > 1) {                                                     // the same for the whole CTA
+        if (group > 0) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) red[group - 1][j][v] = acc[j];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int k = 0; k < kShortGroups - 1; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += red[k][j][v];
+        }
+    }
+    if (beside_clear) grid_dependency_wait();                            // the table is clear
+    if (group == 0 && live) store_row(a, token, c, acc);
+}
+
 // Sorted positions per chunk: at most 1024 chunks (a run over all of them is joined by four groups of 256), at least eight
 // positions (a thread's loads in flight).
 int chunk_of(int n) { const int c = (n + 1023) / 1024; return c < 8 ? 8 : c; }
@@ -399,6 +469,17 @@ ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* toke
     g.chunk = chunk_of(n); g.n_chunks = (n + g.chunk - 1) / g.chunk;
     g.scale = scale; g.dtable = dtable; g.wide = wide; g.add = accumulate;
     g.parts = reinterpret_cast<float*>(ws + s.parts);
+    g.sorted = nullptr;
+    const long long copies = (clear_vecs * 16 + kClearBytes - 1) / kClearBytes, most = 4LL * num_sms;
+    const dim3 clear_ctas((unsigned)(copies < most ? copies : most));
+    if (n <= kShortMax) {
+        if (clear_vecs) {
+            embed_clear_kernel<<<clear_ctas, 128, 0, stream>>>(static_cast<uint4*>(dtable), clear_vecs);
+            if (cudaGetLastError() != cudaSuccess) return EE_ERR_CUDA;
+        }
+        return launch_pdl(embed_short_kernel, dim3(n, (g.nvec + 127) / 128), kShortThreads, 0, stream, g, tokens, clear_vecs ? 1 : 0) == cudaSuccess
+                   ? EE_OK : EE_ERR_CUDA;
+    }
     if (sorts_in_one_cluster(n, V)) {
         int2* sorted = reinterpret_cast<int2*>(ws + s.a);
         cudaLaunchConfig_t cfg;
@@ -406,12 +487,7 @@ ee_status embed_grad_launch(const void* dout, long long ld_dout, const int* toke
         pair_launch_config(cfg, attr, dim3(kSortCtas), kSortThreads, 0, stream);
         attr[1].val.clusterDim.x = kSortCtas;
         if (cudaLaunchKernelEx(&cfg, embed_sort_kernel, tokens, n, V, passes, sorted) != cudaSuccess) return EE_ERR_CUDA;
-        if (clear_vecs) {
-            const long long copies = (clear_vecs * 16 + kClearBytes - 1) / kClearBytes, most = 4LL * num_sms;
-            if (launch_pdl(embed_clear_kernel, dim3((unsigned)(copies < most ? copies : most)), 128, 0, stream, static_cast<uint4*>(dtable), clear_vecs) !=
-                cudaSuccess)
-                return EE_ERR_CUDA;
-        }
+        if (clear_vecs && launch_pdl(embed_clear_kernel, clear_ctas, 128, 0, stream, static_cast<uint4*>(dtable), clear_vecs) != cudaSuccess) return EE_ERR_CUDA;
         g.sorted = sorted;
     } else {
         u64 *a = reinterpret_cast<u64*>(ws + s.a), *b = reinterpret_cast<u64*>(ws + s.b);

@@ -192,3 +192,39 @@ def test_refusals(ee):
     with pytest.raises(ee.EExitError) as e:
         ee.ee_embed_grad(dout, tokens, 5, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.code == 4
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 127, 511, 512, 513])
+@pytest.mark.parametrize("kind", ["one", "two", "none", "mixed"])
+def test_lists_about_the_length_that_is_not_sorted(ee, n, kind):
+    """Exact against the oracle's sum: values of whole numbers up to 8 in magnitude, so every fp32 sum of 513 is exact in any order."""
+    d, V = 1032, 700                                                     # 129 vectors: one more than a CTA takes
+    rng = np.random.default_rng(n)
+    dout = gen.bf16_bits_from_f32(rng.integers(-8, 9, (n, d)).astype(np.float32))
+    tokens = _tokens(rng, kind, n, V)
+    ref, _, count = oracle.embed_grad(dout, tokens, V, np.float32(1.0))
+    out = ee.ee_embed_grad(dev_bf16(dout), dev(tokens), V, 1.0, dtype=torch.float32, out=torch.full((V, d), float("nan"), device="cuda"))
+    assert np.array_equal(_np(out), ref)
+    old = torch.full((V, d), 3.0, device="cuda")
+    ee.ee_embed_grad(dev_bf16(dout), dev(tokens), V, 1.0, out=old, accumulate=True)
+    assert np.array_equal(_np(old), ref + 3.0)
+
+
+def test_a_short_list_behind_work_that_writes_it(ee):
+    """The rows and the tokens are read while the table is being cleared: what an earlier kernel of the stream wrote must be there."""
+    n, d, V = 300, 520, 40000
+    rng = np.random.default_rng(1)
+    outs, wants = [], []
+    src = [dev_bf16(_rand_bits(rng, n, d)) for _ in range(6)]
+    toks = [dev(_tokens(rng, "mixed", n, V)) for _ in range(6)]
+    for s, t in zip(src, toks):
+        torch.cuda.synchronize()
+        wants.append(ee.ee_embed_grad(s, t, V, 2.0))
+    torch.cuda.synchronize()
+    rows, tok = torch.empty_like(src[0]), torch.empty_like(toks[0])
+    for s, t in zip(src, toks):
+        rows.copy_(s)
+        tok.copy_(t)
+        outs.append(ee.ee_embed_grad(rows, tok, V, 2.0))
+    for a, b in zip(outs, wants):
+        assert torch.equal(a, b)
