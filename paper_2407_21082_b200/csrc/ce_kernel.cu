@@ -661,7 +661,7 @@ __device__ __forceinline__ double cta_sum_d(double v, double* part) {
     return r;
 }
 
-// 32 rows per CTA, lane = row, the 32 warps stride over the parts, four loads in flight (8 us at 4096 rows x 197 parts; with eight
+// 32 rows per CTA, lane = row, the 32 warps stride over the parts, nine loads in flight (8 us at 4096 rows x 197 parts; with eight
 // warps and one load 25 us); then the CTA that finishes last adds up the mean over the counted rows, in a fixed order whichever
 // CTA that is.
 __global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const float2* parts, int n_parts, const float* z_label, const int* labels, int M,
