@@ -8,13 +8,14 @@
  * there is no CPU fallback: a device that is not compute capability 10.x yields EE_ERR_ARCH.
  * Identical inputs give bit-identical outputs (all reductions run in a fixed order).
  *
- * Constants of the stream.  A head's parameters -- W, gamma, beta of every call, ee_head_kl's teacher
- * included -- are read while earlier work of the stream may still be running (the kernels request them
+ * Constants of the stream.  A head's parameters -- W, gamma, beta, ee_head_kl's teacher included -- are
+ * read while earlier work of the stream may still be running (the kernels request them
  * ahead of their dependency on that work, through the read-only path).  They must therefore be complete
  * in memory before the call is issued and must not be written by anything still in flight on `stream`
  * or on any other stream: after updating weights, synchronise (or wait on an event on the host) before
  * the next call.  Everything else -- hidden states, thresholds, masks, tokens -- may be produced by
- * earlier work of the same stream, by ordinary or by programmatic dependent launches.
+ * earlier work of the same stream, by ordinary or by programmatic dependent launches; and so may all
+ * that ee_head_ce and ee_head_ce_grad read, W, gamma and beta among it: a training step writes them.
  *
  * Environment switches, read by the library for comparisons and tests (none is needed in normal use):
  * EE_MULTI_KERNEL=stream|skinny|gemm|none forces the kernel of multi-head calls (read per call);
@@ -469,9 +470,8 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that.
  * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
- * initialised once with ee_workspace_init; both 0 if a size is invalid.  W is written by nobody while a call is in
- * flight (see "Constants of the stream" above: a step that updates W must have completed before the next call is
- * issued).  M = 0: ee_head_ce writes loss = {0, 0}; ee_head_ce_grad writes zeros (nothing when accumulating).
+ * initialised once with ee_workspace_init; both 0 if a size is invalid.  The step that updates W, gamma and beta may come
+ * right before and right after a call in the same stream or graph.  M = 0: ee_head_ce writes loss = {0, 0}; ee_head_ce_grad writes zeros (nothing when accumulating).
  */
 size_t    ee_head_ce_workspace_bytes(int M, int d, int V);
 ee_status ee_head_ce(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W, int M,

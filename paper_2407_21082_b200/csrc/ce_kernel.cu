@@ -305,10 +305,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             uint32_t phase = 0, armed = 0, armed_parity = 0;
             bool ok = true;
             int n_pre = 0, issued = 0;
-            if ((kMode == kStats || kMode == kGrad) && worker < total_tiles) {        // W is a constant of the stream: the first
-                int m_tile, n_tile, split, kb0, kb1;                                  // slots' share of it before the wait
+            if ((kMode == kStats || kMode == kGrad) && worker < total_tiles) {        // W was complete before this kernel could start
+                int m_tile, n_tile, split, kb0, kb1;                                  // (see ce_layer_norm_kernel): the first slots' share
                 locate(worker, m_tile, n_tile, split, kb0, kb1);
-                n_pre = min(S, (kb1 - kb0 + kbs - 1) / kbs);
+                n_pre = min(S, (kb1 - kb0 + kbs - 1) / kbs);                          // of it before the wait
                 for (int s = 0; s < n_pre; ++s) {
                     if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), arm_bytes);
                     load_operand<b_mn, kPair>(b_base + s * b_stage, &maps.b, s * kbs * BK, b_mn_off + n_tile * p.bn + (int)rank * b_rows, b_rows,
@@ -549,6 +549,12 @@ __device__ __forceinline__ void put_vec8(uint4* yrow, int c, uint4 v, int permut
 
 // LayerNorm of the rows into y (rounded to fp32 and then to bf16, see layer_norm.cuh), a warp per row.  In the backward pass (`stats` given) it also leaves each row's mean
 // and 1/sigma for the way back, and a row that takes no part in the gradient becomes zeros with 1/sigma = 0.
+//
+// Either form comes first in its call, and W, gamma and beta may have been written by whatever is in front of it in the stream, an
+// optimiser's step or the packing of a table.  So neither lets the next kernel start before that has completed: every other kernel
+// of the call finds the parameters complete, may request W ahead of its own wait, and reads gamma as a constant.  This one is an
+// ordinary launch (a step on 4096 rows of 1024 took 1517 us so, and 1523 launched early with its parameters read through the L2);
+// the other one, for small batches, is there early, waits, and then signals.
 struct CeLnArgs {
     const __nv_bfloat16* h;
     long long ld_h;
@@ -566,13 +572,12 @@ struct CeLnArgs {
 };
 
 __global__ void __launch_bounds__(256) ce_layer_norm_kernel(const __grid_constant__ CeLnArgs a) {
-    launch_dependents();
+    launch_dependents();                                                 // everything in front of this launch has completed
     const int row = blockIdx.x * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= a.M) return;
     const int nvec = a.d >> 3;
     uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.ld_y);
-    grid_dependency_wait();
     if (nvec + lane < a.ld_y >> 3) put_vec8(yrow, nvec + lane, make_uint4(0, 0, 0, 0), a.permuted);      // fewer than eight vectors
     if (a.stats && row_weight(a.labels, a.dce, a.V, row) == 0.f) {
         for (int c = lane; c < nvec; c += 32) yrow[c] = make_uint4(0, 0, 0, 0);
@@ -592,17 +597,17 @@ constexpr int kMergeThreads = 1024;
 constexpr int kLnCtaThreads = 256;
 __global__ void __launch_bounds__(kLnCtaThreads) ce_layer_norm_cta_kernel(const __grid_constant__ CeLnArgs a) {
     __shared__ double sums[2][kLnCtaThreads / 32];
-    launch_dependents();
     const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int nvec = a.d >> 3, warps = blockDim.x >> 5;
     float4 g[2], b[2];
     const bool first = (int)threadIdx.x < nvec;
-    if (first) {                                                         // the first vector's parameters before the wait
-        g[0] = ld_param4(a.gamma + 8 * threadIdx.x); g[1] = ld_param4(a.gamma + 8 * threadIdx.x + 4);
-        b[0] = ld_param4(a.beta + 8 * threadIdx.x); b[1] = ld_param4(a.beta + 8 * threadIdx.x + 4);
-    }
     uint4* yrow = reinterpret_cast<uint4*>(a.y + (size_t)row * a.ld_y);
     grid_dependency_wait();
+    launch_dependents();
+    if (first) {                                                         // the first vector's parameters beside the row's loads
+        g[0] = ld_param4_dep(a.gamma + 8 * threadIdx.x); g[1] = ld_param4_dep(a.gamma + 8 * threadIdx.x + 4);
+        b[0] = ld_param4_dep(a.beta + 8 * threadIdx.x); b[1] = ld_param4_dep(a.beta + 8 * threadIdx.x + 4);
+    }
     for (int c = nvec + threadIdx.x; c < a.ld_y >> 3; c += blockDim.x) put_vec8(yrow, c, make_uint4(0, 0, 0, 0), a.permuted);
     if (a.stats && row_weight(a.labels, a.dce, a.V, row) == 0.f) {
         for (int c = threadIdx.x; c < nvec; c += blockDim.x) yrow[c] = make_uint4(0, 0, 0, 0);
@@ -646,7 +651,7 @@ __global__ void __launch_bounds__(kLnCtaThreads) ce_layer_norm_cta_kernel(const 
 #pragma unroll
     for (int k = 1; k < 4; ++k) {
         const int c = threadIdx.x + k * blockDim.x;
-        if (c < nvec) put_vec8(yrow, c, layer_norm_vec8<true>(x[k], st, a.gamma, a.beta, c), a.permuted);
+        if (c < nvec) put_vec8(yrow, c, layer_norm_vec8<true, true>(x[k], st, a.gamma, a.beta, c), a.permuted);
     }
     if (a.stats && threadIdx.x == 0) a.stats[row] = make_float2(st.mu_f, st.rstd_f);
 }
@@ -1107,7 +1112,8 @@ static ee_status ln_launch(const CeLnArgs& l, cudaStream_t stream) {
         const int warps = (l.d / 8 + 31) / 32;
         return launch_pdl(ce_layer_norm_cta_kernel, dim3(l.M), 32 * (warps < 8 ? warps : 8), 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
     }
-    return launch_pdl(ce_layer_norm_kernel, dim3((l.M + 7) / 8), 256, 0, stream, l) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    ce_layer_norm_kernel<<<(l.M + 7) / 8, 256, 0, stream>>>(l);
+    return cudaGetLastError() == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 ee_status layer_norm_permuted_launch(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, void* y, int ld_y,

@@ -169,7 +169,8 @@ __host__ __device__ inline size_t align_up(size_t x, size_t a) { return (x + a -
 // lifetime: the non-coherent path (ld.global.nc, which the compiler also picks for const __restrict__
 // parameters) may return a line an earlier co-resident kernel left in the SM's L1.  These loads go to L2, the
 // point of coherence; the parameters they read through carry no __restrict__.  Weights and LayerNorm
-// parameters, which no kernel of the stream writes, keep the read-only path.
+// parameters, which no kernel of the stream writes, keep the read-only path; where they may be written (training), a call's
+// first kernel lets no other start before that is done, and reads them as data of the stream if it is itself there early.
 template <class T>
 __device__ __forceinline__ T ld_dep(const T* p) { return __ldcg(p); }
 
@@ -209,8 +210,8 @@ __device__ __forceinline__ float warp_sum(float v) {
 // passed launch_dependents(); a kernel calls grid_dependency_wait() before it touches anything an earlier
 // kernel of the stream writes or still reads (it returns when those kernels have completed and their stores
 // are visible).  Every kernel of the head, compaction, cascade, round and loss calls is launched through
-// launch_pdl and waits before it completes, so completions stay in stream order; the calibration kernels and
-// the diagnostic self-tests are ordinary launches, which wait for everything before them anyway.
+// launch_pdl and waits before it completes, so completions stay in stream order; the calibration kernels, some first
+// kernels of the training calls and the diagnostic self-tests are ordinary launches, which wait for everything before them anyway.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

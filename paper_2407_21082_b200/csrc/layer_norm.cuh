@@ -201,13 +201,18 @@ __device__ __forceinline__ uint4 layer_norm_vec8(uint4 v, const RowStats& st, fl
     return o;
 }
 
-// Same, reading gamma and beta of vector c (columns 8c .. 8c+7) from global memory (weights: read-only path).
-template <bool kTwice = false>
+// gamma and beta where they may come from earlier work of the stream (behind the wait for it).
+__device__ __forceinline__ float4 ld_param4_dep(const float* p) { return ld_dep(reinterpret_cast<const float4*>(p)); }
+
+// Same, reading gamma and beta of vector c (columns 8c .. 8c+7) from global memory: through the read-only path as constants, or
+// (kDep) as data that earlier work of the stream may be writing while this kernel is already there.
+template <bool kTwice = false, bool kDep = false>
 __device__ __forceinline__ uint4 layer_norm_vec8(uint4 v, const RowStats& st, const float* gamma, const float* beta, int c) {
-    const float4 g0 = ld_param4(gamma + 8 * c);
-    const float4 g1 = ld_param4(gamma + 8 * c + 4);
-    const float4 b0 = ld_param4(beta + 8 * c);
-    const float4 b1 = ld_param4(beta + 8 * c + 4);
+    const auto ld = [](const float* p) { return kDep ? ld_param4_dep(p) : ld_param4(p); };
+    const float4 g0 = ld(gamma + 8 * c);
+    const float4 g1 = ld(gamma + 8 * c + 4);
+    const float4 b0 = ld(beta + 8 * c);
+    const float4 b1 = ld(beta + 8 * c + 4);
     return layer_norm_vec8<kTwice>(v, st, g0, g1, b0, b1);
 }
 
