@@ -15,7 +15,8 @@
  * or on any other stream: after updating weights, synchronise (or wait on an event on the host) before
  * the next call.  Everything else -- hidden states, thresholds, masks, tokens -- may be produced by
  * earlier work of the same stream, by ordinary or by programmatic dependent launches; and so may all
- * that ee_head_ce and ee_head_ce_grad read, W, gamma and beta among it: a training step writes them.
+ * that ee_head_ce, ee_head_ce_grad and ee_exit_head_q4 read, W, gamma, beta and the packed head among
+ * it: a training step writes them, ee_head_q4_pack packs what it wrote.
  *
  * Environment switches, read by the library for comparisons and tests (none is needed in normal use):
  * EE_MULTI_KERNEL=stream|skinny|gemm|none forces the kernel of multi-head calls (read per call);
@@ -493,7 +494,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
  * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous.  W and W4 are 32-byte aligned.
  *
  * ee_exit_head_q4 is ee_exit_head with W4 for W and the y of ee_head_ce: same definition otherwise, same outputs, strides,
- * alignment and rules (the packed head is a constant of the stream).  M up to 2^30; up to 16 rows (8 where d is large), and above
+ * alignment and rules, but the packed head, gamma and beta are data of the stream (they may be written right before the call).  M up to 2^30; up to 16 rows (8 where d is large), and above
  * that every 64 rows, are one pass over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
  * with ee_workspace_init.  M = 0 is a no-op.
  */

@@ -151,12 +151,13 @@ __host__ __device__ inline int y_row_bytes(int d) { return (d + 63) / 64 * 128 +
 // their way; a warp takes a 16-row tile of W at a time, streams it through registers and multiplies it with all rows of y; the
 // CTA's tiles are folded into one softmax state per row, and the CTA that finishes last merges the CTAs' states and decides.
 //
-// V = 50304, group 64, one call after the other: 16.3 us for 1 row of 1024 (27 MB of weights), 17.5 for 8, 21.6 for 16; 11.8 for 8
-// rows of 512; 28 for 1 and 31.5 for 8 of 2560 (2.2 TB/s).  Unpacking bounds it: a 64-column block takes a warp some 110
+// V = 50304, group 64, one call after the other: 16.8 us for 1 row of 1024 (27 MB of weights), 17.9 for 8, 21.9 for 16; 12.0 for 8
+// rows of 512; 28.8 for 1 and 31.6 for 8 of 2560 (2.2 TB/s); the first weights ahead of the wait for the stream's earlier work,
+// which may be what writes them, would take 0.1 to 0.7 us off.  Unpacking bounds it: a 64-column block takes a warp some 110
 // instructions, half of them in the pipe that issues every other cycle, 150 cycles of its scheduler; start, LayerNorm and merge are
 // 8 us beside that.  A ring of eight blocks per warp in shared memory, filled by asynchronous copies, was no faster (31.7 us
 // for 8 rows of 2560, 13.0 for 8 of 512): what is in flight is not what it waits for.
-// Up to 16 rows this kernel, above that the tensor-core one: 16 rows of 1024 take 21.6 us here and 25.5 there, 17 rows (two
+// Up to 16 rows this kernel, above that the tensor-core one: 16 rows of 1024 take 21.9 us here and 25.5 there, 17 rows (two
 // passes here) 38 and 26.7; at d = 2560 42 and 46, then 77 and 48.5.
 template <int NT>
 __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_constant__ Q4Params p) {
@@ -176,13 +177,13 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (b0 + u < l.blocks) {
-                w[u] = __ldg(p.weights + ((size_t)tile * l.blocks + b0 + u) * 32 + lane);
-                sc[u] = __ldg(p.scales + ((size_t)tile * l.groups + (((b0 + u) * 64 + c * 16) >> group_shift)) * 8 + g);
+                w[u] = ld_dep(p.weights + ((size_t)tile * l.blocks + b0 + u) * 32 + lane);
+                sc[u] = ld_dep(p.scales + ((size_t)tile * l.groups + (((b0 + u) * 64 + c * 16) >> group_shift)) * 8 + g);
             }
     };
     int tile = blockIdx.x + gridDim.x * warp;
-    if (tile < l.tiles) load(tile, 0);                                   // weights are constants of the stream
-    grid_dependency_wait();
+    grid_dependency_wait();                                              // the weights may just have been packed, gamma and beta learned
+    if (tile < l.tiles) load(tile, 0);                                   // in flight beside the LayerNorm
     {
         // the LayerNorm, above 1024 columns with every warp taking part, kWarps / M of them to a row (M <= 16): 8 rows of 2560 take
         // 31.5 us instead of 35; up to 1024 a warp per row, without the barriers: 8 rows of 512 take 11.8 us instead of 13.4
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_const
         if (live) {
             uint4* yrow = reinterpret_cast<uint4*>(smem + row * ld);
             const RowStats st = row_stats(mu, var, p.ln_eps);
-            for (int k = first; k < nvec; k += step) yrow[k] = layer_norm_vec8<true>(ld_dep(hrow + k), st, p.gamma, p.beta, k);
+            for (int k = first; k < nvec; k += step) yrow[k] = layer_norm_vec8<true, true>(ld_dep(hrow + k), st, p.gamma, p.beta, k);
             for (int k = nvec + first; k < width; k += step) yrow[k] = make_uint4(0, 0, 0, 0);
         }
         for (int r = p.M + warp; r < NT * 8; r += kWarps)

@@ -1,4 +1,4 @@
-"""Weights, gamma and beta that earlier work of the same stream has just written, or is still writing.
+"""Weights, gamma, beta and packed heads that earlier work of the same stream has just written, or is still writing.
 
 The writer is one of the library's own calls, which lets what follows it in the stream start before it has finished: ee_compact
 copies a flat buffer of parameters, row by row and bit for bit, the parameters in its last rows.  The calls behind it have to give the
@@ -41,17 +41,19 @@ class Flat:
         self.ee.ee_compact(self.mask, self.new, out=self.out)
 
     def check(self, call, want, label):
-        """`call` behind the update, captured and eager, from the old values every time."""
+        """`call` behind the update, captured and eager, from the old values every time, which a call in front of the update has read."""
         side = torch.cuda.Stream()
         with torch.cuda.stream(side):
             got = call()                                                 # nothing is set up for the first time in the capture
             torch.cuda.synchronize()
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph, stream=side):
+                call(got)
                 self.update()
                 call(got)
 
             def eager():
+                call(got)
                 self.update()
                 call(got)
 
@@ -147,3 +149,54 @@ def test_steps_and_updates_in_one_graph(ee):
     for k in runs[0]:
         same = torch.equal(runs[0][k], runs[1][k])
         assert same, k
+
+
+@pytest.mark.parametrize("d,group", [(512, 32), (2048, 128)])
+@pytest.mark.parametrize("M", [1, 5, 16, 17, 64, 130])
+def test_4_bit_head_behind_an_update(ee, M, d, group):
+    """Streaming kernel with a warp and with all warps to a row, tensor-core kernel with one pass and with several launches."""
+    V = 20000
+    flat = Flat(ee, dict(packed=ee.ee_head_q4_bytes(V, d, group), gamma=d * 4, beta=d * 4))
+    _norms(flat, d)
+
+    def weights(which):
+        return ee.Q4Weights(flat.view(which, "packed", torch.uint8, (-1,)), V, d, group)
+
+    for which, seed in (("old", 5), ("new", 6)):
+        ee.ee_head_q4_pack(_normal(seed, V, d, scale=0.05).to(torch.bfloat16), group, out=weights(which))
+    h = _normal(7, M, d).to(torch.bfloat16)
+
+    def head(which, out=None):
+        return ee.ee_exit_head_q4(h, flat.view(which, "gamma", torch.float32, (d,)), flat.view(which, "beta", torch.float32, (d,)), 1e-5,
+                                  weights(which), 7.0, out=out, workspace=ws)
+
+    ws = ee.new_exit_head_q4_workspace(M, weights("new"))
+    want = {k: v.clone() for k, v in head("new").items()}
+    flat.check(lambda out=None: head("live", out), want, (M, d))
+    assert ee.ee_query_async_error(ws) == 0
+
+
+@pytest.mark.parametrize("M", [1, 33])
+def test_packing_and_answering_in_one_graph(ee, M):
+    d, V = 512, 9001
+    W = _normal(1, V, d, scale=0.05).to(torch.bfloat16)
+    h = _normal(2, M, d).to(torch.bfloat16)
+    gamma, beta = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
+    q4 = ee.ee_head_q4_pack(W, 64)
+    ws = ee.new_exit_head_q4_workspace(M, q4)
+    out = ee.ee_exit_head_q4(h, gamma, beta, 1e-5, q4, 7.0, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        W.mul_(0.5).add_(0.01)
+        ee.ee_head_q4_pack(W, 64, out=q4)
+        ee.ee_exit_head_q4(h, gamma, beta, 1e-5, q4, 7.0, out=out, workspace=ws)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        fresh = ee.ee_head_q4_pack(W, 64)
+        torch.cuda.synchronize()
+        want = ee.ee_exit_head_q4(h, gamma, beta, 1e-5, fresh, 7.0)
+        for k in want:
+            same = torch.equal(out[k], want[k])
+            assert same, k
