@@ -456,7 +456,8 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  * in pieces of the vocabulary.  With z = y W^T and y = bf16(fp32(LayerNorm(h))) -- rounded as the cast of a LayerNorm that
  * returns fp32 is, which differs from ee_exit_head's y in about one element of 10^5, by one step --:
  *   lse   fp32 [M]: ln sum_v exp(z[i, v])
- *   ce    fp32 [M]: lse[i] - z[i, labels[i]]; 0 for a row that is not counted
+ *   ce    fp32 [M]: lse[i] - z[i, labels[i]]; 0 for a row that is not counted.  Not taken from the rounded lse: the loss of a
+ *         nearly certain row keeps its digits (as far as the logits' own: 1e-5 or so of it) however small it is
  *   loss  fp32 [2]: the mean of ce over the counted rows (0 if there is none), and their number
  * labels int32 [M]; a row whose label is outside [0, V) is not counted: it adds nothing to the loss or to any
  * gradient, whatever its hidden state holds (its lse is computed all the same).
@@ -468,7 +469,8 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  *   dW     bf16 [V, d] contiguous, or NULL;   dgamma, dbeta  bf16 [d], both or neither NULL
  *   accumulate != 0: dW, dgamma and dbeta are added to what the buffers hold (dh is always overwritten)
  * The rounding of y to bf16 is passed through by the gradient.  All gradients are bf16: the products behind dy and dW
- * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that.
+ * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that; and lse is fp32, so that at the label of a nearly
+ * certain row that difference is good to 2^-24 |lse| of the row's weight, not to a part of itself.
  * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
  * initialised once with ee_workspace_init; both 0 if a size is invalid.  The step that updates W, gamma and beta may come

@@ -7,7 +7,7 @@
 //
 // Four matrix products of 2 M V d operations each (the logits twice: they are recomputed in the backward pass), all by
 // one persistent TMA + tcgen05 kernel whose mode decides which operand runs which way and what its epilogue does:
-//   kStats  A = y, B = W (both K-major): per row and tile the maximum and the sum of exponentials, and
+//   kStats  A = y, B = W (both K-major): per row and tile the maximum and the sum of the other exponentials, and
 //           the logit at the label; nothing else leaves the chip
 //   kGrad   the same product for a piece of the vocabulary; the epilogue turns it into G, rounded to bf16
 //   kDy     A = G, B = W with the contraction over the vocabulary: W is read as it lies, as an MN-major operand; fp32
@@ -58,6 +58,13 @@ template <int kMode> struct Layout {
     static constexpr bool b_mn = kMode == kDy || kMode == kDw;
 };
 
+// A part of a row's softmax: m = its largest logit, r = sum of e^(z - m) over the others (m itself left out once); r = -1 for no
+// logits.  Beside the 1 of its largest term the sum of a nearly certain row, and with it a loss of 1e-7, would be rounded to 2^-24.
+struct Part {
+    float m, r;
+};
+__device__ __forceinline__ Part no_part() { return Part{-CUDART_INF_F, -1.f}; }
+
 struct CeMaps {
     CUtensorMap a, b;
 };
@@ -78,7 +85,7 @@ struct CeParams {
     int kbs;               // k-blocks per ring slot: 2 if the operands' widths allow one request for both, else 1
     int a_3d, b_3d;        // an MN-major operand's 64-wide blocks come with one request
     int add;               // kDy: add into the slab; kDw: add to what dW holds
-    float2* parts;         // kStats: [n_tiles][M] maximum and sum
+    Part* parts;           // kStats: [n_tiles][M]
     float* z_label;        // kStats: [M]
     const int* labels;
     const float* lse;      // kGrad
@@ -140,35 +147,60 @@ __device__ __forceinline__ float2 exp_pair(float z0, float z1, unsigned long lon
     return make_float2(ex2(v.x), ex2(v.y));
 }
 
-// Maximum and sum of exponentials of 64 logits (the first nvalid real).  Whole tiles take 1.5 issue slots an element besides
-// the exponential, so that for short rows, whose products do not hide it, the epilogue comes near the exponentials' own rate.
-template <bool kFull>
-__device__ __forceinline__ void fold_stats(const float (&z)[2][32], int nvalid, float& m, float& s) {
-    float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-    if (kFull) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) cm[j & 3] = ptx::max3(cm[j & 3], z[0][j], z[1][j]);
-        m = ptx::max3(fmaxf(cm[0], cm[1]), cm[2], cm[3]);
-        const unsigned long long minus_m = ptx::pack_f32x2(-m, -m);
-        unsigned long long cs[2] = {ptx::pack_f32x2(0.f, 0.f), ptx::pack_f32x2(0.f, 0.f)};
-#pragma unroll
-        for (int j = 0; j < 64; j += 2) {
-            const float2 e = exp_pair(z[j >> 5][j & 31], z[j >> 5][(j & 31) + 1], minus_m);
-            cs[(j >> 1) & 1] = ptx::add_f32x2(cs[(j >> 1) & 1], ptx::pack_f32x2(e.x, e.y));
-        }
-        const float2 sum = ptx::unpack_f32x2(ptx::add_f32x2(cs[0], cs[1]));
-        s = sum.x + sum.y;
-        return;
+// What a part adds to the sum of a row whose largest logit is m: without the 1 where the two are the same (`tops` counts those).
+__device__ __forceinline__ float part_rest(const Part& o, float m, int& tops) {
+    if (o.r == -1.f) return 0.f;                                         // NaN is not: it goes through
+    if (o.m == m) {
+        ++tops;
+        return o.r;
     }
-    float cs[4] = {0.f, 0.f, 0.f, 0.f};
+    return (1.f + o.r) * ex2((o.m - m) * kLog2e);
+}
+template <int N>
+__device__ __forceinline__ Part join(const Part (&v)[N]) {
+    float m = v[0].m, r = 0.f;
 #pragma unroll
-    for (int j = 0; j < 64; ++j)
-        if (j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[j >> 5][j & 31]);
-    m = fmaxf(fmaxf(cm[0], cm[1]), fmaxf(cm[2], cm[3]));
+    for (int k = 1; k < N; ++k) m = fmaxf(m, v[k].m);
+    int tops = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j)
-        if (j < nvalid) cs[j & 3] += ex2((z[j >> 5][j & 31] - m) * kLog2e);
-    s = (cs[0] + cs[1]) + (cs[2] + cs[3]);
+    for (int k = 0; k < N; ++k) r += part_rest(v[k], m, tops);
+    return Part{m, r + (float)(tops - 1)};                               // no logits at all: -1
+}
+
+// The part of 64 logits (the first nvalid real).  Whole tiles take some four issue slots an element besides the exponential, two to
+// leave the largest one out, so that for short rows, whose products do not hide it, the epilogue still comes near the exponentials'
+// own rate (512 rows of 512: 37.5 us with the largest in the sum, 38.5 so; summing again without it where it outweighs the others
+// 39, but 55 on logits so unequal that most warps have such a row).
+template <bool kFull>
+__device__ __forceinline__ Part fold_stats(const float (&z)[2][32], int nvalid) {
+    float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        if (kFull) {
+            cm[j & 3] = ptx::max3(cm[j & 3], z[0][j], z[1][j]);
+        } else {
+            if (j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[0][j]);
+            if (32 + j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], z[1][j]);
+        }
+    }
+    const float m = ptx::max3(fmaxf(cm[0], cm[1]), cm[2], cm[3]);
+    const unsigned long long minus_m = ptx::pack_f32x2(-m, -m);
+    unsigned long long rest[2] = {ptx::pack_f32x2(0.f, 0.f), ptx::pack_f32x2(0.f, 0.f)}, tops[2] = {rest[0], rest[0]};
+#pragma unroll
+    for (int j = 0; j < 64; j += 2) {
+        const float z0 = z[j >> 5][j & 31], z1 = z[j >> 5][(j & 31) + 1];
+        float2 e = exp_pair(z0, z1, minus_m);
+        float t0 = ptx::one_if_equal(z0, m), t1 = ptx::one_if_equal(z1, m);              // e is 1 there
+        if (!kFull) {
+            if (j >= nvalid) e.x = t0 = 0.f;
+            if (j + 1 >= nvalid) e.y = t1 = 0.f;
+        }
+        const int c = (j >> 1) & 1;
+        rest[c] = ptx::add_f32x2(rest[c], ptx::add_f32x2(ptx::pack_f32x2(e.x, e.y), ptx::pack_f32x2(-t0, -t1)));
+        tops[c] = ptx::add_f32x2(tops[c], ptx::pack_f32x2(t0, t1));
+    }
+    const float2 r = ptx::unpack_f32x2(ptx::add_f32x2(rest[0], rest[1])), t = ptx::unpack_f32x2(ptx::add_f32x2(tops[0], tops[1]));
+    return Part{m, (r.x + r.y) + (t.x + t.y - 1.f)};
 }
 
 // 32 consecutive values of a row (the first n of them, a multiple of eight) to memory: as bf16 in whole sectors of 32 bytes where
@@ -418,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         int local = 0;
         grid_dependency_wait();
         const float scale = kMode == kDw ? grad_scale(p.dce, p.dloss, p.loss) : 1.f;
-        float2* xchg = reinterpret_cast<float2*>(bar_mem + 512);
+        Part* xchg = reinterpret_cast<Part*>(bar_mem + 512);
         auto epilogue_barrier = [] { asm volatile("bar.sync 1, 512;" ::: "memory"); };
         bool given_up = false;
         for (int tile = worker; tile < total_tiles; tile += n_workers) {
@@ -462,11 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                 ptx::mbar_arrive(tempty_bar(buf));
             }
             if (kMode == kStats) {
-                float m = -CUDART_INF_F, s = 0.f;                        // an empty part
+                Part part = no_part();
                 if (work) {
                     const int nvalid = col1 - col0;
-                    if (nvalid >= 64) fold_stats<true>(z, 64, m, s);
-                    else fold_stats<false>(z, nvalid, m, s);
+                    part = nvalid >= 64 ? fold_stats<true>(z, 64) : fold_stats<false>(z, nvalid);
                     if (live && (unsigned)(label - col0) < (unsigned)min(nvalid, 64)) {
                         float zl = 0.f;
 #pragma unroll
@@ -475,15 +506,12 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                     }
                 }
                 // the tile's four groups of columns meet in shared memory; two buffers, so that one barrier a tile is enough
-                float2* slot = xchg + (local & 1) * 512 + quarter * 32 + lane;
-                slot[group * 128] = make_float2(m, s);
+                Part* slot = xchg + (local & 1) * 512 + quarter * 32 + lane;
+                slot[group * 128] = part;
                 epilogue_barrier();
                 if (group == 0 && live) {
-                    const float2 o1 = slot[128], o2 = slot[256], o3 = slot[384];
-                    const float mm = fmaxf(fmaxf(m, o1.x), fmaxf(o2.x, o3.x));
-                    auto part = [&](float om, float os) { return os == 0.f ? 0.f : os * ex2((om - mm) * kLog2e); };
-                    const float ss = (part(m, s) + part(o1.x, o1.y)) + (part(o2.x, o2.y) + part(o3.x, o3.y));
-                    p.parts[(size_t)n_tile * p.M + row] = make_float2(mm, ss);
+                    const Part all[4] = {part, slot[128], slot[256], slot[384]};
+                    p.parts[(size_t)n_tile * p.M + row] = join(all);
                 }
                 continue;
             }
@@ -669,47 +697,47 @@ __device__ __forceinline__ double cta_sum_d(double v, double* part) {
 // 32 rows per CTA, lane = row, the 32 warps stride over the parts, nine loads in flight (8 us at 4096 rows x 197 parts; with eight
 // warps and one load 25 us); then the CTA that finishes last adds up the mean over the counted rows, in a fixed order whichever
 // CTA that is.
-__global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const float2* parts, int n_parts, const float* z_label, const int* labels, int M,
+__global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const Part* parts, int n_parts, const float* z_label, const int* labels, int M,
                                                                  int V, float* ce, float* lse, float* loss, Control* ctrl) {
     constexpr int kWarps = kMergeThreads / 32, kAhead = 9;
-    __shared__ float2 part[kWarps][33];
+    __shared__ Part part[kWarps][33];
     __shared__ double sums[kWarps];
     __shared__ int is_last;
     launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x * 32 + lane;
     grid_dependency_wait();
-    float m = -CUDART_INF_F, s = 0.f;
-    auto fold = [&](float om, float os) {
-        const float nm = fmaxf(m, om);
-        s = (s == 0.f ? 0.f : s * ex2((m - nm) * kLog2e)) + (os == 0.f ? 0.f : os * ex2((om - nm) * kLog2e));
-        m = nm;
-    };
+    Part o[1 + kAhead];                                                  // what is joined so far, and what comes next
+    o[0] = no_part();
     if (row < M)
         for (int n0 = warp; n0 < n_parts; n0 += kWarps * kAhead) {
-            float2 o[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const int n = n0 + i * kWarps;
-                o[i] = n < n_parts ? __ldcg(parts + (size_t)n * M + row) : make_float2(-CUDART_INF_F, 0.f);
+                o[1 + i] = no_part();
+                if (n < n_parts) {
+                    const float2 x = ld_dep(reinterpret_cast<const float2*>(parts) + (size_t)n * M + row);
+                    o[1 + i] = Part{x.x, x.y};
+                }
             }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) fold(o[i].x, o[i].y);
+            o[0] = join(o);
         }
-    part[warp][lane] = make_float2(m, s);
+    part[warp][lane] = o[0];
     __syncthreads();
     {   // one row per warp: its 32 parts, one per lane, by shuffles
-        const float2 o = part[lane][warp];
+        const Part mine = part[lane][warp];
         const int r = blockIdx.x * 32 + warp;
-        float mm = o.x;
+        float mm = mine.m;
 #pragma unroll
         for (int k = 16; k > 0; k >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, k));
-        const float ss = warp_sum(o.y == 0.f ? 0.f : o.y * ex2((o.x - mm) * kLog2e));
+        int tops = 0;
+        const float sum = warp_sum(part_rest(mine, mm, tops));
+        const float rest = sum + (float)(__popc(__ballot_sync(0xffffffffu, tops > 0)) - 1);
         if (lane == 0 && r < M) {
-            const float l = mm + logf(ss);
-            lse[r] = l;
+            const float l = log1pf(rest);
+            lse[r] = mm + l;
             const bool counted = (unsigned)ld_dep(labels + r) < (unsigned)V;
-            ce[r] = counted ? l - ld_dep(z_label + r) : 0.f;
+            ce[r] = counted ? (mm - ld_dep(z_label + r)) + l : 0.f;      // not from lse, whose rounding is 1e-6
         }
     }
     __syncthreads();
@@ -1148,12 +1176,12 @@ ee_status ce_launch(const CeArgs& a) {
     p.k_blocks = tiles(a.d, BK);
     p.n_cols = a.V;
     p.m_rows = a.M;
-    p.parts = reinterpret_cast<float2*>(ws + s.parts);
+    p.parts = reinterpret_cast<Part*>(ws + s.parts);
     p.z_label = reinterpret_cast<float*>(ws + s.z_label);
     const ee_status st = launch_product<kStats>(maps, p, pair, a);
     if (st != EE_OK) return st;
     const int n_parts = p.n_tiles;
-    if (launch_pdl(ce_merge_kernel, (a.M + 31) / 32, kMergeThreads, 0, a.stream, (const float2*)p.parts, n_parts, (const float*)p.z_label, a.labels,
+    if (launch_pdl(ce_merge_kernel, (a.M + 31) / 32, kMergeThreads, 0, a.stream, (const Part*)p.parts, n_parts, (const float*)p.z_label, a.labels,
                    a.M, a.V, a.ce, a.lse_out, a.loss_out, p.ctrl) != cudaSuccess)
         return EE_ERR_CUDA;
     return EE_OK;

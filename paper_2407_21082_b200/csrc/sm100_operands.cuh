@@ -71,6 +71,12 @@ __device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, un
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// 1 where a == b, else 0 (NaN too).
+__device__ __forceinline__ float one_if_equal(float a, float b) {
+    float d;
+    asm("set.eq.f32.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 // The largest of three numbers; a NaN among them is passed over.
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
