@@ -49,6 +49,8 @@ constexpr int kMaxStages = 12;
 constexpr int kAccStride = 256;
 constexpr int kTmemCols = 512;
 constexpr int kMinTile = 64;                    // narrowest tile of the logits
+constexpr int kNarrowUnits = 4;                 // row tiles (of pairs: 256 rows) up to which it may be narrower than BN
+constexpr int kNarrowRows = kNarrowUnits * 2 * BM;
 constexpr int kMaxSplits = 32;
 constexpr size_t kGradPieceBytes = (size_t)128 << 20;      // or a quarter of all of G, whichever is more
 
@@ -1009,7 +1011,9 @@ CeSpace ce_space(int M, int d, int V, bool grad) {
     auto take = [&](size_t n) { const size_t o = at; at = align_up(at + n, 256); return o; };
     s.y = take((size_t)M * tiles(d, 64) * 128);
     s.stats = take((size_t)M * 8);
-    s.parts = take((size_t)tiles(V, kMinTile) * M * 8);
+    const int narrow = M < kNarrowRows ? M : kNarrowRows;                // rows that logit_tile may give tiles narrower than BN
+    const size_t wide_parts = (size_t)tiles(V, BN) * M, narrow_parts = (size_t)tiles(V, kMinTile) * narrow;
+    s.parts = take((wide_parts > narrow_parts ? wide_parts : narrow_parts) * sizeof(Part));
     s.z_label = take((size_t)M * 4);
     s.g = s.dy = s.cols = at;
     if (grad) {
@@ -1039,10 +1043,11 @@ int blocks_per_slot(int kMode, bool pair, int bn, int a_rows) {
     return on && ring_stages(kMode, pair, bn, a_rows, 2) >= 3 ? 2 : 1;
 }
 
-// Width of the logits' tiles: 256 for many rows, else the multiple of 16 from kMinTile on that makes rounds x (width + 16) smallest
+// Width of the logits' tiles: 256 for more than four row tiles, else the multiple of 16 from kMinTile on that makes rounds x (width + 16) smallest
 // (the CTAs take whole rounds of tiles: 197 tiles of 256 on 148 SMs are two rounds, as are 286 of 176).
-int logit_tile(int m_units, int V, int workers) {
-    if (m_units > 4) return BN;
+int logit_tile(int M, bool pair, int V, int workers) {
+    const int m_units = tiles(M, pair ? 2 * BM : BM);
+    if (m_units > kNarrowUnits) return BN;
     int best = BN;
     long long best_cost = -1;
     for (int bn = kMinTile; bn <= BN; bn += 16) {
@@ -1167,7 +1172,7 @@ ee_status ce_launch(const CeArgs& a) {
     const bool pair = use_pairs(a.M, a.device);
     CeMaps maps;
     CeParams p = base_params(a);
-    p.bn = logit_tile(pair ? tiles(a.M, 2 * BM) : 1, a.V, pair ? resident_pairs(a.device) : a.num_sms);
+    p.bn = logit_tile(a.M, pair, a.V, pair ? resident_pairs(a.device) : a.num_sms);
     p.a_rows = a.M <= 64 ? 64 : BM;
     p.kbs = blocks_per_slot(kStats, pair, p.bn, p.a_rows);
     if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs)) return EE_ERR_CUDA;
@@ -1207,7 +1212,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
         CeParams p = base_params(a);
         p.v0 = v0;
         {
-            p.bn = logit_tile(pair ? tiles(a.M, 2 * BM) : 1, nv, pair ? resident_pairs(a.device) : a.num_sms);
+            p.bn = logit_tile(a.M, pair, nv, pair ? resident_pairs(a.device) : a.num_sms);
             p.a_rows = a.M <= 64 ? 64 : BM;
             p.kbs = blocks_per_slot(kGrad, pair, p.bn, p.a_rows);
             if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs))
