@@ -474,7 +474,10 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
  * initialised once with ee_workspace_init; both 0 if a size is invalid.  The loss's holds y (2 M d bytes) and 8 bytes per row and
- * 256 columns of the vocabulary (64 up to 1024 rows).  The step that updates W, gamma and beta may come
+ * 256 columns of the vocabulary (64 up to 1024 rows).  The gradient's adds dy in fp32 (4 M d bytes, up to 32 times that where few rows
+ * leave SMs without work) and a piece of the logits' gradient: 128 MB, more for large batches, at most 512 MB or 74 tiles of dW up to
+ * 2 GB, and always 256 columns (512 M bytes).  What fewer rows need may be more (other tiles, more parts): a workspace for
+ * batches of several sizes is as large as the largest of theirs.  The step that updates W, gamma and beta may come
  * right before and right after a call in the same stream or graph.  M = 0: ee_head_ce writes loss = {0, 0}; ee_head_ce_grad writes zeros (nothing when accumulating).
  */
 size_t    ee_head_ce_workspace_bytes(int M, int d, int V);

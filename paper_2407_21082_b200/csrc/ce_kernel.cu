@@ -14,8 +14,8 @@
 //           results are stored (first piece) or added (later ones, one launch after the other, so in a fixed order)
 //           into one slab per split of the contraction
 //   kDw     A = G, B = y with the contraction over the rows: both MN-major as they lie
-// The pieces keep G at 128 MB, or a quarter of the whole where that is more: a piece costs three launches and, in kDy, one
-// way of dy to memory and back.  For small batches one piece is all of it.
+// The pieces keep G at 128 MB, or a quarter of the whole where that is more, up to 512 MB (2 GB where less leaves SMs without a tile of
+// dW): a piece costs three launches and, in kDy, one way of dy to memory and back.  For small batches one piece is all of it.
 // G is rounded to bf16 because the tensor cores take dW and dy from it: each of its elements is off by at most 2^-9
 // of itself, independently, which leaves dy and dW off by about as much as their own rounding to bf16.  G is held
 // without the mean's 1 / n, which is applied to the fp32 results.  Rows whose label is outside [0, V) take no part: their
@@ -52,7 +52,10 @@ constexpr int kMinTile = 64;                    // narrowest tile of the logits
 constexpr int kNarrowUnits = 4;                 // row tiles (of pairs: 256 rows) up to which it may be narrower than BN
 constexpr int kNarrowRows = kNarrowUnits * 2 * BM;
 constexpr int kMaxSplits = 32;
-constexpr size_t kGradPieceBytes = (size_t)128 << 20;      // or a quarter of all of G, whichever is more
+constexpr size_t kGradPieceBytes = (size_t)128 << 20;      // or a quarter of all of G, whichever is more,
+constexpr size_t kGradMostBytes = (size_t)512 << 20;       // but no more than this, or than what gives every SM a tile of dW,
+constexpr size_t kGradRoundBytes = (size_t)2 << 30;        // up to this (65536 x 512 x 128256: 32.4 ms with a quarter of G, 3.7 GB;
+                                                           // 33.0 with a tile of dW for every SM, 1.2 GB; 37.7 with 512 MB)
 
 enum CeMode { kStats, kGrad, kDy, kDw };
 template <int kMode> struct Layout {
@@ -970,8 +973,12 @@ CePlan ce_plan(int M, int d, int V) {
     auto dy_cost = [&](int units, int s) { return (double)rounds((long long)m_units * n_tiles * s, workers) / s * (units * 4.0) + s * slab; };
     // Pieces of the vocabulary in units of 256 columns, from the most that G may take down to half of that: the ones whose tiles come out
     // at whole rounds over the SMs, counted in k-blocks of a 256-wide tile; a launch costs about 20 of them.
-    long long most = (long long)(kGradPieceBytes / 2) / rows / (2 * BM);
-    if (most < vocab_units / 4) most = vocab_units / 4;
+    auto units_in = [&](size_t bytes) { return (long long)(bytes / 2) / rows / (2 * BM); };
+    long long cap = tiles(74, n_tiles), most = vocab_units / 4;
+    if (cap > units_in(kGradRoundBytes)) cap = units_in(kGradRoundBytes);
+    if (cap < units_in(kGradMostBytes)) cap = units_in(kGradMostBytes);
+    if (most > cap) most = cap;
+    if (most < units_in(kGradPieceBytes)) most = units_in(kGradPieceBytes);
     if (most < 1) most = 1;
     if (most > vocab_units) most = vocab_units;
     double best = 0;
