@@ -500,7 +500,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
  * ee_head_q4_unpack writes W4, bf16 [V, d] contiguous.  W and W4 are 32-byte aligned.
  *
  * ee_exit_head_q4 is ee_exit_head with W4 for W and the y of ee_head_ce: same definition otherwise, same outputs, strides,
- * alignment and rules, but the packed head, gamma and beta are data of the stream (they may be written right before the call).  M up to 2^30; up to 16 rows (8 where d is large), and above
+ * alignment and rules, but the packed head, gamma and beta are data of the stream (they may be written right before the call).  M up to 2^30; up to 16 rows (8 where d > 6784), and above
  * that every 64 rows, are one pass over the packed weights.  Workspace: ee_exit_head_q4_workspace_bytes(M, d, V), 256-byte aligned, initialised once
  * with ee_workspace_init.  M = 0 is a no-op.
  */

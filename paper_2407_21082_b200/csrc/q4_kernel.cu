@@ -19,7 +19,6 @@ namespace {
 
 constexpr int kWarps = 24;                       // as many as leave a thread 80 registers: a warp's loads are what is in flight
 constexpr int kThreads = kWarps * 32;
-constexpr int kMaxSlabRows = 16;               // rows per launch; above that the tensor-core kernel takes over, which rereads no weights
 constexpr int kUnroll = 2;                       // blocks (512 bytes of a tile) in flight per warp, twice
 constexpr size_t kSmemBudget = 226 * 1024;
 
@@ -157,8 +156,10 @@ __host__ __device__ inline int y_row_bytes(int d) { return (d + 63) / 64 * 128 +
 // instructions, half of them in the pipe that issues every other cycle, 150 cycles of its scheduler; start, LayerNorm and merge are
 // 8 us beside that.  A ring of eight blocks per warp in shared memory, filled by asynchronous copies, was no faster (31.7 us
 // for 8 rows of 2560, 13.0 for 8 of 512): what is in flight is not what it waits for.
-// Up to 16 rows this kernel, above that the tensor-core one: 16 rows of 1024 take 21.9 us here and 25.5 there, 17 rows (two
-// passes here) 38 and 26.7; at d = 2560 42 and 46, then 77 and 48.5.
+// What one launch takes goes to this kernel, 16 rows or the 8 that fit shared memory at d > 6784, more to the tensor-core one, which
+// reads the weights once: 16 rows of 1024 take 21.9 us here and 25.5 there, 17 rows (two
+// passes here) 38 and 26.7; at d = 2560 42 and 46, then 77 and 48.5;
+// at d = 8192 8 rows 87 and 120, 16 rows (two passes) 173 and 120.
 template <int NT>
 __global__ void __launch_bounds__(kThreads, 1) q4_head_kernel(const __grid_constant__ Q4Params p) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -373,7 +374,7 @@ ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group) {
     __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(ws + kCtrlBytes + parts_bytes());
     // EE_Q4_KERNEL=stream | gemm forces one of the two kernels (for tests and comparisons)
     const char* force = getenv("EE_Q4_KERNEL");
-    const bool gemm = force && force[0] == 'g' ? true : force && force[0] == 's' ? false : a.M > kMaxSlabRows;
+    const bool gemm = force && force[0] == 'g' ? true : force && force[0] == 's' ? false : a.M > slab_rows(a.d);
     const int slab = gemm ? kQ4GemmRows : slab_rows(a.d);
     const int ld_y = (a.d + 63) / 64 * 64;
     if (gemm) {
