@@ -469,7 +469,8 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  *   dW     bf16 [V, d] contiguous, or NULL;   dgamma, dbeta  bf16 [d], both or neither NULL
  *   accumulate != 0: dW, dgamma and dbeta are added to what the buffers hold (dh is always overwritten)
  * The rounding of y to bf16 is passed through by the gradient.  All gradients are bf16: the products behind dy and dW
- * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that; and lse is fp32, so that at the label of a nearly
+ * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that (what the rounding leaves of a row's entry at its
+ * label is added to dy in fp32, so that dh, dgamma and dbeta do not share it; dW does not have it); and lse is fp32, so that at the label of a nearly
  * certain row that difference is good to 2^-24 |lse| of the row's weight, not to a part of itself.
  * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,

@@ -16,9 +16,11 @@
 //   kDw     A = G, B = y with the contraction over the rows: both MN-major as they lie
 // The pieces keep G at 128 MB, or a quarter of the whole where that is more, up to 512 MB (2 GB where less leaves SMs without a tile of
 // dW): a piece costs three launches and, in kDy, one way of dy to memory and back.  For small batches one piece is all of it.
-// G is rounded to bf16 because the tensor cores take dW and dy from it: each of its elements is off by at most 2^-9
-// of itself, independently, which leaves dy and dW off by about as much as their own rounding to bf16.  G is held
-// without the mean's 1 / n, which is applied to the fp32 results.  Rows whose label is outside [0, V) take no part: their
+// G is rounded to bf16 because the tensor cores take dW and dy from it: each of its elements is off by at most 2^-8 of itself,
+// independently.  The entry at a row's label is as large as all the others of the row together, and its rounding would be shared by the
+// whole row of dy (with few rows dbeta was off by 3.5e-3 where its own rounding is 1.8e-3): what the rounding leaves of it is kept
+// in fp32 and added to dy, times W's row, on the way back.  In dW it stays: a row of it that one label dominates is off by up to 2^-8 from G
+// and 2^-8 from its own rounding.  G is held without the mean's 1 / n, which is applied to the fp32 results.  Rows whose label is outside [0, V) take no part: their
 // row of G and of y is zero, whatever their hidden state holds.
 //
 // What bounds it, and what it measured (one B200; loss and gradient, times per step):
@@ -99,6 +101,7 @@ struct CeParams {
     const float* loss;     // loss[1] = number of counted rows
     __nv_bfloat16* G;      // kGrad: [M][ld_g]
     int ld_g;
+    float* label_rest;     // kGrad: [M] what the rounding of a counted row's entry at its label left
     float* dy;             // kDy: [splits][M][d]
     __nv_bfloat16* dW;
     int sectors;           // kDw: rows of dW begin on 32-byte sectors
@@ -533,9 +536,12 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                         z[c][j] = g.x;
                         z[c][j + 1] = g.y;
                     }
-                    if ((unsigned)(label - base) < 32u) {
+                    if ((unsigned)(label - base) < 32u && label < col1) {               // what lies beyond col1 is another tile's
+                        float g = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) z[c][j] -= (base + j == label) ? weight : 0.f;
+                        for (int j = 0; j < 32; ++j)
+                            if (base + j == label) z[c][j] = g = z[c][j] - weight;
+                        p.label_rest[row] = g - __bfloat162float(__float2bfloat16_rn(g));
                     }
                     if (weight == 0.f || base + 32 > p.n_cols) {
 #pragma unroll
@@ -775,6 +781,10 @@ struct CeBackArgs {
     const float2* stats;
     const float* dy;       // [splits][M][d]
     int splits;
+    const int* labels;     // of counted rows: the row of W that label_rest belongs to
+    const float* label_rest;
+    const __nv_bfloat16* W;
+    int V;
     const float* dce;
     const float* dloss;
     const float* loss;
@@ -831,6 +841,13 @@ __global__ void __launch_bounds__(kMostThreads) ce_back_kernel(const __grid_cons
             if (row < r1) st[k] = __ldcg(a.stats + row);
             if (on && row < r1) {
                 xw[k] = ld_dep(reinterpret_cast<const uint4*>(a.h + (size_t)row * a.ld_h) + c);
+                const int label = ld_dep(a.labels + row);
+                if ((unsigned)label < (unsigned)a.V) {                   // a row that takes no part for its weight is dead below
+                    const float rest = __ldcg(a.label_rest + row);
+                    unpack8(ld_dep(reinterpret_cast<const uint4*>(a.W + (size_t)label * a.d) + c), v[k]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[k][j] *= rest;
+                }
                 for (int s = 0; s < a.splits; ++s) add8(v[k], a.dy + ((size_t)s * a.M + row) * a.d + c * 8);
             }
         }
@@ -1010,7 +1027,7 @@ CePlan ce_plan(int M, int d, int V) {
 }
 
 struct CeSpace {
-    size_t y, stats, parts, z_label, g, dy, cols, total;
+    size_t y, stats, parts, z_label, label_rest, g, dy, cols, total;
 };
 CeSpace ce_space(int M, int d, int V, bool grad) {
     CeSpace s;
@@ -1022,9 +1039,10 @@ CeSpace ce_space(int M, int d, int V, bool grad) {
     const size_t wide_parts = (size_t)tiles(V, BN) * M, narrow_parts = (size_t)tiles(V, kMinTile) * narrow;
     s.parts = take((wide_parts > narrow_parts ? wide_parts : narrow_parts) * sizeof(Part));
     s.z_label = take((size_t)M * 4);
-    s.g = s.dy = s.cols = at;
+    s.label_rest = s.g = s.dy = s.cols = at;
     if (grad) {
         const CePlan c = ce_plan(M, d, V);
+        s.label_rest = take((size_t)M * 4);
         s.g = take((size_t)M * c.piece * 2);
         s.dy = take((size_t)c.splits * M * d * 4);
         s.cols = take((size_t)c.back_ctas * c.back_groups * 2 * d * 4);
@@ -1225,6 +1243,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
             if (!map_k(&maps.a, &p.a_3d, l.y, a.M, l.ld_y, l.ld_y, p.a_rows, p.kbs) || !map_k(&maps.b, &p.b_3d, a.W, a.V, a.d, a.d, pair ? p.bn / 2 : p.bn, p.kbs))
                 return EE_ERR_CUDA;
             p.G = G; p.ld_g = ld_g;
+            p.label_rest = reinterpret_cast<float*>(ws + s.label_rest);
             p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv_pad, p.bn); p.k_blocks = tiles(a.d, BK);
             p.n_cols = nv; p.m_rows = a.M;
             const ee_status st = launch_product<kGrad>(maps, p, pair, a);
@@ -1265,6 +1284,8 @@ ee_status ce_grad_launch(const CeArgs& a) {
     CeBackArgs b;
     b.h = l.h; b.ld_h = a.ld_h; b.gamma = a.gamma; b.stats = l.stats;
     b.dy = dy; b.splits = c.splits;
+    b.labels = a.labels; b.label_rest = reinterpret_cast<const float*>(ws + s.label_rest);
+    b.W = static_cast<const __nv_bfloat16*>(a.W); b.V = a.V;
     b.dce = a.dce; b.dloss = a.dloss; b.loss = a.loss;
     b.dh = static_cast<__nv_bfloat16*>(a.dh); b.ld_dh = a.ld_dh;
     b.M = a.M; b.d = a.d;
