@@ -28,7 +28,10 @@
 //   4096 x 1024 x 50304    1.49 ms, 1.13 PFLOP/s; tensor pipe 82 % active in the products, 69 % where G is written, at 1.6 GHz
 //   1003 x 520 x 32003     206 us: tiles of nine k-blocks, a third of a product's time is its start, its end and the tile borders
 //   64 x 512 x 50304       23.6 us, the loss alone: three launches for 8 us of weights
-// The tensor core's accumulator truncates: lse is off by 1 to 3e-6 of itself at these widths (the logits in fp32: 2e-7).
+// The tensor core's accumulator cuts off what falls below its last bit, which adds up: above 1024 columns a logit is summed in parts of up to
+// that many, which the epilogue adds in fp32 while the next part's products run.  lse is off by 1e-7 of itself at d = 512, 5e-7 at 1024, 4e-7 at
+// 2560 (the plain form in fp32: 5e-8, 1.5e-7, 2.7e-7); in one go 1.1e-6 at 2560 and 5e-6 at 8192.  Parts of 512 columns halve that
+// and cost short rows more (1003 x 520: the loss 47 us instead of 43.5); 16384 x 2560 pays 2 % for its three parts.
 #include "common.cuh"
 #include "layer_norm.cuh"
 #include "kernels.h"
@@ -51,6 +54,7 @@ constexpr int kMaxStages = 12;
 constexpr int kAccStride = 256;
 constexpr int kTmemCols = 512;
 constexpr int kMinTile = 64;                    // narrowest tile of the logits
+constexpr int kSegment = 16;                    // k-blocks of a logit that one accumulator sums
 constexpr int kNarrowUnits = 4;                 // row tiles (of pairs: 256 rows) up to which it may be narrower than BN
 constexpr int kNarrowRows = kNarrowUnits * 2 * BM;
 constexpr int kMaxSplits = 32;
@@ -82,6 +86,7 @@ struct CeParams {
     int n_tiles;           // 256-column tiles of the output
     int splits;            // kDy: parts of the contraction, each with a slab of its own
     int k_blocks;          // contraction in blocks of 64
+    int seg_blocks;        // how many of them an accumulator sums: all, or (kStats, kGrad) an even number
     int n_cols;            // columns of the output that exist (vocabulary of the piece, or d)
     int m_rows;            // rows of the output that exist
     int v0;                // first vocabulary row of the piece
@@ -257,7 +262,8 @@ __device__ __forceinline__ void add_bf16x32(const __nv_bfloat16* old, float (&z)
     }
 }
 
-template <int kMode, bool kPair>
+// kSegmented: the contraction of a tile goes through several accumulators, seg_blocks k-blocks each, added up in the epilogue's registers.
+template <int kMode, bool kPair, bool kSegmented>
 __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_constant__ CeMaps maps, const CeParams p) {
     constexpr bool a_mn = Layout<kMode>::a_mn, b_mn = Layout<kMode>::b_mn;
     const int b_rows = kPair ? p.bn / 2 : p.bn;                          // columns whose operand this CTA stages,
@@ -396,57 +402,63 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             for (int tile = worker; ok && tile < total_tiles; tile += n_workers) {
                 int m_tile, n_tile, split, kb0, kb1;
                 locate(tile, m_tile, n_tile, split, kb0, kb1);
-                if (kb0 == kb1) continue;
-                const int buf = local & 1;
-                const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
-                ++local;
-                if (!ptx::mbar_wait(tempty_bar(buf), acc_phase ^ 1u, abort_flag)) {
-                    record_failure(p.ctrl, abort_flag, 2, 0x80 | buf, tile);
-                    break;
-                }
-                ptx::tc_fence_after_sync();
-                const uint32_t d_tmem = tmem_base + (uint32_t)(buf * kAccStride);
-                for (int kb = kb0; kb < kb1; kb += kbs) {
-                    if (!ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
-                        record_failure(p.ctrl, abort_flag, 2, stage, tile);
+                for (int s0 = kb0; ok && s0 < kb1; s0 = kSegmented ? s0 + p.seg_blocks : kb1) {
+                    const int s1 = kSegmented ? min(kb1, s0 + p.seg_blocks) : kb1;
+                    const int buf = local & 1;
+                    const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
+                    ++local;
+                    if (!ptx::mbar_wait(tempty_bar(buf), acc_phase ^ 1u, abort_flag)) {
+                        record_failure(p.ctrl, abort_flag, 2, 0x80 | buf, tile);
                         ok = false;
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t a_addr = a_base + stage * a_stage, b_addr = b_base + stage * b_stage;
-                    const int blocks = min(kbs, kb1 - kb);                // the range's last slot may hold one block too many
-                    for (int h = 0; h < blocks; ++h) {
-                        const uint64_t adesc = a_mn ? ptx::smem_desc_mn128(a_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(a_addr + h * a_block);
-                        const uint64_t bdesc = b_mn ? ptx::smem_desc_mn128(b_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(b_addr + h * b_rows * 128);
-#pragma unroll
-                        for (int k = 0; k < BK / 16; ++k) {
-                            const uint32_t accumulate = (kb == kb0 && h == 0 && k == 0) ? 0u : 1u;
-                            if (kPair) ptx::mma_bf16_ss_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
-                            else ptx::mma_bf16_ss(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                    const uint32_t d_tmem = tmem_base + (uint32_t)(buf * kAccStride);
+                    for (int kb = s0; kb < s1; kb += kbs) {
+                        if (!ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
+                            record_failure(p.ctrl, abort_flag, 2, stage, tile);
+                            ok = false;
+                            break;
                         }
+                        ptx::tc_fence_after_sync();
+                        const uint32_t a_addr = a_base + stage * a_stage, b_addr = b_base + stage * b_stage;
+                        const int blocks = min(kbs, s1 - kb);             // the range's last slot may hold one block too many
+                        for (int h = 0; h < blocks; ++h) {
+                            const uint64_t adesc = a_mn ? ptx::smem_desc_mn128(a_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(a_addr + h * a_block);
+                            const uint64_t bdesc = b_mn ? ptx::smem_desc_mn128(b_addr + h * 8192, mn_lead) : ptx::smem_desc_k128(b_addr + h * b_rows * 128);
+#pragma unroll
+                            for (int k = 0; k < BK / 16; ++k) {
+                                const uint32_t accumulate = (kb == s0 && h == 0 && k == 0) ? 0u : 1u;
+                                if (kPair) ptx::mma_bf16_ss_pair(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                                else ptx::mma_bf16_ss(d_tmem, adesc + a_step * k, bdesc + b_step * k, idesc, accumulate);
+                            }
+                        }
+                        mma_commit_all<kPair>(empty_bar(stage));
+                        if (++stage == S) { stage = 0; phase ^= 1u; }
                     }
-                    mma_commit_all<kPair>(empty_bar(stage));
-                    if (++stage == S) { stage = 0; phase ^= 1u; }
+                    if (ok) mma_commit_all<kPair>(tfull_bar(buf));
                 }
-                if (ok) mma_commit_all<kPair>(tfull_bar(buf));
             }
             if (*abort_flag) mma_drain<kPair>(drain_bar);
         } else if (lane == 0 && kPair) {
             // The second CTA's thread, which has no products to issue, passes its epilogue's hand-over on: an arrival at the
             // partner waits some 600 cycles for its release, which each of the sixteen warps would otherwise spend at every tile.
             int local = 0;
-            for (int tile = worker; tile < total_tiles; tile += n_workers) {
+            bool ok = true;
+            for (int tile = worker; ok && tile < total_tiles; tile += n_workers) {
                 int m_tile, n_tile, split, kb0, kb1;
                 locate(tile, m_tile, n_tile, split, kb0, kb1);
-                if (kb0 == kb1) continue;
-                const int buf = local & 1;
-                const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
-                ++local;
-                if (!ptx::mbar_wait(tempty_bar(buf), acc_phase, abort_flag)) {
-                    record_failure(p.ctrl, abort_flag, 2, 0xc0 | buf, tile);
-                    break;
+                for (int s0 = kb0; ok && s0 < kb1; s0 = kSegmented ? s0 + p.seg_blocks : kb1) {
+                    const int buf = local & 1;
+                    const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
+                    ++local;
+                    if (!ptx::mbar_wait(tempty_bar(buf), acc_phase, abort_flag)) {
+                        record_failure(p.ctrl, abort_flag, 2, 0xc0 | buf, tile);
+                        ok = false;
+                        break;
+                    }
+                    ptx::mbar_arrive_remote(ptx::map_to_cta(tempty_bar(buf), 0));
                 }
-                ptx::mbar_arrive_remote(ptx::map_to_cta(tempty_bar(buf), 0));
             }
         }
     } else {
@@ -465,9 +477,6 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
             int m_tile, n_tile, split, kb0, kb1;
             locate(tile, m_tile, n_tile, split, kb0, kb1);
             if (kb0 == kb1) continue;
-            const int buf = local & 1;
-            const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
-            ++local;
             const int row0 = m_tile * BM + quarter * 32, row = row0 + lane;
             const bool live = row < p.m_rows;
             const int col0 = n_tile * p.bn + group * 64;
@@ -482,24 +491,45 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                     lse = ld_dep(p.lse + row);
                 }
             }
-            if (given_up || !__all_sync(0xffffffffu, ptx::mbar_wait(tfull_bar(buf), acc_phase, abort_flag))) {
-                if (!given_up && lane == 0) record_failure(p.ctrl, abort_flag, 3, buf, tile);
-                given_up = true;
+            float z[2][32];
+            auto take = [&](bool first) {                                // the next accumulator into z
+                const int buf = local & 1;
+                const uint32_t acc_phase = (uint32_t)(local >> 1) & 1u;
+                ++local;
+                if (given_up || !__all_sync(0xffffffffu, ptx::mbar_wait(tfull_bar(buf), acc_phase, abort_flag))) {
+                    if (!given_up && lane == 0) record_failure(p.ctrl, abort_flag, 3, buf, tile);
+                    given_up = true;
+                    return;
+                }
+                ptx::tc_fence_after_sync();
+                if (work) {
+                    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kAccStride + group * 64);
+                    if (first) {
+                        ptx::tmem_ld_32x32(taddr, z[0]);
+                        ptx::tmem_ld_32x32(taddr + 32, z[1]);
+                        ptx::tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < 64; b += 16) {
+                            float x[2][8];
+                            ptx::tmem_ld_32x8(taddr + b, x[0]);
+                            ptx::tmem_ld_32x8(taddr + b + 8, x[1]);
+                            ptx::tmem_ld_wait();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) z[b >> 5][(b & 31) + j] += x[j >> 3][j & 7];
+                        }
+                    }
+                }
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(tempty_bar(buf));
+            };
+            take(true);
+            if (kSegmented)
+                for (int s0 = kb0 + p.seg_blocks; s0 < kb1 && !given_up; s0 += p.seg_blocks) take(false);
+            if (given_up) {
                 if (kMode == kStats) epilogue_barrier();                 // the other warps may still be on their way to it
                 continue;
-            }
-            ptx::tc_fence_after_sync();
-            float z[2][32];
-            if (work) {
-                const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kAccStride + group * 64);
-                ptx::tmem_ld_32x32(taddr, z[0]);
-                ptx::tmem_ld_32x32(taddr + 32, z[1]);
-                ptx::tmem_ld_wait();
-            }
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) {
-                ptx::mbar_arrive(tempty_bar(buf));
             }
             if (kMode == kStats) {
                 Part part = no_part();
@@ -1085,6 +1115,10 @@ int logit_tile(int M, bool pair, int V, int workers) {
     return best;
 }
 
+// k-blocks of a logit that an accumulator sums, the same for the loss and its gradient, whose logits have to be the same: up to
+// kSegment, in parts as equal as pairs of blocks allow.
+int logit_segment(int k_blocks) { return (tiles(k_blocks, tiles(k_blocks, kSegment)) + 1) / 2 * 2; }
+
 // Two-CTA clusters the device runs at once; 0 if the query fails or EE_GEMM_PAIRS=0 switches pairs off.
 int resident_pairs(int device) {
     static int pairs[kMaxDevices];
@@ -1092,12 +1126,12 @@ int resident_pairs(int device) {
     if (!asked[device]) {
         int n = 0;
         const char* e = getenv("EE_GEMM_PAIRS");
-        if (!(e && e[0] == '0') && cudaFuncSetAttribute(ce_gemm_kernel<kGrad, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        if (!(e && e[0] == '0') && cudaFuncSetAttribute(ce_gemm_kernel<kGrad, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                         (int)kSmemBudget) == cudaSuccess) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
             pair_launch_config(cfg, attr, dim3(2), kThreads, kSmemBudget, nullptr);
-            if (cudaOccupancyMaxActiveClusters(&n, ce_gemm_kernel<kGrad, true>, &cfg) != cudaSuccess) {
+            if (cudaOccupancyMaxActiveClusters(&n, ce_gemm_kernel<kGrad, true, false>, &cfg) != cudaSuccess) {
                 n = 0;
                 (void)cudaGetLastError();
             }
@@ -1108,11 +1142,11 @@ int resident_pairs(int device) {
     return pairs[device];
 }
 
-template <int kMode, bool kPair>
+template <int kMode, bool kPair, bool kSegmented>
 ee_status launch_mode(const CeMaps& maps, CeParams p, int workers, int device, cudaStream_t stream) {
     static bool configured[kMaxDevices] = {};
     if (!configured[device]) {
-        if (cudaFuncSetAttribute(ce_gemm_kernel<kMode, kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess)
+        if (cudaFuncSetAttribute(ce_gemm_kernel<kMode, kPair, kSegmented>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) != cudaSuccess)
             return EE_ERR_CUDA;
         configured[device] = true;
     }
@@ -1120,18 +1154,24 @@ ee_status launch_mode(const CeMaps& maps, CeParams p, int workers, int device, c
     const size_t smem = p.n_stages * p.kbs * slot_bytes(kMode, kPair, p.bn, p.a_rows) + kFixedSmem;
     const long long total = (long long)(kPair ? (p.m_tiles + 1) / 2 : p.m_tiles) * p.n_tiles * p.splits;
     const int grid = (int)(total < workers ? total : workers);
-    const cudaError_t e = kPair ? launch_pdl_pairs(ce_gemm_kernel<kMode, kPair>, 2 * grid, kThreads, smem, stream, maps, p)
-                                : launch_pdl(ce_gemm_kernel<kMode, kPair>, grid, kThreads, smem, stream, maps, p);
+    const cudaError_t e = kPair ? launch_pdl_pairs(ce_gemm_kernel<kMode, kPair, kSegmented>, 2 * grid, kThreads, smem, stream, maps, p)
+                                : launch_pdl(ce_gemm_kernel<kMode, kPair, kSegmented>, grid, kThreads, smem, stream, maps, p);
     return e == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 // Pairs of CTAs on 256-row tiles when the output has more than 128 rows and the device can run them: with and without them a step
 // takes 1517 and 2098 us on 4096 rows of 1024, 211 and 225 us on 1003 of 520; the loss of 1003 rows of 1024 56 and 73 us.
 bool use_pairs(int rows, int device) { return rows > BM && resident_pairs(device) > 0; }
+template <int kMode, bool kSegmented>
+ee_status launch_part(const CeMaps& maps, const CeParams& p, bool pair, const CeArgs& a) {
+    return pair ? launch_mode<kMode, true, kSegmented>(maps, p, resident_pairs(a.device), a.device, a.stream)
+                : launch_mode<kMode, false, kSegmented>(maps, p, a.num_sms, a.device, a.stream);
+}
 template <int kMode>
 ee_status launch_product(const CeMaps& maps, const CeParams& p, bool pair, const CeArgs& a) {
-    return pair ? launch_mode<kMode, true>(maps, p, resident_pairs(a.device), a.device, a.stream)
-                : launch_mode<kMode, false>(maps, p, a.num_sms, a.device, a.stream);
+    if constexpr (kMode == kStats || kMode == kGrad)
+        if (p.seg_blocks < p.k_blocks) return launch_part<kMode, true>(maps, p, pair, a);
+    return launch_part<kMode, false>(maps, p, pair, a);
 }
 
 CeLnArgs ln_args(const CeArgs& a, const CeSpace& s, bool grad) {
@@ -1204,6 +1244,7 @@ ee_status ce_launch(const CeArgs& a) {
     p.m_tiles = tiles(a.M, BM);
     p.n_tiles = tiles(a.V, p.bn);
     p.k_blocks = tiles(a.d, BK);
+    p.seg_blocks = logit_segment(p.k_blocks);
     p.n_cols = a.V;
     p.m_rows = a.M;
     p.parts = reinterpret_cast<Part*>(ws + s.parts);
@@ -1245,6 +1286,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
             p.G = G; p.ld_g = ld_g;
             p.label_rest = reinterpret_cast<float*>(ws + s.label_rest);
             p.m_tiles = tiles(a.M, BM); p.n_tiles = tiles(nv_pad, p.bn); p.k_blocks = tiles(a.d, BK);
+            p.seg_blocks = logit_segment(p.k_blocks);
             p.n_cols = nv; p.m_rows = a.M;
             const ee_status st = launch_product<kGrad>(maps, p, pair, a);
             if (st != EE_OK) return st;
@@ -1256,7 +1298,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
             if (!map_k(&maps.a, &q.a_3d, G, a.M, nv_pad, ld_g, q.a_rows, q.kbs) || !map_mn(&maps.b, &q.b_3d, a.W, a.V, a.d, a.d, pair ? q.bn / 2 : q.bn, q.kbs))
                 return EE_ERR_CUDA;
             q.dy = dy;
-            q.m_tiles = tiles(a.M, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = tiles(nv, BK);
+            q.m_tiles = tiles(a.M, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = q.seg_blocks = tiles(nv, BK);
             q.splits = c.splits;
             q.n_cols = a.d; q.m_rows = a.M;
             q.add = i > 0;
@@ -1273,7 +1315,7 @@ ee_status ce_grad_launch(const CeArgs& a) {
                 !map_mn(&maps.b, &q.b_3d, l.y, a.M, l.ld_y, l.ld_y, pair_w ? q.bn / 2 : q.bn, q.kbs))
                 return EE_ERR_CUDA;
             q.sectors = a.d % 16 == 0 && reinterpret_cast<uintptr_t>(a.dW) % 32 == 0;
-            q.m_tiles = tiles(nv, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = tiles(a.M, BK);
+            q.m_tiles = tiles(nv, BM); q.n_tiles = tiles(a.d, q.bn); q.k_blocks = q.seg_blocks = tiles(a.M, BK);
             q.n_cols = a.d; q.m_rows = nv;
             q.add = a.accumulate;
             const ee_status st = launch_product<kDw>(maps, q, pair_w, a);
