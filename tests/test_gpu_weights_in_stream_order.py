@@ -43,6 +43,7 @@ class Flat:
     def check(self, call, want, label):
         """`call` behind the update, captured and eager, from the old values every time, which a call in front of the update has read."""
         side = torch.cuda.Stream()
+        torch.cuda.synchronize()                                         # `want` is there, and its workspace is free for the other stream
         with torch.cuda.stream(side):
             got = call()                                                 # nothing is set up for the first time in the capture
             torch.cuda.synchronize()
