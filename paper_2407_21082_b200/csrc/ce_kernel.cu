@@ -24,10 +24,10 @@
 // row of G and of y is zero, whatever their hidden state holds.
 //
 // What bounds it, and what it measured (one B200; loss and gradient, times per step):
-//   16384 x 2560 x 50304   13.2 ms, 1.28 PFLOP/s over the four products: 0.91 of what cuBLAS sustains under the power cap
-//   4096 x 1024 x 50304    1.49 ms, 1.13 PFLOP/s; tensor pipe 82 % active in the products, 69 % where G is written, at 1.6 GHz
-//   1003 x 520 x 32003     206 us: tiles of nine k-blocks, a third of a product's time is its start, its end and the tile borders
-//   64 x 512 x 50304       23.6 us, the loss alone: three launches for 8 us of weights
+//   16384 x 2560 x 50304   13.5 ms (13.4 to 14.0 by box), 1.25 PFLOP/s over the four products: 0.89 of what cuBLAS sustains under the power cap
+//   4096 x 1024 x 50304    1.52 ms, 1.11 PFLOP/s; tensor pipe 78 to 84 % active in the products, 69 % where G is written, at 1.6 GHz
+//   1003 x 520 x 32003     210 us: tiles of nine k-blocks, a third of a product's time is its start, its end and the tile borders
+//   64 x 512 x 50304       22.5 us, the loss alone: three launches for 8 us of weights
 // The tensor core's accumulator cuts off what falls below its last bit, which adds up: above 1024 columns a logit is summed in parts of up to
 // that many, which the epilogue adds in fp32 while the next part's products run.  lse is off by 1e-7 of itself at d = 512, 5e-7 at 1024, 4e-7 at
 // 2560 (the plain form in fp32: 5e-8, 1.5e-7, 2.7e-7); in one go 1.1e-6 at 2560 and 5e-6 at 8192.  Parts of 512 columns halve that
@@ -735,8 +735,8 @@ __device__ __forceinline__ double cta_sum_d(double v, double* part) {
     return r;
 }
 
-// 32 rows per CTA, lane = row, the 32 warps stride over the parts, nine loads in flight (8 us at 4096 rows x 197 parts; with eight
-// warps and one load 25 us); then the CTA that finishes last adds up the mean over the counted rows, in a fixed order whichever
+// 32 rows per CTA, lane = row, the 32 warps stride over the parts, nine loads in flight: one turn for up to 288 parts, as many as the
+// narrow tiles of some 50000 columns give (64 rows of 512: 0.3 us less than with four; more parts take more turns); then the CTA that finishes last adds up the mean over the counted rows, in a fixed order whichever
 // CTA that is.
 __global__ void __launch_bounds__(kMergeThreads) ce_merge_kernel(const Part* parts, int n_parts, const float* z_label, const int* labels, int M,
                                                                  int V, float* ce, float* lse, float* loss, Control* ctrl) {

@@ -13,7 +13,8 @@
 // Tokens outside [0, V) take no part: they sort behind all others and are skipped.
 //
 // 16384 tokens, d = 1024, V = 50304, bf16: 37 to 40 us (floor 21: 34 MB of rows, 103 MB of table), of which 16 clear the table (6.4 TB/s)
-// beside the sort's 13, 12 add up and 9 join; 16385 tokens through the radix sort 59 us; 257 tokens x 520 into 32003 rows of
+// beside the sort's 13, 12 add up and 9 join; 16385 tokens through the radix sort 56 to 59 us (words, then three launches per eight bits of
+// token, all behind the clearing); 600 tokens x 64 14 us, and 34 where V >= 2^18 does not fit the word; 257 tokens x 520 into 32003 rows of
 // fp32 11.5 us.  The lookup of 32 tokens takes 1.5 us on the device.
 #include "common.cuh"
 #include "kernels.h"

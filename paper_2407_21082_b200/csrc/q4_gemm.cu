@@ -14,7 +14,9 @@
 // have long ended.
 //
 // Then the CTA's logits go through shared memory, so that a thread has one token and some of the rows, and its states to the
-// CTA that finishes last.  A share of more than 24 tiles goes in several passes; more than 64 tokens in several launches.
+// CTA that finishes last.  A share of more than 24 tiles -- on 148 SMs, a vocabulary above 56832 -- goes in several passes, each with its
+// own walk over y and its own softmax (64 rows of 1024: 29.4 us at V = 56832, 39.8 at 56833, 48.9 at 113664, 62.5 at 128256: a pass
+// costs some 10 us beside its weights; more tiles in one would need more rows of tensor memory); more than 64 tokens in several launches.
 //
 // 28 us for 64 rows of 1024 against V = 50304 (27 MB packed), 50 us for 33 of 2560 (66 MB, 1.3 TB/s), 17 to 64 rows within 10 % of
 // each other.  Issue slots bound it: two thirds of all cycles issue an instruction, half of those to unpack (four per two weights), the
