@@ -1160,7 +1160,7 @@ ee_status launch_mode(const CeMaps& maps, CeParams p, int workers, int device, c
 }
 
 // Pairs of CTAs on 256-row tiles when the output has more than 128 rows and the device can run them: with and without them a step
-// takes 1517 and 2098 us on 4096 rows of 1024, 211 and 225 us on 1003 of 520; the loss of 1003 rows of 1024 56 and 73 us.
+// takes 1527 and 1768 us on 4096 rows of 1024, 211 and 231 us on 1003 of 520; the loss of 1003 rows of 1024 87 and 99 us.
 bool use_pairs(int rows, int device) { return rows > BM && resident_pairs(device) > 0; }
 template <int kMode, bool kSegmented>
 ee_status launch_part(const CeMaps& maps, const CeParams& p, bool pair, const CeArgs& a) {
@@ -1202,8 +1202,8 @@ CeParams base_params(const CeArgs& a) {
 
 }  // namespace
 
-// A CTA per row up to kLnCtaRows rows, above that a warp per row: the loss takes 28.4 us with a CTA and 30.6 with a warp per row on 64
-// rows of 1024 (V = 50304), 56.5 and 58.9 on 1003, 125.5 and 122 on 2048 (V = 32003).
+// A CTA per row up to kLnCtaRows rows, above that a warp per row: the loss takes 31.0 us with a CTA and 32.9 with a warp per row on 64
+// rows of 1024 (V = 50304), 86.8 and 87.0 on 1003, 107.3 and 106.2 on 2048 (V = 32003).
 constexpr int kLnCtaRows = 1024;
 static ee_status ln_launch(const CeLnArgs& l, cudaStream_t stream) {
     if (l.M <= kLnCtaRows) {
