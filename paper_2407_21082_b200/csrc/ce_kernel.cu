@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
         // as soon as it is there, and the arithmetic runs beside the next tile's products.
         const int quarter = warp & 3;
         const int group = (warp - 2) >> 2;                  // 64 columns of the tile
-        int local = 0;
+        int local = 0, turn = 0;                             // accumulators taken so far; tiles, modulo two
         grid_dependency_wait();
         const float scale = kMode == kDw ? grad_scale(p.dce, p.dloss, p.loss) : 1.f;
         Part* xchg = reinterpret_cast<Part*>(bar_mem + 512);
@@ -544,7 +544,8 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                     }
                 }
                 // the tile's four groups of columns meet in shared memory; two buffers, so that one barrier a tile is enough
-                Part* slot = xchg + (local & 1) * 512 + quarter * 32 + lane;
+                Part* slot = xchg + turn * 512 + quarter * 32 + lane;
+                turn ^= 1;
                 slot[group * 128] = part;
                 epilogue_barrier();
                 if (group == 0 && live) {

@@ -44,3 +44,30 @@ def test_small_terms_behind_a_large_one_are_not_lost(ee, M, d):
     grad = ee.ee_head_ce_grad(head, labels, 1e-5, fwd, dce=torch.ones(M, device="cuda"))
     db = grad["dbeta"].float().cpu().numpy().astype(np.float64)
     assert (np.abs(db) <= 16 * M * 2.0 ** -8 * (2 + M * 2.0 ** -8)).all()       # every row's G sums to zero up to its roundings, times W <= 16
+
+
+@pytest.mark.parametrize("M,d,V", [(64, 2048, 50304), (300, 1536, 20011), (300, 2048, 50304), (1500, 1088, 20011), (520, 4096, 20011), (520, 2560, 20011)])
+def test_many_tiles_of_even_and_odd_numbers_of_parts(ee, M, d, V):
+    """Several tiles to a CTA, whose four groups of columns meet in shared memory at every one; against the same in 64 bits, and the same
+    bits every time.  lse: dz = 2 u d max_v sum |w y| and what test_gpu_ce.py allows the sum of exponentials."""
+    rng = torch.Generator(device="cuda").manual_seed(d)
+    W = (0.05 * torch.randn(V, d, generator=rng, device="cuda")).to(torch.bfloat16)
+    h = torch.randn(M, d, generator=rng, device="cuda").to(torch.bfloat16)
+    labels = torch.randint(0, V, (M,), generator=rng, device="cuda").to(torch.int32)
+    head = dict(h=h, gamma=torch.ones(d, device="cuda"), beta=torch.zeros(d, device="cuda"), W=W)
+    x = h.double()
+    c = x - x.mean(1, keepdim=True)
+    y = (c * torch.rsqrt((c * c).mean(1, keepdim=True) + 1e-5)).float().to(torch.bfloat16).double()
+    z = y @ W.double().t()
+    lse = torch.logsumexp(z, 1)
+    ce = lse - z.gather(1, labels.long()[:, None])[:, 0]
+    dz = 2 * U * d * (y.abs() @ W.double().abs().t()).amax(1)
+    dlse = dz + 2.0 ** -21 + 2 * U * (64 + V / 64) + 2 * U * lse.abs()
+    first = None
+    for _ in range(20):
+        got = ee.ee_head_ce(head, labels, 1e-5)
+        assert ((got["lse"].double() - lse).abs() <= dlse).all()
+        assert ((got["ce"].double() - ce).abs() <= dlse + dz + 2 * U * ce.abs()).all()
+        first = first or got
+        same = torch.equal(got["lse"], first["lse"]) and torch.equal(got["ce"], first["ce"])
+        assert same
