@@ -470,8 +470,10 @@ ee_status ee_head_kl(const void* h_head, long long ld_head, const float* gamma_h
  *   accumulate != 0: dW, dgamma and dbeta are added to what the buffers hold (dh is always overwritten)
  * The rounding of y to bf16 is passed through by the gradient.  All gradients are bf16: the products behind dy and dW
  * take exp(z - lse) - [label] rounded to bf16, so they carry no more than that (what the rounding leaves of a row's entry at its
- * label is added to dy in fp32, so that dh, dgamma and dbeta do not share it; dW does not have it); and lse is fp32, so that at the label of a nearly
- * certain row that difference is good to 2^-24 |lse| of the row's weight, not to a part of itself.
+ * label is added to dy in fp32, so that dh, dgamma and dbeta do not share it; dW does not have it).
+ * lse is fp32, so that at the label of a nearly certain row that difference is good to 2^-24 |lse| of the row's weight, not to a
+ * part of itself; ee_head_ce_grad_of takes ee_head_ce's ce as well (NULL: the same as ee_head_ce_grad) and exp(-ce) - 1 there, which
+ * keeps its digits.
  * Sizes, strides and alignment as in ee_exit_head, M and V at most 2^30; all gradient buffers 16-byte aligned.  Workspace:
  * ee_head_ce_workspace_bytes / ee_head_ce_grad_workspace_bytes (the second is enough for both calls), 256-byte aligned,
  * initialised once with ee_workspace_init; both 0 if a size is invalid.  The loss's holds y (2 M d bytes) and 8 bytes per row and
@@ -490,6 +492,10 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
                           int M, int d, int V, const int* labels, const float* lse, const float* loss, const float* dce,
                           const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta,
                           int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+ee_status ee_head_ce_grad_of(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W,
+                             int M, int d, int V, const int* labels, const float* ce, const float* lse, const float* loss,
+                             const float* dce, const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma,
+                             void* dbeta, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Heads held in 4 bits, a quarter of the memory.  Drafting (section 4.3.1) evaluates a head for a handful of tokens at a time,

@@ -90,6 +90,8 @@ PROTOTYPES = {
     "ee_head_ce_grad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_head_ce_grad": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_int, C.c_int, C.c_int, _p, _p, _p, _p, _p,
                                   _p, C.c_longlong, _p, _p, _p, C.c_int, _p, C.c_size_t, _p]),
+    "ee_head_ce_grad_of": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_int, C.c_int, C.c_int, _p, _p, _p, _p, _p, _p,
+                                     _p, C.c_longlong, _p, _p, _p, C.c_int, _p, C.c_size_t, _p]),
     "ee_head_q4_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_head_q4_pack": (C.c_int, [_p, C.c_int, C.c_int, C.c_int, _p, C.c_size_t, _p]),
     "ee_head_q4_unpack": (C.c_int, [_p, C.c_size_t, C.c_int, C.c_int, C.c_int, _p, _p]),

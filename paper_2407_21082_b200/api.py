@@ -599,6 +599,9 @@ def prepare_head_ce(head, labels, ln_eps, *, out=None, workspace=None) -> Prepar
 def _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace):
     h, W, ld, M, d, V, dev = _head_ce_inputs(head, labels)
     lse, loss = _vector(forward["lse"], "lse", torch.float32, M, dev), _vector(forward["loss"], "loss", torch.float32, 2, dev)
+    ce = forward.get("ce")
+    if ce is not None:
+        _vector(ce, "ce", torch.float32, M, dev)
     if dce is not None:
         _vector(dce, "dce", torch.float32, M, dev)
     if dloss is not None:
@@ -620,24 +623,25 @@ def _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, ou
                 _vector(out[name], f"out[{name!r}]", bf16, d, dev)
     workspace = new_head_ce_grad_workspace(M, d, V, h.device) if workspace is None else _scratch(workspace, dev)
     args = (h.data_ptr(), ld, head["gamma"].data_ptr(), head["beta"].data_ptr(), ln_eps, W.data_ptr(), M, d, V, labels.data_ptr(),
-            lse.data_ptr(), loss.data_ptr(), _ptr(dce), _ptr(dloss), _ptr(out.get("dh")), ld_dh, _ptr(out.get("dW")), _ptr(out.get("dgamma")),
+            _ptr(ce), lse.data_ptr(), loss.data_ptr(), _ptr(dce), _ptr(dloss), _ptr(out.get("dh")), ld_dh, _ptr(out.get("dW")), _ptr(out.get("dgamma")),
             _ptr(out.get("dbeta")), int(bool(accumulate)), workspace.data_ptr(), workspace.numel(), _stream())
     return args, out, (h, W, head, labels, forward, dce, dloss, out, workspace)
 
 
 def ee_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None, accumulate=False, out=None, workspace=None) -> dict:
     """Gradient of the cross-entropy (see include/eexit.h): dict(dh, dW, dgamma, dbeta), bf16.  `forward` is what
-    ee_head_ce returned for the same inputs (its lse and loss).  By default the gradient of the mean, times the device
+    ee_head_ce returned for the same inputs (its lse and loss, and its ce if it is there: with it the gradient of a nearly certain
+    row keeps its digits).  By default the gradient of the mean, times the device
     scalar `dloss` if given; `dce` [M] gives every row's own weight instead.  With `out`, entries left out or None are
     not computed; accumulate=True adds dW, dgamma and dbeta to the buffers in it."""
     args, out, _ = _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace)
-    _check(_lib.load().ee_head_ce_grad(*args), "ee_head_ce_grad")
+    _check(_lib.load().ee_head_ce_grad_of(*args), "ee_head_ce_grad")
     return out
 
 
 def prepare_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None, accumulate=False, out=None, workspace=None) -> PreparedCall:
     args, out, keep = _head_ce_grad_args(head, labels, ln_eps, forward, dce, dloss, accumulate, out, workspace)
-    return PreparedCall(_lib.load().ee_head_ce_grad, args, "ee_head_ce_grad", keep, out)
+    return PreparedCall(_lib.load().ee_head_ce_grad_of, args, "ee_head_ce_grad", keep, out)
 
 
 class Q4Weights:

@@ -652,6 +652,14 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
                           int M, int d, int V, const int* labels, const float* lse, const float* loss, const float* dce,
                           const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta, int accumulate,
                           void* workspace, size_t workspace_bytes_, void* stream) {
+    return ee_head_ce_grad_of(h, ld_h, gamma, beta, ln_eps, W, M, d, V, labels, nullptr, lse, loss, dce, dloss, dh, ld_dh, dW, dgamma,
+                              dbeta, accumulate, workspace, workspace_bytes_, stream);
+}
+
+ee_status ee_head_ce_grad_of(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* W,
+                             int M, int d, int V, const int* labels, const float* ce, const float* lse, const float* loss,
+                             const float* dce, const float* dloss, void* dh, long long ld_dh, void* dW, void* dgamma, void* dbeta,
+                             int accumulate, void* workspace, size_t workspace_bytes_, void* stream) {
     if (!train_sizes_ok(M, d, V)) return EE_ERR_SHAPE;
     if ((dgamma != nullptr) != (dbeta != nullptr)) return EE_ERR_NULL;
     if (dce && dloss) return EE_ERR_SHAPE;                               // the rows' weights and the mean's gradient exclude each other
@@ -678,7 +686,7 @@ ee_status ee_head_ce_grad(const void* h, long long ld_h, const float* gamma, con
     }
     a.h = h; a.ld_h = ld_h; a.gamma = gamma; a.beta = beta; a.ln_eps = ln_eps; a.W = W;
     a.M = M; a.d = d; a.V = V; a.labels = labels;
-    a.lse = lse; a.loss = loss; a.dce = dce; a.dloss = dloss;
+    a.lse = lse; a.ce_in = ce; a.loss = loss; a.dce = dce; a.dloss = dloss;
     a.dh = dh; a.ld_dh = ld_dh; a.dW = dW; a.dgamma = dgamma; a.dbeta = dbeta; a.accumulate = accumulate ? 1 : 0;
     a.workspace = workspace;
     return ce_grad_launch(a);

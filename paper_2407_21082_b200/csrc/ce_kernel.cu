@@ -101,6 +101,7 @@ struct CeParams {
     float* z_label;        // kStats: [M]
     const int* labels;
     const float* lse;      // kGrad
+    const float* ce;       // kGrad: the rows' losses, or NULL
     const float* dce;      // row weights, or NULL: every counted row 1, and `scale` at the end
     const float* dloss;    // fp32 [1] or NULL (one)
     const float* loss;     // loss[1] = number of counted rows
@@ -568,10 +569,11 @@ __global__ void __launch_bounds__(kThreads, 1) ce_gemm_kernel(const __grid_const
                         z[c][j + 1] = g.y;
                     }
                     if ((unsigned)(label - base) < 32u && label < col1) {               // what lies beyond col1 is another tile's
-                        float g = 0.f;
+                        // p - 1 from the loss: of exp(z - lse) - 1 a nearly certain row keeps no digit, lse being rounded to 1e-6
+                        float g = p.ce ? weight * expm1f(-ld_dep(p.ce + row)) : 0.f;
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
-                            if (base + j == label) z[c][j] = g = z[c][j] - weight;
+                            if (base + j == label) z[c][j] = g = p.ce ? g : z[c][j] - weight;
                         p.label_rest[row] = g - __bfloat162float(__float2bfloat16_rn(g));
                     }
                     if (weight == 0.f || base + 32 > p.n_cols) {
@@ -1195,7 +1197,7 @@ CeParams base_params(const CeArgs& a) {
     p.splits = 1;
     p.bn = BN;
     p.a_rows = BM;
-    p.labels = a.labels; p.lse = a.lse; p.dce = a.dce; p.dloss = a.dloss; p.loss = a.loss;
+    p.labels = a.labels; p.lse = a.lse; p.ce = a.ce_in; p.dce = a.dce; p.dloss = a.dloss; p.loss = a.loss;
     p.dW = static_cast<__nv_bfloat16*>(a.dW);
     p.ctrl = reinterpret_cast<Control*>(a.workspace);
     return p;

@@ -106,7 +106,8 @@ struct CeArgs {
     float* ce;             // forward outputs
     float* lse_out;
     float* loss_out;
-    const float* lse;      // backward: what the forward call wrote
+    const float* lse;      // backward: what the forward call wrote, ce_in its ce or NULL
+    const float* ce_in;
     const float* loss;
     const float* dce;
     const float* dloss;

@@ -13,6 +13,7 @@ import torch
 import gen
 import oracle
 from _util import dev, dev_bf16
+from test_gpu_ce import E, _np
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -75,3 +76,59 @@ def test_the_loss_of_nearly_certain_rows_keeps_its_digits(ee, M, d, V, twins):
     assert (np.abs(got["lse"].cpu().numpy().astype(np.float64) - ref["lse"]) <= dlse).all()
     mean = want.sum() / counted.sum()
     assert abs(float(got["loss"][0]) - mean) <= bound.max() + 2 * U * mean
+
+
+@pytest.mark.parametrize("M,d,V", SIZES)
+def test_the_gradient_of_nearly_certain_rows_keeps_its_digits(ee, M, d, V):
+    """Row by row in dh.  The entries of G: e^(z - lse) is off by r = dz + dlse + 2^-21 of itself and rounded to bf16 (e = 2^-8); at the
+    label e^(-ce) - 1 by what ce is off by, x (1 - p), plus 2 dz p where the label is not the largest logit, and 8u of itself; its
+    rounding does not reach dy (test_gpu_ce_few_rows.py).  From G on as in test_gpu_ce.py."""
+    h_bits, head, labels = _case(M, d, V, M + d + V)
+    weights = np.ones(M, np.float32)
+    ref = oracle.cross_entropy(h_bits, head, labels, weights)
+    W, y, P = ref["W"], ref["y"], ref["P"]
+    z = y @ W.T
+    m, top = z.max(1), z.argmax(1)
+    e = np.exp(z - m[:, None])
+    e[np.arange(M), top] = 0.0
+    ce = (m - z[np.arange(M), np.where(labels < 0, 0, labels)]) + np.log1p(e.sum(1))
+    rows = np.flatnonzero(labels >= 0)
+    at = labels[rows]
+    G = ref["G"].copy()
+    G[rows, at] = np.expm1(-ce[rows])                                    # 1 - p by its digits in 64 bits too
+    dy = G @ W
+    g, x_hat, s = head["gamma"].astype(np.float64), ref["xhat"], ref["rstd"]
+    t = dy * g
+    want = s * (t - t.mean(1, keepdims=True) - x_hat * (t * x_hat).mean(1, keepdims=True))
+    dz = 2 * U * d * (np.abs(y) @ np.abs(W).T).max(1)
+    x = 2 * dz + 2 * U * 88 + 2.0 ** -21 + 2 * U * (64 + V / 64)
+    r = dz + (dz + x + 2 * U * np.abs(ref["lse"])) + 2.0 ** -21
+    dG = np.where((labels >= 0)[:, None], r[:, None] * P * (1 + E) + E * np.abs(G), 0.0)
+    off = np.abs(G[rows, at])
+    dG[rows, at] = (x[rows] + 8 * U) * off + np.where(at != top[rows], 2 * dz[rows] * P[rows, at], 0.0)
+    Ddy = dG @ np.abs(W) + 2 * U * (V + 40) * (np.abs(G) @ np.abs(W))
+    ta, xa = np.abs(t), np.abs(x_hat)
+    Dt = Ddy * g + 4 * U * ta
+    inner = Dt + Dt.mean(1, keepdims=True) + xa * (Dt * xa).mean(1, keepdims=True)
+    size = ta + ta.mean(1, keepdims=True) + xa * (ta * xa).mean(1, keepdims=True)
+    bound = s * (inner + 2 * U * (d + 16) * size + 8 * U * (xa + 4.0) * (ta * (xa + 1)).mean(1, keepdims=True))
+    bound = bound * (1 + E) + E * np.abs(want) + 1e-38
+    dhead = dict(h=dev_bf16(h_bits), gamma=dev(head["gamma"]), beta=dev(head["beta"]), W=dev_bf16(head["W"]))
+    fwd = ee.ee_head_ce(dhead, dev(labels), 1e-5)
+    got = ee.ee_head_ce_grad(dhead, dev(labels), 1e-5, fwd, dce=dev(weights))
+    err = np.abs(_np(got["dh"]) - want)
+    worst = np.unravel_index(np.argmax(err / bound), err.shape)
+    assert (err <= bound).all(), (worst, err[worst], bound[worst], want[worst], ce[worst[0]])
+    # without the losses the same to what lse in fp32 allows
+    rough = _np(ee.ee_head_ce_grad(dhead, dev(labels), 1e-5, {k: fwd[k] for k in ("lse", "loss")}, dce=dev(weights))["dh"])
+    slack = 2 * U * np.abs(ref["lse"])[:, None] * s * (np.abs(W).max() * g).max() * (3 + xa)
+    assert (np.abs(rough - want) <= bound + (1 + E) * (slack + 2 * dz[:, None] * s * (np.abs(W).max() * g).max() * (3 + xa))).all()
+
+
+def test_losses_of_another_shape_are_refused(ee):
+    h_bits, head, labels = _case(40, 64, 200, 1)
+    dhead = dict(h=dev_bf16(h_bits), gamma=dev(head["gamma"]), beta=dev(head["beta"]), W=dev_bf16(head["W"]))
+    fwd = ee.ee_head_ce(dhead, dev(labels), 1e-5)
+    for bad in (fwd["ce"][:39], fwd["ce"].double(), fwd["ce"].cpu()):
+        with pytest.raises(ValueError):
+            ee.ee_head_ce_grad(dhead, dev(labels), 1e-5, dict(fwd, ce=bad))
