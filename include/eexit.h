@@ -524,6 +524,86 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
                           size_t workspace_bytes, void* stream);
 
 /*
+ * Heads held in microscaled 4-bit floating point: elements 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, and a scale per row and group of
+ * columns.  The tensor core multiplies two matrices of this form, so these heads are not unpacked at all, and the activations take the same form:
+ * what a drafting head needs, whose errors cost acceptance and not correctness.  With t the largest magnitude of a group:
+ *   group 32: s = 2^e, e = floor(log2 t) - 2 (between -127 and 127)
+ *   group 16: s = 2^k e4m3(t / (6 * 2^k)), e4m3 = nearest number of four exponent and three mantissa bits; k = floor(log2 T) - 10 (at
+ *             least -126; 0 where T = 0), T the largest magnitude of the whole matrix (weights) or of the row (activations)
+ *   q = nearest element of x / s (ties to the even code, at most 6; 0 where s = 0);   x4 = s q, which bf16 holds exactly
+ *   (the reader rounds to it where that is below its normal numbers)
+ * W must be finite.  d % group == 0, group <= d <= 8192, 1 <= V <= 2^30.  A packed head is ee_head_fp4_bytes(V, d, group) bytes (0 if a size is
+ * invalid), 256-byte aligned, in a layout of the library's own; ee_head_fp4_unpack writes the values, bf16 [V, d] contiguous.  W is
+ * 16-byte aligned.
+ *
+ * ee_exit_head_fp4 is ee_exit_head with the values of the packed head for W and y4 for y, y being that of ee_head_ce: same definition otherwise
+ * (sums in fp32), same outputs, strides, alignment and rules; a row whose y is not finite has an entropy that is not a number.  The packed
+ * head, gamma and beta are data of the stream (they may be written right before the call).  M up to 2^30; up to 128 rows are one pass over the packed weights.
+ * Workspace: ee_exit_head_fp4_workspace_bytes(M, d, V, group), 256-byte aligned, initialised once with ee_workspace_init; that of fewer
+ * rows may be larger (other tiles).  M = 0 is a no-op.
+ */
+size_t    ee_head_fp4_bytes(int V, int d, int group);
+ee_status ee_head_fp4_pack(const void* W, int V, int d, int group, void* fp4, size_t fp4_bytes, void* stream);
+ee_status ee_head_fp4_unpack(const void* fp4, size_t fp4_bytes, int V, int d, int group, void* W, void* stream);
+size_t    ee_exit_head_fp4_workspace_bytes(int M, int d, int V, int group);
+ee_status ee_exit_head_fp4(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* fp4,
+                           size_t fp4_bytes, int group, int M, int d, int V, const float* tau_per_row, float tau,
+                           int* argmax, float* entropy, float* maxprob, unsigned char* exit_mask, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/*
+ * Losses over the tokens of sequences, for heads that are improved by what they drafted.  They stand between ee_head_ce, whose ce is every
+ * token's -ln p, and ee_head_ce_grad, whose dce is every token's weight: dce below is the gradient of the loss with respect to ce.  A token
+ * is counted if its label is inside [0, V), as in ee_head_ce; dce is 0 for the others, whatever the other arrays hold there.
+ *
+ * ee_policy_loss, per counted token with r = exp(old_ce - ce) (its probability over that at drafting time) and the advantage a:
+ *   policy = -min(r a, clamp(r, 1 - clip_low, 1 + clip_high) a);   kl = exp(g) - 1 - g with g = ce - ref_ce (ref_ce NULL: 0)
+ *   loss fp32 [4]: means of policy + kl_weight kl, of policy, of kl, and of whether the clamp decided
+ *   seq_start NULL: adv fp32 [M]; the mean is over the counted tokens, whose number is counted[1] (fp32 [2] on the device: ee_head_ce's loss)
+ *   seq_start int32 [S + 1] on the device, not decreasing: sequence s is the rows seq_start[s] .. seq_start[s + 1] - 1; adv fp32 [S]; the mean is over
+ *   the S sequences of the mean over each one's counted tokens (0 for a sequence without any); counted may be NULL
+ *   0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl_weight (0 if ref_ce is NULL)
+ * ee_preference_loss, for P pairs of sequences 2p (preferred) and 2p + 1 (rejected), seq_start int32 [2 P + 1], with the reward of a
+ * sequence R = beta * sum over its counted tokens of (ref_ce - ce) (ref_ce NULL: of -ce) and the margin m = R(2p) - R(2p + 1):
+ *   -(1 - smoothing) ln sigma(m) - smoothing ln sigma(-m);   margin fp32 [P]
+ *   loss fp32 [4]: means over the pairs of that, of whether m > 0, of the preferred and of the rejected sequences' rewards
+ *   0 <= beta, 0 <= smoothing <= 1
+ * ce, old_ce, ref_ce, dce fp32 [M], labels int32 [M].  Rows outside all sequences get dce = 0.  The means and sums are added up in fp64 in a
+ * fixed order.  0 <= M <= 2^30, 1 <= S, P <= 2^29.  One launch.  Workspace: ee_token_loss_workspace_bytes(), 256-byte aligned, initialised once with
+ * ee_workspace_init.
+ */
+size_t    ee_token_loss_workspace_bytes(void);
+ee_status ee_policy_loss(const float* ce, const float* old_ce, const float* ref_ce, const float* adv, const int* labels, int M, int V,
+                         const int* seq_start, int S, const float* counted, float clip_low, float clip_high, float kl_weight,
+                         float* dce, float* loss, void* workspace, size_t workspace_bytes, void* stream);
+ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* labels, int M, int V, const int* seq_start, int P,
+                             float beta, float smoothing, float* dce, float* margin, float* loss, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * The norm over all gradients of a step, and their scaling where it is too large: what stands between the gradient calls above and the step.
+ *   ee_grad_norm:  norm[0] = sqrt(sum over all tensors of the sum of g^2), added up in fp32 by eights and in fp64 above, in a fixed order
+ *   ee_grad_clip:  out = round(g * min(1, max_norm / (norm[0] + 1e-6))) in the tensor's type; `out` NULL: in place, where nothing is written if the
+ *                  factor is 1.  A norm that is not a number makes everything that.
+ * The tensors (a HOST array; contiguous, n >= 0 elements of the type, aligned to it, at most 2^36 elements each) must not overlap; norm is fp32 [1]
+ * on the device, so that a sum over several GPUs may be put in between.  out is a HOST array of pointers, one per tensor, aligned alike; an out equal to its
+ * tensor is that tensor in place.  Tensors that begin on a 16-byte border are accessed by 16 bytes.  The arrays are read before the call
+ * returns; up to 512 tensors are one launch of each call.  Workspace of the norm: ee_grad_norm_workspace_bytes(n_tensors) (0 if that is negative),
+ * 256-byte aligned, initialised once with ee_workspace_init.
+ */
+#define EE_BFLOAT16 0
+#define EE_FLOAT16  1
+#define EE_FLOAT32  2
+typedef struct {
+    void* data;
+    long long n;
+    int type;
+} ee_tensor;
+size_t    ee_grad_norm_workspace_bytes(int n_tensors);
+ee_status ee_grad_norm(const ee_tensor* tensors, int n_tensors, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+ee_status ee_grad_clip(const ee_tensor* tensors, void* const* out, int n_tensors, float max_norm, const float* norm, void* stream);
+
+/*
  * The embedding of tokens and its gradient.  A head's weights and the model's embedding may be one table (tied
  * weights): a training step then adds the lookup's gradient to what ee_head_ce_grad left in dW, and a decoding step
  * looks up the tokens a round has committed.

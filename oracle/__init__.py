@@ -20,3 +20,5 @@ from .dssd_round import dssd_commit, dssd_round, dssd_round_multi  # noqa: F401,
 from .kl_loss import ce_from_logits, kl_from_logits, kl_to_teacher  # noqa: F401,E402
 from .ce_loss import cross_entropy  # noqa: F401,E402
 from .q4 import embed, embed_grad, q4_quantise, q4_values  # noqa: F401,E402
+from .fp4 import exit_head_fp4, fp4_values  # noqa: F401,E402
+from .token_loss import policy_loss, preference_loss  # noqa: F401,E402

@@ -45,6 +45,14 @@ class EEHiddenTables(C.Structure):
     _fields_ = [("table", _p * (EE_ROUND_MAX_DRAFT_HEADS + 1)), ("d", C.c_int), ("V", C.c_int), ("chained", C.c_int)]
 
 
+EE_BFLOAT16, EE_FLOAT16, EE_FLOAT32 = 0, 1, 2
+
+
+class EETensor(C.Structure):
+    """Mirror of `ee_tensor` in include/eexit.h."""
+    _fields_ = [("data", _p), ("n", C.c_longlong), ("type", C.c_int)]
+
+
 PROTOTYPES = {
     "ee_status_string": (C.c_char_p, [C.c_int]),
     "ee_exit_head_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
@@ -98,6 +106,19 @@ PROTOTYPES = {
     "ee_exit_head_q4_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_exit_head_q4": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_size_t, C.c_int, C.c_int, C.c_int, C.c_int,
                                   _p, C.c_float, _p, _p, _p, _p, _p, C.c_size_t, _p]),
+    "ee_head_fp4_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
+    "ee_head_fp4_pack": (C.c_int, [_p, C.c_int, C.c_int, C.c_int, _p, C.c_size_t, _p]),
+    "ee_head_fp4_unpack": (C.c_int, [_p, C.c_size_t, C.c_int, C.c_int, C.c_int, _p, _p]),
+    "ee_exit_head_fp4_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int, C.c_int]),
+    "ee_exit_head_fp4": (C.c_int, [_p, C.c_longlong, _p, _p, C.c_float, _p, C.c_size_t, C.c_int, C.c_int, C.c_int, C.c_int,
+                                   _p, C.c_float, _p, _p, _p, _p, _p, C.c_size_t, _p]),
+    "ee_token_loss_workspace_bytes": (C.c_size_t, []),
+    "ee_policy_loss": (C.c_int, [_p, _p, _p, _p, _p, C.c_int, C.c_int, _p, C.c_int, _p, C.c_float, C.c_float, C.c_float,
+                                 _p, _p, _p, C.c_size_t, _p]),
+    "ee_preference_loss": (C.c_int, [_p, _p, _p, C.c_int, C.c_int, _p, C.c_int, C.c_float, C.c_float, _p, _p, _p, _p, C.c_size_t, _p]),
+    "ee_grad_norm_workspace_bytes": (C.c_size_t, [C.c_int]),
+    "ee_grad_norm": (C.c_int, [C.POINTER(EETensor), C.c_int, _p, _p, C.c_size_t, _p]),
+    "ee_grad_clip": (C.c_int, [C.POINTER(EETensor), C.POINTER(_p), C.c_int, C.c_float, _p, _p]),
     "ee_embed": (C.c_int, [_p, C.c_int, C.c_int, _p, C.c_int, C.c_float, _p, C.c_longlong, _p]),
     "ee_embed_grad_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int, C.c_int]),
     "ee_embed_grad": (C.c_int, [_p, C.c_longlong, _p, C.c_int, C.c_int, C.c_int, C.c_float, _p, C.c_int, C.c_int,

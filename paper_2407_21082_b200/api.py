@@ -700,7 +700,7 @@ def new_exit_head_q4_workspace(M: int, q4: Q4Weights) -> torch.Tensor:
     return _workspace_of(ee_exit_head_q4_workspace_bytes(M, q4.d, q4.V), "ee_exit_head_q4_workspace_bytes", q4.data.device)
 
 
-def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
+def _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_workspace):
     h = _bf16(h)
     dev = _device_of(h, "h")
     d = q4.d
@@ -710,7 +710,7 @@ def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
     ld = _row_stride(h, "h", M, d, dev)
     data = q4.data
     if data.get_device() != dev:
-        raise ValueError(f"q4 is on {data.device}, h on {h.device}")
+        raise ValueError(f"the weights are on {data.device}, h on {h.device}")
     _vector(gamma, "gamma", torch.float32, d, dev)
     _vector(beta, "beta", torch.float32, d, dev)
     tau_t = tau_ptr = None
@@ -724,7 +724,7 @@ def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
             t = out.get(name)
             if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < M:
                 raise ValueError(f"out[{name!r}] must be a contiguous {dtype} tensor of at least M = {M} elements on cuda:{dev}")
-    workspace = new_exit_head_q4_workspace(M, q4) if workspace is None else _scratch(workspace, dev)
+    workspace = new_workspace(M, q4) if workspace is None else _scratch(workspace, dev)
     args = (h.data_ptr(), ld, gamma.data_ptr(), beta.data_ptr(), ln_eps, data.data_ptr(), data.numel(), q4.group, M, d, q4.V, tau_ptr, tau,
             out["argmax"].data_ptr(), out["entropy"].data_ptr(), out["maxprob"].data_ptr(), out["exit_mask"].data_ptr(),
             workspace.data_ptr(), workspace.numel(), _stream())
@@ -733,14 +733,262 @@ def _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace):
 
 def ee_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> dict:
     """ee_exit_head with weights held in 4 bits (ee_head_q4_pack); see there for the arguments."""
-    args, out, _ = _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace)
+    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_exit_head_q4_workspace)
     _check(_lib.load().ee_exit_head_q4(*args), "ee_exit_head_q4")
     return out
 
 
 def prepare_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> PreparedCall:
-    args, out, keep = _exit_head_q4_args(h, gamma, beta, ln_eps, q4, tau, out, workspace)
+    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_exit_head_q4_workspace)
     return PreparedCall(_lib.load().ee_exit_head_q4, args, "ee_exit_head_q4", keep, out)
+
+
+class Fp4Weights:
+    """A head's weights in microscaled 4-bit floating point (see include/eexit.h): the packed bytes (a device tensor) and what they are of."""
+    __slots__ = ("data", "V", "d", "group")
+
+    def __init__(self, data: torch.Tensor, V: int, d: int, group: int):
+        need = ee_head_fp4_bytes(V, d, group)
+        if need == 0:
+            raise EExitError(2, "ee_head_fp4_bytes")
+        if not (isinstance(data, torch.Tensor) and data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous() and data.numel() >= need):
+            raise ValueError(f"data must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+        self.data, self.V, self.d, self.group = data, int(V), int(d), int(group)
+
+
+def ee_head_fp4_bytes(V: int, d: int, group: int) -> int:
+    return int(_lib.load().ee_head_fp4_bytes(int(V), int(d), int(group)))
+
+
+def ee_head_fp4_pack(W, group: int = 16, *, out: Fp4Weights | None = None) -> Fp4Weights:
+    """Writes a head's weights (bf16 [V, d]) in 4-bit floating point with a scale per row and 16 or 32 columns (see include/eexit.h)."""
+    W = _bf16(W)
+    dev = _device_of(W, "W")
+    if W.dim() != 2 or not W.is_contiguous():
+        raise ValueError("W must be contiguous [V, d]")
+    V, d = W.shape
+    if out is None:
+        nbytes = ee_head_fp4_bytes(V, d, group)
+        if nbytes == 0:
+            raise EExitError(2, "ee_head_fp4_pack")
+        out = Fp4Weights(torch.empty(nbytes, dtype=torch.uint8, device=W.device), V, d, group)
+    elif (out.V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
+        raise ValueError("out was made for other weights")
+    _check(_lib.load().ee_head_fp4_pack(W.data_ptr(), V, d, int(group), out.data.data_ptr(), out.data.numel(), _stream()), "ee_head_fp4_pack")
+    return out
+
+
+def ee_head_fp4_unpack(fp4: Fp4Weights, *, out=None) -> torch.Tensor:
+    """What the packed weights stand for, bf16 [V, d]."""
+    dev = _device_of(fp4.data, "fp4")
+    if out is None:
+        out = torch.empty((fp4.V, fp4.d), dtype=torch.bfloat16, device=fp4.data.device)
+    else:
+        _matrix(out, "out", torch.bfloat16, fp4.V, fp4.d, dev)
+    _check(_lib.load().ee_head_fp4_unpack(fp4.data.data_ptr(), fp4.data.numel(), fp4.V, fp4.d, fp4.group, out.data_ptr(), _stream()),
+           "ee_head_fp4_unpack")
+    return out
+
+
+def ee_exit_head_fp4_workspace_bytes(M: int, d: int, V: int, group: int) -> int:
+    return int(_lib.load().ee_exit_head_fp4_workspace_bytes(int(M), int(d), int(V), int(group)))
+
+
+def new_exit_head_fp4_workspace(M: int, fp4: Fp4Weights) -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace for ee_exit_head_fp4 with these weights."""
+    return _workspace_of(ee_exit_head_fp4_workspace_bytes(M, fp4.d, fp4.V, fp4.group), "ee_exit_head_fp4_workspace_bytes", fp4.data.device)
+
+
+def ee_exit_head_fp4(h, gamma, beta, ln_eps, fp4: Fp4Weights, tau, *, out=None, workspace=None) -> dict:
+    """ee_exit_head with weights held in 4-bit floating point (ee_head_fp4_pack) and activations in the same form; see there for the
+    arguments."""
+    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, fp4, tau, out, workspace, new_exit_head_fp4_workspace)
+    _check(_lib.load().ee_exit_head_fp4(*args), "ee_exit_head_fp4")
+    return out
+
+
+def prepare_exit_head_fp4(h, gamma, beta, ln_eps, fp4: Fp4Weights, tau, *, out=None, workspace=None) -> PreparedCall:
+    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, fp4, tau, out, workspace, new_exit_head_fp4_workspace)
+    return PreparedCall(_lib.load().ee_exit_head_fp4, args, "ee_exit_head_fp4", keep, out)
+
+
+def new_token_loss_workspace(device="cuda") -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace for ee_policy_loss and ee_preference_loss, of any size."""
+    return _workspace_of(int(_lib.load().ee_token_loss_workspace_bytes()), "ee_token_loss_workspace_bytes", device)
+
+
+def new_policy_loss_outputs(M: int, device="cuda") -> dict:
+    return dict(loss=torch.empty(4, dtype=torch.float32, device=device), dce=torch.empty(M, dtype=torch.float32, device=device))
+
+
+def new_preference_loss_outputs(M: int, P: int, device="cuda") -> dict:
+    return dict(loss=torch.empty(4, dtype=torch.float32, device=device), margin=torch.empty(P, dtype=torch.float32, device=device),
+                dce=torch.empty(M, dtype=torch.float32, device=device))
+
+
+def _token_loss_inputs(forward, labels, seq_start, units_per, ref_ce, out):
+    """ce, M, device ordinal and the number of units that seq_start delimits (None without it)."""
+    ce = forward["ce"]
+    dev = _device_of(ce, "ce")
+    M = ce.numel()
+    f32 = torch.float32
+    _vector(ce, "ce", f32, M, dev)
+    _vector(labels, "labels", torch.int32, M, dev)
+    if ref_ce is not None:
+        _vector(ref_ce, "ref_ce", f32, M, dev)
+    units = None
+    if seq_start is not None:
+        if not isinstance(seq_start, torch.Tensor):
+            raise ValueError("seq_start must be an int32 CUDA tensor")
+        n = seq_start.numel()
+        if n < 1 + units_per or (n - 1) % units_per:
+            raise ValueError(f"seq_start must have 1 + {units_per} n elements, n >= 1" if units_per > 1 else "seq_start must have at least two elements")
+        _vector(seq_start, "seq_start", torch.int32, n, dev)
+        units = (n - 1) // units_per
+    if out is not None:
+        _vector(out.get("loss"), "out['loss']", f32, 4, dev)
+        _vector(out.get("dce"), "out['dce']", f32, M, dev)
+    return ce, M, dev, units
+
+
+def _policy_loss_args(forward, labels, V, old_ce, adv, ref_ce, kl_weight, clip, seq_start, out, workspace):
+    ce, M, dev, S = _token_loss_inputs(forward, labels, seq_start, 1, ref_ce, out)
+    f32 = torch.float32
+    _vector(old_ce, "old_ce", f32, M, dev)
+    _vector(adv, "adv", f32, M if S is None else S, dev)
+    counted = None
+    if S is None:
+        counted = _vector(forward["loss"], "loss", f32, 2, dev)
+    if out is None:
+        out = new_policy_loss_outputs(M, ce.device)
+    workspace = new_token_loss_workspace(ce.device) if workspace is None else _scratch(workspace, dev)
+    args = (ce.data_ptr(), old_ce.data_ptr(), _ptr(ref_ce), adv.data_ptr(), labels.data_ptr(), M, V, _ptr(seq_start), S or 0, _ptr(counted),
+            clip[0], clip[1], kl_weight, out["dce"].data_ptr(), out["loss"].data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    return args, out, (ce, old_ce, ref_ce, adv, labels, seq_start, counted, out, workspace)
+
+
+def ee_policy_loss(forward, labels, V: int, old_ce, adv, *, ref_ce=None, kl_weight: float = 0.0, clip=(0.2, 0.2), seq_start=None, out=None,
+                   workspace=None) -> dict:
+    """Clipped policy loss over drafted tokens (see include/eexit.h): dict(loss [4], dce [M]).  `forward` is what ee_head_ce returned for the
+    tokens at `labels`, old_ce their cross-entropies when they were drafted, ref_ce those of a reference head.  Without seq_start every counted
+    token counts alike and adv is [M]; with it (int32 [S + 1]) every sequence does, and adv is [S].  dce goes to ee_head_ce_grad as dce."""
+    args, out, _ = _policy_loss_args(forward, labels, V, old_ce, adv, ref_ce, kl_weight, clip, seq_start, out, workspace)
+    _check(_lib.load().ee_policy_loss(*args), "ee_policy_loss")
+    return out
+
+
+def prepare_policy_loss(forward, labels, V: int, old_ce, adv, *, ref_ce=None, kl_weight: float = 0.0, clip=(0.2, 0.2), seq_start=None, out=None,
+                        workspace=None) -> PreparedCall:
+    args, out, keep = _policy_loss_args(forward, labels, V, old_ce, adv, ref_ce, kl_weight, clip, seq_start, out, workspace)
+    return PreparedCall(_lib.load().ee_policy_loss, args, "ee_policy_loss", keep, out)
+
+
+def _preference_loss_args(forward, labels, V, seq_start, ref_ce, beta, smoothing, out, workspace):
+    if seq_start is None:
+        raise ValueError("seq_start must be an int32 CUDA tensor")
+    ce, M, dev, P = _token_loss_inputs(forward, labels, seq_start, 2, ref_ce, out)
+    if out is None:
+        out = new_preference_loss_outputs(M, P, ce.device)
+    else:
+        _vector(out.get("margin"), "out['margin']", torch.float32, P, dev)
+    workspace = new_token_loss_workspace(ce.device) if workspace is None else _scratch(workspace, dev)
+    args = (ce.data_ptr(), _ptr(ref_ce), labels.data_ptr(), M, V, seq_start.data_ptr(), P, beta, smoothing, out["dce"].data_ptr(),
+            out["margin"].data_ptr(), out["loss"].data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    return args, out, (ce, ref_ce, labels, seq_start, out, workspace)
+
+
+def ee_preference_loss(forward, labels, V: int, seq_start, *, ref_ce=None, beta: float = 0.1, smoothing: float = 0.0, out=None, workspace=None) -> dict:
+    """Loss of pairs of sequences 2p (preferred) and 2p + 1 (rejected), delimited by seq_start int32 [2 P + 1] (see include/eexit.h):
+    dict(loss [4], margin [P], dce [M]).  `forward` is what ee_head_ce returned for their tokens, ref_ce a reference head's
+    cross-entropies; dce goes to ee_head_ce_grad as dce."""
+    args, out, _ = _preference_loss_args(forward, labels, V, seq_start, ref_ce, beta, smoothing, out, workspace)
+    _check(_lib.load().ee_preference_loss(*args), "ee_preference_loss")
+    return out
+
+
+def prepare_preference_loss(forward, labels, V: int, seq_start, *, ref_ce=None, beta: float = 0.1, smoothing: float = 0.0, out=None,
+                            workspace=None) -> PreparedCall:
+    args, out, keep = _preference_loss_args(forward, labels, V, seq_start, ref_ce, beta, smoothing, out, workspace)
+    return PreparedCall(_lib.load().ee_preference_loss, args, "ee_preference_loss", keep, out)
+
+
+_GRAD_TYPES = {torch.bfloat16: _lib.EE_BFLOAT16, torch.float16: _lib.EE_FLOAT16, torch.float32: _lib.EE_FLOAT32}
+
+
+class GradClip:
+    """The norm over a list of gradients (contiguous bf16, fp16 or fp32 tensors) and their scaling, with the list marshalled once: gradient
+    buffers are the same from step to step (see ee_grad_norm and ee_grad_clip in include/eexit.h).  Calling it with max_norm computes the norm,
+    scales the gradients, in place or into `out` (a list of tensors like them), and returns the norm, fp32 [1] on the device.  norm() and
+    scale(max_norm) are its two halves, for a sum over several GPUs in between: scale reads self.value.  It launches on the
+    stream that is current when it is called."""
+
+    def __init__(self, grads, *, out=None, workspace=None):
+        import ctypes as C
+        grads = list(grads)
+        dev = _device_of(grads[0], "grads[0]") if grads else torch.cuda.current_device()
+        seen = set()
+        self._tensors = (_lib.EETensor * max(1, len(grads)))()
+        for i, g in enumerate(grads):
+            self._one(g, f"grads[{i}]", dev)
+            if g.numel() and g.data_ptr() in seen:
+                raise ValueError(f"grads[{i}] is in the list twice")
+            seen.add(g.data_ptr())
+            self._tensors[i].data, self._tensors[i].n, self._tensors[i].type = g.data_ptr() or None, g.numel(), _GRAD_TYPES[g.dtype]
+        self._out = None
+        if out is not None:
+            out = list(out)
+            if len(out) != len(grads):
+                raise ValueError("out must have a tensor for each of grads")
+            self._out = (C.c_void_p * max(1, len(grads)))()
+            for i, (o, g) in enumerate(zip(out, grads)):
+                self._one(o, f"out[{i}]", dev)
+                if o.dtype is not g.dtype or o.numel() != g.numel():
+                    raise ValueError(f"out[{i}] must be like grads[{i}]")
+                self._out[i] = o.data_ptr() or None
+        self._n, self._dev, self._keep = len(grads), dev, grads
+        self.out = grads if out is None else out
+        self.value = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
+        self.workspace = new_grad_norm_workspace(grads, self.value.device) if workspace is None else _scratch(workspace, dev)
+
+    @staticmethod
+    def _one(t, name, dev):
+        if not isinstance(t, torch.Tensor) or t.dtype not in _GRAD_TYPES or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous bfloat16, float16 or float32 tensor on cuda:{dev}")
+
+    def _here(self):
+        if torch._C._cuda_getDevice() != self._dev:
+            raise ValueError(f"the gradients are on cuda:{self._dev}, the current device is cuda:{torch.cuda.current_device()}")
+        return _stream()
+
+    def norm(self) -> torch.Tensor:
+        _check(_lib.load().ee_grad_norm(self._tensors, self._n, self.value.data_ptr(), self.workspace.data_ptr(), self.workspace.numel(), self._here()),
+               "ee_grad_norm")
+        return self.value
+
+    def scale(self, max_norm: float) -> None:
+        _check(_lib.load().ee_grad_clip(self._tensors, self._out, self._n, max_norm, self.value.data_ptr(), self._here()), "ee_grad_clip")
+
+    def __call__(self, max_norm: float) -> torch.Tensor:
+        value = self.norm()
+        self.scale(max_norm)
+        return value
+
+
+def new_grad_norm_workspace(grads, device="cuda") -> torch.Tensor:
+    """Allocates (through torch) and initialises a workspace for the norm over these gradients (a list, or their number)."""
+    n = grads if isinstance(grads, int) else len(grads)
+    return _workspace_of(int(_lib.load().ee_grad_norm_workspace_bytes(n)), "ee_grad_norm_workspace_bytes", device)
+
+
+def ee_grad_norm(grads, *, workspace=None) -> torch.Tensor:
+    """The norm over all elements of a list of gradients, fp32 [1] on the device (see include/eexit.h)."""
+    return GradClip(grads, workspace=workspace).norm()
+
+
+def ee_grad_clip(grads, max_norm: float, *, out=None, workspace=None) -> torch.Tensor:
+    """Scales a list of gradients by min(1, max_norm / (norm + 1e-6)), in place or into `out`; returns their norm before that, fp32 [1] on the
+    device.  A loop keeps a GradClip instead."""
+    return GradClip(grads, out=out, workspace=workspace)(max_norm)
 
 
 def _embed_args(table, tokens, scale, out):

@@ -1,4 +1,5 @@
 // The C ABI: argument validation, device checks, kernel selection.  No compute happens here.
+#include <math.h>
 #include <stdint.h>
 #include <stdlib.h>
 #include <string.h>
@@ -750,6 +751,161 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
     a.workspace = workspace; a.workspace_bytes = workspace_bytes_;
     a.stream = static_cast<cudaStream_t>(stream);
     return q4_head_launch(a, q4, group);
+}
+
+namespace {
+bool fp4_sizes_ok(int V, int d, int group) {
+    return V >= 1 && V <= kMaxCount && (group == 16 || group == 32) && d >= group && d <= 8192 && d % group == 0;
+}
+ee_status fp4_call_ok(const void* W, const void* fp4, size_t fp4_bytes, int V, int d, int group) {
+    if (!fp4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (!W || !fp4) return EE_ERR_NULL;
+    if (!aligned(W, 16) || !aligned(fp4, 256)) return EE_ERR_ALIGN;
+    return fp4_bytes < fp4_weight_bytes(V, d, group) ? EE_ERR_WORKSPACE : EE_OK;
+}
+}  // namespace
+
+size_t ee_head_fp4_bytes(int V, int d, int group) {
+    if (!fp4_sizes_ok(V, d, group)) return 0;
+    return fp4_weight_bytes(V, d, group);
+}
+
+ee_status ee_head_fp4_pack(const void* W, int V, int d, int group, void* fp4, size_t fp4_bytes, void* stream) {
+    const ee_status ok = fp4_call_ok(W, fp4, fp4_bytes, V, d, group);
+    if (ok != EE_OK) return ok;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return fp4_pack_launch(W, V, d, group, fp4, num_sms, static_cast<cudaStream_t>(stream));
+}
+
+ee_status ee_head_fp4_unpack(const void* fp4, size_t fp4_bytes, int V, int d, int group, void* W, void* stream) {
+    const ee_status ok = fp4_call_ok(W, fp4, fp4_bytes, V, d, group);
+    if (ok != EE_OK) return ok;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return fp4_unpack_launch(fp4, V, d, group, W, num_sms, static_cast<cudaStream_t>(stream));
+}
+
+size_t ee_exit_head_fp4_workspace_bytes(int M, int d, int V, int group) {
+    if (!train_sizes_ok(M, d, V) || !fp4_sizes_ok(V, d, group)) return 0;
+    return fp4_head_workspace_bytes(M, d, V, group);
+}
+
+ee_status ee_exit_head_fp4(const void* h, long long ld_h, const float* gamma, const float* beta, float ln_eps, const void* fp4,
+                           size_t fp4_bytes, int group, int M, int d, int V, const float* tau_per_row, float tau, int* argmax,
+                           float* entropy, float* maxprob, unsigned char* exit_mask, void* workspace, size_t workspace_bytes_,
+                           void* stream) {
+    if (!train_sizes_ok(M, d, V) || !fp4_sizes_ok(V, d, group)) return EE_ERR_SHAPE;
+    if (M == 0) return EE_OK;
+    if (!h || !gamma || !beta || !fp4 || !argmax || !entropy || !maxprob || !exit_mask || !workspace) return EE_ERR_NULL;
+    if (ld_h < d || (ld_h % 8) != 0) return EE_ERR_SHAPE;
+    if (!aligned(h, 16) || !aligned(fp4, 256) || !aligned(gamma, 16) || !aligned(beta, 16) || !aligned(workspace, 256))
+        return EE_ERR_ALIGN;
+    if (fp4_bytes < fp4_weight_bytes(V, d, group) || workspace_bytes_ < fp4_head_workspace_bytes(M, d, V, group)) return EE_ERR_WORKSPACE;
+    HeadArgs a{};
+    const ee_status dev = current_device(&a.device, &a.num_sms);
+    if (dev != EE_OK) return dev;
+    a.h = h; a.ld_h = ld_h; a.gamma = gamma; a.beta = beta; a.ln_eps = ln_eps;
+    a.M = M; a.d = d; a.V = V; a.tau_per_row = tau_per_row; a.tau = tau;
+    a.argmax = argmax; a.entropy = entropy; a.maxprob = maxprob; a.exit_mask = exit_mask;
+    a.workspace = workspace; a.workspace_bytes = workspace_bytes_;
+    a.stream = static_cast<cudaStream_t>(stream);
+    return fp4_head_launch(a, fp4, group);
+}
+
+size_t ee_token_loss_workspace_bytes(void) { return token_loss_workspace_bytes(); }
+
+ee_status ee_policy_loss(const float* ce, const float* old_ce, const float* ref_ce, const float* adv, const int* labels, int M, int V,
+                         const int* seq_start, int S, const float* counted, float clip_low, float clip_high, float kl_weight, float* dce,
+                         float* loss, void* workspace, size_t workspace_bytes_, void* stream) {
+    if (M < 0 || M > kMaxCount || V < 1 || V > kMaxCount || (seq_start && (S < 1 || S > kMaxCount / 2))) return EE_ERR_SHAPE;
+    if (!(clip_low >= 0.f && clip_low <= 1.f) || !(clip_high >= 0.f) || !(kl_weight >= 0.f) || (kl_weight > 0.f && !ref_ce)) return EE_ERR_SHAPE;
+    if (!loss || !workspace || (seq_start && !adv) || (!seq_start && !counted)) return EE_ERR_NULL;
+    if (M > 0 && (!ce || !old_ce || !adv || !labels || !dce)) return EE_ERR_NULL;
+    if (!aligned(workspace, 256)) return EE_ERR_ALIGN;
+    if (workspace_bytes_ < token_loss_workspace_bytes()) return EE_ERR_WORKSPACE;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (M == 0) return cudaMemsetAsync(loss, 0, 4 * sizeof(float), s) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    PolicyArgs p{};
+    p.ce = ce; p.old_ce = old_ce; p.ref_ce = ref_ce; p.adv = adv; p.labels = labels;
+    p.seq_start = seq_start; p.counted = counted;
+    p.M = M; p.V = V; p.S = seq_start ? S : 0;
+    p.log_low = log1p(-(double)clip_low); p.log_high = log1p((double)clip_high);
+    p.low = (float)(1.0 - (double)clip_low); p.high = (float)(1.0 + (double)clip_high);
+    p.kl_weight = kl_weight;
+    p.dce = dce; p.loss = loss; p.workspace = workspace;
+    return policy_loss_launch(p, num_sms, s);
+}
+
+ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* labels, int M, int V, const int* seq_start, int P,
+                             float beta, float smoothing, float* dce, float* margin, float* loss, void* workspace,
+                             size_t workspace_bytes_, void* stream) {
+    if (M < 0 || M > kMaxCount || V < 1 || V > kMaxCount || P < 1 || P > kMaxCount / 2) return EE_ERR_SHAPE;
+    if (!(beta >= 0.f) || !(smoothing >= 0.f && smoothing <= 1.f)) return EE_ERR_SHAPE;
+    if (!seq_start || !margin || !loss || !workspace) return EE_ERR_NULL;
+    if (M > 0 && (!ce || !labels || !dce)) return EE_ERR_NULL;
+    if (!aligned(workspace, 256)) return EE_ERR_ALIGN;
+    if (workspace_bytes_ < token_loss_workspace_bytes()) return EE_ERR_WORKSPACE;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    PreferenceArgs p{};
+    p.ce = ce; p.ref_ce = ref_ce; p.labels = labels; p.seq_start = seq_start;
+    p.M = M; p.V = V; p.P = P;
+    p.beta = beta; p.smoothing = smoothing;
+    p.dce = dce; p.margin = margin; p.loss = loss; p.workspace = workspace;
+    return preference_loss_launch(p, num_sms, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+ee_status tensors_ok(const ee_tensor* tensors, int n_tensors) {
+    if (n_tensors < 0) return EE_ERR_SHAPE;
+    if (n_tensors > 0 && !tensors) return EE_ERR_NULL;
+    long long bytes = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const ee_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > 1ll << 36 || t.type < EE_BFLOAT16 || t.type > EE_FLOAT32) return EE_ERR_SHAPE;
+        if (t.n > 0 && !t.data) return EE_ERR_NULL;
+        if (!aligned(t.data, t.type == EE_FLOAT32 ? 4 : 2)) return EE_ERR_ALIGN;
+        bytes += t.n * 4;
+        if (bytes > 1ll << 45) return EE_ERR_SHAPE;                      // pieces are numbered in 32 bits
+    }
+    return EE_OK;
+}
+}  // namespace
+
+size_t ee_grad_norm_workspace_bytes(int n_tensors) { return n_tensors < 0 ? 0 : grad_norm_workspace_bytes(n_tensors); }
+
+ee_status ee_grad_norm(const ee_tensor* tensors, int n_tensors, float* norm, void* workspace, size_t workspace_bytes_, void* stream) {
+    const ee_status ok = tensors_ok(tensors, n_tensors);
+    if (ok != EE_OK) return ok;
+    if (!norm || !workspace) return EE_ERR_NULL;
+    if (!aligned(workspace, 256)) return EE_ERR_ALIGN;
+    if (workspace_bytes_ < grad_norm_workspace_bytes(n_tensors)) return EE_ERR_WORKSPACE;
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return grad_norm_launch(tensors, n_tensors, norm, workspace, num_sms, static_cast<cudaStream_t>(stream));
+}
+
+ee_status ee_grad_clip(const ee_tensor* tensors, void* const* out, int n_tensors, float max_norm, const float* norm, void* stream) {
+    const ee_status ok = tensors_ok(tensors, n_tensors);
+    if (ok != EE_OK) return ok;
+    if (!(max_norm >= 0.f)) return EE_ERR_SHAPE;
+    if (!norm) return EE_ERR_NULL;
+    for (int i = 0; out && i < n_tensors; ++i) {
+        if (tensors[i].n > 0 && !out[i]) return EE_ERR_NULL;
+        if (!aligned(out[i], tensors[i].type == EE_FLOAT32 ? 4 : 2)) return EE_ERR_ALIGN;
+    }
+    int device, num_sms;
+    const ee_status dev = current_device(&device, &num_sms);
+    if (dev != EE_OK) return dev;
+    return grad_clip_launch(tensors, out, n_tensors, max_norm, norm, num_sms, static_cast<cudaStream_t>(stream));
 }
 
 ee_status ee_embed(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, void* stream) {

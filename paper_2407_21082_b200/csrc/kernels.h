@@ -136,6 +136,52 @@ ee_status q4_unpack_launch(const void* q4, int V, int d, int group, void* W, cud
 size_t q4_head_workspace_bytes(int M, int d);
 ee_status q4_head_launch(const HeadArgs& a, const void* q4, int group);      // a.W is not read
 
+// ---- losses over the tokens of sequences ----
+struct PolicyArgs {
+    const float* ce;
+    const float* old_ce;
+    const float* ref_ce;       // NULL: no penalty
+    const float* adv;          // per token, or per sequence where seq_start is given
+    const int* labels;
+    const int* seq_start;      // [S + 1] or NULL
+    const float* counted;      // ee_head_ce's loss: [1] is the number of counted rows (read where seq_start is NULL)
+    int M, V, S;
+    double log_low, log_high;  // ln of the clip's borders
+    float low, high;           // the borders
+    float kl_weight;
+    float* dce;
+    float* loss;
+    void* workspace;
+};
+struct PreferenceArgs {
+    const float* ce;
+    const float* ref_ce;       // NULL: none
+    const int* labels;
+    const int* seq_start;      // [2 P + 1]
+    int M, V, P;
+    float beta, smoothing;
+    float* dce;
+    float* margin;
+    float* loss;
+    void* workspace;
+};
+size_t token_loss_workspace_bytes();
+ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, cudaStream_t stream);
+ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, cudaStream_t stream);
+
+// ---- norm over many tensors, and their scaling ----
+size_t grad_norm_workspace_bytes(int n_tensors);
+ee_status grad_norm_launch(const ee_tensor* tensors, int n_tensors, float* norm, void* workspace, int num_sms, cudaStream_t stream);
+ee_status grad_clip_launch(const ee_tensor* tensors, void* const* out, int n_tensors, float max_norm, const float* norm, int num_sms,
+                           cudaStream_t stream);
+
+// ---- heads in microscaled 4-bit floating point ----
+size_t fp4_weight_bytes(int V, int d, int group);
+ee_status fp4_pack_launch(const void* W, int V, int d, int group, void* fp4, int num_sms, cudaStream_t stream);
+ee_status fp4_unpack_launch(const void* fp4, int V, int d, int group, void* W, int num_sms, cudaStream_t stream);
+size_t fp4_head_workspace_bytes(int M, int d, int V, int group);
+ee_status fp4_head_launch(const HeadArgs& a, const void* fp4, int group);     // a.W is not read
+
 // ---- embedding lookup and its gradient ----
 ee_status embed_launch(const void* table, int V, int d, const int* tokens, int n, float scale, void* out, long long ld_out, int num_sms,
                        cudaStream_t stream);

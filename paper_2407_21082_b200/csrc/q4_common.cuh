@@ -159,7 +159,8 @@ struct Q4Params {
 };
 
 // A row's results, and whether it may leave.
-__device__ __forceinline__ void rest_finish(const RestState& a, const Q4Params& p, int row) {
+template <class Params>
+__device__ __forceinline__ void rest_finish(const RestState& a, const Params& p, int row) {
     const float n = 1.f + a.s, H = log1pf(a.s) - a.t / n;
     p.argmax[row] = a.idx;
     p.entropy[row] = H;

@@ -1,0 +1,69 @@
+// Matrix products of microscaled 4-bit floating point (tcgen05.mma kind::mxf4nvf4, 64 columns per instruction) and the copies that bring
+// their scales to tensor memory.
+#pragma once
+
+#include "sm100_ptx.cuh"
+
+namespace ee {
+namespace ptx {
+
+// Contiguous copy global -> shared, 16-byte aligned, a multiple of 16 bytes; its bytes are signalled on `bar`.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Shared-memory descriptor of a K-major tile whose rows are 64 bytes wide, with the 64-byte swizzle: 8-row groups of 512 bytes.
+__device__ __forceinline__ uint64_t smem_desc_k64(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)(512 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)4 << 61;
+    return d;
+}
+// ... of 32 rows of 16 bytes, one behind the other, without a swizzle: 8-row groups of 128 bytes.
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3ffffu) >> 4);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)(128 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    return d;
+}
+// 512 bytes of scales to four columns of tensor memory, the same in all four quarters of its lanes.  Products issued behind it by the same
+// thread see it.
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// Instruction descriptor of kind::mxf4nvf4: A and B e2m1 (1 in bits [7,10) and [10,13)), both K-major, N >> 3 in bits [17,23), the scales'
+// type in bit 23 (0: four exponent and three mantissa bits, 1: a power of two), M >> 4 in bits [24,29).  Where a word of scales serves two
+// instructions (groups of 32), bits [4,6) and [29,31) say which half of B's and A's the instruction takes: 0 or 2.
+template <int kGroup>
+__host__ __device__ constexpr uint32_t idesc_fp4(int m, int n) {
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((kGroup == 32 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
+}
+constexpr uint32_t kIdescFp4SecondHalf = (2u << 4) | (2u << 29);
+
+// D[tmem] (+)= (A scales_a)[smem] * (B scales_b)[smem], fp32 accumulation; issued by one thread.
+template <int kGroup>
+__device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t scales_a, uint32_t scales_b,
+                                        uint32_t accumulate) {
+    if constexpr (kGroup == 16)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
+            : "memory");
+}
+
+}  // namespace ptx
+}  // namespace ee

@@ -71,6 +71,11 @@ __device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, un
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
 // 1 where a == b, else 0 (NaN too).
 __device__ __forceinline__ float one_if_equal(float a, float b) {
     float d;

@@ -1,0 +1,346 @@
+// Losses over the tokens of sequences, between ee_head_ce, which gives every token's cross-entropy ce = -ln p, and ee_head_ce_grad, which
+// takes every token's weight: the clipped policy loss with a penalty for leaving a reference, and the loss of preferred and rejected
+// sequences.  Each call is one launch that writes the weights and the means.
+//
+// The work is light -- 12 to 24 bytes and some twenty operations per token -- so that what counts is the shape: a mean over each
+// sequence's own tokens, or a sequence's sum, is needed before any of its weights.  A unit (a sequence, a pair of sequences, or, where
+// all tokens count alike, a stretch of tokens) is therefore walked twice, the second time out of L1 or L2, by a warp where units are
+// short, by a CTA where they are long, and by a cluster of eight CTAs, which exchange their sums through distributed shared memory,
+// where there are so few that the SMs would stand idle.
+//
+// What decides or cancels is done in fp64, which costs nothing here: the difference of two cross-entropies before the comparison with the
+// clip's border, and all sums, in a fixed order (a unit's by its threads, the units' by CTA, the CTAs' by the one that finishes last).
+#include <cooperative_groups.h>
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace ee {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kClusterCtas = 8;
+constexpr int kMaxCtas = 2048;
+constexpr int kSums = 4;
+
+enum Span { kWarpSpan, kCtaSpan, kClusterSpan };         // what walks a unit
+
+struct LossSpace {
+    Control ctrl;
+    double parts[kMaxCtas][kSums];
+};
+
+struct Term {
+    float policy, kl, grad;
+    bool cut;
+};
+
+// expm1(g) - g without the cancellation of small g: the series of g^2 (1/2 + g/6 + ...), whose next term is below 2^-26 of it.
+__device__ __forceinline__ float expm1_minus(float g, float expm1_g) {
+    if (fabsf(g) < 0.25f) {
+        float s = 1.f / 40320.f;
+        s = fmaf(s, g, 1.f / 5040.f);
+        s = fmaf(s, g, 1.f / 720.f);
+        s = fmaf(s, g, 1.f / 120.f);
+        s = fmaf(s, g, 1.f / 24.f);
+        s = fmaf(s, g, 1.f / 6.f);
+        s = fmaf(s, g, 0.5f);
+        return g * g * s;
+    }
+    return expm1_g - g;
+}
+
+__device__ __forceinline__ Term policy_term(const PolicyArgs& p, float ce, float old_ce, float ref_ce, float adv) {
+    Term t;
+    const double x = (double)old_ce - (double)ce;                        // ln of the ratio of the new to the old probability
+    t.cut = adv > 0.f ? x > p.log_high : adv < 0.f && x < p.log_low;
+    const float ratio = expf((float)x);
+    t.policy = -adv * (t.cut ? (adv > 0.f ? p.high : p.low) : ratio);
+    t.grad = t.cut ? 0.f : adv * ratio;
+    t.kl = 0.f;
+    if (p.ref_ce) {
+        const float g = (float)((double)ce - (double)ref_ce), e = expm1f(g);
+        t.kl = expm1_minus(g, e);
+        t.grad = fmaf(p.kl_weight, e, t.grad);
+    }
+    return t;
+}
+
+__device__ __forceinline__ double warp_total(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The sum of v over the threads that walk a unit, the same in each of them.  Two arrays of shared memory take turns, so that one barrier
+// (or two of the cluster) is enough.
+template <int kSpan>
+__device__ __forceinline__ double span_total(double v, double (&slots)[2][kWarps + 1], int& turn) {
+    v = warp_total(v);
+    if (kSpan == kWarpSpan) return v;
+    double* slot = slots[turn];
+    turn ^= 1;
+    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < kWarps; ++w) s += slot[w];
+    if (kSpan == kCtaSpan) return s;
+    if (threadIdx.x == 0) slot[kWarps] = s;
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    double all = 0.0;
+    for (int r = 0; r < kClusterCtas; ++r) all += *cluster.map_shared_rank(slot + kWarps, r);
+    return all;
+}
+
+// Four sums over the CTA's units, to the means: the CTA that finishes last adds up the CTAs'.
+__device__ __forceinline__ void finish(double (&sums)[kSums], LossSpace* space, float* loss) {
+    __shared__ double warp_sums[kWarps][kSums];
+    __shared__ int last;
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        const double v = warp_total(sums[k]);
+        if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5][k] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < kSums) {
+        double v = 0.0;
+        for (int w = 0; w < kWarps; ++w) v += warp_sums[w][threadIdx.x];
+        if (gridDim.x == 1) loss[threadIdx.x] = (float)v;
+        else space->parts[blockIdx.x][threadIdx.x] = v;
+    }
+    if (gridDim.x == 1) return;
+    __syncthreads();
+    if (threadIdx.x == 0) last = ticket_arrive_is_last(&space->ctrl.head_ticket[0], gridDim.x) ? 1 : 0;
+    __syncthreads();
+    if (!last) return;
+    double total[kSums] = {};
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) {
+        const double2* part = reinterpret_cast<const double2*>(space->parts[b]);
+        const double2 lo = __ldcg(part), hi = __ldcg(part + 1);
+        total[0] += lo.x; total[1] += lo.y; total[2] += hi.x; total[3] += hi.y;
+    }
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) {
+        const double v = warp_total(total[k]);
+        if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5][k] = v;
+    }
+    __syncthreads();
+    if (threadIdx.x < kSums) {
+        double v = 0.0;
+        for (int w = 0; w < kWarps; ++w) v += warp_sums[w][threadIdx.x];
+        loss[threadIdx.x] = (float)v;
+    }
+    if (threadIdx.x == 0) space->ctrl.head_ticket[0] = 0;                // ready for the next launch
+}
+
+// Boundaries of sequences are data: brought into the range of the rows, whatever they say.
+__device__ __forceinline__ int boundary(const int* seq_start, int i, int M) { return min(max(ld_dep(seq_start + i), 0), M); }
+
+// Rows before the first sequence and behind the last belong to none: their weight is zero.
+__device__ __forceinline__ void clear_outside(const int* seq_start, int n, int M, float* dce) {
+    const int first = boundary(seq_start, 0, M), end = max(boundary(seq_start, n, M), first);
+    const long long stride = (long long)gridDim.x * kThreads, at = (long long)blockIdx.x * kThreads + threadIdx.x;
+    for (long long i = at; i < first; i += stride) dce[i] = 0.f;
+    for (long long i = end + at; i < M; i += stride) dce[i] = 0.f;
+}
+
+__device__ __forceinline__ bool is_counted(const int* labels, long long i, int V) { return (unsigned)ld_dep(labels + i) < (unsigned)V; }
+
+// All tokens count alike.
+__global__ void __launch_bounds__(kThreads) policy_tokens_kernel(const PolicyArgs p) {
+    launch_dependents();
+    grid_dependency_wait();
+    const float n = ld_dep(p.counted + 1);
+    const double w = n > 0.f ? 1.0 / (double)n : 0.0;
+    const float wf = (float)w;
+    double sums[kSums] = {};
+    const long long stride = (long long)gridDim.x * kThreads;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < p.M; i += stride) {
+        float d = 0.f;
+        const float ce = ld_dep(p.ce + i), old_ce = ld_dep(p.old_ce + i), adv = ld_dep(p.adv + i), ref = p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+        if (is_counted(p.labels, i, p.V)) {
+            const Term t = policy_term(p, ce, old_ce, ref, adv);
+            d = wf * t.grad;
+            sums[1] += (double)t.policy;
+            sums[2] += (double)t.kl;
+            sums[3] += t.cut ? 1.0 : 0.0;
+        }
+        p.dce[i] = d;
+    }
+#pragma unroll
+    for (int k = 1; k < kSums; ++k) sums[k] *= w;
+    sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
+    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+}
+
+// Which units a thread has part in, and where in them it begins and how far it steps.
+template <int kSpan>
+struct Walk {
+    int unit, units_step, from, step;
+    bool leads;
+    __device__ __forceinline__ Walk() {
+        if (kSpan == kWarpSpan) {
+            unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
+            units_step = gridDim.x * kWarps;
+            from = threadIdx.x & 31;
+            step = 32;
+        } else if (kSpan == kCtaSpan) {
+            unit = blockIdx.x;
+            units_step = gridDim.x;
+            from = threadIdx.x;
+            step = kThreads;
+        } else {
+            unit = blockIdx.x / kClusterCtas;
+            units_step = gridDim.x / kClusterCtas;
+            from = (blockIdx.x % kClusterCtas) * kThreads + threadIdx.x;
+            step = kClusterCtas * kThreads;
+        }
+        leads = from == 0;
+    }
+};
+
+// Every sequence counts alike, and within a sequence every token.
+template <int kSpan>
+__global__ void __launch_bounds__(kThreads) policy_sequences_kernel(const PolicyArgs p) {
+    __shared__ double slots[2][kWarps + 1];
+    launch_dependents();
+    grid_dependency_wait();
+    clear_outside(p.seq_start, p.S, p.M, p.dce);
+    double sums[kSums] = {};
+    int turn = 0;
+    const Walk<kSpan> walk;
+    for (int unit = walk.unit; unit < p.S; unit += walk.units_step) {
+        const int begin = boundary(p.seq_start, unit, p.M), end = boundary(p.seq_start, unit + 1, p.M);
+        const float adv = ld_dep(p.adv + unit);
+        int have = 0;
+#pragma unroll 4
+        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) have += is_counted(p.labels, i, p.V) ? 1 : 0;
+        const double n = span_total<kSpan>((double)have, slots, turn);
+        const double w = n > 0.0 ? 1.0 / (n * (double)p.S) : 0.0;
+        const float wf = (float)w;
+        double policy = 0.0, kl = 0.0, cut = 0.0;
+#pragma unroll 4
+        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) {
+            float d = 0.f;
+            const float ce = ld_dep(p.ce + i), old_ce = ld_dep(p.old_ce + i), ref = p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+            if (is_counted(p.labels, i, p.V)) {
+                const Term t = policy_term(p, ce, old_ce, ref, adv);
+                d = wf * t.grad;
+                policy += (double)t.policy;
+                kl += (double)t.kl;
+                cut += t.cut ? 1.0 : 0.0;
+            }
+            p.dce[i] = d;
+        }
+        if (n > 0.0) {
+            sums[1] = fma(w, policy, sums[1]);
+            sums[2] = fma(w, kl, sums[2]);
+            sums[3] = fma(w, cut, sums[3]);
+        }
+    }
+    sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
+    if (kSpan == kClusterSpan) cg::this_cluster().sync();                // nobody leaves while its sums may still be read
+    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+}
+
+// Pairs of sequences 2u (preferred) and 2u + 1 (rejected).
+template <int kSpan>
+__global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceArgs p) {
+    __shared__ double slots[2][kWarps + 1];
+    launch_dependents();
+    grid_dependency_wait();
+    clear_outside(p.seq_start, 2 * p.P, p.M, p.dce);
+    double sums[kSums] = {};
+    int turn = 0;
+    const Walk<kSpan> walk;
+    for (int unit = walk.unit; unit < p.P; unit += walk.units_step) {
+        const int begin = boundary(p.seq_start, 2 * unit, p.M);
+        const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin), end = max(boundary(p.seq_start, 2 * unit + 2, p.M), middle);
+        double good = 0.0, bad = 0.0;
+#pragma unroll 4
+        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) {
+            const float ce = ld_dep(p.ce + i), ref = p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+            const double gain = is_counted(p.labels, i, p.V) ? (double)ref - (double)ce : 0.0;
+            good += i < middle ? gain : 0.0;
+            bad += i < middle ? 0.0 : gain;
+        }
+        good = (double)p.beta * span_total<kSpan>(good, slots, turn);
+        bad = (double)p.beta * span_total<kSpan>(bad, slots, turn);
+        // with t = e^-|m|: -ln sigma(m) = ln(1 + t) + max(-m, 0), and sigma(m) is 1 / (1 + t) or t / (1 + t)
+        const double margin = good - bad;
+        const float m = (float)margin, t = expf(-fabsf(m)), near = 1.f / (1.f + t), far = t * near;
+        const float up = log1pf(t) + fmaxf(-m, 0.f), down = log1pf(t) + fmaxf(m, 0.f);
+        const float slope = p.smoothing * (m >= 0.f ? near : far) - (1.f - p.smoothing) * (m >= 0.f ? far : near);
+        const float d = (float)((double)p.beta * (double)slope / (double)p.P);
+        if (walk.leads) {
+            p.margin[unit] = m;
+            sums[0] += (double)((1.f - p.smoothing) * up + (p.smoothing > 0.f ? p.smoothing * down : 0.f));
+            sums[1] += m > 0.f ? 1.0 : 0.0;
+            sums[2] += good;
+            sums[3] += bad;
+        }
+#pragma unroll 4
+        for (long long i = (long long)begin + walk.from; i < end; i += walk.step)
+            p.dce[i] = is_counted(p.labels, i, p.V) ? (i < middle ? -d : d) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) sums[k] /= (double)p.P;
+    if (kSpan == kClusterSpan) cg::this_cluster().sync();
+    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+}
+
+// What walks a unit: a cluster where whole CTAs would leave SMs without one and a unit has several tokens for each of the cluster's
+// threads, a CTA where a unit has several tokens for each of its threads, a warp otherwise.
+int span_of(int M, int units, int num_sms) {
+    const int each = M / units;
+    if (units * 2 <= num_sms && each >= 2 * kThreads) return kClusterSpan;
+    return each >= 2 * kThreads || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
+}
+
+template <class Args>
+cudaError_t launch_spans(void (*warp)(Args), void (*cta)(Args), void (*cluster)(Args), const Args& p, int M, int units, int num_sms,
+                         cudaStream_t stream) {
+    const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
+    switch (span_of(M, units, num_sms)) {
+        case kWarpSpan: {
+            const int grid = (units + kWarps - 1) / kWarps;
+            return launch_pdl(warp, dim3(grid < most ? grid : most), kThreads, 0, stream, p);
+        }
+        case kCtaSpan: return launch_pdl(cta, dim3(units < most ? units : most), kThreads, 0, stream, p);
+        default: {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            pair_launch_config(cfg, attr, dim3(units * kClusterCtas), kThreads, 0, stream);
+            attr[1].val.clusterDim.x = kClusterCtas;
+            return cudaLaunchKernelEx(&cfg, cluster, p);
+        }
+    }
+}
+
+}  // namespace
+
+size_t token_loss_workspace_bytes() { return sizeof(LossSpace); }
+
+ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, cudaStream_t stream) {
+    cudaError_t e;
+    if (p.seq_start) {
+        e = launch_spans<PolicyArgs>(policy_sequences_kernel<kWarpSpan>, policy_sequences_kernel<kCtaSpan>, policy_sequences_kernel<kClusterSpan>, p,
+                                     p.M, p.S, num_sms, stream);
+    } else {
+        const long long need = ((long long)p.M + kThreads - 1) / kThreads;
+        const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
+        e = launch_pdl(policy_tokens_kernel, dim3(need < most ? (int)need : most), kThreads, 0, stream, p);
+    }
+    return e == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, cudaStream_t stream) {
+    return launch_spans<PreferenceArgs>(preference_kernel<kWarpSpan>, preference_kernel<kCtaSpan>, preference_kernel<kClusterSpan>, p, p.M, p.P, num_sms,
+                                        stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+}
+
+}  // namespace ee
