@@ -146,7 +146,8 @@ size_t fp4_stream_parts_bytes(int M);
 ee_status fp4_stream_launch(const Fp4Head& p, int group, void* parts, int num_sms, int device, cudaStream_t stream);
 
 // Many rows (fp4_gemm.cu): activations as the M operand, 128 rows to a tile.
+int fp4_gemm_act_tiles(int M);                   // tiles of activations, the last of them perhaps unused
 size_t fp4_gemm_parts_bytes(int M, int V);
-ee_status fp4_gemm_launch(const Fp4Head& p, int group, void* parts, int num_sms, int device, cudaStream_t stream);
+ee_status fp4_gemm_launch(const Fp4Head& p, int group, void* parts, int device, cudaStream_t stream);
 
 }  // namespace ee

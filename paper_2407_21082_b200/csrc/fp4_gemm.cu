@@ -12,6 +12,7 @@
 #include "kernels.h"
 #include "sm100_fp4.cuh"
 #include "sm100_operands.cuh"
+#include "tensor_map.h"
 
 namespace ee {
 
@@ -19,36 +20,49 @@ namespace {
 
 constexpr int kThreads = 320;
 constexpr int kFoldWarps = 8;
-constexpr int kUnits = 2;                        // units per stage and operand
+constexpr int kUnits = 2;                        // units of weights per stage
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
-constexpr int kMaxWorkers = 256;
+constexpr int kMaxPairs = 128;
 constexpr int kMergeThreads = 256;
-constexpr int kBarBytes = 256;
+constexpr int kBarBytes = 512;
+constexpr size_t kSmemBudget = 226 * 1024;
+constexpr int kResidentBlocks = 20;              // units of a row tile that stay in shared memory
+constexpr int kMaxStages = 16;
 
+struct GemmMaps {
+    CUtensorMap acts, weights, scales;           // boxes: a unit; the half of two units' elements that a CTA loads; two units' scales
+};
 struct GemmParams {
     Fp4Head q;
     RestState* parts;              // [row][slot][half of the columns]
-    int m_tiles, n_tiles, slots;
+    int m_pairs, n_tiles, slots, n_stages;
 };
 
-template <int kGroup>
+// kResident: the activations of a row tile stay in shared memory, and their scales in tensor memory, while the weights pass by.
+template <int kGroup, bool kResident>
 struct Shape {
-    static constexpr int kUnit = fp4_unit_bytes(kGroup, kFp4Rows);
-    static constexpr int kOperandBytes = kUnits * kUnit;
-    static constexpr int kStageBytes = (2 * kOperandBytes + 1023) / 1024 * 1024;
-    static constexpr int kScaleCols = kUnits * fp4_scale_bytes(kGroup) / 512 * 8;
-    static constexpr int kStages = 6;
-    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kBarBytes + 1024;
-    static_assert(2 * kAccCols + kStages * kScaleCols <= kTmemCols && kSmem <= 227 * 1024, "fits");
+    static constexpr int kUnit = fp4_unit_bytes(kGroup, kFp4Rows), kScales = fp4_scale_bytes(kGroup), kHalf = kFp4Rows * kFp4Cols / 4;
+    static constexpr int kActBytes = kResident ? 0 : kUnits * kUnit;           // of a stage
+    static constexpr int kStageBytes = kActBytes + kUnits * (kHalf + kScales);
+    static constexpr int kAtoms = kScales / 512;
+    static constexpr int kUnitCols = kAtoms * 4;                               // of a unit's scales in tensor memory
+    static constexpr int kActCols = kResident ? kResidentBlocks * kUnitCols : 0;
+    static constexpr int kStageCols = kUnits * kUnitCols * (kResident ? 1 : 2);
+    static constexpr int kByTmem = (kTmemCols - 2 * kAccCols - kActCols) / kStageCols;
+    static int stages(int blocks) {
+        const int fit = (int)(kSmemBudget - kBarBytes - 1024 - (kResident ? blocks * kUnit : 0)) / kStageBytes;
+        return fit < kByTmem ? (fit < kMaxStages ? fit : kMaxStages) : (kByTmem < kMaxStages ? kByTmem : kMaxStages);
+    }
+    static size_t smem(int blocks) { return (size_t)stages(blocks) * kStageBytes + (kResident ? blocks * kUnit : 0) + kBarBytes + 1024; }
 };
 
 // The run of tiles of worker w of n, and the worker that has tile t.
 __host__ __device__ inline long long run_begin(int w, int n, long long total) { return (long long)w * total / n; }
 __host__ __device__ inline int worker_of(long long t, int n, long long total) { return (int)(((t + 1) * n - 1) / total); }
 // Workers that share a row tile, at most.
-int max_slots(int m_tiles, int n_tiles, int workers) {
-    const long long total = (long long)m_tiles * n_tiles, each = total / workers > 0 ? total / workers : 1;
+int max_slots(int m_pairs, int n_tiles, int workers) {
+    const long long total = (long long)m_pairs * n_tiles, each = total / workers > 0 ? total / workers : 1;
     return (int)((n_tiles + each - 1) / each) + 1;
 }
 
@@ -108,128 +122,183 @@ __device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[32], 
     add_terms<false>(st, v, c, j0, nvalid);
 }
 
-template <int kGroup>
-__global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const GemmParams p) {
-    using S = Shape<kGroup>;
+template <int kGroup, bool kResident>
+__global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
+    using S = Shape<kGroup, kResident>;
     const Fp4Head& q = p.q;
+    const int rank = (int)ptx::cluster_cta_rank(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+    const int n_stages = p.n_stages;
     const int blocks = fp4_blocks(q.d), steps = (blocks + kUnits - 1) / kUnits;
-    const long long total = (long long)p.m_tiles * p.n_tiles;
-    const long long begin = run_begin(blockIdx.x, gridDim.x, total), end = run_begin(blockIdx.x + 1, gridDim.x, total);
+    const long long total = (long long)p.m_pairs * p.n_tiles;
+    const long long begin = run_begin(pair, pairs, total), end = run_begin(pair + 1, pairs, total);
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     unsigned char* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
-    const uint32_t ring = ptx::smem_addr(smem);
-    unsigned char* bar_mem = smem + S::kStages * S::kStageBytes;
+    const uint32_t ring = ptx::smem_addr(smem), resident = ring + n_stages * S::kStageBytes;
+    unsigned char* bar_mem = smem + n_stages * S::kStageBytes + (kResident ? blocks * S::kUnit : 0);
     const uint32_t bar_base = ptx::smem_addr(bar_mem);
-    auto full_bar = [&](int s) { return bar_base + 8u * s; };
-    auto empty_bar = [&](int s) { return bar_base + 8u * (S::kStages + s); };
-    auto accfull_bar = [&](int b) { return bar_base + 8u * (2 * S::kStages + b); };
-    auto accfree_bar = [&](int b) { return bar_base + 8u * (2 * S::kStages + 2 + b); };
-    const uint32_t drain_bar = bar_base + 8u * (2 * S::kStages + 4);
-    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + 8 * (2 * S::kStages + 5));
+    auto full_bar = [&](int s) { return bar_base + 8u * s; };                            // in rank 0: both CTAs' loads have landed
+    auto empty_bar = [&](int s) { return bar_base + 8u * (kMaxStages + s); };
+    auto act_bar = [&](int u) { return bar_base + 8u * (2 * kMaxStages + u); };          // in rank 0, likewise
+    const uint32_t act_free = bar_base + 8u * (2 * kMaxStages + kResidentBlocks);
+    auto accfull_bar = [&](int b) { return act_free + 8u * (1 + b); };
+    auto accfree_bar = [&](int b) { return act_free + 8u * (3 + b); };                   // in rank 0: both CTAs' epilogues
+    const uint32_t drain_bar = act_free + 8u * 5;
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + 8 * (2 * kMaxStages + kResidentBlocks + 6));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+    static_assert(8 * (2 * kMaxStages + kResidentBlocks + 6) + 8 <= kBarBytes, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < n_stages; ++s) {
             ptx::mbar_init(full_bar(s), 1);
             ptx::mbar_init(empty_bar(s), 1);
         }
+        for (int u = 0; u < kResidentBlocks; ++u) ptx::mbar_init(act_bar(u), 1);
+        ptx::mbar_init(act_free, 1);
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(accfull_bar(b), 1);
-            ptx::mbar_init(accfree_bar(b), kFoldWarps);
+            ptx::mbar_init(accfree_bar(b), 2 * kFoldWarps);
         }
         ptx::mbar_init(drain_bar, 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
+        ptx::prefetch_tensormap(&maps.acts);
+        ptx::prefetch_tensormap(&maps.weights);
+        ptx::prefetch_tensormap(&maps.scales);
     }
     if (warp == 1) {
-        ptx::tmem_alloc(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), kTmemCols);
-        ptx::tmem_relinquish();
+        ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), kTmemCols);
+        ptx::tmem_relinquish_pair();
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
+    ptx::cluster_sync_all();                              // the partner's barriers exist before anything signals them
     ptx::tc_fence_after_sync();
-    const uint32_t tmem_base = *tmem_holder, scales_base = tmem_base + 2 * kAccCols;
+    const uint32_t tmem_base = *tmem_holder, act_cols = tmem_base + 2 * kAccCols, stage_cols = act_cols + S::kActCols;
 
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
         if (lane == 0) {
-            int stage = 0;
+            int stage = 0, fills = 0;
             uint32_t phase = 0, armed = 0, armed_parity = 0;
+            long long m_before = -1;
             bool ok = true;
             grid_dependency_wait();
             for (long long t = begin; ok && t < end; ++t) {
                 if (t + 1 == end) launch_dependents();
-                const size_t m_tile = (size_t)(t / p.n_tiles), n_tile = (size_t)(t - (long long)m_tile * p.n_tiles);
+                const long long m_pair = t / p.n_tiles;
+                const int n_tile = (int)(t - m_pair * p.n_tiles), act_unit = (int)(2 * m_pair + rank) * blocks;
+                const bool fresh = kResident && m_pair != m_before;
+                if (fresh) {
+                    // the products of the row tile before have read their activations
+                    if (fills > 0 && !ptx::mbar_wait(act_free, (uint32_t)(fills - 1) & 1u, abort_flag)) {
+                        record_failure(q.ctrl, abort_flag, 1, 0x80, (unsigned)t);
+                        break;
+                    }
+                    ++fills;
+                    m_before = m_pair;
+                }
                 for (int step = 0; step < steps; ++step) {
                     if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {
                         record_failure(q.ctrl, abort_flag, 1, stage, (unsigned)t);
                         ok = false;
                         break;
                     }
-                    const uint32_t bytes = (uint32_t)min(kUnits, blocks - step * kUnits) * S::kUnit, to = ring + stage * S::kStageBytes;
-                    ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * bytes);
-                    ptx::bulk_load(to, q.acts + (m_tile * blocks + step * kUnits) * S::kUnit, bytes, full_bar(stage));
-                    ptx::bulk_load(to + S::kOperandBytes, q.weights + (n_tile * blocks + step * kUnits) * S::kUnit, bytes, full_bar(stage));
+                    const int u0 = step * kUnits;
+                    if (fresh)
+                        for (int u = u0; u < min(u0 + kUnits, blocks); ++u) {
+                            if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kUnit);
+                            ptx::tma_load_3d_pair(resident + u * S::kUnit, &maps.acts, 0, 0, act_unit + u, ptx::map_to_cta(act_bar(u), 0));
+                        }
+                    const uint32_t to = ring + stage * S::kStageBytes, bar = ptx::map_to_cta(full_bar(stage), 0);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * S::kStageBytes);
+                    const int unit = n_tile * blocks + u0;
+                    ptx::tma_load_3d_pair(to, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit, bar);
+                    ptx::tma_load_3d_pair(to + kUnits * S::kHalf, &maps.scales, 0, 0, unit, bar);
+                    if (!kResident)
+                        for (int u = 0; u < kUnits; ++u)
+                            ptx::tma_load_3d_pair(to + kUnits * (S::kHalf + S::kScales) + u * S::kUnit, &maps.acts, 0, 0, act_unit + u0 + u, bar);
                     armed |= 1u << stage;
                     armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
-                    if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                 }
             }
-            if (*abort_flag) producer_drain(0, S::kStages, full_bar(0), armed, armed_parity);
+            if (*abort_flag) {
+                producer_drain(rank, n_stages, full_bar(0), armed, armed_parity);
+                if (kResident && rank == 0 && fills > 0) producer_drain(0, blocks, act_bar(0), (1u << blocks) - 1u, (fills - 1) & 1 ? ~0u : 0u);
+            }
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---------------------------------------------------------------- products
-        if (lane == 0) {
-            constexpr uint32_t idesc = ptx::idesc_fp4<kGroup>(kFp4Rows, kFp4Rows);
-            constexpr int kAtoms = fp4_scale_bytes(kGroup) / 512;
-            int stage = 0;
+        // ---------------------------------------------------------------- products (rank 0: the whole warp, one lane of it issuing)
+        if (rank == 0) {
+            constexpr uint32_t idesc = ptx::idesc_fp4<kGroup>(2 * kFp4Rows, kFp4Rows);
+            int stage = 0, fills = 0;
             uint32_t phase = 0;
+            long long m_before = -1;
             bool ok = true;
             for (long long t = begin; ok && t < end; ++t) {
                 const int local = (int)(t - begin), buf = local & 1;
-                if (!ptx::mbar_wait(accfree_bar(buf), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag)) {
-                    record_failure(q.ctrl, abort_flag, 2, 0x80 | buf, (unsigned)t);
+                const long long m_pair = t / p.n_tiles;
+                const bool fresh = kResident && m_pair != m_before;
+                const bool last_of_rows = kResident && t + 1 < end && (t + 1) / p.n_tiles != m_pair;
+                if (fresh) {
+                    ++fills;
+                    m_before = m_pair;
+                }
+                if (!__all_sync(0xffffffffu, ptx::mbar_wait(accfree_bar(buf), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag))) {
+                    if (lane == 0) record_failure(q.ctrl, abort_flag, 2, 0x80 | buf, (unsigned)t);
                     break;
                 }
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem_base + buf * kAccCols;
                 for (int step = 0; step < steps; ++step) {
-                    if (!ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
-                        record_failure(q.ctrl, abort_flag, 2, stage, (unsigned)t);
+                    const int n = min(kUnits, blocks - step * kUnits);
+                    bool landed = ptx::mbar_wait(full_bar(stage), phase, abort_flag);
+                    if (fresh)
+                        for (int u = 0; u < n; ++u) landed = landed && ptx::mbar_wait(act_bar(step * kUnits + u), (uint32_t)(fills - 1) & 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, landed)) {
+                        if (lane == 0) record_failure(q.ctrl, abort_flag, 2, stage, (unsigned)t);
                         ok = false;
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t x = ring + stage * S::kStageBytes, w = x + S::kOperandBytes;
-                    const uint32_t scales = scales_base + stage * S::kScaleCols;
+                    const uint32_t w = ring + stage * S::kStageBytes, w_scales = w + kUnits * S::kHalf;
+                    const uint32_t x = kResident ? resident + step * kUnits * S::kUnit : w_scales + kUnits * S::kScales;
+                    const uint32_t w_cols = stage_cols + stage * S::kStageCols;
+                    const uint32_t x_cols = kResident ? act_cols + step * kUnits * S::kUnitCols : w_cols + kUnits * S::kUnitCols;
+                    if (ptx::elect_one()) {
 #pragma unroll
-                    for (int u = 0; u < kUnits; ++u) {
-                        if (step * kUnits + u < blocks) {
-                            const uint32_t xu = x + u * S::kUnit, wu = w + u * S::kUnit, su = scales + u * kAtoms * 8;
+                        for (int u = 0; u < kUnits; ++u) {
+                            if (u < n) {
+                                const uint32_t xu = x + u * S::kUnit, xc = x_cols + u * S::kUnitCols, wc = w_cols + u * S::kUnitCols;
 #pragma unroll
-                            for (int k = 0; k < kAtoms; ++k) {
-                                ptx::tmem_cp_scales(su + 8 * k, ptx::smem_desc_scales(xu + 512 * k));
-                                ptx::tmem_cp_scales(su + 8 * k + 4, ptx::smem_desc_scales(wu + 512 * k));
-                            }
-                            const uint64_t a = ptx::smem_desc_k64(xu + fp4_scale_bytes(kGroup)), b = ptx::smem_desc_k64(wu + fp4_scale_bytes(kGroup));
+                                for (int k = 0; k < S::kAtoms; ++k) {
+                                    if (!kResident || fresh) ptx::tmem_cp_scales<true>(xc + 4 * k, ptx::smem_desc_scales(xu + 512 * k));
+                                    ptx::tmem_cp_scales<true>(wc + 4 * k, ptx::smem_desc_scales(w_scales + u * S::kScales + 512 * k));
+                                }
+                                const uint64_t a = ptx::smem_desc_k64(xu + S::kScales), b = ptx::smem_desc_k64(w + u * S::kHalf);
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {                // 64 columns are 32 bytes, 2 descriptor units
-                                const uint32_t sk = su + (kGroup == 16 ? 8 * k : 0);
-                                const uint32_t which = kGroup == 32 && k == 1 ? ptx::kIdescFp4SecondHalf : 0u;
-                                ptx::mma_fp4<kGroup>(acc, a + 2u * k, b + 2u * k, idesc | which, sk, sk + 4, step > 0 || u > 0 || k > 0 ? 1u : 0u);
+                                for (int k = 0; k < 2; ++k) {            // 64 columns are 32 bytes, 2 descriptor units
+                                    const uint32_t at = kGroup == 16 ? 4 * k : 0;
+                                    const uint32_t which = kGroup == 32 && k == 1 ? ptx::kIdescFp4SecondHalf : 0u;
+                                    ptx::mma_fp4<kGroup, true>(acc, a + 2u * k, b + 2u * k, idesc | which, xc + at, wc + at, step > 0 || u > 0 || k > 0 ? 1u : 0u);
+                                }
                             }
                         }
+                        ptx::mma_commit_pair(empty_bar(stage), 3);
+                        if (step + 1 == steps) {
+                            ptx::mma_commit_pair(accfull_bar(buf), 3);
+                            if (last_of_rows) ptx::mma_commit_pair(act_free, 3);
+                        }
                     }
-                    ptx::mma_commit(empty_bar(stage));
-                    if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
+                    __syncwarp();
+                    if (++stage == n_stages) { stage = 0; phase ^= 1u; }
                 }
-                if (ok) ptx::mma_commit(accfull_bar(buf));
             }
-            if (*abort_flag) mma_drain<false>(drain_bar);
+            if (lane == 0 && *abort_flag) mma_drain<true>(drain_bar);
+            __syncwarp();
         }
-        __syncwarp();
     } else {
         // ---------------------------------------------------------------- states
         const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -238,19 +307,19 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const GemmParams 
         const float weight_factor = ld_dep(q.weight_factor);
         float factor = 0.f, c = 0.f;
         int m_before = -1;
-        auto flush = [&](int m_tile) {
-            const long long row = (long long)m_tile * kFp4Rows + quarter * 32 + lane;
-            const int slot = (int)blockIdx.x - worker_of((long long)m_tile * p.n_tiles, gridDim.x, total);
+        auto flush = [&](int m_pair) {
+            const long long row = (2ll * m_pair + rank) * kFp4Rows + quarter * 32 + lane;
+            const int slot = pair - worker_of((long long)m_pair * p.n_tiles, pairs, total);
             if (row < q.M) p.parts[(row * p.slots + slot) * 2 + half] = RestState{st.m * factor, st.s, st.t * factor, st.idx};
             st = rest_empty();
         };
         for (long long t = begin; t < end; ++t) {
             const int local = (int)(t - begin), buf = local & 1;
-            const int m_tile = (int)(t / p.n_tiles), n_tile = (int)(t - (long long)m_tile * p.n_tiles);
-            if (m_tile != m_before) {
+            const int m_pair = (int)(t / p.n_tiles), n_tile = (int)(t - (long long)m_pair * p.n_tiles);
+            if (m_pair != m_before) {
                 if (m_before >= 0) flush(m_before);
-                m_before = m_tile;
-                const long long row = (long long)m_tile * kFp4Rows + quarter * 32 + lane;
+                m_before = m_pair;
+                const long long row = (2ll * m_pair + rank) * kFp4Rows + quarter * 32 + lane;
                 factor = row < q.M ? ld_dep(q.factor + row) * weight_factor : 1.f;
                 c = factor * kLog2e;
             }
@@ -270,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const GemmParams 
                 if (k == 1) {
                     ptx::tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(accfree_bar(buf));
+                    if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
                 }
                 const int nvalid = q.V - (col0 + 32 * k);
                 if (nvalid > 0) fold_chunk(st, v, c, col0 + 32 * k, nvalid);
@@ -281,21 +350,23 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const GemmParams 
     if (warp < 2) grid_dependency_wait();
     ptx::tc_fence_before_sync();
     __syncthreads();
+    ptx::cluster_sync_all();                              // neither CTA leaves while the other may still signal it or write its accumulators
     if (warp == 1) {
+        __syncwarp();
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc(tmem_base, kTmemCols);
+        ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
     }
 }
 
-// A warp per row: the states of the workers that shared its tile.
-__global__ void __launch_bounds__(kMergeThreads) fp4_merge_kernel(const GemmParams p, int workers) {
+// A warp per row: the states of the pairs that shared its tile.
+__global__ void __launch_bounds__(kMergeThreads) fp4_merge_kernel(const GemmParams p, int pairs) {
     launch_dependents();
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5);
     if (row >= p.q.M) return;
-    const long long total = (long long)p.m_tiles * p.n_tiles, first = row / kFp4Rows * p.n_tiles;
-    const int n = 2 * (worker_of(first + p.n_tiles - 1, workers, total) - worker_of(first, workers, total) + 1);
+    const long long total = (long long)p.m_pairs * p.n_tiles, first = row / (2 * kFp4Rows) * p.n_tiles;
+    const int n = 2 * (worker_of(first + p.n_tiles - 1, pairs, total) - worker_of(first, pairs, total) + 1);
     const RestState* parts = p.parts + row * p.slots * 2;
     RestState mine = rest_empty();
     for (int k = lane; k < n; k += 32) rest_merge(mine, rest_load_cg(parts + k));
@@ -303,40 +374,79 @@ __global__ void __launch_bounds__(kMergeThreads) fp4_merge_kernel(const GemmPara
     if (lane == 0) rest_finish(all, p.q, (int)row);
 }
 
-template <int kGroup>
-ee_status launch_group(GemmParams p, int workers, int device, cudaStream_t stream) {
-    using S = Shape<kGroup>;
-    static bool configured[kMaxDevices] = {};
-    if (!configured[device]) {
-        if (cudaFuncSetAttribute(fp4_gemm_kernel<kGroup>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem) != cudaSuccess) return EE_ERR_CUDA;
-        configured[device] = true;
-    }
-    if (launch_pdl(fp4_gemm_kernel<kGroup>, dim3(workers), kThreads, S::kSmem, stream, p) != cudaSuccess) return EE_ERR_CUDA;
-    const int rows = kMergeThreads / 32;
-    return launch_pdl(fp4_merge_kernel, dim3((p.q.M + rows - 1) / rows), kMergeThreads, 0, stream, p, workers) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+// Units of 128 rows as [units][lines of 128 bytes], boxes of `lines` of `units` neighbouring units.
+bool make_unit_map(CUtensorMap* map, const void* base, int group, long long n_units, int lines, int units) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t unit = fp4_unit_bytes(group, kFp4Rows);
+    const cuuint64_t dims[3] = {128u, unit / 128, (cuuint64_t)n_units};
+    const cuuint64_t strides[2] = {128u, unit};
+    const cuuint32_t box[3] = {128u, (cuuint32_t)lines, (cuuint32_t)units};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int workers_of(long long total, int num_sms) {
-    const int most = num_sms < kMaxWorkers ? num_sms : kMaxWorkers;
-    return total < most ? (int)total : most;
+// Pairs of CTAs the device runs at once; 0 if the query fails.
+template <int kGroup, bool kResident>
+int resident_pairs(int device) {
+    static int pairs[kMaxDevices];
+    static bool asked[kMaxDevices] = {};
+    if (!asked[device]) {
+        int n = 0;
+        if (cudaFuncSetAttribute(fp4_gemm_kernel<kGroup, kResident>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget) == cudaSuccess) {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            pair_launch_config(cfg, attr, dim3(2), kThreads, kSmemBudget, nullptr);
+            if (cudaOccupancyMaxActiveClusters(&n, fp4_gemm_kernel<kGroup, kResident>, &cfg) != cudaSuccess) {
+                n = 0;
+                (void)cudaGetLastError();
+            }
+        }
+        pairs[device] = n < kMaxPairs ? n : kMaxPairs;
+        asked[device] = true;
+    }
+    return pairs[device];
+}
+
+int pairs_of(long long total, int most) { return total < most ? (int)total : most; }
+
+template <int kGroup, bool kResident>
+ee_status launch_shape(GemmParams p, int device, cudaStream_t stream) {
+    using S = Shape<kGroup, kResident>;
+    const int most = resident_pairs<kGroup, kResident>(device);
+    if (most == 0) return EE_ERR_CUDA;
+    const int blocks = fp4_blocks(p.q.d), pairs = pairs_of((long long)p.m_pairs * p.n_tiles, most);
+    p.slots = max_slots(p.m_pairs, p.n_tiles, pairs);
+    p.n_stages = S::stages(blocks);
+    GemmMaps maps;
+    if (!make_unit_map(&maps.acts, p.q.acts, kGroup, 2ll * p.m_pairs * blocks, S::kUnit / 128, 1) ||
+        !make_unit_map(&maps.weights, p.q.weights, kGroup, (long long)p.n_tiles * blocks, S::kHalf / 128, kUnits) ||
+        !make_unit_map(&maps.scales, p.q.weights, kGroup, (long long)p.n_tiles * blocks, S::kScales / 128, kUnits))
+        return EE_ERR_CUDA;
+    if (launch_pdl_pairs(fp4_gemm_kernel<kGroup, kResident>, dim3(2 * pairs), kThreads, S::smem(blocks), stream, maps, p) != cudaSuccess) return EE_ERR_CUDA;
+    const int rows = kMergeThreads / 32;
+    return launch_pdl(fp4_merge_kernel, dim3((p.q.M + rows - 1) / rows), kMergeThreads, 0, stream, p, pairs) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t fp4_gemm_parts_bytes(int M, int V) {      // for any number of SMs
-    const int m_tiles = fp4_tiles(M, kFp4Rows), n_tiles = fp4_tiles(V, kFp4Rows);
-    return (size_t)M * max_slots(m_tiles, n_tiles, workers_of((long long)m_tiles * n_tiles, kMaxWorkers)) * 2 * sizeof(RestState);
+int fp4_gemm_act_tiles(int M) { return (fp4_tiles(M, kFp4Rows) + 1) / 2 * 2; }
+
+size_t fp4_gemm_parts_bytes(int M, int V) {      // for any number of pairs
+    const int m_pairs = fp4_gemm_act_tiles(M) / 2, n_tiles = fp4_tiles(V, kFp4Rows);
+    return (size_t)M * max_slots(m_pairs, n_tiles, pairs_of((long long)m_pairs * n_tiles, kMaxPairs)) * 2 * sizeof(RestState);
 }
 
-ee_status fp4_gemm_launch(const Fp4Head& q, int group, void* parts, int num_sms, int device, cudaStream_t stream) {
+ee_status fp4_gemm_launch(const Fp4Head& q, int group, void* parts, int device, cudaStream_t stream) {
     GemmParams p;
     p.q = q;
     p.parts = static_cast<RestState*>(parts);
-    p.m_tiles = fp4_tiles(q.M, kFp4Rows);
+    p.m_pairs = fp4_gemm_act_tiles(q.M) / 2;
     p.n_tiles = fp4_tiles(q.V, kFp4Rows);
-    const int workers = workers_of((long long)p.m_tiles * p.n_tiles, num_sms);
-    p.slots = max_slots(p.m_tiles, p.n_tiles, workers);
-    return group == 16 ? launch_group<16>(p, workers, device, stream) : launch_group<32>(p, workers, device, stream);
+    const bool fits = fp4_blocks(q.d) <= kResidentBlocks;
+    if (group == 16) return fits ? launch_shape<16, true>(p, device, stream) : launch_shape<16, false>(p, device, stream);
+    return fits ? launch_shape<32, true>(p, device, stream) : launch_shape<32, false>(p, device, stream);
 }
 
 }  // namespace ee

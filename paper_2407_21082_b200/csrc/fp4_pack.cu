@@ -226,9 +226,10 @@ struct HeadSpace {
 HeadSpace head_space(int M, int d, int V, int group) {
     HeadSpace s;
     const int rows = M <= kFp4StreamRows ? fp4_stream_padded(M) : kFp4Rows;
+    const int tiles = M <= kFp4StreamRows ? 1 : fp4_gemm_act_tiles(M);
     s.factor = kCtrlBytes;
     s.acts = align_up(s.factor + (size_t)M * sizeof(float), 1024);
-    s.parts = align_up(s.acts + (size_t)fp4_tiles(M, rows) * fp4_blocks(d) * fp4_unit_bytes(group, rows), 256);
+    s.parts = align_up(s.acts + (size_t)tiles * fp4_blocks(d) * fp4_unit_bytes(group, rows), 256);
     s.total = s.parts + (M <= kFp4StreamRows ? fp4_stream_parts_bytes(M) : fp4_gemm_parts_bytes(M, V));
     return s;
 }
@@ -284,7 +285,7 @@ ee_status fp4_head_launch(const HeadArgs& a, const void* fp4, int group) {
     p.argmax = a.argmax; p.entropy = a.entropy; p.maxprob = a.maxprob; p.exit_mask = a.exit_mask;
     p.ctrl = reinterpret_cast<Control*>(a.workspace);
     return few ? fp4_stream_launch(p, group, ws + s.parts, a.num_sms, a.device, a.stream)
-               : fp4_gemm_launch(p, group, ws + s.parts, a.num_sms, a.device, a.stream);
+               : fp4_gemm_launch(p, group, ws + s.parts, a.device, a.stream);
 }
 
 }  // namespace ee

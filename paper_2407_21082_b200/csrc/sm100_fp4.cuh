@@ -32,10 +32,12 @@ __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t saddr) {
     d |= (uint64_t)1 << 46;
     return d;
 }
-// 512 bytes of scales to four columns of tensor memory, the same in all four quarters of its lanes.  Products issued behind it by the same
-// thread see it.
+// 512 bytes of scales to four columns of tensor memory, the same in all four quarters of its lanes (kPair: in each CTA of a pair from its own
+// shared memory to its own tensor memory).  Products issued behind it by the same thread see it.
+template <bool kPair = false>
 __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
 // Instruction descriptor of kind::mxf4nvf4: A and B e2m1 (1 in bits [7,10) and [10,13)), both K-major, N >> 3 in bits [17,23), the scales'
@@ -47,23 +49,22 @@ __host__ __device__ constexpr uint32_t idesc_fp4(int m, int n) {
 }
 constexpr uint32_t kIdescFp4SecondHalf = (2u << 4) | (2u << 29);
 
-// D[tmem] (+)= (A scales_a)[smem] * (B scales_b)[smem], fp32 accumulation; issued by one thread.
-template <int kGroup>
+// D[tmem] (+)= (A scales_a)[smem] * (B scales_b)[smem], fp32 accumulation; issued by one thread (of rank 0 of a pair: each CTA has its 128 rows
+// of A and of D and half of B's rows, and the scales of its own rows of A and of all of B).
+#define EE_MMA_FP4(cta_group, scale_vec)                                                                                                      \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                                           \
+                 "tcgen05.mma.cta_group::" cta_group ".kind::mxf4nvf4.block_scale.scale_vec::" scale_vec " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)                           \
+                 : "memory")
+template <int kGroup, bool kPair = false>
 __device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t scales_a, uint32_t scales_b,
                                         uint32_t accumulate) {
-    if constexpr (kGroup == 16)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(scales_a), "r"(scales_b), "r"(accumulate)
-            : "memory");
+    if constexpr (kGroup == 16 && kPair) EE_MMA_FP4("2", "4X");
+    else if constexpr (kGroup == 16) EE_MMA_FP4("1", "4X");
+    else if constexpr (kPair) EE_MMA_FP4("2", "2X");
+    else EE_MMA_FP4("1", "2X");
 }
+#undef EE_MMA_FP4
 
 }  // namespace ptx
 }  // namespace ee
