@@ -20,18 +20,19 @@ namespace {
 
 constexpr int kThreads = 320;
 constexpr int kFoldWarps = 8;
-constexpr int kUnits = 2;                        // units of weights per stage
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
 constexpr int kMaxPairs = 128;
 constexpr int kMergeThreads = 256;
-constexpr int kBarBytes = 512;
+constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
-constexpr int kResidentBlocks = 20;              // units of a row tile that stay in shared memory
-constexpr int kMaxStages = 16;
+constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
+constexpr int kMaxStages = 24;
 
 struct GemmMaps {
-    CUtensorMap acts, weights, scales;           // boxes: a unit; the half of two units' elements that a CTA loads; two units' scales
+    // boxes: a weight unit's scales, the half of its elements that a CTA loads; a unit of activations (or its elements alone), the scales of
+    // several
+    CUtensorMap scales, weights, acts, act_scales;
 };
 struct GemmParams {
     Fp4Head q;
@@ -39,22 +40,25 @@ struct GemmParams {
     int m_pairs, n_tiles, slots, n_stages;
 };
 
-// kResident: the activations of a row tile stay in shared memory, and their scales in tensor memory, while the weights pass by.
+// A stage of the ring holds 128 columns: the CTA's half of a weight unit and all its scales, and, unless they are resident, a unit of activations.
+// kResident: the elements of a row tile's activations stay in shared memory, and their scales, which come through the ring as well, in tensor
+// memory, while the weights pass by.
 template <int kGroup, bool kResident>
 struct Shape {
-    static constexpr int kUnit = fp4_unit_bytes(kGroup, kFp4Rows), kScales = fp4_scale_bytes(kGroup), kHalf = kFp4Rows * kFp4Cols / 4;
-    static constexpr int kActBytes = kResident ? 0 : kUnits * kUnit;           // of a stage
-    static constexpr int kStageBytes = kActBytes + kUnits * (kHalf + kScales);
+    static constexpr int kUnit = fp4_unit_bytes(kGroup, kFp4Rows), kScales = fp4_scale_bytes(kGroup), kElements = kUnit - kScales, kHalf = kElements / 2;
+    static constexpr int kStageBytes = kHalf + kScales + (kResident ? 0 : kUnit);
     static constexpr int kAtoms = kScales / 512;
     static constexpr int kUnitCols = kAtoms * 4;                               // of a unit's scales in tensor memory
-    static constexpr int kActCols = kResident ? kResidentBlocks * kUnitCols : 0;
-    static constexpr int kStageCols = kUnits * kUnitCols * (kResident ? 1 : 2);
-    static constexpr int kByTmem = (kTmemCols - 2 * kAccCols - kActCols) / kStageCols;
+    static constexpr int kStageCols = kResident ? kUnitCols : 2 * kUnitCols;
+    static constexpr int kScaleUnits = kStageBytes / kScales;                  // whose scales one stage brings
+    static int resident_bytes(int blocks) { return kResident ? blocks * kElements : 0; }
     static int stages(int blocks) {
-        const int fit = (int)(kSmemBudget - kBarBytes - 1024 - (kResident ? blocks * kUnit : 0)) / kStageBytes;
-        return fit < kByTmem ? (fit < kMaxStages ? fit : kMaxStages) : (kByTmem < kMaxStages ? kByTmem : kMaxStages);
+        const int by_smem = (int)(kSmemBudget - kBarBytes - 1024 - resident_bytes(blocks)) / kStageBytes;
+        const int by_tmem = (kTmemCols - 2 * kAccCols - (kResident ? blocks * kUnitCols : 0)) / kStageCols;
+        const int fit = by_smem < by_tmem ? by_smem : by_tmem;
+        return fit < kMaxStages ? fit : kMaxStages;
     }
-    static size_t smem(int blocks) { return (size_t)stages(blocks) * kStageBytes + (kResident ? blocks * kUnit : 0) + kBarBytes + 1024; }
+    static size_t smem(int blocks) { return (size_t)stages(blocks) * kStageBytes + resident_bytes(blocks) + kBarBytes + 1024; }
 };
 
 // The run of tiles of worker w of n, and the worker that has tile t.
@@ -127,15 +131,14 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
     using S = Shape<kGroup, kResident>;
     const Fp4Head& q = p.q;
     const int rank = (int)ptx::cluster_cta_rank(), pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
-    const int n_stages = p.n_stages;
-    const int blocks = fp4_blocks(q.d), steps = (blocks + kUnits - 1) / kUnits;
+    const int n_stages = p.n_stages, blocks = fp4_blocks(q.d);
     const long long total = (long long)p.m_pairs * p.n_tiles;
     const long long begin = run_begin(pair, pairs, total), end = run_begin(pair + 1, pairs, total);
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw_addr = ptx::smem_addr(smem_raw);
     unsigned char* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
     const uint32_t ring = ptx::smem_addr(smem), resident = ring + n_stages * S::kStageBytes;
-    unsigned char* bar_mem = smem + n_stages * S::kStageBytes + (kResident ? blocks * S::kUnit : 0);
+    unsigned char* bar_mem = smem + n_stages * S::kStageBytes + (kResident ? blocks * S::kElements : 0);
     const uint32_t bar_base = ptx::smem_addr(bar_mem);
     auto full_bar = [&](int s) { return bar_base + 8u * s; };                            // in rank 0: both CTAs' loads have landed
     auto empty_bar = [&](int s) { return bar_base + 8u * (kMaxStages + s); };
@@ -165,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         ptx::prefetch_tensormap(&maps.acts);
         ptx::prefetch_tensormap(&maps.weights);
         ptx::prefetch_tensormap(&maps.scales);
+        if (kResident) ptx::prefetch_tensormap(&maps.act_scales);
     }
     if (warp == 1) {
         ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), kTmemCols);
@@ -174,21 +178,41 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
     __syncthreads();
     ptx::cluster_sync_all();                              // the partner's barriers exist before anything signals them
     ptx::tc_fence_after_sync();
-    const uint32_t tmem_base = *tmem_holder, act_cols = tmem_base + 2 * kAccCols, stage_cols = act_cols + S::kActCols;
+    const uint32_t tmem_base = *tmem_holder, act_cols = tmem_base + 2 * kAccCols, stage_cols = act_cols + (kResident ? blocks * S::kUnitCols : 0);
 
+    // The two issuing threads have some hundred cycles per stage, at four to five per instruction of a single thread: positions in the ring are
+    // moved along by additions.
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
-        if (lane == 0) {
-            int stage = 0, fills = 0;
-            uint32_t phase = 0, armed = 0, armed_parity = 0;
-            long long m_before = -1;
+        if (ptx::elect_one()) {
+            const uint32_t ring_end = ring + n_stages * S::kStageBytes;
+            const uint32_t full0 = ptx::map_to_cta(full_bar(0), 0), act0 = ptx::map_to_cta(act_bar(0), 0);         // where loads report
+            uint32_t to = ring, full = full0, empty = empty_bar(0), phase = 1;
+            int fills = 0;
             bool ok = true;
+            auto next_stage = [&](unsigned what) {
+                if (ptx::mbar_wait(empty, phase, abort_flag)) return true;
+                record_failure(q.ctrl, abort_flag, 1, (to - ring) / S::kStageBytes, what);
+                return ok = false;
+            };
+            auto stage_done = [&]() {
+                to += S::kStageBytes;
+                full += 8;
+                empty += 8;
+                if (to == ring_end) {
+                    to = ring;
+                    full = full0;
+                    empty = empty_bar(0);
+                    phase ^= 1u;
+                }
+            };
             grid_dependency_wait();
+            long long m_pair = begin / p.n_tiles;
+            int n_tile = (int)(begin - m_pair * p.n_tiles);
+            bool fresh = kResident;
             for (long long t = begin; ok && t < end; ++t) {
                 if (t + 1 == end) launch_dependents();
-                const long long m_pair = t / p.n_tiles;
-                const int n_tile = (int)(t - m_pair * p.n_tiles), act_unit = (int)(2 * m_pair + rank) * blocks;
-                const bool fresh = kResident && m_pair != m_before;
+                const int act_unit = (int)(2 * m_pair + rank) * blocks;
                 if (fresh) {
                     // the products of the row tile before have read their activations
                     if (fills > 0 && !ptx::mbar_wait(act_free, (uint32_t)(fills - 1) & 1u, abort_flag)) {
@@ -196,109 +220,116 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                         break;
                     }
                     ++fills;
-                    m_before = m_pair;
-                }
-                for (int step = 0; step < steps; ++step) {
-                    if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {
-                        record_failure(q.ctrl, abort_flag, 1, stage, (unsigned)t);
-                        ok = false;
-                        break;
+                    for (int u0 = 0; u0 < blocks && next_stage((unsigned)t); u0 += S::kScaleUnits) {
+                        if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * S::kScaleUnits * S::kScales);
+                        ptx::tma_load_3d_pair(to, &maps.act_scales, 0, 0, act_unit + u0, full);
+                        stage_done();
                     }
-                    const int u0 = step * kUnits;
-                    if (fresh)
-                        for (int u = u0; u < min(u0 + kUnits, blocks); ++u) {
-                            if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kUnit);
-                            ptx::tma_load_3d_pair(resident + u * S::kUnit, &maps.acts, 0, 0, act_unit + u, ptx::map_to_cta(act_bar(u), 0));
-                        }
-                    const uint32_t to = ring + stage * S::kStageBytes, bar = ptx::map_to_cta(full_bar(stage), 0);
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(stage), 2 * S::kStageBytes);
-                    const int unit = n_tile * blocks + u0;
-                    ptx::tma_load_3d_pair(to, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit, bar);
-                    ptx::tma_load_3d_pair(to + kUnits * S::kHalf, &maps.scales, 0, 0, unit, bar);
-                    if (!kResident)
-                        for (int u = 0; u < kUnits; ++u)
-                            ptx::tma_load_3d_pair(to + kUnits * (S::kHalf + S::kScales) + u * S::kUnit, &maps.acts, 0, 0, act_unit + u0 + u, bar);
-                    armed |= 1u << stage;
-                    armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
-                    if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+                }
+                int unit = n_tile * blocks;
+                for (int u = 0; u < blocks && ok && next_stage((unsigned)t); ++u, ++unit) {
+                    if (fresh) {
+                        if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
+                        ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
+                    }
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * S::kStageBytes);
+                    ptx::tma_load_3d_pair(to, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit, full);
+                    ptx::tma_load_3d_pair(to + S::kHalf, &maps.scales, 0, 0, unit, full);
+                    if (!kResident) ptx::tma_load_3d_pair(to + S::kHalf + S::kScales, &maps.acts, 0, 0, act_unit + u, full);
+                    stage_done();
+                }
+                fresh = false;
+                if (++n_tile == p.n_tiles) {
+                    n_tile = 0;
+                    ++m_pair;
+                    fresh = kResident;
                 }
             }
-            if (*abort_flag) {
-                producer_drain(rank, n_stages, full_bar(0), armed, armed_parity);
-                if (kResident && rank == 0 && fills > 0) producer_drain(0, blocks, act_bar(0), (1u << blocks) - 1u, (fills - 1) & 1 ? ~0u : 0u);
+            if (*abort_flag) {                            // copies still in flight: of the stages' last or last but one fill, and of the activations
+                if (rank != 0) producer_drain(1, 0, 0, 0, 0);
+                else
+                    for (int i = 0; i < 10000; ++i) __nanosleep(1000);
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---------------------------------------------------------------- products (rank 0: the whole warp, one lane of it issuing)
-        if (rank == 0) {
+        // ---------------------------------------------------------------- products
+        if (rank == 0 && ptx::elect_one()) {
             constexpr uint32_t idesc = ptx::idesc_fp4<kGroup>(2 * kFp4Rows, kFp4Rows);
-            int stage = 0, fills = 0;
-            uint32_t phase = 0;
-            long long m_before = -1;
+            const uint32_t low0 = ptx::desc_low(ring), low_end = low0 + n_stages * (S::kStageBytes / 16), act_low = ptx::desc_low(resident);
+            uint32_t low = low0, cols = stage_cols, full = full_bar(0), empty = empty_bar(0), phase = 0;
+            uint32_t acc_phase = 1, act_phase = 1;
             bool ok = true;
+            auto landed = [&](uint32_t bar, uint32_t parity, unsigned what) {
+                if (ptx::mbar_wait(bar, parity, abort_flag)) return true;
+                record_failure(q.ctrl, abort_flag, 2, (bar - bar_base) / 8, what);
+                return ok = false;
+            };
+            auto stage_done = [&]() {                     // frees the stage, in both CTAs, once all products so far have been computed
+                ptx::mma_commit_pair(empty, 3);
+                low += S::kStageBytes / 16;
+                cols += S::kStageCols;
+                full += 8;
+                empty += 8;
+                if (low == low_end) {
+                    low = low0;
+                    cols = stage_cols;
+                    full = full_bar(0);
+                    empty = empty_bar(0);
+                    phase ^= 1u;
+                }
+            };
+            int n_tile = (int)(begin % p.n_tiles), buf = 0;
+            bool fresh = kResident;
             for (long long t = begin; ok && t < end; ++t) {
-                const int local = (int)(t - begin), buf = local & 1;
-                const long long m_pair = t / p.n_tiles;
-                const bool fresh = kResident && m_pair != m_before;
-                const bool last_of_rows = kResident && t + 1 < end && (t + 1) / p.n_tiles != m_pair;
                 if (fresh) {
-                    ++fills;
-                    m_before = m_pair;
+                    act_phase ^= 1u;
+                    for (int u0 = 0; u0 < blocks && landed(full, phase, (unsigned)t); u0 += S::kScaleUnits) {
+                        ptx::tc_fence_after_sync();
+                        for (int k = 0; k < min(S::kScaleUnits, blocks - u0) * S::kAtoms; ++k)
+                            ptx::tmem_cp_scales<true>(act_cols + u0 * S::kUnitCols + 4 * k, low + 32 * k);
+                        stage_done();
+                    }
                 }
-                if (!__all_sync(0xffffffffu, ptx::mbar_wait(accfree_bar(buf), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag))) {
-                    if (lane == 0) record_failure(q.ctrl, abort_flag, 2, 0x80 | buf, (unsigned)t);
-                    break;
-                }
+                if (!ok || !landed(accfree_bar(buf), acc_phase, (unsigned)t)) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem_base + buf * kAccCols;
-                for (int step = 0; step < steps; ++step) {
-                    const int n = min(kUnits, blocks - step * kUnits);
-                    bool landed = ptx::mbar_wait(full_bar(stage), phase, abort_flag);
-                    if (fresh)
-                        for (int u = 0; u < n; ++u) landed = landed && ptx::mbar_wait(act_bar(step * kUnits + u), (uint32_t)(fills - 1) & 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, landed)) {
-                        if (lane == 0) record_failure(q.ctrl, abort_flag, 2, stage, (unsigned)t);
-                        ok = false;
-                        break;
-                    }
+                uint32_t x_low = act_low, x_cols = act_cols;
+                for (int u = 0; u < blocks; ++u) {
+                    if (!landed(full, phase, (unsigned)t) || (fresh && !landed(act_bar(u), act_phase, (unsigned)t))) break;
                     ptx::tc_fence_after_sync();
-                    const uint32_t w = ring + stage * S::kStageBytes, w_scales = w + kUnits * S::kHalf;
-                    const uint32_t x = kResident ? resident + step * kUnits * S::kUnit : w_scales + kUnits * S::kScales;
-                    const uint32_t w_cols = stage_cols + stage * S::kStageCols;
-                    const uint32_t x_cols = kResident ? act_cols + step * kUnits * S::kUnitCols : w_cols + kUnits * S::kUnitCols;
-                    if (ptx::elect_one()) {
-#pragma unroll
-                        for (int u = 0; u < kUnits; ++u) {
-                            if (u < n) {
-                                const uint32_t xu = x + u * S::kUnit, xc = x_cols + u * S::kUnitCols, wc = w_cols + u * S::kUnitCols;
-#pragma unroll
-                                for (int k = 0; k < S::kAtoms; ++k) {
-                                    if (!kResident || fresh) ptx::tmem_cp_scales<true>(xc + 4 * k, ptx::smem_desc_scales(xu + 512 * k));
-                                    ptx::tmem_cp_scales<true>(wc + 4 * k, ptx::smem_desc_scales(w_scales + u * S::kScales + 512 * k));
-                                }
-                                const uint64_t a = ptx::smem_desc_k64(xu + S::kScales), b = ptx::smem_desc_k64(w + u * S::kHalf);
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) {            // 64 columns are 32 bytes, 2 descriptor units
-                                    const uint32_t at = kGroup == 16 ? 4 * k : 0;
-                                    const uint32_t which = kGroup == 32 && k == 1 ? ptx::kIdescFp4SecondHalf : 0u;
-                                    ptx::mma_fp4<kGroup, true>(acc, a + 2u * k, b + 2u * k, idesc | which, xc + at, wc + at, step > 0 || u > 0 || k > 0 ? 1u : 0u);
-                                }
-                            }
-                        }
-                        ptx::mma_commit_pair(empty_bar(stage), 3);
-                        if (step + 1 == steps) {
-                            ptx::mma_commit_pair(accfull_bar(buf), 3);
-                            if (last_of_rows) ptx::mma_commit_pair(act_free, 3);
-                        }
+                    const uint32_t scales = low + S::kHalf / 16, act_scales = scales + S::kScales / 16;
+                    if (!kResident) {
+                        x_low = act_scales + S::kScales / 16;
+                        x_cols = cols + S::kUnitCols;
                     }
-                    __syncwarp();
-                    if (++stage == n_stages) { stage = 0; phase ^= 1u; }
+#pragma unroll
+                    for (int k = 0; k < S::kAtoms; ++k) {
+                        ptx::tmem_cp_scales<true>(cols + 4 * k, scales + 32 * k);
+                        if (!kResident) ptx::tmem_cp_scales<true>(x_cols + 4 * k, act_scales + 32 * k);
+                    }
+                    // 64 columns are 32 bytes: two steps of the descriptor
+                    constexpr uint32_t kSecond = kGroup == 16 ? 4 : 0;   // the other scales, or the other half of the same ones
+                    ptx::mma_fp4<kGroup, true>(acc, x_low, low, idesc, x_cols, cols, u > 0 ? 1u : 0u);
+                    ptx::mma_fp4<kGroup, true>(acc, x_low + 2, low + 2, idesc | (kGroup == 32 ? ptx::kIdescFp4SecondHalf : 0u), x_cols + kSecond, cols + kSecond, 1u);
+                    x_low += S::kElements / 16;
+                    x_cols += S::kUnitCols;
+                    stage_done();
                 }
+                if (!ok) break;
+                ptx::mma_commit_pair(accfull_bar(buf), 3);
+                fresh = false;
+                if (++n_tile == p.n_tiles) {
+                    n_tile = 0;
+                    fresh = kResident;
+                    if (kResident && t + 1 < end) ptx::mma_commit_pair(act_free, 3);
+                }
+                buf ^= 1;
+                acc_phase ^= buf == 0 ? 1u : 0u;
             }
-            if (lane == 0 && *abort_flag) mma_drain<true>(drain_bar);
-            __syncwarp();
+            if (*abort_flag) mma_drain<true>(drain_bar);
         }
+        __syncwarp();
     } else {
         // ---------------------------------------------------------------- states
         const int quarter = warp & 3, half = (warp - 2) >> 2;
@@ -323,8 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                 factor = row < q.M ? ld_dep(q.factor + row) * weight_factor : 1.f;
                 c = factor * kLog2e;
             }
-            const bool landed = ptx::mbar_wait(accfull_bar(buf), (uint32_t)(local >> 1) & 1u, abort_flag);
-            if (!__all_sync(0xffffffffu, landed)) {
+            if (!warp_wait(accfull_bar(buf), (uint32_t)(local >> 1) & 1u, abort_flag)) {
                 if (lane == 0) record_failure(q.ctrl, abort_flag, 3, buf, (unsigned)t);
                 break;
             }
@@ -420,9 +450,11 @@ ee_status launch_shape(GemmParams p, int device, cudaStream_t stream) {
     p.slots = max_slots(p.m_pairs, p.n_tiles, pairs);
     p.n_stages = S::stages(blocks);
     GemmMaps maps;
-    if (!make_unit_map(&maps.acts, p.q.acts, kGroup, 2ll * p.m_pairs * blocks, S::kUnit / 128, 1) ||
-        !make_unit_map(&maps.weights, p.q.weights, kGroup, (long long)p.n_tiles * blocks, S::kHalf / 128, kUnits) ||
-        !make_unit_map(&maps.scales, p.q.weights, kGroup, (long long)p.n_tiles * blocks, S::kScales / 128, kUnits))
+    const long long act_units = 2ll * p.m_pairs * blocks, weight_units = (long long)p.n_tiles * blocks;
+    if (!make_unit_map(&maps.scales, p.q.weights, kGroup, weight_units, S::kScales / 128, 1) ||
+        !make_unit_map(&maps.weights, p.q.weights, kGroup, weight_units, S::kHalf / 128, 1) ||
+        !make_unit_map(&maps.acts, p.q.acts, kGroup, act_units, (kResident ? S::kElements : S::kUnit) / 128, 1) ||
+        !make_unit_map(&maps.act_scales, p.q.acts, kGroup, act_units, S::kScales / 128, kResident ? S::kScaleUnits : 1))
         return EE_ERR_CUDA;
     if (launch_pdl_pairs(fp4_gemm_kernel<kGroup, kResident>, dim3(2 * pairs), kThreads, S::smem(blocks), stream, maps, p) != cudaSuccess) return EE_ERR_CUDA;
     const int rows = kMergeThreads / 32;

@@ -113,92 +113,109 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
 
     if (warp == 0) {
         // ---------------------------------------------------------------- producer
-        if (lane == 0) {
+        if (ptx::elect_one()) {
             int stage = 0, issued = 0;
-            uint32_t phase = 0, armed = 0, armed_parity = 0;
+            uint32_t phase = 1, armed = 0, armed_parity = 0;
             bool ok = true;
-            auto units = [&](int step) { return (uint32_t)min(kUnits, blocks - step * kUnits); };
-            auto load_w = [&](int s, int tile, int step) {
-                ptx::bulk_load(ring + s * S::kStageBytes, q.weights + ((size_t)tile * blocks + step * kUnits) * S::kWUnit, units(step) * S::kWUnit, full_bar(s));
-            };
-            auto load_x = [&](int s, int step) {
-                ptx::bulk_load(ring + s * S::kStageBytes + kUnits * S::kWUnit, q.acts + (size_t)step * kUnits * S::kXUnit, units(step) * S::kXUnit, full_bar(s));
+            const unsigned char* x0 = q.acts;
+            const int last_units = blocks - (steps - 1) * kUnits;
+            auto load_w = [&](int s, const unsigned char* w, int units) { ptx::bulk_load(ring + s * S::kStageBytes, w, units * S::kWUnit, full_bar(s)); };
+            auto load_x = [&](int s, const unsigned char* x, int units) {
+                ptx::bulk_load(ring + s * S::kStageBytes + kUnits * S::kWUnit, x, units * S::kXUnit, full_bar(s));
             };
             const int n_pre = (int)blockIdx.x < tiles ? min(S::kStages, steps) : 0;
             for (int step = 0; step < n_pre; ++step) {
-                ptx::mbar_arrive_expect_tx(full_bar(step), units(step) * (S::kWUnit + S::kXUnit));
-                load_w(step, blockIdx.x, step);
+                const int units = step + 1 < steps ? kUnits : last_units;
+                ptx::mbar_arrive_expect_tx(full_bar(step), units * (S::kWUnit + S::kXUnit));
+                load_w(step, q.weights + ((size_t)blockIdx.x * blocks + step * kUnits) * S::kWUnit, units);
                 armed |= 1u << step;
             }
             grid_dependency_wait();
-            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x)
+            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+                const unsigned char* w = q.weights + (size_t)tile * blocks * S::kWUnit;
+                const unsigned char* x = x0;
                 for (int step = 0; step < steps; ++step, ++issued) {
-                    if (issued < n_pre) {
-                        load_x(stage, step);
-                    } else {
-                        if (!ptx::mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag)) {
+                    const int units = step + 1 < steps ? kUnits : last_units;
+                    if (issued >= n_pre) {
+                        if (!ptx::mbar_wait(empty_bar(stage), phase, abort_flag)) {
                             record_failure(q.ctrl, abort_flag, 1, stage, tile);
                             ok = false;
                             break;
                         }
-                        ptx::mbar_arrive_expect_tx(full_bar(stage), units(step) * (S::kWUnit + S::kXUnit));
-                        load_w(stage, tile, step);
-                        load_x(stage, step);
+                        ptx::mbar_arrive_expect_tx(full_bar(stage), units * (S::kWUnit + S::kXUnit));
+                        load_w(stage, w, units);
                         armed |= 1u << stage;
-                        armed_parity = (armed_parity & ~(1u << stage)) | (phase << stage);
+                        armed_parity = (armed_parity & ~(1u << stage)) | ((phase ^ 1u) << stage);
                     }
+                    load_x(stage, x, units);
+                    w += kUnits * S::kWUnit;
+                    x += kUnits * S::kXUnit;
                     if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
                 }
+            }
             if (*abort_flag) producer_drain(0, S::kStages, full_bar(0), armed, armed_parity);
         }
         __syncwarp();
     } else if (warp == 1) {
-        // ---------------------------------------------------------------- products
-        if (lane == 0) {
+        // ---------------------------------------------------------------- products (positions by addition: a single thread takes four to five
+        // cycles for an instruction)
+        if (ptx::elect_one()) {
             constexpr uint32_t idesc = ptx::idesc_fp4<kGroup>(kFp4Rows, N);
             constexpr int kAtoms = fp4_scale_bytes(kGroup) / 512;        // copies of scales per unit and operand
-            int stage = 0, local = 0;
-            uint32_t phase = 0;
+            const uint32_t low0 = ptx::desc_low(ring);
+            uint32_t low = low0, cols = scales_base, full = full_bar(0), empty = empty_bar(0), phase = 0, acc_phase = 1;
+            int stage = 0, buf = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++local) {
-                const int buf = local & 1;
-                if (!ptx::mbar_wait(accfree_bar(buf), ((uint32_t)(local >> 1) & 1u) ^ 1u, abort_flag)) {
+            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+                if (!ptx::mbar_wait(accfree_bar(buf), acc_phase, abort_flag)) {
                     record_failure(q.ctrl, abort_flag, 2, 0x80 | buf, tile);
                     break;
                 }
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem_base + buf * acc_cols(N);
-                for (int step = 0; step < steps; ++step) {
-                    if (!ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
+                uint32_t accumulate = 0;
+                int left = blocks;
+                for (int step = 0; step < steps; ++step, left -= kUnits) {
+                    if (!ptx::mbar_wait(full, phase, abort_flag)) {
                         record_failure(q.ctrl, abort_flag, 2, stage, tile);
                         ok = false;
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t w = ring + stage * S::kStageBytes, x = w + kUnits * S::kWUnit;
-                    const uint32_t scales = scales_base + stage * S::kScaleCols;
 #pragma unroll
                     for (int u = 0; u < kUnits; ++u) {
-                        if (step * kUnits + u < blocks) {
-                            const uint32_t wu = w + u * S::kWUnit, xu = x + u * S::kXUnit, su = scales + u * kAtoms * 8;
+                        if (u < left) {
+                            const uint32_t wu = low + u * (S::kWUnit / 16), xu = low + (kUnits * S::kWUnit + u * S::kXUnit) / 16, su = cols + u * kAtoms * 8;
 #pragma unroll
                             for (int k = 0; k < kAtoms; ++k) {
-                                ptx::tmem_cp_scales(su + 8 * k, ptx::smem_desc_scales(wu + 512 * k));
-                                ptx::tmem_cp_scales(su + 8 * k + 4, ptx::smem_desc_scales(xu + 512 * k));
+                                ptx::tmem_cp_scales(su + 8 * k, wu + 32 * k);
+                                ptx::tmem_cp_scales(su + 8 * k + 4, xu + 32 * k);
                             }
-                            const uint64_t a = ptx::smem_desc_k64(wu + fp4_scale_bytes(kGroup)), b = ptx::smem_desc_k64(xu + fp4_scale_bytes(kGroup));
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {                // 64 columns are 32 bytes, 2 descriptor units
-                                const uint32_t sk = su + (kGroup == 16 ? 8 * k : 0);
-                                const uint32_t which = kGroup == 32 && k == 1 ? ptx::kIdescFp4SecondHalf : 0u;
-                                ptx::mma_fp4<kGroup>(acc, a + 2u * k, b + 2u * k, idesc | which, sk, sk + 4, step > 0 || u > 0 || k > 0 ? 1u : 0u);
-                            }
+                            constexpr uint32_t at = fp4_scale_bytes(kGroup) / 16, kSecond = kGroup == 16 ? 8 : 0;
+                            // 64 columns are 32 bytes: two steps of the descriptor
+                            ptx::mma_fp4<kGroup>(acc, wu + at, xu + at, idesc, su, su + 4, accumulate);
+                            ptx::mma_fp4<kGroup>(acc, wu + at + 2, xu + at + 2, idesc | (kGroup == 32 ? ptx::kIdescFp4SecondHalf : 0u), su + kSecond,
+                                                 su + kSecond + 4, 1u);
+                            accumulate = 1;
                         }
                     }
-                    ptx::mma_commit(empty_bar(stage));
-                    if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
+                    ptx::mma_commit(empty);
+                    low += S::kStageBytes / 16;
+                    cols += S::kScaleCols;
+                    full += 8;
+                    empty += 8;
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        low = low0;
+                        cols = scales_base;
+                        full = full_bar(0);
+                        empty = empty_bar(0);
+                        phase ^= 1u;
+                    }
                 }
                 if (ok) ptx::mma_commit(accfull_bar(buf));
+                buf ^= 1;
+                acc_phase ^= buf == 0 ? 1u : 0u;
             }
             if (*abort_flag) mma_drain<false>(drain_bar);
         }
@@ -214,8 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
         int local = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++local) {
             const int buf = local & 1;
-            const bool landed = ptx::mbar_wait(accfull_bar(buf), (uint32_t)(local >> 1) & 1u, abort_flag);
-            if (!__all_sync(0xffffffffu, landed) && lane == 0) record_failure(q.ctrl, abort_flag, 3, buf, tile);
+            const bool landed = warp_wait(accfull_bar(buf), (uint32_t)(local >> 1) & 1u, abort_flag);
+            if (!landed && lane == 0) record_failure(q.ctrl, abort_flag, 3, buf, tile);
             if (fold_barrier_any(!landed)) break;                        // all eight warps or none; the tile before has been read
             ptx::tc_fence_after_sync();
             if (N >= 16 || half == 0) {

@@ -34,6 +34,14 @@ __device__ __forceinline__ void record_failure(Control* ctrl, volatile int* abor
     __threadfence_block();
 }
 
+// A whole warp waits through one of its lanes: 32 lanes that poll a barrier are 32 requests to shared memory at a time, which the other roles'
+// barriers queue behind.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const volatile int* abort_flag) {
+    int ok = 1;
+    if ((threadIdx.x & 31) == 0) ok = ptx::mbar_wait(bar, parity, abort_flag) ? 1 : 0;
+    return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+
 // One stage by the MMA-issuing thread: wait until the stage's operands have landed, four MMAs of K = 16 on the
 // 128-byte-swizzled tiles at a_addr / b_addr into the accumulator at d_tmem (the first MMA of a tile overwrites
 // it) -- and, if the stage holds a second k-block (a_second != 0: its tiles lie a_second / b_second bytes further
