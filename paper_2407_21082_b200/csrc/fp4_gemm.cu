@@ -27,7 +27,8 @@ constexpr int kMergeThreads = 256;
 constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
-constexpr int kMaxStages = 24;
+constexpr int kMaxStages = 12;
+constexpr int kUnits = 4;                        // units per stage: taking and giving one costs each issuing thread some 250 cycles
 
 struct GemmMaps {
     // boxes: a weight unit's scales, the half of its elements that a CTA loads; a unit of activations (or its elements alone), the scales of
@@ -40,16 +41,16 @@ struct GemmParams {
     int m_pairs, n_tiles, slots, n_stages;
 };
 
-// A stage of the ring holds 128 columns: the CTA's half of a weight unit and all its scales, and, unless they are resident, a unit of activations.
+// A stage of the ring holds kUnits times: the CTA's half of a weight unit and all its scales, and, unless they are resident, a unit of activations.
 // kResident: the elements of a row tile's activations stay in shared memory, and their scales, which come through the ring as well, in tensor
 // memory, while the weights pass by.
 template <int kGroup, bool kResident>
 struct Shape {
     static constexpr int kUnit = fp4_unit_bytes(kGroup, kFp4Rows), kScales = fp4_scale_bytes(kGroup), kElements = kUnit - kScales, kHalf = kElements / 2;
-    static constexpr int kStageBytes = kHalf + kScales + (kResident ? 0 : kUnit);
+    static constexpr int kPartBytes = kHalf + kScales + (kResident ? 0 : kUnit), kStageBytes = kUnits * kPartBytes;
     static constexpr int kAtoms = kScales / 512;
     static constexpr int kUnitCols = kAtoms * 4;                               // of a unit's scales in tensor memory
-    static constexpr int kStageCols = kResident ? kUnitCols : 2 * kUnitCols;
+    static constexpr int kPartCols = kResident ? kUnitCols : 2 * kUnitCols, kStageCols = kUnits * kPartCols;
     static constexpr int kScaleUnits = kStageBytes / kScales;                  // whose scales one stage brings
     static int resident_bytes(int blocks) { return kResident ? blocks * kElements : 0; }
     static int stages(int blocks) {
@@ -227,15 +228,22 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                     }
                 }
                 int unit = n_tile * blocks;
-                for (int u = 0; u < blocks && ok && next_stage((unsigned)t); ++u, ++unit) {
-                    if (fresh) {
-                        if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
-                        ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
+                for (int u0 = 0; u0 < blocks && ok && next_stage((unsigned)t); u0 += kUnits) {
+                    const int n = min(kUnits, blocks - u0);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * n * S::kPartBytes);
+#pragma unroll
+                    for (int k = 0; k < kUnits; ++k) {
+                        if (k >= n) break;
+                        const int u = u0 + k;
+                        const uint32_t at = to + k * S::kPartBytes;
+                        if (fresh) {
+                            if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
+                            ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
+                        }
+                        ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit + u, full);
+                        ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, unit + u, full);
+                        if (!kResident) ptx::tma_load_3d_pair(at + S::kHalf + S::kScales, &maps.acts, 0, 0, act_unit + u, full);
                     }
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * S::kStageBytes);
-                    ptx::tma_load_3d_pair(to, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit, full);
-                    ptx::tma_load_3d_pair(to + S::kHalf, &maps.scales, 0, 0, unit, full);
-                    if (!kResident) ptx::tma_load_3d_pair(to + S::kHalf + S::kScales, &maps.acts, 0, 0, act_unit + u, full);
                     stage_done();
                 }
                 fresh = false;
@@ -295,25 +303,30 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem_base + buf * kAccCols;
                 uint32_t x_low = act_low, x_cols = act_cols;
-                for (int u = 0; u < blocks; ++u) {
-                    if (!landed(full, phase, (unsigned)t) || (fresh && !landed(act_bar(u), act_phase, (unsigned)t))) break;
+                for (int u0 = 0; u0 < blocks && landed(full, phase, (unsigned)t); u0 += kUnits) {
+                    const int n = min(kUnits, blocks - u0);
+                    for (int k = 0; fresh && k < n; ++k) landed(act_bar(u0 + k), act_phase, (unsigned)t);
                     ptx::tc_fence_after_sync();
-                    const uint32_t scales = low + S::kHalf / 16, act_scales = scales + S::kScales / 16;
-                    if (!kResident) {
-                        x_low = act_scales + S::kScales / 16;
-                        x_cols = cols + S::kUnitCols;
-                    }
 #pragma unroll
-                    for (int k = 0; k < S::kAtoms; ++k) {
-                        ptx::tmem_cp_scales<true>(cols + 4 * k, scales + 32 * k);
-                        if (!kResident) ptx::tmem_cp_scales<true>(x_cols + 4 * k, act_scales + 32 * k);
+                    for (int k = 0; k < kUnits; ++k) {
+                        if (k >= n) break;
+                        const uint32_t w_low = low + k * (S::kPartBytes / 16), scales = w_low + S::kHalf / 16, act_scales = scales + S::kScales / 16;
+                        const uint32_t w_cols = cols + k * S::kPartCols;
+                        const uint32_t a_low = kResident ? x_low + k * (S::kElements / 16) : act_scales + S::kScales / 16;
+                        const uint32_t a_cols = kResident ? x_cols + k * S::kUnitCols : w_cols + S::kUnitCols;
+#pragma unroll
+                        for (int i = 0; i < S::kAtoms; ++i) {
+                            ptx::tmem_cp_scales<true>(w_cols + 4 * i, scales + 32 * i);
+                            if (!kResident) ptx::tmem_cp_scales<true>(a_cols + 4 * i, act_scales + 32 * i);
+                        }
+                        // 64 columns are 32 bytes: two steps of the descriptor
+                        constexpr uint32_t kSecond = kGroup == 16 ? 4 : 0;   // the other scales, or the other half of the same ones
+                        ptx::mma_fp4<kGroup, true>(acc, a_low, w_low, idesc, a_cols, w_cols, k > 0 || u0 > 0 ? 1u : 0u);
+                        ptx::mma_fp4<kGroup, true>(acc, a_low + 2, w_low + 2, idesc | (kGroup == 32 ? ptx::kIdescFp4SecondHalf : 0u), a_cols + kSecond,
+                                                   w_cols + kSecond, 1u);
                     }
-                    // 64 columns are 32 bytes: two steps of the descriptor
-                    constexpr uint32_t kSecond = kGroup == 16 ? 4 : 0;   // the other scales, or the other half of the same ones
-                    ptx::mma_fp4<kGroup, true>(acc, x_low, low, idesc, x_cols, cols, u > 0 ? 1u : 0u);
-                    ptx::mma_fp4<kGroup, true>(acc, x_low + 2, low + 2, idesc | (kGroup == 32 ? ptx::kIdescFp4SecondHalf : 0u), x_cols + kSecond, cols + kSecond, 1u);
-                    x_low += S::kElements / 16;
-                    x_cols += S::kUnitCols;
+                    x_low += kUnits * (S::kElements / 16);
+                    x_cols += kUnits * S::kUnitCols;
                     stage_done();
                 }
                 if (!ok) break;
