@@ -26,6 +26,8 @@ constexpr int kThreads = 320;
 constexpr int kFoldWarps = 8;
 constexpr int kUnits = 2;                        // units per stage
 constexpr int kMaxStages = 12;
+constexpr int kMergeHere = 8;                    // rows up to which the CTA that finishes last merges the states; more are a kernel of their own
+constexpr int kMergeThreads = 128;
 constexpr int kTmemCols = 512;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kBarBytes = 8 * (2 * kMaxStages + 5) + 64;
@@ -51,6 +53,38 @@ struct Shape {
     static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
     static constexpr size_t kSmem = (size_t)kStages * kStageBytes + kTail;
 };
+
+// Four more logits of a row into its state, in increasing order of their indices from idx on; without branches, so that the tokens of a warp overlap.
+__device__ __forceinline__ void push4(RestState& a, float4 z, int idx) {
+    const float top = fmaxf(fmaxf(z.x, z.y), fmaxf(z.z, z.w));
+    const bool up = top > a.m;
+    const bool at0 = z.x == top, at1 = !at0 && z.y == top, at2 = !at0 && !at1 && z.z == top, at3 = !at0 && !at1 && !at2;
+    const float m = up ? top : a.m;
+    const float d0 = z.x - m, d1 = z.y - m, d2 = z.z - m, d3 = z.w - m;
+    // a new maximum leaves its term out of the sum, the old one's comes in
+    const float e0 = up && at0 ? 0.f : ex2(d0 * kLog2e), e1 = up && at1 ? 0.f : ex2(d1 * kLog2e);
+    const float e2 = up && at2 ? 0.f : ex2(d2 * kLog2e), e3 = up && at3 ? 0.f : ex2(d3 * kLog2e);
+    const bool fresh = a.s == -1.f;
+    const float dl = up && !fresh ? a.m - m : 0.f, al = ex2(dl * kLog2e);
+    const float n = up ? 1.f + a.s : a.s;                                // 0 for a new state
+    const float t = up ? al * fmaf(dl, n, a.t) : a.t;
+    a.s = fmaf(al, n, (e0 + e1) + (e2 + e3));
+    a.t = t + (fmaf(e0, d0, e1 * d1) + fmaf(e2, d2, e3 * d3));
+    a.m = m;
+    a.idx = up ? idx + (at0 ? 0 : at1 ? 1 : at2 ? 2 : 3) : a.idx;
+}
+
+// A warp: the CTAs' states of a token, a lane every 32nd CTA's.
+__device__ __forceinline__ void merge_token(const StreamParams& p, int padded, int ctas, int tok, int lane) {
+    RestState v[kStreamMaxCtas / 32];
+#pragma unroll
+    for (int i = 0; i < kStreamMaxCtas / 32; ++i) {
+        const int b = lane + 32 * i;
+        v[i] = b < ctas ? rest_load_cg(p.parts + (size_t)b * padded + tok) : rest_empty();
+    }
+    const RestState all = rest_reduce_lanes<1>(rest_combine(kStreamMaxCtas / 32, [&](int k) -> const RestState& { return v[k]; }));
+    if (lane == 0) rest_finish(all, p.q, tok);
+}
 
 // Barrier of the eight epilogue warps; whether any of their threads says so.
 __device__ __forceinline__ bool fold_barrier_any(bool mine) {
@@ -257,10 +291,14 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
                 const int tok = e + i * kFoldWarps;
                 if (tok < q.M && valid > 0) {
                     const float4 v = *reinterpret_cast<const float4*>(z_mem + tok * (kFp4Rows + 4) + lane * 4);
-                    float z[4] = {v.x * factor[i], v.y * factor[i], v.z * factor[i], v.w * factor[i]};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (j < valid) rest_push(st[i], z[j], first + j);
+                    const float4 z = make_float4(v.x * factor[i], v.y * factor[i], v.z * factor[i], v.w * factor[i]);
+                    if (valid >= 4) {
+                        push4(st[i], z, first);
+                    } else {
+                        rest_push(st[i], z.x, first);
+                        if (valid > 1) rest_push(st[i], z.y, first + 1);
+                        if (valid > 2) rest_push(st[i], z.z, first + 2);
+                    }
                 }
             }
         }
@@ -280,22 +318,19 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
         ptx::tc_fence_after_sync();
         ptx::tmem_dealloc(tmem_base, kTmemCols);
     }
+    if (N > kMergeHere) return;
     if (threadIdx.x == 0) *is_last = ticket_arrive_is_last(&q.ctrl->head_ticket[0], gridDim.x) ? 1 : 0;
     __syncthreads();
     if (!*is_last) return;
-    // the CTAs' states: a warp per token, a lane every 32nd CTA
-    for (int tok = warp; tok < q.M; tok += kThreads / 32) {
-        RestState v[kStreamMaxCtas / 32];
-#pragma unroll
-        for (int i = 0; i < kStreamMaxCtas / 32; ++i) {
-            const int b = lane + 32 * i;
-            v[i] = b < (int)gridDim.x ? rest_load_cg(p.parts + (size_t)b * N + tok) : rest_empty();
-        }
-        const RestState mine = rest_combine(kStreamMaxCtas / 32, [&](int k) -> const RestState& { return v[k]; });
-        const RestState all = rest_reduce_lanes<1>(mine);
-        if (lane == 0) rest_finish(all, q, tok);
-    }
+    for (int tok = warp; tok < q.M; tok += kThreads / 32) merge_token(p, N, (int)gridDim.x, tok, lane);
     if (threadIdx.x == 0) q.ctrl->head_ticket[0] = 0;                    // ready for the next launch
+}
+
+__global__ void __launch_bounds__(kMergeThreads) fp4_stream_merge_kernel(const StreamParams p, int padded, int ctas) {
+    launch_dependents();
+    grid_dependency_wait();
+    const int tok = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5);
+    if (tok < p.q.M) merge_token(p, padded, ctas, tok, threadIdx.x & 31);
 }
 
 template <int kGroup, int N>
@@ -313,7 +348,10 @@ ee_status launch_tokens(const Fp4Head& q, void* parts, int num_sms, int device, 
     const int tiles = fp4_tiles(q.V, kFp4Rows);
     int grid = tiles < num_sms ? tiles : num_sms;
     if (grid > kStreamMaxCtas) grid = kStreamMaxCtas;
-    return launch_pdl(fp4_stream_kernel<kGroup, N>, dim3(grid), kThreads, S::kSmem, stream, p) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    if (launch_pdl(fp4_stream_kernel<kGroup, N>, dim3(grid), kThreads, S::kSmem, stream, p) != cudaSuccess) return EE_ERR_CUDA;
+    if (N <= kMergeHere) return EE_OK;
+    const int rows = kMergeThreads / 32;
+    return launch_pdl(fp4_stream_merge_kernel, dim3((q.M + rows - 1) / rows), kMergeThreads, 0, stream, p, N, grid) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 template <int kGroup>
 ee_status launch_group(const Fp4Head& q, void* parts, int num_sms, int device, cudaStream_t stream) {

@@ -21,7 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kClusterThreads = 1024, kMaxWarps = kClusterThreads / 32;
 constexpr int kClusterCtas = 8;
 constexpr int kMaxCtas = 2048;
 constexpr int kSums = 4;
@@ -78,15 +78,21 @@ __device__ __forceinline__ double warp_total(double v) {
 // The sum of v over the threads that walk a unit, the same in each of them.  Two arrays of shared memory take turns, so that one barrier
 // (or two of the cluster) is enough.
 template <int kSpan>
-__device__ __forceinline__ double span_total(double v, double (&slots)[2][kWarps + 1], int& turn) {
+__device__ __forceinline__ double span_total(double v, double (&slots)[2][kMaxWarps + 1], int& turn) {
+    constexpr int kWarps = (kSpan == kClusterSpan ? kClusterThreads : kThreads) / 32;
     v = warp_total(v);
     if (kSpan == kWarpSpan) return v;
     double* slot = slots[turn];
     turn ^= 1;
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
     __syncthreads();
-    double s = 0.0;
-    for (int w = 0; w < kWarps; ++w) s += slot[w];
+    double s;
+    if (kWarps == 32) {
+        s = warp_total(slot[threadIdx.x & 31]);
+    } else {
+        s = 0.0;
+        for (int w = 0; w < kWarps; ++w) s += slot[w];
+    }
     if (kSpan == kCtaSpan) return s;
     if (threadIdx.x == 0) slot[kWarps] = s;
     cg::cluster_group cluster = cg::this_cluster();
@@ -97,6 +103,7 @@ __device__ __forceinline__ double span_total(double v, double (&slots)[2][kWarps
 }
 
 // Four sums over the CTA's units, to the means: the CTA that finishes last adds up the CTAs'.
+template <int kWarps>
 __device__ __forceinline__ void finish(double (&sums)[kSums], LossSpace* space, float* loss) {
     __shared__ double warp_sums[kWarps][kSums];
     __shared__ int last;
@@ -118,7 +125,7 @@ __device__ __forceinline__ void finish(double (&sums)[kSums], LossSpace* space, 
     __syncthreads();
     if (!last) return;
     double total[kSums] = {};
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += kThreads) {
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += 32 * kWarps) {
         const double2* part = reinterpret_cast<const double2*>(space->parts[b]);
         const double2 lo = __ldcg(part), hi = __ldcg(part + 1);
         total[0] += lo.x; total[1] += lo.y; total[2] += hi.x; total[3] += hi.y;
@@ -143,7 +150,7 @@ __device__ __forceinline__ int boundary(const int* seq_start, int i, int M) { re
 // Rows before the first sequence and behind the last belong to none: their weight is zero.
 __device__ __forceinline__ void clear_outside(const int* seq_start, int n, int M, float* dce) {
     const int first = boundary(seq_start, 0, M), end = max(boundary(seq_start, n, M), first);
-    const long long stride = (long long)gridDim.x * kThreads, at = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const long long stride = (long long)gridDim.x * blockDim.x, at = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     for (long long i = at; i < first; i += stride) dce[i] = 0.f;
     for (long long i = end + at; i < M; i += stride) dce[i] = 0.f;
 }
@@ -174,12 +181,15 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(const PolicyArg
 #pragma unroll
     for (int k = 1; k < kSums; ++k) sums[k] *= w;
     sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
-    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+    finish<kThreads / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
 // Which units a thread has part in, and where in them it begins and how far it steps.
 template <int kSpan>
+constexpr int threads_of = kSpan == kClusterSpan ? kClusterThreads : kThreads;
+template <int kSpan>
 struct Walk {
+    static constexpr int kThreads = threads_of<kSpan>, kWarps = kThreads / 32;
     int unit, units_step, from, step;
     bool leads;
     __device__ __forceinline__ Walk() {
@@ -205,8 +215,8 @@ struct Walk {
 
 // Every sequence counts alike, and within a sequence every token.
 template <int kSpan>
-__global__ void __launch_bounds__(kThreads) policy_sequences_kernel(const PolicyArgs p) {
-    __shared__ double slots[2][kWarps + 1];
+__global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(const PolicyArgs p) {
+    __shared__ double slots[2][kMaxWarps + 1];
     launch_dependents();
     grid_dependency_wait();
     clear_outside(p.seq_start, p.S, p.M, p.dce);
@@ -244,13 +254,13 @@ __global__ void __launch_bounds__(kThreads) policy_sequences_kernel(const Policy
     }
     sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
     if (kSpan == kClusterSpan) cg::this_cluster().sync();                // nobody leaves while its sums may still be read
-    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+    finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
 // Pairs of sequences 2u (preferred) and 2u + 1 (rejected).
 template <int kSpan>
-__global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceArgs p) {
-    __shared__ double slots[2][kWarps + 1];
+__global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const PreferenceArgs p) {
+    __shared__ double slots[2][kMaxWarps + 1];
     launch_dependents();
     grid_dependency_wait();
     clear_outside(p.seq_start, 2 * p.P, p.M, p.dce);
@@ -290,15 +300,15 @@ __global__ void __launch_bounds__(kThreads) preference_kernel(const PreferenceAr
 #pragma unroll
     for (int k = 0; k < kSums; ++k) sums[k] /= (double)p.P;
     if (kSpan == kClusterSpan) cg::this_cluster().sync();
-    finish(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
+    finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
-// What walks a unit: a cluster where whole CTAs would leave SMs without one and a unit has several tokens for each of the cluster's
-// threads, a CTA where a unit has several tokens for each of its threads, a warp otherwise.
+// What walks a unit: a cluster where a CTA for each would leave most SMs without one and a unit has several tokens for each of a CTA's threads; a
+// CTA where a unit has tokens for half of its threads, or where there are hardly any units; a warp otherwise.
 int span_of(int M, int units, int num_sms) {
     const int each = M / units;
-    if (units * 2 <= num_sms && each >= 2 * kThreads) return kClusterSpan;
-    return each >= 2 * kThreads || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
+    if (units * 4 <= num_sms && each >= 4 * kThreads) return kClusterSpan;
+    return each >= kThreads / 2 || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
 }
 
 template <class Args>
@@ -307,14 +317,14 @@ cudaError_t launch_spans(void (*warp)(Args), void (*cta)(Args), void (*cluster)(
     const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
     switch (span_of(M, units, num_sms)) {
         case kWarpSpan: {
-            const int grid = (units + kWarps - 1) / kWarps;
+            const int grid = (units + kThreads / 32 - 1) / (kThreads / 32);
             return launch_pdl(warp, dim3(grid < most ? grid : most), kThreads, 0, stream, p);
         }
         case kCtaSpan: return launch_pdl(cta, dim3(units < most ? units : most), kThreads, 0, stream, p);
         default: {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
-            pair_launch_config(cfg, attr, dim3(units * kClusterCtas), kThreads, 0, stream);
+            pair_launch_config(cfg, attr, dim3(units * kClusterCtas), kClusterThreads, 0, stream);
             attr[1].val.clusterDim.x = kClusterCtas;
             return cudaLaunchKernelEx(&cfg, cluster, p);
         }
