@@ -56,6 +56,13 @@ __device__ __forceinline__ uint32_t fp4_pack8(const float (&x)[8]) {
         : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
     return r;
 }
+// A byte's two elements, the low half first.
+__device__ __forceinline__ float2 fp4_unpack2(uint32_t byte) {
+    float2 x;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t.reg .b32 h;\n\t.reg .b16 l, u;\n\tmov.b32 {b0, b1, b2, b3}, %2;\n\tcvt.rn.f16x2.e2m1x2 h, b0;\n\t"
+        "mov.b32 {l, u}, h;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(x.x), "=f"(x.y) : "r"(byte));
+    return x;
+}
 // A positive float to four exponent and three mantissa bits, ties to the even code, and back.
 __device__ __forceinline__ uint32_t fp4_scale_code(float s) {
     uint16_t r;

@@ -11,6 +11,7 @@ namespace ee {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kAhead = 4;                        // 512-byte pieces of a row that a warp has in flight
 
 struct Fp4Pack {
     const uint4* W;                // [V][d] bf16
@@ -53,51 +54,63 @@ __global__ void __launch_bounds__(kThreads) fp4_pack_kernel(const Fp4Pack p) {
         const int r = (int)(row % kFp4Rows);
         unsigned char* tile = p.fp4 + kFp4Header + (row / kFp4Rows) * blocks * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
         const uint4* src = p.W + row * nvec;
-        for (int c0 = 0; c0 < blocks * 16; c0 += 32) {
-            const int c = c0 + lane;
-            const uint4 v = row < p.V && c < nvec ? ld_dep(src + c) : make_uint4(0, 0, 0, 0);
-            uint32_t code;
-            const uint32_t word = fp4_quantise8<kGroup>(v, fp4_group_top<kGroup>(fp4_top8(v)), common, code);
-            const uint32_t codes = fp4_gather_codes<kGroup>(code);
-            if (c < blocks * 16) {
-                unsigned char* unit = tile + (c >> 4) * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
-                *reinterpret_cast<uint32_t*>(unit + fp4_scale_bytes(kGroup) + fp4_word_offset(r, c & 15)) = word;
-                if (kGroup == 16 ? (c & 7) == 0 : (c & 15) == 0)
-                    *reinterpret_cast<uint32_t*>(unit + fp4_scales_offset(r, kGroup == 16 ? (c >> 3) & 1 : 0)) = codes;
+        for (int c0 = 0; c0 < blocks * 16; c0 += 32 * kAhead) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int c = c0 + 32 * k + lane;
+                v[k] = row < p.V && c < nvec ? ld_dep(src + c) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (c0 + 32 * k >= blocks * 16) break;                   // the same for the whole warp
+                const int c = c0 + 32 * k + lane;
+                uint32_t code;
+                const uint32_t word = fp4_quantise8<kGroup>(v[k], fp4_group_top<kGroup>(fp4_top8(v[k])), common, code);
+                const uint32_t codes = fp4_gather_codes<kGroup>(code);
+                if (c < blocks * 16) {
+                    unsigned char* unit = tile + (c >> 4) * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
+                    *reinterpret_cast<uint32_t*>(unit + fp4_scale_bytes(kGroup) + fp4_word_offset(r, c & 15)) = word;
+                    if (kGroup == 16 ? (c & 7) == 0 : (c & 15) == 0)
+                        *reinterpret_cast<uint32_t*>(unit + fp4_scales_offset(r, kGroup == 16 ? (c >> 3) & 1 : 0)) = codes;
+                }
             }
         }
     }
 }
 
+// A warp per row, likewise.
 template <int kGroup>
 __global__ void __launch_bounds__(kThreads) fp4_unpack_kernel(const unsigned char* fp4, int V, int d, uint4* W) {
     const int blocks = fp4_blocks(d), nvec = d >> 3;
     const float factor = ld_dep(reinterpret_cast<const float*>(fp4));
-    const long long n = (long long)V * nvec, stride = (long long)gridDim.x * kThreads;
-    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += stride) {
-        const long long row = i / nvec;
-        const int c = (int)(i - row * nvec), r = (int)(row % kFp4Rows);
-        const unsigned char* unit = fp4 + kFp4Header + ((row / kFp4Rows) * blocks + (c >> 4)) * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
-        const uint32_t word = ld_dep(reinterpret_cast<const uint32_t*>(unit + fp4_scale_bytes(kGroup) + fp4_word_offset(r, c & 15)));
-        const int group = (c & 15) * 8 / kGroup;                             // of the unit's
-        const uint32_t codes = ld_dep(reinterpret_cast<const uint32_t*>(unit + fp4_scales_offset(r, group >> 2)));
-        const uint32_t code = (codes >> (8 * (group & 3))) & 0xffu;
-        const float s = kGroup == 32 ? fp4_two_to((int)code - 127) : fp4_scale_value(code) * factor;
-        uint32_t o[4];
+    const int lane = threadIdx.x & 31;
+    for (long long row = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5); row < V; row += (long long)gridDim.x * kWarps) {
+        const int r = (int)(row % kFp4Rows);
+        const unsigned char* tile = fp4 + kFp4Header + (row / kFp4Rows) * blocks * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
+        for (int c0 = lane; c0 < nvec; c0 += 32 * kAhead) {
+            uint32_t word[kAhead], codes[kAhead];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t b = (word >> (8 * k)) & 0xffu;
-            float x[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                // magnitude codes 0 .. 7: 0, 1/2, then 1 + m/2 times 2^(e - 1)
-                const uint32_t m = (b >> (4 * j)) & 7u, sign = ((b >> (4 * j)) & 8u) << 28;
-                const float a = m < 2 ? 0.5f * (float)m : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-                x[j] = __uint_as_float(__float_as_uint(a * s) | sign);
+            for (int k = 0; k < kAhead; ++k) {
+                const int c = c0 + 32 * k;
+                const unsigned char* unit = tile + (c >> 4) * (long long)fp4_unit_bytes(kGroup, kFp4Rows);
+                word[k] = c < nvec ? ld_dep(reinterpret_cast<const uint32_t*>(unit + fp4_scale_bytes(kGroup) + fp4_word_offset(r, c & 15))) : 0u;
+                codes[k] = c < nvec ? ld_dep(reinterpret_cast<const uint32_t*>(unit + fp4_scales_offset(r, kGroup == 16 ? (c >> 3) & 1 : 0))) : 0u;
             }
-            o[k] = pack_bf16(x[0], x[1]);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int c = c0 + 32 * k, group = (c & 15) * 8 / kGroup;                // of the unit's
+                const uint32_t code = (codes[k] >> (8 * (group & 3))) & 0xffu;
+                const float s = kGroup == 32 ? fp4_two_to((int)code - 127) : fp4_scale_value(code) * factor;
+                uint32_t o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 x = fp4_unpack2(word[k] >> (8 * i));
+                    o[i] = pack_bf16(x.x * s, x.y * s);
+                }
+                if (c < nvec) __stcs(W + row * nvec + c, make_uint4(o[0], o[1], o[2], o[3]));
+            }
         }
-        W[i] = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
 #pragma unroll
             for (int i = 0; i < kTokens; ++i) {
                 const int tok = e + i * kFoldWarps;
-                if (tok < q.M && valid > 0) {
+                if (valid > 0) {                                         // padding tokens too: the tokens of a warp overlap without a test between them
                     const float4 v = *reinterpret_cast<const float4*>(z_mem + tok * (kFp4Rows + 4) + lane * 4);
                     const float4 z = make_float4(v.x * factor[i], v.y * factor[i], v.z * factor[i], v.w * factor[i]);
                     if (valid >= 4) {
@@ -303,13 +303,10 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_stream_kernel(const StreamPar
             }
         }
 #pragma unroll
-        for (int i = 0; i < kTokens; ++i) {
-            const int tok = e + i * kFoldWarps;
-            if (tok < q.M) {                                             // the same for the whole warp
-                const RestState r = rest_reduce_lanes<1>(st[i]);
-                if (lane == 0) p.parts[(size_t)blockIdx.x * N + tok] = r;
-            }
-        }
+        for (int i = 0; i < kTokens; ++i) st[i] = rest_reduce_lanes<1>(st[i]);
+#pragma unroll
+        for (int i = 0; i < kTokens; ++i)
+            if (lane == 0 && e + i * kFoldWarps < q.M) p.parts[(size_t)blockIdx.x * N + e + i * kFoldWarps] = st[i];
     }
     if (warp < 2) grid_dependency_wait();
     ptx::tc_fence_before_sync();

@@ -24,6 +24,7 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 256, kClusterThreads = 1024, kMaxWarps = kClusterThreads / 32;
 constexpr int kClusterCtas = 8;
 constexpr int kMaxCtas = 2048;
+constexpr int kBatch = 8, kHalfBatch = 4;        // tokens whose loads a thread issues at once: a loop that tests for its end in between waits for each
 constexpr int kSums = 4;
 
 enum Span { kWarpSpan, kCtaSpan, kClusterSpan };         // what walks a unit
@@ -227,24 +228,40 @@ __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(con
         const int begin = boundary(p.seq_start, unit, p.M), end = boundary(p.seq_start, unit + 1, p.M);
         const float adv = ld_dep(p.adv + unit);
         int have = 0;
-#pragma unroll 4
-        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) have += is_counted(p.labels, i, p.V) ? 1 : 0;
+        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kBatch * walk.step) {
+            bool in[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) in[u] = i0 + u * walk.step < end && is_counted(p.labels, i0 + u * walk.step, p.V);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) have += in[u] ? 1 : 0;
+        }
         const double n = span_total<kSpan>((double)have, slots, turn);
         const double w = n > 0.0 ? 1.0 / (n * (double)p.S) : 0.0;
         const float wf = (float)w;
         double policy = 0.0, kl = 0.0, cut = 0.0;
-#pragma unroll 4
-        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) {
-            float d = 0.f;
-            const float ce = ld_dep(p.ce + i), old_ce = ld_dep(p.old_ce + i), ref = p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
-            if (is_counted(p.labels, i, p.V)) {
-                const Term t = policy_term(p, ce, old_ce, ref, adv);
-                d = wf * t.grad;
-                policy += (double)t.policy;
-                kl += (double)t.kl;
-                cut += t.cut ? 1.0 : 0.0;
+        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kHalfBatch * walk.step) {
+            float ce[kHalfBatch], old_ce[kHalfBatch], ref[kHalfBatch];
+            bool in[kHalfBatch];
+#pragma unroll
+            for (int u = 0; u < kHalfBatch; ++u) {
+                const long long i = i0 + u * walk.step;
+                ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
+                old_ce[u] = i < end ? ld_dep(p.old_ce + i) : 0.f;
+                ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+                in[u] = i < end && is_counted(p.labels, i, p.V);
             }
-            p.dce[i] = d;
+#pragma unroll
+            for (int u = 0; u < kHalfBatch; ++u) {
+                float d = 0.f;
+                if (in[u]) {
+                    const Term t = policy_term(p, ce[u], old_ce[u], ref[u], adv);
+                    d = wf * t.grad;
+                    policy += (double)t.policy;
+                    kl += (double)t.kl;
+                    cut += t.cut ? 1.0 : 0.0;
+                }
+                if (i0 + u * walk.step < end) p.dce[i0 + u * walk.step] = d;
+            }
         }
         if (n > 0.0) {
             sums[1] = fma(w, policy, sums[1]);
@@ -271,12 +288,26 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
         const int begin = boundary(p.seq_start, 2 * unit, p.M);
         const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin), end = max(boundary(p.seq_start, 2 * unit + 2, p.M), middle);
         double good = 0.0, bad = 0.0;
-#pragma unroll 4
-        for (long long i = (long long)begin + walk.from; i < end; i += walk.step) {
-            const float ce = ld_dep(p.ce + i), ref = p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
-            const double gain = is_counted(p.labels, i, p.V) ? (double)ref - (double)ce : 0.0;
-            good += i < middle ? gain : 0.0;
-            bad += i < middle ? 0.0 : gain;
+        unsigned long long counted = 0;                                  // of the thread's first 64 tokens
+        int k = 0;
+        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kBatch * walk.step) {
+            float ce[kBatch], ref[kBatch];
+            bool in[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {                           // the loads of a batch at once
+                const long long i = i0 + u * walk.step;
+                ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
+                ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+                in[u] = i < end && is_counted(p.labels, i, p.V);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u, ++k) {
+                if (k < 64) counted |= (unsigned long long)in[u] << k;
+                const double gain = in[u] ? (double)ref[u] - (double)ce[u] : 0.0;
+                const bool first = i0 + u * walk.step < middle;
+                good += first ? gain : 0.0;
+                bad += first ? 0.0 : gain;
+            }
         }
         good = (double)p.beta * span_total<kSpan>(good, slots, turn);
         bad = (double)p.beta * span_total<kSpan>(bad, slots, turn);
@@ -293,9 +324,12 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
             sums[2] += good;
             sums[3] += bad;
         }
+        k = 0;
 #pragma unroll 4
-        for (long long i = (long long)begin + walk.from; i < end; i += walk.step)
-            p.dce[i] = is_counted(p.labels, i, p.V) ? (i < middle ? -d : d) : 0.f;
+        for (long long i = (long long)begin + walk.from; i < end; i += walk.step, ++k) {
+            const bool in = k < 64 ? (counted >> k & 1u) != 0 : is_counted(p.labels, i, p.V);
+            p.dce[i] = in ? (i < middle ? -d : d) : 0.f;
+        }
     }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) sums[k] /= (double)p.P;
