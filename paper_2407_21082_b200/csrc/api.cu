@@ -839,7 +839,7 @@ ee_status ee_policy_loss(const float* ce, const float* old_ce, const float* ref_
     p.low = (float)(1.0 - (double)clip_low); p.high = (float)(1.0 + (double)clip_high);
     p.kl_weight = kl_weight;
     p.dce = dce; p.loss = loss; p.workspace = workspace;
-    return policy_loss_launch(p, num_sms, s);
+    return policy_loss_launch(p, num_sms, device, s);
 }
 
 ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* labels, int M, int V, const int* seq_start, int P,
@@ -859,7 +859,7 @@ ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* la
     p.M = M; p.V = V; p.P = P;
     p.beta = beta; p.smoothing = smoothing;
     p.dce = dce; p.margin = margin; p.loss = loss; p.workspace = workspace;
-    return preference_loss_launch(p, num_sms, static_cast<cudaStream_t>(stream));
+    return preference_loss_launch(p, num_sms, device, static_cast<cudaStream_t>(stream));
 }
 
 namespace {

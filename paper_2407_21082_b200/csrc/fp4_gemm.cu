@@ -28,6 +28,7 @@ constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
 constexpr int kMaxStages = 12;
+constexpr int kChunk = 32;                       // columns folded at a time
 constexpr int kUnits = 4;                        // units per stage: taking and giving one costs each issuing thread some 250 cycles
 
 struct GemmMaps {
@@ -71,14 +72,17 @@ int max_slots(int m_pairs, int n_tiles, int workers) {
     return (int)((n_tiles + each - 1) / each) + 1;
 }
 
-// Adds 32 logits' terms, all but those of columns j0 and from nvalid on, to a state whose maximum is at least theirs.  The order of the sums is
+__device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[32]) { ptx::tmem_ld_32x32(from, v); }
+__device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[16]) { ptx::tmem_ld_32x16(from, v); }
+
+// Adds a chunk's terms, all but those of columns j0 and from nvalid on, to a state whose maximum is at least theirs.  The order of the sums is
 // the same in either form, so that a row's result does not depend on which one its warp takes.
 template <bool kAll>
-__device__ __forceinline__ void add_terms(RestState& st, const float (&v)[32], float c, int j0, int nvalid) {
+__device__ __forceinline__ void add_terms(RestState& st, const float (&v)[kChunk], float c, int j0, int nvalid) {
     const unsigned long long minus_m = ptx::pack_f32x2(-st.m, -st.m), cc = ptx::pack_f32x2(c, c);
     unsigned long long s[2] = {0, 0}, t[2] = {0, 0};
 #pragma unroll
-    for (int j = 0; j < 32; j += 2) {
+    for (int j = 0; j < kChunk; j += 2) {
         const unsigned long long dz = ptx::add_f32x2(ptx::pack_f32x2(v[j], v[j + 1]), minus_m);
         const float2 a = ptx::unpack_f32x2(ptx::mul_f32x2(dz, cc));
         float2 x = make_float2(ex2(a.x), ex2(a.y));
@@ -95,27 +99,27 @@ __device__ __forceinline__ void add_terms(RestState& st, const float (&v)[32], f
     st.t += tt.x + tt.y;
 }
 
-// 32 consecutive logits of a row, before the power of two they have in common (`c` is that times log2 e), into its state, which is in the same
+// A chunk of consecutive logits of a row, before the power of two they have in common (`c` is that times log2 e), into its state, which is in the same
 // units.  A new maximum, which leaves its term out of the sum, is rare: some ten of a row's thousand chunks bring one.
-__device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[32], float c, int col0, int nvalid) {
+__device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[kChunk], float c, int col0, int nvalid) {
     float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-    if (nvalid >= 32) {
+    if (nvalid >= kChunk) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) cm[(j >> 1) & 3] = ptx::max3(cm[(j >> 1) & 3], v[j], v[j + 1]);
+        for (int j = 0; j < kChunk; j += 2) cm[(j >> 1) & 3] = ptx::max3(cm[(j >> 1) & 3], v[j], v[j + 1]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < kChunk; ++j)
             if (j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], v[j]);
     }
     const float top = fmaxf(ptx::max3(cm[0], cm[1], cm[2]), cm[3]);
-    if (nvalid >= 32 && !__any_sync(0xffffffffu, top > st.m)) {
-        add_terms<true>(st, v, c, 0, 32);
+    if (nvalid >= kChunk && !__any_sync(0xffffffffu, top > st.m)) {
+        add_terms<true>(st, v, c, 0, kChunk);
         return;
     }
     int j0 = -1;
     if (top > st.m) {
 #pragma unroll
-        for (int j = 31; j >= 0; --j)
+        for (int j = kChunk - 1; j >= 0; --j)
             if (j < nvalid && v[j] == top) j0 = j;
         const bool none = st.s == -1.f;
         const float dl = st.m - top, al = none ? 0.f : ex2(dl * c), n = 1.f + st.s;
@@ -207,10 +211,25 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                     phase ^= 1u;
                 }
             };
-            grid_dependency_wait();
             long long m_pair = begin / p.n_tiles;
             int n_tile = (int)(begin - m_pair * p.n_tiles);
             bool fresh = kResident;
+            // The weights of the first stages do not wait for the kernel that writes the activations.
+            constexpr int kScaleStages = kResident ? (kResidentBlocks + S::kScaleUnits - 1) / S::kScaleUnits : 0;
+            const int scale_stages = kResident ? (blocks + S::kScaleUnits - 1) / S::kScaleUnits : 0;
+            static_assert(kScaleStages < 3, "the first stages");
+            int ahead = 0;                                // steps of the first tile whose weights are under way
+            if (begin < end) ahead = max(0, min(n_stages - scale_stages, (blocks + kUnits - 1) / kUnits));
+            for (int step = 0; step < ahead; ++step) {
+                const int n = min(kUnits, blocks - step * kUnits), s = scale_stages + step;
+                if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * n * S::kPartBytes);
+                for (int k = 0; k < n; ++k) {
+                    const uint32_t at = ring + s * S::kStageBytes + k * S::kPartBytes;
+                    ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), n_tile * blocks + step * kUnits + k, full0 + 8 * s);
+                    ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, n_tile * blocks + step * kUnits + k, full0 + 8 * s);
+                }
+            }
+            grid_dependency_wait();
             for (long long t = begin; ok && t < end; ++t) {
                 if (t + 1 == end) launch_dependents();
                 const int act_unit = (int)(2 * m_pair + rank) * blocks;
@@ -230,7 +249,9 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                 int unit = n_tile * blocks;
                 for (int u0 = 0; u0 < blocks && ok && next_stage((unsigned)t); u0 += kUnits) {
                     const int n = min(kUnits, blocks - u0);
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * n * S::kPartBytes);
+                    const bool here = ahead == 0;
+                    ahead -= here ? 0 : 1;
+                    if (rank == 0 && here) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * n * S::kPartBytes);
 #pragma unroll
                     for (int k = 0; k < kUnits; ++k) {
                         if (k >= n) break;
@@ -240,8 +261,10 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                             if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
                             ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
                         }
-                        ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit + u, full);
-                        ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, unit + u, full);
+                        if (here) {
+                            ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit + u, full);
+                            ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, unit + u, full);
+                        }
                         if (!kResident) ptx::tma_load_3d_pair(at + S::kHalf + S::kScales, &maps.acts, 0, 0, act_unit + u, full);
                     }
                     stage_done();
@@ -375,17 +398,17 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
             const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * kAccCols + half * 64;
             const int col0 = n_tile * kFp4Rows + half * 64;
 #pragma unroll 1
-            for (int k = 0; k < 2; ++k) {
-                float v[32];
-                ptx::tmem_ld_32x32(from + 32 * k, v);
+            for (int k = 0; k < 64 / kChunk; ++k) {
+                float v[kChunk];
+                load_chunk(from + kChunk * k, v);
                 ptx::tmem_ld_wait();
-                if (k == 1) {
+                if (k == 64 / kChunk - 1) {
                     ptx::tc_fence_before_sync();
                     __syncwarp();
                     if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
                 }
-                const int nvalid = q.V - (col0 + 32 * k);
-                if (nvalid > 0) fold_chunk(st, v, c, col0 + 32 * k, nvalid);
+                const int nvalid = q.V - (col0 + kChunk * k);
+                if (nvalid > 0) fold_chunk(st, v, c, col0 + kChunk * k, nvalid);
             }
         }
         if (m_before >= 0) flush(m_before);

@@ -166,8 +166,8 @@ struct PreferenceArgs {
     void* workspace;
 };
 size_t token_loss_workspace_bytes();
-ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, cudaStream_t stream);
-ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, cudaStream_t stream);
+ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, int device, cudaStream_t stream);
+ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, int device, cudaStream_t stream);
 
 // ---- norm over many tensors, and their scaling ----
 size_t grad_norm_workspace_bytes(int n_tensors);

@@ -22,7 +22,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kClusterThreads = 1024, kMaxWarps = kClusterThreads / 32;
-constexpr int kClusterCtas = 8;
+constexpr int kClusterCtas = 8, kWideClusterCtas = 16;  // the second where the device can run as many as there are units
 constexpr int kMaxCtas = 2048;
 constexpr int kBatch = 8, kHalfBatch = 4;        // tokens whose loads a thread issues at once: a loop that tests for its end in between waits for each
 constexpr int kSums = 4;
@@ -99,7 +99,7 @@ __device__ __forceinline__ double span_total(double v, double (&slots)[2][kMaxWa
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
     double all = 0.0;
-    for (int r = 0; r < kClusterCtas; ++r) all += *cluster.map_shared_rank(slot + kWarps, r);
+    for (int r = 0; r < (int)cluster.num_blocks(); ++r) all += *cluster.map_shared_rank(slot + kWarps, r);
     return all;
 }
 
@@ -205,10 +205,11 @@ struct Walk {
             from = threadIdx.x;
             step = kThreads;
         } else {
-            unit = blockIdx.x / kClusterCtas;
-            units_step = gridDim.x / kClusterCtas;
-            from = (blockIdx.x % kClusterCtas) * kThreads + threadIdx.x;
-            step = kClusterCtas * kThreads;
+            const int ctas = (int)cg::this_cluster().num_blocks();
+            unit = blockIdx.x / ctas;
+            units_step = gridDim.x / ctas;
+            from = (blockIdx.x % ctas) * kThreads + threadIdx.x;
+            step = ctas * kThreads;
         }
         leads = from == 0;
     }
@@ -274,6 +275,44 @@ __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(con
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
+// A thread's part of the sum of a sequence's gains, rows first, first + step, .. below end, and which of its first 64 tokens are counted, so that
+// their labels are read once.  (Rows are at most 2^30, so that 32 bits hold every index.)
+__device__ __forceinline__ double gains(const PreferenceArgs& p, int first, int end, int step, unsigned long long& counted) {
+    double sum = 0.0;
+    int k = 0;
+    counted = 0;
+    for (int i0 = first; i0 < end; i0 += kBatch * step, k += kBatch) {
+        float ce[kBatch], ref[kBatch];
+        bool in[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {                               // the loads of a batch at once
+            const int i = i0 + u * step;
+            ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
+            ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+            in[u] = i < end && is_counted(p.labels, i, p.V);
+        }
+        unsigned bits = 0;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            bits |= in[u] ? 1u << u : 0u;
+            sum += in[u] ? (double)ref[u] - (double)ce[u] : 0.0;
+        }
+        if (k < 64) counted |= (unsigned long long)bits << k;
+    }
+    return sum;
+}
+__device__ __forceinline__ void put_weights(const PreferenceArgs& p, int first, int end, int step, unsigned long long counted, float d) {
+    int k = 0;
+    for (int i0 = first; i0 < end; i0 += kBatch * step, k += kBatch) {
+        const unsigned bits = (unsigned)(counted >> (k & 63));
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = i0 + u * step;
+            if (i < end) p.dce[i] = (k < 64 ? (bits >> u & 1u) != 0 : is_counted(p.labels, i, p.V)) ? d : 0.f;
+        }
+    }
+}
+
 // Pairs of sequences 2u (preferred) and 2u + 1 (rejected).
 template <int kSpan>
 __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const PreferenceArgs p) {
@@ -287,28 +326,8 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
     for (int unit = walk.unit; unit < p.P; unit += walk.units_step) {
         const int begin = boundary(p.seq_start, 2 * unit, p.M);
         const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin), end = max(boundary(p.seq_start, 2 * unit + 2, p.M), middle);
-        double good = 0.0, bad = 0.0;
-        unsigned long long counted = 0;                                  // of the thread's first 64 tokens
-        int k = 0;
-        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kBatch * walk.step) {
-            float ce[kBatch], ref[kBatch];
-            bool in[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) {                           // the loads of a batch at once
-                const long long i = i0 + u * walk.step;
-                ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
-                ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
-                in[u] = i < end && is_counted(p.labels, i, p.V);
-            }
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u, ++k) {
-                if (k < 64) counted |= (unsigned long long)in[u] << k;
-                const double gain = in[u] ? (double)ref[u] - (double)ce[u] : 0.0;
-                const bool first = i0 + u * walk.step < middle;
-                good += first ? gain : 0.0;
-                bad += first ? 0.0 : gain;
-            }
-        }
+        unsigned long long counted[2];                                   // of the thread's first 64 tokens of each sequence
+        double good = gains(p, begin + walk.from, middle, walk.step, counted[0]), bad = gains(p, middle + walk.from, end, walk.step, counted[1]);
         good = (double)p.beta * span_total<kSpan>(good, slots, turn);
         bad = (double)p.beta * span_total<kSpan>(bad, slots, turn);
         // with t = e^-|m|: -ln sigma(m) = ln(1 + t) + max(-m, 0), and sigma(m) is 1 / (1 + t) or t / (1 + t)
@@ -324,12 +343,8 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
             sums[2] += good;
             sums[3] += bad;
         }
-        k = 0;
-#pragma unroll 4
-        for (long long i = (long long)begin + walk.from; i < end; i += walk.step, ++k) {
-            const bool in = k < 64 ? (counted >> k & 1u) != 0 : is_counted(p.labels, i, p.V);
-            p.dce[i] = in ? (i < middle ? -d : d) : 0.f;
-        }
+        put_weights(p, begin + walk.from, middle, walk.step, counted[0], -d);
+        put_weights(p, middle + walk.from, end, walk.step, counted[1], d);
     }
 #pragma unroll
     for (int k = 0; k < kSums; ++k) sums[k] /= (double)p.P;
@@ -345,9 +360,30 @@ int span_of(int M, int units, int num_sms) {
     return each >= kThreads / 2 || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
 }
 
+// How many clusters of sixteen CTAs of this kernel (`kind`: which of the two it is) the device runs at once; 0 if it cannot.
+int wide_clusters(const void* kernel, int kind, int device) {
+    static int clusters[2][kMaxDevices];
+    static bool asked[2][kMaxDevices] = {};
+    if (!asked[kind][device]) {
+        int n = 0;
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        pair_launch_config(cfg, attr, dim3(kWideClusterCtas), kClusterThreads, 0, nullptr);
+        attr[1].val.clusterDim.x = kWideClusterCtas;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+            n = 0;
+            (void)cudaGetLastError();
+        }
+        clusters[kind][device] = n;
+        asked[kind][device] = true;
+    }
+    return clusters[kind][device];
+}
+
 template <class Args>
-cudaError_t launch_spans(void (*warp)(Args), void (*cta)(Args), void (*cluster)(Args), const Args& p, int M, int units, int num_sms,
-                         cudaStream_t stream) {
+cudaError_t launch_spans(int kind, void (*warp)(Args), void (*cta)(Args), void (*cluster)(Args), const Args& p, int M, int units, int num_sms,
+                         int device, cudaStream_t stream) {
     const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
     switch (span_of(M, units, num_sms)) {
         case kWarpSpan: {
@@ -356,10 +392,11 @@ cudaError_t launch_spans(void (*warp)(Args), void (*cta)(Args), void (*cluster)(
         }
         case kCtaSpan: return launch_pdl(cta, dim3(units < most ? units : most), kThreads, 0, stream, p);
         default: {
+            const int ctas = units <= wide_clusters(reinterpret_cast<const void*>(cluster), kind, device) ? kWideClusterCtas : kClusterCtas;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
-            pair_launch_config(cfg, attr, dim3(units * kClusterCtas), kClusterThreads, 0, stream);
-            attr[1].val.clusterDim.x = kClusterCtas;
+            pair_launch_config(cfg, attr, dim3(units * ctas), kClusterThreads, 0, stream);
+            attr[1].val.clusterDim.x = ctas;
             return cudaLaunchKernelEx(&cfg, cluster, p);
         }
     }
@@ -369,11 +406,11 @@ cudaError_t launch_spans(void (*warp)(Args), void (*cta)(Args), void (*cluster)(
 
 size_t token_loss_workspace_bytes() { return sizeof(LossSpace); }
 
-ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, cudaStream_t stream) {
+ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, int device, cudaStream_t stream) {
     cudaError_t e;
     if (p.seq_start) {
-        e = launch_spans<PolicyArgs>(policy_sequences_kernel<kWarpSpan>, policy_sequences_kernel<kCtaSpan>, policy_sequences_kernel<kClusterSpan>, p,
-                                     p.M, p.S, num_sms, stream);
+        e = launch_spans<PolicyArgs>(0, policy_sequences_kernel<kWarpSpan>, policy_sequences_kernel<kCtaSpan>, policy_sequences_kernel<kClusterSpan>, p,
+                                     p.M, p.S, num_sms, device, stream);
     } else {
         const long long need = ((long long)p.M + kThreads - 1) / kThreads;
         const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
@@ -382,9 +419,9 @@ ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, cudaStream_t stre
     return e == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
-ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, cudaStream_t stream) {
-    return launch_spans<PreferenceArgs>(preference_kernel<kWarpSpan>, preference_kernel<kCtaSpan>, preference_kernel<kClusterSpan>, p, p.M, p.P, num_sms,
-                                        stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, int device, cudaStream_t stream) {
+    return launch_spans<PreferenceArgs>(1, preference_kernel<kWarpSpan>, preference_kernel<kCtaSpan>, preference_kernel<kClusterSpan>, p, p.M, p.P, num_sms,
+                                        device, stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 }  // namespace ee
