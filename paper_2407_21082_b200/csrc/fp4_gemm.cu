@@ -75,20 +75,26 @@ int max_slots(int m_pairs, int n_tiles, int workers) {
 __device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[32]) { ptx::tmem_ld_32x32(from, v); }
 __device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[16]) { ptx::tmem_ld_32x16(from, v); }
 
-// Adds a chunk's terms, all but those of columns j0 and from nvalid on, to a state whose maximum is at least theirs.  The order of the sums is
-// the same in either form, so that a row's result does not depend on which one its warp takes.
-template <bool kAll>
-__device__ __forceinline__ void add_terms(RestState& st, const float (&v)[kChunk], float c, int j0, int nvalid) {
+// Adds a chunk's terms to a state whose maximum is at least theirs.  In the plain form all of them; otherwise the first nvalid, and where the maximum
+// is new (`up`) all but those that equal it, whose columns come back as bits.  The order of the sums is the same, so that a row's result does
+// not depend on which form its warp takes.
+template <bool kPlain, bool kFull>
+__device__ __forceinline__ uint32_t add_terms(RestState& st, const float (&v)[kChunk], float c, bool up, int nvalid) {
     const unsigned long long minus_m = ptx::pack_f32x2(-st.m, -st.m), cc = ptx::pack_f32x2(c, c);
     unsigned long long s[2] = {0, 0}, t[2] = {0, 0};
+    uint32_t tops = 0;
 #pragma unroll
     for (int j = 0; j < kChunk; j += 2) {
         const unsigned long long dz = ptx::add_f32x2(ptx::pack_f32x2(v[j], v[j + 1]), minus_m);
         const float2 a = ptx::unpack_f32x2(ptx::mul_f32x2(dz, cc));
         float2 x = make_float2(ex2(a.x), ex2(a.y));
-        if (!kAll) {
-            if (j == j0 || j >= nvalid) x.x = 0.f;
-            if (j + 1 == j0 || j + 1 >= nvalid) x.y = 0.f;
+        if (!kPlain) {
+            const bool top0 = up && v[j] == st.m, top1 = up && v[j + 1] == st.m;
+            const bool in0 = kFull || j < nvalid, in1 = kFull || j + 1 < nvalid;
+            if (top0 || !in0) x.x = 0.f;
+            if (top1 || !in1) x.y = 0.f;
+            if (top0 && in0) tops |= 1u << j;
+            if (top1 && in1) tops |= 2u << j;
         }
         const unsigned long long e = ptx::pack_f32x2(x.x, x.y);
         s[(j >> 1) & 1] = ptx::add_f32x2(s[(j >> 1) & 1], e);
@@ -97,10 +103,11 @@ __device__ __forceinline__ void add_terms(RestState& st, const float (&v)[kChunk
     const float2 ss = ptx::unpack_f32x2(ptx::add_f32x2(s[0], s[1])), tt = ptx::unpack_f32x2(ptx::add_f32x2(t[0], t[1]));
     st.s += ss.x + ss.y;
     st.t += tt.x + tt.y;
+    return tops;
 }
 
 // A chunk of consecutive logits of a row, before the power of two they have in common (`c` is that times log2 e), into its state, which is in the same
-// units.  A new maximum, which leaves its term out of the sum, is rare: some ten of a row's thousand chunks bring one.
+// units.  A new maximum, which leaves its term out of the sum, is rare in a long row: some ten of a thousand chunks bring one.
 __device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[kChunk], float c, int col0, int nvalid) {
     float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
     if (nvalid >= kChunk) {
@@ -112,23 +119,23 @@ __device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[kChun
             if (j < nvalid) cm[j & 3] = fmaxf(cm[j & 3], v[j]);
     }
     const float top = fmaxf(ptx::max3(cm[0], cm[1], cm[2]), cm[3]);
-    if (nvalid >= kChunk && !__any_sync(0xffffffffu, top > st.m)) {
-        add_terms<true>(st, v, c, 0, kChunk);
+    const bool up = top > st.m;
+    if (nvalid >= kChunk && !__any_sync(0xffffffffu, up)) {
+        add_terms<true, true>(st, v, c, false, kChunk);
         return;
     }
-    int j0 = -1;
-    if (top > st.m) {
-#pragma unroll
-        for (int j = kChunk - 1; j >= 0; --j)
-            if (j < nvalid && v[j] == top) j0 = j;
+    if (up) {
         const bool none = st.s == -1.f;
         const float dl = st.m - top, al = none ? 0.f : ex2(dl * c), n = 1.f + st.s;
         st.t = none ? 0.f : al * fmaf(dl, n, st.t);
         st.s = none ? 0.f : al * n;
         st.m = top;
-        st.idx = col0 + j0;
     }
-    add_terms<false>(st, v, c, j0, nvalid);
+    const uint32_t tops = nvalid >= kChunk ? add_terms<false, true>(st, v, c, up, kChunk) : add_terms<false, false>(st, v, c, up, nvalid);
+    if (up) {
+        st.idx = col0 + __ffs(tops) - 1;
+        st.s += (float)(__popc(tops) - 1);
+    }
 }
 
 template <int kGroup, bool kResident>

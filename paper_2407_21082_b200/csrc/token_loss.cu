@@ -76,31 +76,29 @@ __device__ __forceinline__ double warp_total(double v) {
     return v;
 }
 
-// The sum of v over the threads that walk a unit, the same in each of them.  Two arrays of shared memory take turns, so that one barrier
-// (or two of the cluster) is enough.
+// The sums of v and w over the threads that walk a unit, the same in each of them.  Two arrays of shared memory take turns, so that one barrier
+// (or two of the cluster) is enough.  Of a cluster each warp reads all CTAs' sums at once, one to a lane.
+struct Slots {
+    double2 of_warp[kMaxWarps], of_cta;
+};
 template <int kSpan>
-__device__ __forceinline__ double span_total(double v, double (&slots)[2][kMaxWarps + 1], int& turn) {
+__device__ __forceinline__ double2 span_totals(double v, double w, Slots (&slots)[2], int& turn) {
     constexpr int kWarps = (kSpan == kClusterSpan ? kClusterThreads : kThreads) / 32;
-    v = warp_total(v);
-    if (kSpan == kWarpSpan) return v;
-    double* slot = slots[turn];
+    const int lane = threadIdx.x & 31;
+    double2 sum = make_double2(warp_total(v), warp_total(w));
+    if (kSpan == kWarpSpan) return sum;
+    Slots& slot = slots[turn];
     turn ^= 1;
-    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = v;
+    if (lane == 0) slot.of_warp[threadIdx.x >> 5] = sum;
     __syncthreads();
-    double s;
-    if (kWarps == 32) {
-        s = warp_total(slot[threadIdx.x & 31]);
-    } else {
-        s = 0.0;
-        for (int w = 0; w < kWarps; ++w) s += slot[w];
-    }
-    if (kSpan == kCtaSpan) return s;
-    if (threadIdx.x == 0) slot[kWarps] = s;
+    sum = lane < kWarps ? slot.of_warp[lane] : make_double2(0.0, 0.0);
+    sum = make_double2(warp_total(sum.x), warp_total(sum.y));
+    if (kSpan == kCtaSpan) return sum;
+    if (threadIdx.x == 0) slot.of_cta = sum;
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    double all = 0.0;
-    for (int r = 0; r < (int)cluster.num_blocks(); ++r) all += *cluster.map_shared_rank(slot + kWarps, r);
-    return all;
+    sum = lane < (int)cluster.num_blocks() ? *cluster.map_shared_rank(&slot.of_cta, lane) : make_double2(0.0, 0.0);
+    return make_double2(warp_total(sum.x), warp_total(sum.y));
 }
 
 // Four sums over the CTA's units, to the means: the CTA that finishes last adds up the CTAs'.
@@ -218,7 +216,7 @@ struct Walk {
 // Every sequence counts alike, and within a sequence every token.
 template <int kSpan>
 __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(const PolicyArgs p) {
-    __shared__ double slots[2][kMaxWarps + 1];
+    __shared__ Slots slots[2];
     launch_dependents();
     grid_dependency_wait();
     clear_outside(p.seq_start, p.S, p.M, p.dce);
@@ -236,7 +234,7 @@ __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(con
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) have += in[u] ? 1 : 0;
         }
-        const double n = span_total<kSpan>((double)have, slots, turn);
+        const double n = span_totals<kSpan>((double)have, 0.0, slots, turn).x;
         const double w = n > 0.0 ? 1.0 / (n * (double)p.S) : 0.0;
         const float wf = (float)w;
         double policy = 0.0, kl = 0.0, cut = 0.0;
@@ -316,7 +314,7 @@ __device__ __forceinline__ void put_weights(const PreferenceArgs& p, int first, 
 // Pairs of sequences 2u (preferred) and 2u + 1 (rejected).
 template <int kSpan>
 __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const PreferenceArgs p) {
-    __shared__ double slots[2][kMaxWarps + 1];
+    __shared__ Slots slots[2];
     launch_dependents();
     grid_dependency_wait();
     clear_outside(p.seq_start, 2 * p.P, p.M, p.dce);
@@ -327,9 +325,9 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
         const int begin = boundary(p.seq_start, 2 * unit, p.M);
         const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin), end = max(boundary(p.seq_start, 2 * unit + 2, p.M), middle);
         unsigned long long counted[2];                                   // of the thread's first 64 tokens of each sequence
-        double good = gains(p, begin + walk.from, middle, walk.step, counted[0]), bad = gains(p, middle + walk.from, end, walk.step, counted[1]);
-        good = (double)p.beta * span_total<kSpan>(good, slots, turn);
-        bad = (double)p.beta * span_total<kSpan>(bad, slots, turn);
+        const double first = gains(p, begin + walk.from, middle, walk.step, counted[0]), second = gains(p, middle + walk.from, end, walk.step, counted[1]);
+        const double2 sum = span_totals<kSpan>(first, second, slots, turn);
+        const double good = (double)p.beta * sum.x, bad = (double)p.beta * sum.y;
         // with t = e^-|m|: -ln sigma(m) = ln(1 + t) + max(-m, 0), and sigma(m) is 1 / (1 + t) or t / (1 + t)
         const double margin = good - bad;
         const float m = (float)margin, t = expf(-fabsf(m)), near = 1.f / (1.f + t), far = t * near;
