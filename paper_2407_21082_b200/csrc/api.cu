@@ -857,7 +857,7 @@ ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* la
     PreferenceArgs p{};
     p.ce = ce; p.ref_ce = ref_ce; p.labels = labels; p.seq_start = seq_start;
     p.M = M; p.V = V; p.P = P;
-    p.beta = beta; p.smoothing = smoothing;
+    p.beta = beta; p.smoothing = smoothing; p.share = 1.0 / P;
     p.dce = dce; p.margin = margin; p.loss = loss; p.workspace = workspace;
     return preference_loss_launch(p, num_sms, device, static_cast<cudaStream_t>(stream));
 }

@@ -160,6 +160,7 @@ struct PreferenceArgs {
     const int* seq_start;      // [2 P + 1]
     int M, V, P;
     float beta, smoothing;
+    double share;              // of a pair: 1 / P
     float* dce;
     float* margin;
     float* loss;

@@ -112,11 +112,11 @@ __device__ __forceinline__ void finish(double (&sums)[kSums], LossSpace* space, 
         if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5][k] = v;
     }
     __syncthreads();
-    if (threadIdx.x < kSums) {
-        double v = 0.0;
-        for (int w = 0; w < kWarps; ++w) v += warp_sums[w][threadIdx.x];
-        if (gridDim.x == 1) loss[threadIdx.x] = (float)v;
-        else space->parts[blockIdx.x][threadIdx.x] = v;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;          // warp k adds up sum k
+    if (warp < kSums) {
+        const double v = warp_total(lane < kWarps ? warp_sums[lane][warp] : 0.0);
+        if (lane == 0 && gridDim.x == 1) loss[warp] = (float)v;
+        if (lane == 0 && gridDim.x > 1) space->parts[blockIdx.x][warp] = v;
     }
     if (gridDim.x == 1) return;
     __syncthreads();
@@ -135,10 +135,9 @@ __device__ __forceinline__ void finish(double (&sums)[kSums], LossSpace* space, 
         if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5][k] = v;
     }
     __syncthreads();
-    if (threadIdx.x < kSums) {
-        double v = 0.0;
-        for (int w = 0; w < kWarps; ++w) v += warp_sums[w][threadIdx.x];
-        loss[threadIdx.x] = (float)v;
+    if (warp < kSums) {
+        const double v = warp_total(lane < kWarps ? warp_sums[lane][warp] : 0.0);
+        if (lane == 0) loss[warp] = (float)v;
     }
     if (threadIdx.x == 0) space->ctrl.head_ticket[0] = 0;                // ready for the next launch
 }
@@ -333,7 +332,7 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
         const float m = (float)margin, t = expf(-fabsf(m)), near = 1.f / (1.f + t), far = t * near;
         const float up = log1pf(t) + fmaxf(-m, 0.f), down = log1pf(t) + fmaxf(m, 0.f);
         const float slope = p.smoothing * (m >= 0.f ? near : far) - (1.f - p.smoothing) * (m >= 0.f ? far : near);
-        const float d = (float)((double)p.beta * (double)slope / (double)p.P);
+        const float d = (float)((double)p.beta * (double)slope * p.share);
         if (walk.leads) {
             p.margin[unit] = m;
             sums[0] += (double)((1.f - p.smoothing) * up + (p.smoothing > 0.f ? p.smoothing * down : 0.f));
@@ -345,7 +344,7 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
         put_weights(p, middle + walk.from, end, walk.step, counted[1], d);
     }
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) sums[k] /= (double)p.P;
+    for (int k = 0; k < kSums; ++k) sums[k] *= p.share;
     if (kSpan == kClusterSpan) cg::this_cluster().sync();
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
