@@ -4,7 +4,7 @@
 // tiles of the M x V plane are numbered row tile by row tile and every CTA takes an equal run of them, so that it stays with a row tile and its
 // epilogue keeps the rows' softmax states in registers from weight tile to weight tile: a state leaves the chip only where a run or a row tile
 // ends, and the weights, which all CTAs walk at the same time, stay in L2.
-//   warp 0 (one lane)  producer      warp 1 (one lane)  scale copies and products      warps 2 .. 9  states
+//   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 9  states      warp 10 (one lane)  scales to tensor memory
 // Two warps share a quarter of the accumulator's lanes (thread = row), each half of its columns.
 #include "q4_common.cuh"
 #include "fp4_common.cuh"
@@ -18,8 +18,8 @@ namespace ee {
 
 namespace {
 
-constexpr int kThreads = 320;
-constexpr int kFoldWarps = 8;
+constexpr int kFoldWarps = 8, kScaleWarp = 2 + kFoldWarps;
+constexpr int kThreads = (3 + kFoldWarps) * 32;
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
 constexpr int kMaxPairs = 128;
@@ -32,9 +32,9 @@ constexpr int kChunk = 32;                       // columns folded at a time
 constexpr int kUnits = 4;                        // units per stage: taking and giving one costs each issuing thread some 250 cycles
 
 struct GemmMaps {
-    // boxes: a weight unit's scales, the half of its elements that a CTA loads; a unit of activations (or its elements alone), the scales of
-    // several
-    CUtensorMap scales, weights, acts, act_scales;
+    // boxes: the scales of kUnits weight units, the halves of their elements that a CTA loads; the same of one unit; a unit of activations (or its
+    // elements alone), the scales of several
+    CUtensorMap scales, weights, scales_one, weights_one, acts, act_scales;
 };
 struct GemmParams {
     Fp4Head q;
@@ -42,7 +42,7 @@ struct GemmParams {
     int m_pairs, n_tiles, slots, n_stages;
 };
 
-// A stage of the ring holds kUnits times: the CTA's half of a weight unit and all its scales, and, unless they are resident, a unit of activations.
+// A stage of the ring holds kUnits halves of weight units, all those units' scales, and, unless they are resident, as many units of activations.
 // kResident: the elements of a row tile's activations stay in shared memory, and their scales, which come through the ring as well, in tensor
 // memory, while the weights pass by.
 template <int kGroup, bool kResident>
@@ -159,14 +159,16 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
     auto accfull_bar = [&](int b) { return act_free + 8u * (1 + b); };
     auto accfree_bar = [&](int b) { return act_free + 8u * (3 + b); };                   // in rank 0: both CTAs' epilogues
     const uint32_t drain_bar = act_free + 8u * 5;
-    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + 8 * (2 * kMaxStages + kResidentBlocks + 6));
+    auto ready_bar = [&](int s) { return act_free + 8u * (6 + s); };                     // in rank 0: the scales are in tensor memory too
+    volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(bar_mem + 8 * (3 * kMaxStages + kResidentBlocks + 6));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-    static_assert(8 * (2 * kMaxStages + kResidentBlocks + 6) + 8 <= kBarBytes, "barriers");
+    static_assert(8 * (3 * kMaxStages + kResidentBlocks + 6) + 8 <= kBarBytes, "barriers");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < n_stages; ++s) {
             ptx::mbar_init(full_bar(s), 1);
             ptx::mbar_init(empty_bar(s), 1);
+            ptx::mbar_init(ready_bar(s), 1);
         }
         for (int u = 0; u < kResidentBlocks; ++u) ptx::mbar_init(act_bar(u), 1);
         ptx::mbar_init(act_free, 1);
@@ -181,6 +183,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         ptx::prefetch_tensormap(&maps.weights);
         ptx::prefetch_tensormap(&maps.scales);
         if (kResident) ptx::prefetch_tensormap(&maps.act_scales);
+        ptx::prefetch_tensormap(&maps.weights_one);
+        ptx::prefetch_tensormap(&maps.scales_one);
     }
     if (warp == 1) {
         ptx::tmem_alloc_pair(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), kTmemCols);
@@ -227,14 +231,22 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
             static_assert(kScaleStages < 3, "the first stages");
             int ahead = 0;                                // steps of the first tile whose weights are under way
             if (begin < end) ahead = max(0, min(n_stages - scale_stages, (blocks + kUnits - 1) / kUnits));
+            const int half_line = S::kScales / 128 + rank * (S::kHalf / 128);
+            auto load_weights = [&](uint32_t at, int unit, int n, uint32_t bar) {        // n units: one request of kUnits, or one by one
+                if (n == kUnits) {
+                    ptx::tma_load_3d_pair(at, &maps.weights, 0, half_line, unit, bar);
+                    ptx::tma_load_3d_pair(at + kUnits * S::kHalf, &maps.scales, 0, 0, unit, bar);
+                } else {
+                    for (int k = 0; k < n; ++k) {
+                        ptx::tma_load_3d_pair(at + k * S::kHalf, &maps.weights_one, 0, half_line, unit + k, bar);
+                        ptx::tma_load_3d_pair(at + kUnits * S::kHalf + k * S::kScales, &maps.scales_one, 0, 0, unit + k, bar);
+                    }
+                }
+            };
             for (int step = 0; step < ahead; ++step) {
                 const int n = min(kUnits, blocks - step * kUnits), s = scale_stages + step;
                 if (rank == 0) ptx::mbar_arrive_expect_tx(full_bar(s), 2 * n * S::kPartBytes);
-                for (int k = 0; k < n; ++k) {
-                    const uint32_t at = ring + s * S::kStageBytes + k * S::kPartBytes;
-                    ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), n_tile * blocks + step * kUnits + k, full0 + 8 * s);
-                    ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, n_tile * blocks + step * kUnits + k, full0 + 8 * s);
-                }
+                load_weights(ring + s * S::kStageBytes, n_tile * blocks + step * kUnits, n, full0 + 8 * s);
             }
             grid_dependency_wait();
             for (long long t = begin; ok && t < end; ++t) {
@@ -253,27 +265,19 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                         stage_done();
                     }
                 }
-                int unit = n_tile * blocks;
+                const int unit = n_tile * blocks;
                 for (int u0 = 0; u0 < blocks && ok && next_stage((unsigned)t); u0 += kUnits) {
                     const int n = min(kUnits, blocks - u0);
                     const bool here = ahead == 0;
                     ahead -= here ? 0 : 1;
                     if (rank == 0 && here) ptx::mbar_arrive_expect_tx(full_bar(0) + (full - full0), 2 * n * S::kPartBytes);
-#pragma unroll
-                    for (int k = 0; k < kUnits; ++k) {
-                        if (k >= n) break;
-                        const int u = u0 + k;
-                        const uint32_t at = to + k * S::kPartBytes;
-                        if (fresh) {
-                            if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
-                            ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
-                        }
-                        if (here) {
-                            ptx::tma_load_3d_pair(at, &maps.weights, 0, S::kScales / 128 + rank * (S::kHalf / 128), unit + u, full);
-                            ptx::tma_load_3d_pair(at + S::kHalf, &maps.scales, 0, 0, unit + u, full);
-                        }
-                        if (!kResident) ptx::tma_load_3d_pair(at + S::kHalf + S::kScales, &maps.acts, 0, 0, act_unit + u, full);
+                    if (here) load_weights(to, unit + u0, n, full);
+                    for (int u = u0; fresh && u < u0 + n; ++u) {
+                        if (rank == 0) ptx::mbar_arrive_expect_tx(act_bar(u), 2 * S::kElements);
+                        ptx::tma_load_3d_pair(resident + u * S::kElements, &maps.acts, 0, S::kScales / 128, act_unit + u, act0 + 8 * u);
                     }
+                    for (int k = 0; !kResident && k < n; ++k)
+                        ptx::tma_load_3d_pair(to + kUnits * (S::kHalf + S::kScales) + k * S::kUnit, &maps.acts, 0, 0, act_unit + u0 + k, full);
                     stage_done();
                 }
                 fresh = false;
@@ -294,25 +298,27 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         // ---------------------------------------------------------------- products
         if (rank == 0 && ptx::elect_one()) {
             constexpr uint32_t idesc = ptx::idesc_fp4<kGroup>(2 * kFp4Rows, kFp4Rows);
-            const uint32_t low0 = ptx::desc_low(ring), low_end = low0 + n_stages * (S::kStageBytes / 16), act_low = ptx::desc_low(resident);
-            uint32_t low = low0, cols = stage_cols, full = full_bar(0), empty = empty_bar(0), phase = 0;
+            const int scale_stages = kResident ? (blocks + S::kScaleUnits - 1) / S::kScaleUnits : 0;
+            const uint32_t low0 = ptx::desc_low(ring), act_low = ptx::desc_low(resident);
+            uint32_t low = low0, cols = stage_cols, ready = ready_bar(0), empty = empty_bar(0), phase = 0;
             uint32_t acc_phase = 1, act_phase = 1;
+            int left = n_stages;
             bool ok = true;
             auto landed = [&](uint32_t bar, uint32_t parity, unsigned what) {
                 if (ptx::mbar_wait(bar, parity, abort_flag)) return true;
                 record_failure(q.ctrl, abort_flag, 2, (bar - bar_base) / 8, what);
                 return ok = false;
             };
-            auto stage_done = [&]() {                     // frees the stage, in both CTAs, once all products so far have been computed
-                ptx::mma_commit_pair(empty, 3);
+            auto next_stage = [&]() {
                 low += S::kStageBytes / 16;
                 cols += S::kStageCols;
-                full += 8;
+                ready += 8;
                 empty += 8;
-                if (low == low_end) {
+                if (--left == 0) {
+                    left = n_stages;
                     low = low0;
                     cols = stage_cols;
-                    full = full_bar(0);
+                    ready = ready_bar(0);
                     empty = empty_bar(0);
                     phase ^= 1u;
                 }
@@ -320,35 +326,24 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
             int n_tile = (int)(begin % p.n_tiles), buf = 0;
             bool fresh = kResident;
             for (long long t = begin; ok && t < end; ++t) {
-                if (fresh) {
+                if (fresh) {                              // stages of the activations' scales are the scale warp's alone
                     act_phase ^= 1u;
-                    for (int u0 = 0; u0 < blocks && landed(full, phase, (unsigned)t); u0 += S::kScaleUnits) {
-                        ptx::tc_fence_after_sync();
-                        for (int k = 0; k < min(S::kScaleUnits, blocks - u0) * S::kAtoms; ++k)
-                            ptx::tmem_cp_scales<true>(act_cols + u0 * S::kUnitCols + 4 * k, low + 32 * k);
-                        stage_done();
-                    }
+                    for (int i = 0; i < scale_stages; ++i) next_stage();
                 }
-                if (!ok || !landed(accfree_bar(buf), acc_phase, (unsigned)t)) break;
+                if (!landed(accfree_bar(buf), acc_phase, (unsigned)t)) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t acc = tmem_base + buf * kAccCols;
                 uint32_t x_low = act_low, x_cols = act_cols;
-                for (int u0 = 0; u0 < blocks && landed(full, phase, (unsigned)t); u0 += kUnits) {
+                for (int u0 = 0; u0 < blocks && landed(ready, phase, (unsigned)t); u0 += kUnits) {
                     const int n = min(kUnits, blocks - u0);
                     for (int k = 0; fresh && k < n; ++k) landed(act_bar(u0 + k), act_phase, (unsigned)t);
                     ptx::tc_fence_after_sync();
 #pragma unroll
                     for (int k = 0; k < kUnits; ++k) {
                         if (k >= n) break;
-                        const uint32_t w_low = low + k * (S::kPartBytes / 16), scales = w_low + S::kHalf / 16, act_scales = scales + S::kScales / 16;
-                        const uint32_t w_cols = cols + k * S::kPartCols;
-                        const uint32_t a_low = kResident ? x_low + k * (S::kElements / 16) : act_scales + S::kScales / 16;
-                        const uint32_t a_cols = kResident ? x_cols + k * S::kUnitCols : w_cols + S::kUnitCols;
-#pragma unroll
-                        for (int i = 0; i < S::kAtoms; ++i) {
-                            ptx::tmem_cp_scales<true>(w_cols + 4 * i, scales + 32 * i);
-                            if (!kResident) ptx::tmem_cp_scales<true>(a_cols + 4 * i, act_scales + 32 * i);
-                        }
+                        const uint32_t w_low = low + k * (S::kHalf / 16), w_cols = cols + k * S::kUnitCols;
+                        const uint32_t a_low = kResident ? x_low + k * (S::kElements / 16) : low + (kUnits * (S::kHalf + S::kScales) + k * S::kUnit + S::kScales) / 16;
+                        const uint32_t a_cols = kResident ? x_cols + k * S::kUnitCols : cols + (kUnits + k) * S::kUnitCols;
                         // 64 columns are 32 bytes: two steps of the descriptor
                         constexpr uint32_t kSecond = kGroup == 16 ? 4 : 0;   // the other scales, or the other half of the same ones
                         ptx::mma_fp4<kGroup, true>(acc, a_low, w_low, idesc, a_cols, w_cols, k > 0 || u0 > 0 ? 1u : 0u);
@@ -357,7 +352,8 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                     }
                     x_low += kUnits * (S::kElements / 16);
                     x_cols += kUnits * S::kUnitCols;
-                    stage_done();
+                    ptx::mma_commit_pair(empty, 3);       // frees the stage, in both CTAs, once all products so far have been computed
+                    next_stage();
                 }
                 if (!ok) break;
                 ptx::mma_commit_pair(accfull_bar(buf), 3);
@@ -371,6 +367,62 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                 acc_phase ^= buf == 0 ? 1u : 0u;
             }
             if (*abort_flag) mma_drain<true>(drain_bar);
+        }
+        __syncwarp();
+    } else if (warp == kScaleWarp) {
+        // ---------------------------------------------------------------- scales to tensor memory, in both CTAs
+        if (rank == 0 && ptx::elect_one()) {
+            const uint32_t low0 = ptx::desc_low(ring);
+            uint32_t low = low0, cols = stage_cols, phase = 0;
+            int stage = 0;
+            bool ok = true;
+            auto landed = [&](unsigned what) {
+                if (ptx::mbar_wait(full_bar(stage), phase, abort_flag)) {
+                    ptx::tc_fence_after_sync();
+                    return true;
+                }
+                record_failure(q.ctrl, abort_flag, 4, stage, what);
+                return ok = false;
+            };
+            auto next_stage = [&]() {
+                low += S::kStageBytes / 16;
+                cols += S::kStageCols;
+                if (++stage == n_stages) {
+                    stage = 0;
+                    low = low0;
+                    cols = stage_cols;
+                    phase ^= 1u;
+                }
+            };
+            int n_tile = (int)(begin % p.n_tiles);
+            bool fresh = kResident;
+            for (long long t = begin; ok && t < end; ++t) {
+                for (int u0 = 0; fresh && u0 < blocks && landed((unsigned)t); u0 += S::kScaleUnits) {
+                    for (int k = 0; k < min(S::kScaleUnits, blocks - u0) * S::kAtoms; ++k)
+                        ptx::tmem_cp_scales<true>(act_cols + u0 * S::kUnitCols + 4 * k, low + 32 * k);
+                    ptx::mma_commit_pair(ready_bar(stage), 1);           // nobody waits for it here, but its phases go with the ring's turns
+                    ptx::mma_commit_pair(empty_bar(stage), 3);
+                    next_stage();
+                }
+                for (int u0 = 0; u0 < blocks && ok && landed((unsigned)t); u0 += kUnits) {
+                    const int n = min(kUnits, blocks - u0);
+#pragma unroll
+                    for (int k = 0; k < kUnits * S::kAtoms; ++k)
+                        if (k < n * S::kAtoms) ptx::tmem_cp_scales<true>(cols + 4 * k, low + kUnits * S::kHalf / 16 + 32 * k);
+                    for (int k = 0; !kResident && k < n * S::kAtoms; ++k)
+                        ptx::tmem_cp_scales<true>(cols + kUnits * S::kUnitCols + 4 * k,
+                                                  low + (kUnits * (S::kHalf + S::kScales) + k / S::kAtoms * S::kUnit) / 16 + 32 * (k % S::kAtoms));
+                    ptx::mma_commit_pair(ready_bar(stage), 1);
+                    next_stage();
+                }
+                fresh = false;
+                if (++n_tile == p.n_tiles) {
+                    n_tile = 0;
+                    fresh = kResident;
+                }
+            }
+            if (*abort_flag)                              // copies still on their way
+                for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
         __syncwarp();
     } else {
@@ -420,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         }
         if (m_before >= 0) flush(m_before);
     }
-    if (warp < 2) grid_dependency_wait();
+    if (warp < 2 || warp == kScaleWarp) grid_dependency_wait();
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::cluster_sync_all();                              // neither CTA leaves while the other may still signal it or write its accumulators
@@ -494,8 +546,10 @@ ee_status launch_shape(GemmParams p, int device, cudaStream_t stream) {
     p.n_stages = S::stages(blocks);
     GemmMaps maps;
     const long long act_units = 2ll * p.m_pairs * blocks, weight_units = (long long)p.n_tiles * blocks;
-    if (!make_unit_map(&maps.scales, p.q.weights, kGroup, weight_units, S::kScales / 128, 1) ||
-        !make_unit_map(&maps.weights, p.q.weights, kGroup, weight_units, S::kHalf / 128, 1) ||
+    if (!make_unit_map(&maps.scales, p.q.weights, kGroup, weight_units, S::kScales / 128, kUnits) ||
+        !make_unit_map(&maps.weights, p.q.weights, kGroup, weight_units, S::kHalf / 128, kUnits) ||
+        !make_unit_map(&maps.scales_one, p.q.weights, kGroup, weight_units, S::kScales / 128, 1) ||
+        !make_unit_map(&maps.weights_one, p.q.weights, kGroup, weight_units, S::kHalf / 128, 1) ||
         !make_unit_map(&maps.acts, p.q.acts, kGroup, act_units, (kResident ? S::kElements : S::kUnit) / 128, 1) ||
         !make_unit_map(&maps.act_scales, p.q.acts, kGroup, act_units, S::kScales / 128, kResident ? S::kScaleUnits : 1))
         return EE_ERR_CUDA;
