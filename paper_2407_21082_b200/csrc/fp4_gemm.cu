@@ -4,8 +4,8 @@
 // tiles of the M x V plane are numbered row tile by row tile and every CTA takes an equal run of them, so that it stays with a row tile and its
 // epilogue keeps the rows' softmax states in registers from weight tile to weight tile: a state leaves the chip only where a run or a row tile
 // ends, and the weights, which all CTAs walk at the same time, stay in L2.
-//   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 9  states      warp 10 (one lane)  scales to tensor memory
-// Two warps share a quarter of the accumulator's lanes (thread = row), each half of its columns.
+//   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 17  states      warp 18 (one lane)  scales to tensor memory
+// Four warps share a quarter of the accumulator's lanes (thread = row), each a quarter of its columns.
 #include "q4_common.cuh"
 #include "fp4_common.cuh"
 #include "gemm_roles.cuh"
@@ -18,17 +18,18 @@ namespace ee {
 
 namespace {
 
-constexpr int kFoldWarps = 8, kScaleWarp = 2 + kFoldWarps;
+constexpr int kFoldWarps = 16, kParts = kFoldWarps / 4, kScaleWarp = 2 + kFoldWarps;
 constexpr int kThreads = (3 + kFoldWarps) * 32;
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
+static_assert(kAccCols / kParts == 32, "a warp folds 32 columns");
 constexpr int kMaxPairs = 128;
 constexpr int kMergeThreads = 256;
 constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
 constexpr int kMaxStages = 12;
-constexpr int kChunk = 32;                       // columns folded at a time
+constexpr int kChunk = kAccCols / kParts;        // columns of a tile that a warp folds
 constexpr int kUnits = 4;                        // units per stage: taking and giving one costs each issuing thread some 250 cycles
 
 struct GemmMaps {
@@ -38,7 +39,7 @@ struct GemmMaps {
 };
 struct GemmParams {
     Fp4Head q;
-    RestState* parts;              // [row][slot][half of the columns]
+    RestState* parts;              // [row][slot][part of the columns]
     int m_pairs, n_tiles, slots, n_stages;
 };
 
@@ -72,21 +73,24 @@ int max_slots(int m_pairs, int n_tiles, int workers) {
     return (int)((n_tiles + each - 1) / each) + 1;
 }
 
-__device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[32]) { ptx::tmem_ld_32x32(from, v); }
-__device__ __forceinline__ void load_chunk(uint32_t from, float (&v)[16]) { ptx::tmem_ld_32x16(from, v); }
+// The state of a row while its logits v (before the power of two they have in common; `c` is that times log2 e) pass by: the largest, m, and sums of
+// the others' 2^(v c - R) and 2^(v c - R) (v c - R) for R = round(m c), so that a term is one multiplication and addition, one power and two
+// additions.  The maximum's own term, left out, is 2^d with d = m c - R, which is as good as exact and taken out at the end.
+__device__ __forceinline__ float reference(float m, float c) { return __fmul_rn(m, c); }
+__device__ __forceinline__ float beside_reference(float m, float c) { return fmaf(m, c, -__fmul_rn(m, c)); }
 
-// Adds a chunk's terms to a state whose maximum is at least theirs.  In the plain form all of them; otherwise the first nvalid, and where the maximum
-// is new (`up`) all but those that equal it, whose columns come back as bits.  The order of the sums is the same, so that a row's result does
-// not depend on which form its warp takes.
+// Adds a chunk's terms.  In the plain form all of them; otherwise the first nvalid, and where the maximum is new (`up`) all but those that equal
+// it, whose columns come back as bits.  The order of the sums is the same, so that a row's result does not depend on which form its warp takes.
 template <bool kPlain, bool kFull>
 __device__ __forceinline__ uint32_t add_terms(RestState& st, const float (&v)[kChunk], float c, bool up, int nvalid) {
-    const unsigned long long minus_m = ptx::pack_f32x2(-st.m, -st.m), cc = ptx::pack_f32x2(c, c);
+    const float r = -reference(st.m, c);
+    const unsigned long long minus_r = ptx::pack_f32x2(r, r), cc = ptx::pack_f32x2(c, c);
     unsigned long long s[2] = {0, 0}, t[2] = {0, 0};
     uint32_t tops = 0;
 #pragma unroll
     for (int j = 0; j < kChunk; j += 2) {
-        const unsigned long long dz = ptx::add_f32x2(ptx::pack_f32x2(v[j], v[j + 1]), minus_m);
-        const float2 a = ptx::unpack_f32x2(ptx::mul_f32x2(dz, cc));
+        const unsigned long long a2 = ptx::fma_f32x2(ptx::pack_f32x2(v[j], v[j + 1]), cc, minus_r);
+        const float2 a = ptx::unpack_f32x2(a2);
         float2 x = make_float2(ex2(a.x), ex2(a.y));
         if (!kPlain) {
             const bool top0 = up && v[j] == st.m, top1 = up && v[j + 1] == st.m;
@@ -98,7 +102,7 @@ __device__ __forceinline__ uint32_t add_terms(RestState& st, const float (&v)[kC
         }
         const unsigned long long e = ptx::pack_f32x2(x.x, x.y);
         s[(j >> 1) & 1] = ptx::add_f32x2(s[(j >> 1) & 1], e);
-        t[(j >> 1) & 1] = ptx::fma_f32x2(e, dz, t[(j >> 1) & 1]);
+        t[(j >> 1) & 1] = ptx::fma_f32x2(e, a2, t[(j >> 1) & 1]);
     }
     const float2 ss = ptx::unpack_f32x2(ptx::add_f32x2(s[0], s[1])), tt = ptx::unpack_f32x2(ptx::add_f32x2(t[0], t[1]));
     st.s += ss.x + ss.y;
@@ -106,8 +110,7 @@ __device__ __forceinline__ uint32_t add_terms(RestState& st, const float (&v)[kC
     return tops;
 }
 
-// A chunk of consecutive logits of a row, before the power of two they have in common (`c` is that times log2 e), into its state, which is in the same
-// units.  A new maximum, which leaves its term out of the sum, is rare in a long row: some ten of a thousand chunks bring one.
+// A chunk of consecutive logits.  A new maximum is rare in a long row: some ten of a thousand chunks bring one.
 __device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[kChunk], float c, int col0, int nvalid) {
     float cm[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
     if (nvalid >= kChunk) {
@@ -125,17 +128,30 @@ __device__ __forceinline__ void fold_chunk(RestState& st, const float (&v)[kChun
         return;
     }
     if (up) {
-        const bool none = st.s == -1.f;
-        const float dl = st.m - top, al = none ? 0.f : ex2(dl * c), n = 1.f + st.s;
-        st.t = none ? 0.f : al * fmaf(dl, n, st.t);
-        st.s = none ? 0.f : al * n;
+        if (st.s == -1.f) {
+            st.s = st.t = 0.f;
+        } else {                                                         // the old maximum's term comes in, all of them go to the new reference
+            const float d = beside_reference(st.m, c), w = ex2(d), n = st.s + w;
+            const float dl = reference(st.m, c) - reference(top, c), al = ex2(dl);
+            st.t = al * fmaf(dl, n, fmaf(w, d, st.t));
+            st.s = al * n;
+        }
         st.m = top;
     }
     const uint32_t tops = nvalid >= kChunk ? add_terms<false, true>(st, v, c, up, kChunk) : add_terms<false, false>(st, v, c, up, nvalid);
     if (up) {
+        const float more = (float)(__popc(tops) - 1), d = beside_reference(top, c), w = ex2(d);
         st.idx = col0 + __ffs(tops) - 1;
-        st.s += (float)(__popc(tops) - 1);
+        st.s = fmaf(more, w, st.s);
+        st.t = fmaf(more, w * d, st.t);
     }
+}
+
+// ... as a state in nats beside its own maximum.
+__device__ __forceinline__ RestState finished(const RestState& st, float factor, float c) {
+    if (st.s == -1.f) return st;
+    const float d = beside_reference(st.m, c), w = ex2(-d);
+    return RestState{st.m * factor, st.s * w, kLn2 * w * fmaf(-d, st.s, st.t), st.idx};
 }
 
 template <int kGroup, bool kResident>
@@ -427,22 +443,22 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- states
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int quarter = warp & 3, part = (warp - 2) >> 2;
         RestState st = rest_empty();
         grid_dependency_wait();
         const float weight_factor = ld_dep(q.weight_factor);
         float factor = 0.f, c = 0.f;
-        int m_before = -1;
-        auto flush = [&](int m_pair) {
-            const long long row = (2ll * m_pair + rank) * kFp4Rows + quarter * 32 + lane;
-            const int slot = pair - worker_of((long long)m_pair * p.n_tiles, pairs, total);
-            if (row < q.M) p.parts[(row * p.slots + slot) * 2 + half] = RestState{st.m * factor, st.s, st.t * factor, st.idx};
+        int m_before = -1, m_pair = (int)(begin / p.n_tiles), n_tile = (int)(begin - (long long)m_pair * p.n_tiles) - 1;
+        auto flush = [&](int m_of) {
+            const long long row = (2ll * m_of + rank) * kFp4Rows + quarter * 32 + lane;
+            const int slot = pair - worker_of((long long)m_of * p.n_tiles, pairs, total);
+            if (row < q.M) p.parts[(row * p.slots + slot) * kParts + part] = finished(st, factor, c);
             st = rest_empty();
         };
         for (long long t = begin; t < end; ++t) {
             const int local = (int)(t - begin), buf = local & 1;
-            const int m_pair = (int)(t / p.n_tiles), n_tile = (int)(t - (long long)m_pair * p.n_tiles);
-            if (m_pair != m_before) {
+            if (++n_tile == p.n_tiles || t == begin) {
+                if (t > begin) n_tile = 0, ++m_pair;
                 if (m_before >= 0) flush(m_before);
                 m_before = m_pair;
                 const long long row = (2ll * m_pair + rank) * kFp4Rows + quarter * 32 + lane;
@@ -454,21 +470,14 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
                 break;
             }
             ptx::tc_fence_after_sync();
-            const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * kAccCols + half * 64;
-            const int col0 = n_tile * kFp4Rows + half * 64;
-#pragma unroll 1
-            for (int k = 0; k < 64 / kChunk; ++k) {
-                float v[kChunk];
-                load_chunk(from + kChunk * k, v);
-                ptx::tmem_ld_wait();
-                if (k == 64 / kChunk - 1) {
-                    ptx::tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
-                }
-                const int nvalid = q.V - (col0 + kChunk * k);
-                if (nvalid > 0) fold_chunk(st, v, c, col0 + kChunk * k, nvalid);
-            }
+            float v[kChunk];
+            ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * kAccCols + part * kChunk, v);
+            ptx::tmem_ld_wait();
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
+            const int col0 = n_tile * kFp4Rows + part * kChunk, nvalid = q.V - col0;
+            if (nvalid > 0) fold_chunk(st, v, c, col0, nvalid);
         }
         if (m_before >= 0) flush(m_before);
     }
@@ -491,8 +500,8 @@ __global__ void __launch_bounds__(kMergeThreads) fp4_merge_kernel(const GemmPara
     const long long row = (long long)blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5);
     if (row >= p.q.M) return;
     const long long total = (long long)p.m_pairs * p.n_tiles, first = row / (2 * kFp4Rows) * p.n_tiles;
-    const int n = 2 * (worker_of(first + p.n_tiles - 1, pairs, total) - worker_of(first, pairs, total) + 1);
-    const RestState* parts = p.parts + row * p.slots * 2;
+    const int n = kParts * (worker_of(first + p.n_tiles - 1, pairs, total) - worker_of(first, pairs, total) + 1);
+    const RestState* parts = p.parts + row * p.slots * kParts;
     RestState mine = rest_empty();
     for (int k = lane; k < n; k += 32) rest_merge(mine, rest_load_cg(parts + k));
     const RestState all = rest_reduce_lanes<1>(mine);
@@ -564,7 +573,7 @@ int fp4_gemm_act_tiles(int M) { return (fp4_tiles(M, kFp4Rows) + 1) / 2 * 2; }
 
 size_t fp4_gemm_parts_bytes(int M, int V) {      // for any number of pairs
     const int m_pairs = fp4_gemm_act_tiles(M) / 2, n_tiles = fp4_tiles(V, kFp4Rows);
-    return (size_t)M * max_slots(m_pairs, n_tiles, pairs_of((long long)m_pairs * n_tiles, kMaxPairs)) * 2 * sizeof(RestState);
+    return (size_t)M * max_slots(m_pairs, n_tiles, pairs_of((long long)m_pairs * n_tiles, kMaxPairs)) * kParts * sizeof(RestState);
 }
 
 ee_status fp4_gemm_launch(const Fp4Head& q, int group, void* parts, int device, cudaStream_t stream) {
