@@ -5,7 +5,7 @@
 // epilogue keeps the rows' softmax states in registers from weight tile to weight tile: a state leaves the chip only where a run or a row tile
 // ends, and the weights, which all CTAs walk at the same time, stay in L2.
 //   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 17  states      warp 18 (one lane)  scales to tensor memory
-// Four warps share a quarter of the accumulator's lanes (thread = row), each a quarter of its columns.
+// Two warps share a quarter of an accumulator's lanes (thread = row), each half of its columns; of the two accumulators each has eight such warps.
 #include "q4_common.cuh"
 #include "fp4_common.cuh"
 #include "gemm_roles.cuh"
@@ -22,14 +22,14 @@ constexpr int kFoldWarps = 16, kParts = kFoldWarps / 4, kScaleWarp = 2 + kFoldWa
 constexpr int kThreads = (3 + kFoldWarps) * 32;
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
-static_assert(kAccCols / kParts == 32, "a warp folds 32 columns");
 constexpr int kMaxPairs = 128;
 constexpr int kMergeThreads = 256;
 constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
 constexpr int kMaxStages = 12;
-constexpr int kChunk = kAccCols / kParts;        // columns of a tile that a warp folds
+constexpr int kChunk = 32;                       // columns folded at a time
+constexpr int kWarpCols = kAccCols / 2;          // ... of a tile, by a warp
 constexpr int kUnits = 4;                        // units per stage: taking and giving one costs each issuing thread some 250 cycles
 
 struct GemmMaps {
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         ptx::mbar_init(act_free, 1);
         for (int b = 0; b < 2; ++b) {
             ptx::mbar_init(accfull_bar(b), 1);
-            ptx::mbar_init(accfree_bar(b), 2 * kFoldWarps);
+            ptx::mbar_init(accfree_bar(b), kFoldWarps);          // half of the warps, of both CTAs
         }
         ptx::mbar_init(drain_bar, 1);
         *abort_flag = 0;
@@ -442,44 +442,58 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
         }
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- states
-        const int quarter = warp & 3, part = (warp - 2) >> 2;
+        // ---------------------------------------------------------------- states (every second tile: a set of eight warps has an accumulator
+        // for itself, so that the way from products to states and back is hidden behind the other set's work)
+        const int quarter = warp & 3, part = (warp - 2) >> 2, buf = part >> 1, half = part & 1;
         RestState st = rest_empty();
         grid_dependency_wait();
         const float weight_factor = ld_dep(q.weight_factor);
         float factor = 0.f, c = 0.f;
-        int m_before = -1, m_pair = (int)(begin / p.n_tiles), n_tile = (int)(begin - (long long)m_pair * p.n_tiles) - 1;
-        auto flush = [&](int m_of) {
-            const long long row = (2ll * m_of + rank) * kFp4Rows + quarter * 32 + lane;
-            const int slot = pair - worker_of((long long)m_of * p.n_tiles, pairs, total);
+        int m_pair = (int)(begin / p.n_tiles), n_tile = (int)(begin - (long long)m_pair * p.n_tiles);
+        auto row_of = [&](int m) { return (2ll * m + rank) * kFp4Rows + quarter * 32 + lane; };
+        auto take = [&]() {                               // the rows of tile pair m_pair
+            factor = row_of(m_pair) < q.M ? ld_dep(q.factor + row_of(m_pair)) * weight_factor : 1.f;
+            c = factor * kLog2e;
+        };
+        auto flush = [&]() {
+            const long long row = row_of(m_pair);
+            const int slot = pair - worker_of((long long)m_pair * p.n_tiles, pairs, total);
             if (row < q.M) p.parts[(row * p.slots + slot) * kParts + part] = finished(st, factor, c);
             st = rest_empty();
         };
-        for (long long t = begin; t < end; ++t) {
-            const int local = (int)(t - begin), buf = local & 1;
-            if (++n_tile == p.n_tiles || t == begin) {
-                if (t > begin) n_tile = 0, ++m_pair;
-                if (m_before >= 0) flush(m_before);
-                m_before = m_pair;
-                const long long row = (2ll * m_pair + rank) * kFp4Rows + quarter * 32 + lane;
-                factor = row < q.M ? ld_dep(q.factor + row) * weight_factor : 1.f;
-                c = factor * kLog2e;
+        take();
+        uint32_t phase = 0;
+        for (long long t = begin; t < end; ++t, ++n_tile) {
+            if (n_tile == p.n_tiles) {
+                flush();
+                n_tile = 0;
+                ++m_pair;
+                take();
             }
-            if (!warp_wait(accfull_bar(buf), (uint32_t)(local >> 1) & 1u, abort_flag)) {
+            if (((int)(t - begin) & 1) != buf) continue;
+            if (!warp_wait(accfull_bar(buf), phase, abort_flag)) {
                 if (lane == 0) record_failure(q.ctrl, abort_flag, 3, buf, (unsigned)t);
                 break;
             }
+            phase ^= 1u;
             ptx::tc_fence_after_sync();
-            float v[kChunk];
-            ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * kAccCols + part * kChunk, v);
-            ptx::tmem_ld_wait();
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
-            const int col0 = n_tile * kFp4Rows + part * kChunk, nvalid = q.V - col0;
-            if (nvalid > 0) fold_chunk(st, v, c, col0, nvalid);
+            const uint32_t from = tmem_base + ((uint32_t)(quarter * 32) << 16) + buf * kAccCols + half * kWarpCols;
+            const int col0 = n_tile * kFp4Rows + half * kWarpCols;
+#pragma unroll 1
+            for (int k = 0; k < kWarpCols; k += kChunk) {
+                float v[kChunk];
+                ptx::tmem_ld_32x32(from + k, v);
+                ptx::tmem_ld_wait();
+                if (k + kChunk == kWarpCols) {
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(accfree_bar(buf), 0));
+                }
+                const int nvalid = q.V - (col0 + k);
+                if (nvalid > 0) fold_chunk(st, v, c, col0 + k, nvalid);
+            }
         }
-        if (m_before >= 0) flush(m_before);
+        flush();
     }
     if (warp < 2 || warp == kScaleWarp) grid_dependency_wait();
     ptx::tc_fence_before_sync();
