@@ -15,6 +15,7 @@
 #pragma once
 
 #include "common.cuh"
+#include "sm100_operands.cuh"
 
 namespace ee {
 
@@ -97,12 +98,30 @@ __device__ __forceinline__ uint32_t fp4_quantise8(uint4 v, uint32_t top, float c
             x[2 * i + 1] = bf16_hi(w[i]) * r;
         }
     } else {
-        code = fp4_scale_code(__fdiv_rn(__uint_as_float(top << 16) * common, 6.f));
-        const float s = fp4_scale_value(code), r = s > 0.f ? __frcp_rn(s) : 0.f;
+        // t / 6 rounded once: a quotient, its exact remainder, and the correction
+        const float t = __uint_as_float(top << 16) * common, q = t * (1.f / 6.f);
+        code = fp4_scale_code(fmaf(fmaf(-6.f, q, t), 1.f / 6.f, q));
+        const float s = fp4_scale_value(code);
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+        r = s > 0.f ? r : 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __fadd_rn(__fadd_rn(__fmul_rn(bf16_lo(w[i]) * common, r), 1536.f), -1536.f);
-            x[2 * i + 1] = __fadd_rn(__fadd_rn(__fmul_rn(bf16_hi(w[i]) * common, r), 1536.f), -1536.f);
+            x[2 * i] = bf16_lo(w[i]);
+            x[2 * i + 1] = bf16_hi(w[i]);
+        }
+        if (common > 1e30f) {                                            // the product of the two would leave the range
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] *= common;
+        } else {
+            r *= common;
+        }
+        const unsigned long long rr = ptx::pack_f32x2(r, r), up = ptx::pack_f32x2(1536.f, 1536.f), down = ptx::pack_f32x2(-1536.f, -1536.f);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float2 y = ptx::unpack_f32x2(ptx::add_f32x2(ptx::add_f32x2(ptx::mul_f32x2(ptx::pack_f32x2(x[i], x[i + 1]), rr), up), down));
+            x[i] = y.x;
+            x[i + 1] = y.y;
         }
     }
     return fp4_pack8(x);

@@ -23,7 +23,7 @@ constexpr int kThreads = (3 + kFoldWarps) * 32;
 constexpr int kTmemCols = 512;
 constexpr int kAccCols = 128;
 constexpr int kMaxPairs = 128;
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 256, kMergeLoads = 8;
 constexpr int kBarBytes = 1024;
 constexpr size_t kSmemBudget = 226 * 1024;
 constexpr int kResidentBlocks = 20;              // units of a row tile that may stay on the chip
@@ -517,7 +517,12 @@ __global__ void __launch_bounds__(kMergeThreads) fp4_merge_kernel(const GemmPara
     const int n = kParts * (worker_of(first + p.n_tiles - 1, pairs, total) - worker_of(first, pairs, total) + 1);
     const RestState* parts = p.parts + row * p.slots * kParts;
     RestState mine = rest_empty();
-    for (int k = lane; k < n; k += 32) rest_merge(mine, rest_load_cg(parts + k));
+    for (int k0 = lane; k0 < n; k0 += 32 * kMergeLoads) {
+        RestState v[kMergeLoads];
+#pragma unroll
+        for (int i = 0; i < kMergeLoads; ++i) v[i] = k0 + 32 * i < n ? rest_load_cg(parts + k0 + 32 * i) : rest_empty();
+        rest_merge(mine, rest_combine(kMergeLoads, [&](int k) -> const RestState& { return v[k]; }));
+    }
     const RestState all = rest_reduce_lanes<1>(mine);
     if (lane == 0) rest_finish(all, p.q, (int)row);
 }
