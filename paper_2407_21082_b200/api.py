@@ -920,7 +920,7 @@ class GradClip:
     buffers are the same from step to step (see ee_grad_norm and ee_grad_clip in include/eexit.h).  Calling it with max_norm computes the norm,
     scales the gradients, in place or into `out` (a list of tensors like them), and returns the norm, fp32 [1] on the device.  norm() and
     scale(max_norm) are its two halves, for a sum over several GPUs in between: scale reads self.value.  It launches on the
-    stream that is current when it is called."""
+    stream that is current when it is called; value and workspace are its own, so that its calls must not run at the same time."""
 
     def __init__(self, grads, *, out=None, workspace=None):
         import ctypes as C

@@ -165,8 +165,10 @@ struct Fp4Head {
     Control* ctrl;
 };
 
-// Few rows (fp4_stream.cu): weights as the M operand.  parts: [CTAs][rows padded] states.
-constexpr int kFp4StreamRows = 128;
+// Few rows (fp4_stream.cu): weights as the M operand.  parts: [CTAs][rows padded] states.  A tile of 128 padded rows was built too and not kept: at
+// V = 50304 the kernel for many rows takes 21.2 us instead of 26.0 for 65 rows of 512, 24.8 instead of 27.1 for 100 of 1024, and 35.6 instead
+// of 32.5 for 128 of 2560.
+constexpr int kFp4StreamRows = 64;
 int fp4_stream_padded(int M);                    // rows of a tile of activations
 size_t fp4_stream_parts_bytes(int M);
 ee_status fp4_stream_launch(const Fp4Head& p, int group, void* parts, int num_sms, int device, cudaStream_t stream);

@@ -1,11 +1,23 @@
 // A head in microscaled 4-bit floating point for many rows.
 //
-// Persistent CTAs; the activations (128 rows to a tile) are the M operand of the products, the weight tiles of 128 rows the N operand.  The
-// tiles of the M x V plane are numbered row tile by row tile and every CTA takes an equal run of them, so that it stays with a row tile and its
-// epilogue keeps the rows' softmax states in registers from weight tile to weight tile: a state leaves the chip only where a run or a row tile
-// ends, and the weights, which all CTAs walk at the same time, stay in L2.
+// Persistent pairs of CTAs; the activations (256 rows to a pair, 128 to a CTA) are the M operand of the products, the weight tiles of 128 rows the
+// N operand, half of each staged by either CTA.  The tiles of the M x V plane are numbered row tile by row tile and every pair takes an equal run
+// of them, so that it stays with its rows: up to d = 2560 their elements stay in shared memory, and their scales in tensor memory, while the
+// weights pass by (40 bytes per cycle and SM instead of 112; L2 gave 63), and the epilogue keeps the rows' softmax states in registers from
+// tile to tile.  A state leaves the chip only where a run or a row tile ends.
 //   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 17  states      warp 18 (one lane)  scales to tensor memory
 // Two warps share a quarter of an accumulator's lanes (thread = row), each half of its columns; of the two accumulators each has eight such warps.
+//
+// What it measured on the way, 16384 rows against V = 50304 (d = 2560 / 1024): 2.30 ms / - with one CTA per 128 x 128 tile, 1.37 with the tensor core's
+// instructions issued under elect.sync instead of lane == 0, 1.32 as pairs with resident activations and one unit per stage, 0.93 / 0.69 with four
+// (taking and giving a stage costs an issuing thread 250 cycles), 0.94 / 0.53 with sixteen epilogue warps instead of eight, each set with its own
+// accumulator (a warp alone needs 1500 cycles for 32 columns: the terms depend on one another; eight warps could not hide that).
+// 4096 x 512 takes 124 us, 203 x 1056 26 us.
+//
+// What bounds it: at d = 2560 the products, some 200 cycles per 128 columns where 128 would be the tensor core's rate (with the loads left
+// out of a copy 0.80 instead of 0.95 ms): a product of 256 x 128 reads 6 KB of operands per SM for 64 cycles of work.  256 weight rows at a
+// time would halve that, but two such accumulators fill tensor memory, scales beside them do not fit.  At d <= 1024 the epilogue: a third of the chunks of a
+// short run bring some row of the warp a new maximum, which costs three more instructions per logit, and 32 powers per chunk take 256 cycles.
 #include "q4_common.cuh"
 #include "fp4_common.cuh"
 #include "gemm_roles.cuh"

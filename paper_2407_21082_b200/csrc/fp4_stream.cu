@@ -1,16 +1,22 @@
-// A head in microscaled 4-bit floating point for few rows (up to 128): what counts is the read of the weights.
+// A head in microscaled 4-bit floating point for few rows (up to 64): what counts is the read of the weights.
 //
 // One persistent CTA per SM takes every so-manieth weight tile of 128 rows.  The weights are the M operand of the products and the
-// activations, padded to 8 .. 128 rows, the N operand; both arrive by plain bulk copies in the layout that the tensor core reads, so no
+// activations, padded to 8, 16, 32 or 64 rows, the N operand; both arrive by plain bulk copies in the layout that the tensor core reads, so no
 // thread touches a weight.  A stage of the ring holds two units (256 columns) of either operand: their scales go to tensor memory by
-// tcgen05.cp, into columns of the stage's own, then the four (two units) products of 64 columns are issued behind them.
+// tcgen05.cp, into columns of the stage's own, then the four products of 64 columns are issued behind them.
 //   warp 0 (one lane)  producer      warp 1 (one lane)  scale copies and products      warps 2 .. 9  logits
 // The accumulators (lanes: the tile's rows, columns: the tokens) are double-buffered.  The eight epilogue warps move a tile of logits to
 // shared memory, token by token, and then a warp takes every eighth token: a lane four of the tile's rows, folded into states in its registers,
-// which it keeps from tile to tile.  The lanes' states, and then the CTAs', are merged once, by the CTA that finishes last.
+// which it keeps from tile to tile.  The lanes' states are merged once, and the CTAs' by the CTA that finishes last (up to 8 rows, a warp
+// for each) or by a kernel of their own (64 rows in one CTA took longer than the head: 30 us of 512 instead of 16).
 //
 // The weights' first stages are requested before the wait for the kernel that writes the activations: at d = 1024 the ring of all SMs
 // together holds most of the head.
+//
+// V = 50304: 10.4 us for a row of 1024 (29.6 MB packed, 4.5 us at the copy rate), 15.7 for one of 2560, 15.6 for 64 of 1024, 22 for 64 of 2560 (74 MB,
+// 3.3 TB/s).  Start, LayerNorm and merge are some 6 us of that.  The issuing threads bound the rest: a single thread takes four to five cycles
+// for an instruction (a hundred for one to the tensor core, as long as the compiler keeps its operands out of uniform registers, which it does under
+// `lane == 0` but not under elect.sync: one row of 1024 took 13.7 us), and a stage of 21 KB takes it some 500.
 #include "q4_common.cuh"
 #include "fp4_common.cuh"
 #include "gemm_roles.cuh"
@@ -356,14 +362,13 @@ ee_status launch_group(const Fp4Head& q, void* parts, int num_sms, int device, c
         case 8: return launch_tokens<kGroup, 8>(q, parts, num_sms, device, stream);
         case 16: return launch_tokens<kGroup, 16>(q, parts, num_sms, device, stream);
         case 32: return launch_tokens<kGroup, 32>(q, parts, num_sms, device, stream);
-        case 64: return launch_tokens<kGroup, 64>(q, parts, num_sms, device, stream);
-        default: return launch_tokens<kGroup, 128>(q, parts, num_sms, device, stream);
+        default: return launch_tokens<kGroup, 64>(q, parts, num_sms, device, stream);
     }
 }
 
 }  // namespace
 
-int fp4_stream_padded(int M) { return M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128; }
+int fp4_stream_padded(int M) { return M <= 8 ? 8 : M <= 16 ? 16 : M <= 32 ? 32 : 64; }
 size_t fp4_stream_parts_bytes(int M) { return (size_t)kStreamMaxCtas * fp4_stream_padded(M) * sizeof(RestState); }
 
 ee_status fp4_stream_launch(const Fp4Head& q, int group, void* parts, int num_sms, int device, cudaStream_t stream) {

