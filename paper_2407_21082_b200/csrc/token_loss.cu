@@ -354,11 +354,13 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
-// What walks a unit: a cluster where a CTA for each would leave most SMs without one and a unit has several tokens for each of a CTA's threads; a
-// CTA where a unit has tokens for half of its threads, or where there are hardly any units; a warp otherwise.
+// What walks a unit: a cluster where it has tokens for several turns of a CTA and there are few enough for all clusters to be there at once; a CTA
+// where it has tokens for half of its threads, or where there are hardly any units; a warp otherwise.  Policy loss of 65536 tokens, a warp /
+// a CTA / a cluster per sequence: 4096 sequences 7.5 / 18.7 / - us, 1024 7.9 / 10.3 / -, 512 12.6 / 7.2 / -, 64 75 / 12.5 / 17.0, 36 91 / 14.1 / 15.3,
+// 16 181 / 24.1 / 9.7; preference loss of 300000 tokens in 36 pairs 237 / 41.7 / 16.3.
 int span_of(int M, int units, int num_sms) {
     const int each = M / units;
-    if (units * 4 <= num_sms && each >= 4 * kThreads) return kClusterSpan;
+    if (units <= num_sms && each >= 8 * kThreads) return kClusterSpan;
     return each >= kThreads / 2 || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
 }
 

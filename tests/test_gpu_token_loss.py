@@ -99,7 +99,7 @@ def test_policy_loss_over_tokens(ee, M, kl_weight):
     _check_policy(got, want, _policy_scales(ce, old, r, adv, labels, V, kw, None), kw, M)
 
 
-@pytest.mark.parametrize("M,S,gap", [(1, 1, 0), (1, 5, 0), (40, 3, 0), (3000, 3000, 0), (5000, 700, 9), (5000, 3, 100), (70000, 2, 0), (70000, 90, 1),
+@pytest.mark.parametrize("M,S,gap", [(1, 1, 0), (1, 5, 0), (40, 3, 0), (3000, 3000, 0), (5000, 700, 9), (5000, 3, 100), (70000, 2, 0), (70000, 30, 0), (70000, 90, 1),
                                      (300001, 9000, 0)])
 def test_policy_loss_over_sequences(ee, M, S, gap):
     rng = np.random.default_rng(M + S)
@@ -141,7 +141,7 @@ def test_policy_loss_at_its_borders(ee):
     assert not empty["loss"].any()
 
 
-@pytest.mark.parametrize("M,P,gap", [(0, 2, 0), (1, 1, 0), (50, 4, 0), (4001, 8, 0), (5000, 900, 3), (20000, 40, 0), (70000, 1, 50), (300001, 3, 0), (300001, 3000, 0)])
+@pytest.mark.parametrize("M,P,gap", [(0, 2, 0), (1, 1, 0), (50, 4, 0), (4001, 8, 0), (5000, 900, 3), (20000, 40, 0), (70000, 1, 50), (300001, 3, 0), (300001, 100, 0), (300001, 3000, 0)])
 @pytest.mark.parametrize("with_ref,smoothing", [(True, 0.0), (False, 0.1)])
 def test_preference_loss(ee, M, P, gap, with_ref, smoothing):
     rng = np.random.default_rng(M + P)
