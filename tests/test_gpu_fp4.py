@@ -72,7 +72,8 @@ def test_ties_and_the_ends_of_the_range(ee, group, scale):
 
 HEADS = [(1, 32, 1), (1, 1024, 5000), (2, 96, 47), (7, 64, 16), (8, 512, 50304), (9, 128, 1000), (16, 320, 515), (17, 256, 3001), (31, 384, 2049),
          (33, 2560, 700), (64, 1024, 2500), (65, 64, 300), (100, 160, 900), (128, 512, 1111), (129, 512, 1111), (150, 192, 129), (300, 1056, 2000),
-         (1100, 96, 700), (3, 8192, 200), (40, 8192, 100), (140, 8192, 90), (1030, 2592, 130)]
+         (1100, 96, 700), (3, 8192, 200), (40, 8192, 100), (140, 8192, 90), (1030, 2592, 130),
+         (20000, 96, 300), (40000, 32, 100), (12000, 2592, 260)]          # runs of tiles that go through several row tiles
 
 
 @pytest.mark.parametrize("group", [16, 32])
