@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) fp4_gemm_kernel(const __grid_cons
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_holder, act_cols = tmem_base + 2 * kAccCols, stage_cols = act_cols + (kResident ? blocks * S::kUnitCols : 0);
 
-    // The two issuing threads have some hundred cycles per stage, at four to five per instruction of a single thread: positions in the ring are
+    // The two issuing threads have some hundred cycles per unit, at four to five per instruction of a single thread: positions in the ring are
     // moved along by additions.
     if (warp == 0) {
         // ---------------------------------------------------------------- producer

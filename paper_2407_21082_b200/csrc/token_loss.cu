@@ -5,7 +5,7 @@
 // The work is light -- 12 to 24 bytes and some twenty operations per token -- so that what counts is the shape: a mean over each
 // sequence's own tokens, or a sequence's sum, is needed before any of its weights.  A unit (a sequence, a pair of sequences, or, where
 // all tokens count alike, a stretch of tokens) is therefore walked twice, the second time out of L1 or L2, by a warp where units are
-// short, by a CTA where they are long, and by a cluster of eight CTAs, which exchange their sums through distributed shared memory,
+// short, by a CTA where they are long, and by a cluster of eight or sixteen CTAs, which exchange their sums through distributed shared memory,
 // where there are so few that the SMs would stand idle.
 //
 // What decides or cancels is done in fp64, which costs little here: the difference of two cross-entropies before the comparison with the
