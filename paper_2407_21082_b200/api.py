@@ -949,6 +949,9 @@ class GradClip:
         self.out = grads if out is None else out
         self.value = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
         self.workspace = new_grad_norm_workspace(grads, self.value.device) if workspace is None else _scratch(workspace, dev)
+        lib, value = _lib.load(), C.c_void_p(self.value.data_ptr())
+        self._norm_fn, self._norm_args = lib.ee_grad_norm, (self._tensors, self._n, value, C.c_void_p(self.workspace.data_ptr()), C.c_size_t(self.workspace.numel()))
+        self._clip_fn, self._clip_args = lib.ee_grad_clip, (self._tensors, self._out, self._n, value)
 
     @staticmethod
     def _one(t, name, dev):
@@ -961,17 +964,19 @@ class GradClip:
         return _stream()
 
     def norm(self) -> torch.Tensor:
-        _check(_lib.load().ee_grad_norm(self._tensors, self._n, self.value.data_ptr(), self.workspace.data_ptr(), self.workspace.numel(), self._here()),
-               "ee_grad_norm")
+        _check(self._norm_fn(*self._norm_args, self._here()), "ee_grad_norm")
         return self.value
 
     def scale(self, max_norm: float) -> None:
-        _check(_lib.load().ee_grad_clip(self._tensors, self._out, self._n, max_norm, self.value.data_ptr(), self._here()), "ee_grad_clip")
+        tensors, out, n, value = self._clip_args
+        _check(self._clip_fn(tensors, out, n, max_norm, value, self._here()), "ee_grad_clip")
 
     def __call__(self, max_norm: float) -> torch.Tensor:
-        value = self.norm()
-        self.scale(max_norm)
-        return value
+        stream = self._here()
+        _check(self._norm_fn(*self._norm_args, stream), "ee_grad_norm")
+        tensors, out, n, value = self._clip_args
+        _check(self._clip_fn(tensors, out, n, max_norm, value, stream), "ee_grad_clip")
+        return self.value
 
 
 def new_grad_norm_workspace(grads, device="cuda") -> torch.Tensor:
