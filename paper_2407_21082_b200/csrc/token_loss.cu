@@ -56,7 +56,7 @@ __device__ __forceinline__ float expm1_minus(float g, float expm1_g) {
         s = fmaf(s, g, 0.5f);
         return g * g * s;
     }
-    return expm1_g - g;
+    return isinf(expm1_g) ? expm1_g : expm1_g - g;                       // (infinity - infinity otherwise)
 }
 
 __device__ __forceinline__ Term policy_term(const PolicyArgs& p, float ce, float old_ce, float ref_ce, float adv) {

@@ -1,0 +1,38 @@
+"""Values at which a formula of the token losses read literally would be 0 times infinity.  Bounds as in test_gpu_token_loss: the exponentials' arguments
+are rounded once, 2^-24 of at most 16, everything else adds a few 2^-24, together 2^-19 of the magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from _util import dev
+
+pytestmark = pytest.mark.gpu
+R = 2.0 ** -19
+
+
+@pytest.fixture(scope="module")
+def ee():
+    import paper_2407_21082_b200 as ee
+    return ee
+
+
+def _np(t):
+    return t.cpu().numpy().astype(np.float64)
+
+
+def _forward(ce, labels, V):
+    return {"ce": dev(ce), "loss": dev(np.array([0.0, ((labels >= 0) & (labels < V)).sum()], np.float32))}
+
+
+@pytest.mark.parametrize("gap", [np.inf, -np.inf, 100.0])
+def test_a_divergence_without_bound_is_infinite(ee, gap):
+    """exp(g) - 1 - g of an infinite g, on either side, and where the exponential leaves fp32."""
+    V, ce, labels = 10, np.full(6, 2.0, np.float32), np.array([0, 1, -1, 2, 3, 4], np.int32)
+    ref = ce.copy()
+    ref[3] = ce[3] - np.float32(gap)
+    got = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(ce), dev(np.ones(6, np.float32)), ref_ce=dev(ref), kl_weight=0.1)
+    loss = _np(got["loss"])
+    assert loss[0] == np.inf and abs(loss[1] + 1.0) <= R and loss[2] == np.inf and loss[3] == 0
+    others = _np(got["dce"])[[0, 1, 4, 5]]
+    assert np.abs(others - 0.2).max() <= R and _np(got["dce"])[2] == 0 and not np.isnan(_np(got["dce"])).any()
