@@ -560,7 +560,8 @@ ee_status ee_exit_head_fp4(const void* h, long long ld_h, const float* gamma, co
  *
  * ee_policy_loss, per counted token with r = exp(old_ce - ce) (its probability over that at drafting time) and the advantage a:
  *   policy = -min(r a, clamp(r, 1 - clip_low, 1 + clip_high) a);   kl = exp(g) - 1 - g with g = ce - ref_ce (ref_ce NULL: 0)
- *   loss fp32 [4]: means of policy + kl_weight kl, of policy, of kl, and of whether the clamp decided
+ *   loss fp32 [4]: means of policy + kl_weight kl, of policy, of kl, and of whether the clamp decided; with kl_weight 0 the divergence from
+ *   ref_ce is watched in loss[2] alone, and neither loss[0] nor dce depends on it, however large it is
  *   seq_start NULL: adv fp32 [M]; the mean is over the counted tokens, whose number is counted[1] (fp32 [2] on the device: ee_head_ce's loss)
  *   seq_start int32 [S + 1] on the device, not decreasing: sequence s is the rows seq_start[s] .. seq_start[s + 1] - 1; adv fp32 [S]; the mean is over
  *   the S sequences of the mean over each one's counted tokens (0 for a sequence without any); counted may be NULL

@@ -70,9 +70,13 @@ __device__ __forceinline__ Term policy_term(const PolicyArgs& p, float ce, float
     if (p.ref_ce) {
         const float g = (float)((double)ce - (double)ref_ce), e = expm1f(g);
         t.kl = expm1_minus(g, e);
-        t.grad = fmaf(p.kl_weight, e, t.grad);
+        if (p.kl_weight != 0.f) t.grad = fmaf(p.kl_weight, e, t.grad);   // 0 only watches the divergence, which may be infinite
     }
     return t;
+}
+
+__device__ __forceinline__ double total_loss(const PolicyArgs& p, double policy, double kl) {
+    return p.kl_weight != 0.f ? fma((double)p.kl_weight, kl, policy) : policy;
 }
 
 __device__ __forceinline__ double warp_total(double v) {
@@ -183,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(const PolicyArg
     }
 #pragma unroll
     for (int k = 1; k < kSums; ++k) sums[k] *= w;
-    sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
+    sums[0] = total_loss(p, sums[1], sums[2]);
     finish<kThreads / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(con
             sums[3] = fma(w, cut, sums[3]);
         }
     }
-    sums[0] = fma((double)p.kl_weight, p.ref_ce ? sums[2] : 0.0, sums[1]);
+    sums[0] = total_loss(p, sums[1], sums[2]);
     if (kSpan == kClusterSpan) cg::this_cluster().sync();                // nobody leaves while its sums may still be read
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }

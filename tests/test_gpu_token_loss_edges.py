@@ -36,3 +36,27 @@ def test_a_divergence_without_bound_is_infinite(ee, gap):
     assert loss[0] == np.inf and abs(loss[1] + 1.0) <= R and loss[2] == np.inf and loss[3] == 0
     others = _np(got["dce"])[[0, 1, 4, 5]]
     assert np.abs(others - 0.2).max() <= R and _np(got["dce"])[2] == 0 and not np.isnan(_np(got["dce"])).any()
+
+
+@pytest.mark.parametrize("by_sequence", [False, True])
+@pytest.mark.parametrize("gap", [88.0, 100.0, np.inf])
+def test_a_penalty_of_weight_zero_only_watches(ee, by_sequence, gap):
+    """One counted token far from the reference: the divergence is reported, the loss and the weights do not know of it."""
+    rng = np.random.default_rng(0)
+    M, V = 300, 50
+    ce = np.abs(rng.normal(0, 1.5, M)).astype(np.float32)
+    old, ref = (np.abs(ce + rng.normal(0, s, M)).astype(np.float32) for s in (0.3, 0.5))
+    labels = rng.integers(0, V, M).astype(np.int32)
+    labels[::3] = -1
+    ref[4] = ce[4] - np.float32(gap)
+    starts = np.array([0, 100, 300], np.int32) if by_sequence else None
+    adv = rng.normal(0, 1, 2 if by_sequence else M).astype(np.float32)
+    args = dict(seq_start=None if starts is None else dev(starts))
+    got = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv), ref_ce=dev(ref), kl_weight=0.0, **args)
+    without = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv), **args)
+    want = oracle.policy_loss(ce, old, adv, labels, V, None, 0.0, (0.2, 0.2), starts)
+    assert torch.equal(got["dce"], without["dce"]) and torch.equal(got["loss"][[0, 1, 3]], without["loss"][[0, 1, 3]])
+    size = np.abs(np.where(want["dce"] == 0, 1.0 / M, want["dce"]))
+    assert (np.abs(_np(got["dce"]) - want["dce"]) <= R * size).all()
+    assert abs(_np(got["loss"])[0] - want["loss"][0]) <= R * 4                # a mean of |adv| e^x, each below 4
+    assert _np(got["loss"])[2] > 1e30
