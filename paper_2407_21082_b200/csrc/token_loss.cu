@@ -63,7 +63,8 @@ __device__ __forceinline__ Term policy_term(const PolicyArgs& p, float ce, float
     Term t;
     const double x = (double)old_ce - (double)ce;                        // ln of the ratio of the new to the old probability
     t.cut = adv > 0.f ? x > p.log_high : adv < 0.f && x < p.log_low;
-    const float ratio = expf((float)x);
+    float ratio = expf((float)x);
+    if (adv == 0.f && isinf(ratio)) ratio = 0.f;                         // a token that asks for nothing, however far its probability has come
     t.policy = -adv * (t.cut ? (adv > 0.f ? p.high : p.low) : ratio);
     t.grad = t.cut ? 0.f : adv * ratio;
     t.kl = 0.f;

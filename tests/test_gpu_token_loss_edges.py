@@ -60,3 +60,22 @@ def test_a_penalty_of_weight_zero_only_watches(ee, by_sequence, gap):
     assert (np.abs(_np(got["dce"]) - want["dce"]) <= R * size).all()
     assert abs(_np(got["loss"])[0] - want["loss"][0]) <= R * 4                # a mean of |adv| e^x, each below 4
     assert _np(got["loss"])[2] > 1e30
+
+
+@pytest.mark.parametrize("by_sequence", [False, True])
+def test_an_advantage_of_zero_asks_for_nothing(ee, by_sequence):
+    """Also where the ratio of the probabilities leaves fp32, or the drafting head gave the token none; a cross-entropy that is not a number stays one."""
+    V, labels = 10, np.zeros(6, np.int32)
+    ce, old = np.zeros(6, np.float32), np.array([100.0, np.inf, 1.0, 100.0, 0.0, 0.05], np.float32)
+    adv = np.array([0, -0.0, 0, 0, 1, -1], np.float32)
+    starts = None
+    if by_sequence:
+        starts, adv = dev(np.array([0, 4, 6], np.int32)), np.array([0, 1], np.float32)
+    got = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv), seq_start=starts)
+    w = np.array([0.25] * 4 + [0.5] * 2) / 2 if by_sequence else np.full(6, 1 / 6)
+    a = np.repeat(adv, [4, 2]) if by_sequence else adv
+    want = w * a * np.exp(np.where(a == 0, 0.0, old))
+    assert np.abs(_np(got["dce"]) - want).max() <= R and abs(_np(got["loss"])[0] + want.sum()) <= R and _np(got["loss"])[3] == 0
+    ce[0] = np.nan
+    got = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv), seq_start=starts)
+    assert np.isnan(_np(got["dce"])[0]) and np.isnan(_np(got["loss"])[0]) and not np.isnan(_np(got["dce"])[1:]).any()
