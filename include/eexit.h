@@ -537,8 +537,9 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
  * 16-byte aligned.
  *
  * ee_exit_head_fp4 is ee_exit_head with the values of the packed head for W and y4 for y, y being that of ee_head_ce: same definition otherwise
- * (sums in fp32), same outputs, strides, alignment and rules; a row whose y is not finite has an entropy that is not a number.  The packed
- * head, gamma and beta are data of the stream (they may be written right before the call).  M up to 2^30; up to 64 rows are one pass over the packed weights.
+ * (sums in fp32), same outputs, strides, alignment and rules; a row whose y is not finite has an entropy that is not a number and, as
+ * with the other heads where no logit is a number, the argmax 2^31 - 1, which is no index into the vocabulary.  The packed head, gamma and beta
+ * are data of the stream (they may be written right before the call).  M up to 2^30; up to 64 rows are one pass over the packed weights.
  * V = 50304, single calls in a graph, bf16 head / 4-bit whole numbers in groups of 64 / this in groups of 16, us: 8 rows of 1024 24.7 / 17.8 / 11.4,
  * 64 of 1024 25.1 / 28.3 / 15.6, 256 of 1024 31.4 / 101.6 / 25.6, 64 of 2560 48.7 / 49.4 / 22.0, 16384 of 2560 2600 / - / 1100.
  * Workspace: ee_exit_head_fp4_workspace_bytes(M, d, V, group), 256-byte aligned, initialised once with ee_workspace_init; that of fewer
