@@ -1,9 +1,12 @@
-"""Heads in microscaled 4-bit floating point: what rows without a value give."""
+"""Heads in microscaled 4-bit floating point: what rows without a value give, and what the two head kernels do in runs of many tiles.  Bounds as in
+test_gpu_fp4 (assert_close)."""
 import numpy as np
 import pytest
 
 import gen
+import oracle
 from _util import dev_bf16, head_to_dev
+from test_gpu_fp4 import assert_close
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +31,22 @@ def test_a_row_without_a_value_has_no_index_in_any_head(ee, M):
         argmax = out["argmax"].cpu().numpy()
         assert (argmax[3:5] == 2 ** 31 - 1).all() and np.isnan(out["entropy"][3:5].cpu().numpy()).all() and not out["exit_mask"][3:5].any()
         assert (np.delete(argmax, [3, 4]) < V).all() and (argmax >= 0).all()
+
+
+# What a CTA or a pair of them carries from tile to tile, on some 148 SMs.  Up to 64 rows: 313 to 469 weight tiles, two to four to a CTA, of one to four
+# stages each, with the accumulators in turn.  Above: 5 to 21 tiles to a pair, of several units each; those of 1500 and 3000 rows cross from one row
+# tile to the next, where the activations and their scales are replaced.  2688 columns are more than a pair keeps of a row.
+LONG_RUNS = [(12, 256, 60000), (32, 640, 40000), (64, 1024, 50304), (203, 1056, 50257), (1000, 128, 50304), (3000, 1024, 5000), (3000, 2560, 5000), (1500, 2688, 6000)]
+
+
+@pytest.mark.parametrize("group", [16, 32])
+@pytest.mark.parametrize("M,d,V", LONG_RUNS)
+def test_runs_of_many_tiles_match_the_oracle(ee, M, d, V, group):
+    cfg = gen.make_config("c1", seed=23, planted=True, M=M, d=d, V=V, heads=1)
+    head = cfg["heads"][0]
+    hd = head_to_dev(head)
+    fp4 = ee.ee_head_fp4_pack(hd["W"], group)
+    workspace = ee.new_exit_head_fp4_workspace(M, fp4)
+    out = ee.ee_exit_head_fp4(dev_bf16(cfg["h"]), hd["gamma"], hd["beta"], 1e-5, fp4, 1.0, workspace=workspace)
+    assert_close(out, oracle.exit_head_fp4(cfg["h"], head, 1.0, group), d, V, f"{M} {d} {V} {group}")
+    assert ee.ee_query_async_error(workspace) == 0
