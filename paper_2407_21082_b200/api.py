@@ -644,6 +644,13 @@ def prepare_head_ce_grad(head, labels, ln_eps, forward, *, dce=None, dloss=None,
     return PreparedCall(_lib.load().ee_head_ce_grad_of, args, "ee_head_ce_grad", keep, out)
 
 
+def _packed(weights, kind):
+    """Weights packed in the form `kind`: the two 4-bit forms have the same attributes, and sizes that fit one another."""
+    if not isinstance(weights, kind):
+        raise TypeError(f"expected {kind.__name__}, got {type(weights).__name__}")
+    return weights
+
+
 class Q4Weights:
     """A head's weights in 4 bits (see include/eexit.h): the packed bytes (a device tensor) and what they are of."""
     __slots__ = ("data", "V", "d", "group")
@@ -673,7 +680,7 @@ def ee_head_q4_pack(W, group: int = 64, *, out: Q4Weights | None = None) -> Q4We
         if nbytes == 0:
             raise EExitError(2, "ee_head_q4_pack")
         out = Q4Weights(torch.empty(nbytes, dtype=torch.uint8, device=W.device), V, d, group)
-    elif (out.V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
+    elif (_packed(out, Q4Weights).V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
         raise ValueError("out was made for other weights")
     _check(_lib.load().ee_head_q4_pack(W.data_ptr(), V, d, int(group), out.data.data_ptr(), out.data.numel(), _stream()), "ee_head_q4_pack")
     return out
@@ -681,7 +688,7 @@ def ee_head_q4_pack(W, group: int = 64, *, out: Q4Weights | None = None) -> Q4We
 
 def ee_head_q4_unpack(q4: Q4Weights, *, out=None) -> torch.Tensor:
     """What the packed weights stand for, bf16 [V, d]."""
-    dev = _device_of(q4.data, "q4")
+    dev = _device_of(_packed(q4, Q4Weights).data, "q4")
     if out is None:
         out = torch.empty((q4.V, q4.d), dtype=torch.bfloat16, device=q4.data.device)
     else:
@@ -733,13 +740,13 @@ def _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_wo
 
 def ee_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> dict:
     """ee_exit_head with weights held in 4 bits (ee_head_q4_pack); see there for the arguments."""
-    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_exit_head_q4_workspace)
+    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, _packed(q4, Q4Weights), tau, out, workspace, new_exit_head_q4_workspace)
     _check(_lib.load().ee_exit_head_q4(*args), "ee_exit_head_q4")
     return out
 
 
 def prepare_exit_head_q4(h, gamma, beta, ln_eps, q4: Q4Weights, tau, *, out=None, workspace=None) -> PreparedCall:
-    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_exit_head_q4_workspace)
+    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, _packed(q4, Q4Weights), tau, out, workspace, new_exit_head_q4_workspace)
     return PreparedCall(_lib.load().ee_exit_head_q4, args, "ee_exit_head_q4", keep, out)
 
 
@@ -772,7 +779,7 @@ def ee_head_fp4_pack(W, group: int = 16, *, out: Fp4Weights | None = None) -> Fp
         if nbytes == 0:
             raise EExitError(2, "ee_head_fp4_pack")
         out = Fp4Weights(torch.empty(nbytes, dtype=torch.uint8, device=W.device), V, d, group)
-    elif (out.V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
+    elif (_packed(out, Fp4Weights).V, out.d, out.group) != (V, d, group) or out.data.get_device() != dev:
         raise ValueError("out was made for other weights")
     _check(_lib.load().ee_head_fp4_pack(W.data_ptr(), V, d, int(group), out.data.data_ptr(), out.data.numel(), _stream()), "ee_head_fp4_pack")
     return out
@@ -780,7 +787,7 @@ def ee_head_fp4_pack(W, group: int = 16, *, out: Fp4Weights | None = None) -> Fp
 
 def ee_head_fp4_unpack(fp4: Fp4Weights, *, out=None) -> torch.Tensor:
     """What the packed weights stand for, bf16 [V, d]."""
-    dev = _device_of(fp4.data, "fp4")
+    dev = _device_of(_packed(fp4, Fp4Weights).data, "fp4")
     if out is None:
         out = torch.empty((fp4.V, fp4.d), dtype=torch.bfloat16, device=fp4.data.device)
     else:
@@ -802,13 +809,13 @@ def new_exit_head_fp4_workspace(M: int, fp4: Fp4Weights) -> torch.Tensor:
 def ee_exit_head_fp4(h, gamma, beta, ln_eps, fp4: Fp4Weights, tau, *, out=None, workspace=None) -> dict:
     """ee_exit_head with weights held in 4-bit floating point (ee_head_fp4_pack) and activations in the same form; see there for the
     arguments."""
-    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, fp4, tau, out, workspace, new_exit_head_fp4_workspace)
+    args, out, _ = _exit_head_4bit_args(h, gamma, beta, ln_eps, _packed(fp4, Fp4Weights), tau, out, workspace, new_exit_head_fp4_workspace)
     _check(_lib.load().ee_exit_head_fp4(*args), "ee_exit_head_fp4")
     return out
 
 
 def prepare_exit_head_fp4(h, gamma, beta, ln_eps, fp4: Fp4Weights, tau, *, out=None, workspace=None) -> PreparedCall:
-    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, fp4, tau, out, workspace, new_exit_head_fp4_workspace)
+    args, out, keep = _exit_head_4bit_args(h, gamma, beta, ln_eps, _packed(fp4, Fp4Weights), tau, out, workspace, new_exit_head_fp4_workspace)
     return PreparedCall(_lib.load().ee_exit_head_fp4, args, "ee_exit_head_fp4", keep, out)
 
 

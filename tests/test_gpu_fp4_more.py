@@ -2,6 +2,7 @@
 test_gpu_fp4 (assert_close)."""
 import numpy as np
 import pytest
+import torch
 
 import gen
 import oracle
@@ -50,3 +51,12 @@ def test_runs_of_many_tiles_match_the_oracle(ee, M, d, V, group):
     out = ee.ee_exit_head_fp4(dev_bf16(cfg["h"]), hd["gamma"], hd["beta"], 1e-5, fp4, 1.0, workspace=workspace)
     assert_close(out, oracle.exit_head_fp4(cfg["h"], head, 1.0, group), d, V, f"{M} {d} {V} {group}")
     assert ee.ee_query_async_error(workspace) == 0
+
+
+def test_packing_into_the_other_form_is_refused(ee):
+    W = torch.zeros((128, 256), dtype=torch.bfloat16, device="cuda")
+    whole, floating = ee.ee_head_q4_pack(W, 32), ee.ee_head_fp4_pack(W, 32)
+    for pack, out in ((ee.ee_head_fp4_pack, whole), (ee.ee_head_q4_pack, floating)):
+        with pytest.raises(TypeError):
+            pack(W, 32, out=out)
+    assert ee.ee_head_fp4_pack(W, 32, out=floating) is floating and ee.ee_head_q4_pack(W, 32, out=whole) is whole
