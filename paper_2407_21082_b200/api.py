@@ -714,6 +714,8 @@ def _exit_head_4bit_args(h, gamma, beta, ln_eps, q4, tau, out, workspace, new_wo
     if h.dim() != 2:
         raise ValueError(f"h must be row-major [M, d = {d}]")
     M = h.shape[0]
+    if M > _INT_MAX:
+        raise EExitError(2, "an exit head of 4-bit weights")
     ld = _row_stride(h, "h", M, d, dev)
     data = q4.data
     if data.get_device() != dev:
@@ -763,7 +765,17 @@ class Fp4Weights:
         self.data, self.V, self.d, self.group = data, int(V), int(d), int(group)
 
 
+# ctypes cuts an int off at 32 bits, and what is left of an invalid size may be a valid one.
+_INT_MAX = 2 ** 31 - 1
+
+
+def _are_ints(*sizes) -> bool:
+    return all(-_INT_MAX <= n <= _INT_MAX for n in sizes)
+
+
 def ee_head_fp4_bytes(V: int, d: int, group: int) -> int:
+    if not _are_ints(V, d, group):
+        return 0
     return int(_lib.load().ee_head_fp4_bytes(int(V), int(d), int(group)))
 
 
@@ -798,6 +810,8 @@ def ee_head_fp4_unpack(fp4: Fp4Weights, *, out=None) -> torch.Tensor:
 
 
 def ee_exit_head_fp4_workspace_bytes(M: int, d: int, V: int, group: int) -> int:
+    if not _are_ints(M, d, V, group):
+        return 0
     return int(_lib.load().ee_exit_head_fp4_workspace_bytes(int(M), int(d), int(V), int(group)))
 
 
@@ -833,11 +847,13 @@ def new_preference_loss_outputs(M: int, P: int, device="cuda") -> dict:
                 dce=torch.empty(M, dtype=torch.float32, device=device))
 
 
-def _token_loss_inputs(forward, labels, seq_start, units_per, ref_ce, out):
+def _token_loss_inputs(forward, labels, V, seq_start, units_per, ref_ce, out):
     """ce, M, device ordinal and the number of units that seq_start delimits (None without it)."""
     ce = forward["ce"]
     dev = _device_of(ce, "ce")
     M = ce.numel()
+    if M > _INT_MAX or not -_INT_MAX <= V <= _INT_MAX:
+        raise EExitError(2, "a loss over tokens")
     f32 = torch.float32
     _vector(ce, "ce", f32, M, dev)
     _vector(labels, "labels", torch.int32, M, dev)
@@ -852,6 +868,8 @@ def _token_loss_inputs(forward, labels, seq_start, units_per, ref_ce, out):
             raise ValueError(f"seq_start must have 1 + {units_per} n elements, n >= 1" if units_per > 1 else "seq_start must have at least two elements")
         _vector(seq_start, "seq_start", torch.int32, n, dev)
         units = (n - 1) // units_per
+        if units > _INT_MAX:
+            raise EExitError(2, "a loss over tokens")
     if out is not None:
         _vector(out.get("loss"), "out['loss']", f32, 4, dev)
         _vector(out.get("dce"), "out['dce']", f32, M, dev)
@@ -859,7 +877,7 @@ def _token_loss_inputs(forward, labels, seq_start, units_per, ref_ce, out):
 
 
 def _policy_loss_args(forward, labels, V, old_ce, adv, ref_ce, kl_weight, clip, seq_start, out, workspace):
-    ce, M, dev, S = _token_loss_inputs(forward, labels, seq_start, 1, ref_ce, out)
+    ce, M, dev, S = _token_loss_inputs(forward, labels, V, seq_start, 1, ref_ce, out)
     f32 = torch.float32
     _vector(old_ce, "old_ce", f32, M, dev)
     _vector(adv, "adv", f32, M if S is None else S, dev)
@@ -893,7 +911,7 @@ def prepare_policy_loss(forward, labels, V: int, old_ce, adv, *, ref_ce=None, kl
 def _preference_loss_args(forward, labels, V, seq_start, ref_ce, beta, smoothing, out, workspace):
     if seq_start is None:
         raise ValueError("seq_start must be an int32 CUDA tensor")
-    ce, M, dev, P = _token_loss_inputs(forward, labels, seq_start, 2, ref_ce, out)
+    ce, M, dev, P = _token_loss_inputs(forward, labels, V, seq_start, 2, ref_ce, out)
     if out is None:
         out = new_preference_loss_outputs(M, P, ce.device)
     else:

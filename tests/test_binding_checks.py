@@ -27,3 +27,15 @@ def test_the_two_4_bit_forms_are_not_taken_for_one_another():
         ee.ee_head_fp4_unpack(whole)
     with pytest.raises(TypeError):
         ee.ee_head_q4_unpack(floating)
+
+
+def test_sizes_beyond_32_bits_are_invalid_and_not_cut_off():
+    """2^32 + n is n to a 32-bit int: each of these had the bytes of the valid size that is left of it."""
+    over = 1 << 32
+    for bad in ((over + 5, 64, 16), (5, over + 64, 16), (5, 64, over + 16), (5 - over, 64, 16)):
+        assert ee.ee_head_fp4_bytes(*bad) == 0
+    for bad in ((over + 4, 64, 10, 16), (4, over + 64, 10, 16), (4, 64, over + 10, 16), (4, 64, 10, over + 32)):
+        assert ee.ee_exit_head_fp4_workspace_bytes(*bad) == 0
+    assert ee.ee_head_fp4_bytes(5, 64, 16) > 0 and ee.ee_exit_head_fp4_workspace_bytes(4, 64, 10, 16) > 0
+    with pytest.raises(ee.EExitError):
+        ee.Fp4Weights(torch.zeros(16, dtype=torch.uint8), over + 5, 64, 16)

@@ -79,3 +79,21 @@ def test_an_advantage_of_zero_asks_for_nothing(ee, by_sequence):
     ce[0] = np.nan
     got = ee.ee_policy_loss(_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv), seq_start=starts)
     assert np.isnan(_np(got["dce"])[0]) and np.isnan(_np(got["loss"])[0]) and not np.isnan(_np(got["dce"])[1:]).any()
+
+
+def test_sizes_beyond_32_bits_are_refused(ee):
+    """2^32 + n tokens or labels' values are n to a 32-bit int, and the call answered for those."""
+    small = torch.zeros(4, device="cuda")
+    labels, starts = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    forward = {"ce": small, "loss": torch.ones(2, device="cuda")}
+    for V in ((1 << 32) + 10, 10 - (1 << 32), 1 << 40):
+        with pytest.raises(ee.EExitError):
+            ee.ee_policy_loss(forward, labels, V, small, small)
+        with pytest.raises(ee.EExitError):
+            ee.ee_preference_loss(forward, labels, V, starts)
+    many = torch.empty((1 << 32) + 5, device="cuda")
+    forward, out = {"ce": many, "loss": torch.ones(2, device="cuda")}, {"loss": torch.zeros(4, device="cuda"), "margin": torch.zeros(1, device="cuda"), "dce": many}
+    with pytest.raises(ee.EExitError):
+        ee.ee_policy_loss(forward, many.view(torch.int32), 10, many, many, out=out)
+    with pytest.raises(ee.EExitError):
+        ee.ee_preference_loss(forward, many.view(torch.int32), 10, starts, out=out)
