@@ -589,10 +589,10 @@ ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* la
  *   ee_grad_norm:  norm[0] = sqrt(sum over all tensors of the sum of g^2), added up in fp32 by eights and in fp64 above, in a fixed order
  *   ee_grad_clip:  out = round(g * min(1, max_norm / (norm[0] + 1e-6))) in the tensor's type; `out` NULL: in place, where nothing is written if the
  *                  factor is 1.  A norm that is not a number makes everything that.
- * The tensors (a HOST array; contiguous, n >= 0 elements of the type, aligned to it, at most 2^36 elements each) must not overlap; norm is fp32 [1]
- * on the device, so that a sum over several GPUs may be put in between.  out is a HOST array of pointers, one per tensor, aligned alike; an out equal to its
+ * The tensors (a HOST array of at most 2^29; contiguous, n >= 0 elements of the type, aligned to it, at most 2^36 elements each) must not
+ * overlap; norm is fp32 [1] on the device, so that a sum over several GPUs may be put in between.  out is a HOST array of pointers, one per tensor, aligned alike; an out equal to its
  * tensor is that tensor in place.  Tensors that begin on a 16-byte border are accessed by 16 bytes.  The arrays are read before the call
- * returns; up to 512 tensors are one launch of each call.  Workspace of the norm: ee_grad_norm_workspace_bytes(n_tensors) (0 if that is negative),
+ * returns; up to 512 tensors are one launch of each call.  Workspace of the norm: ee_grad_norm_workspace_bytes(n_tensors) (0 if that is out of range),
  * 256-byte aligned, initialised once with ee_workspace_init.
  */
 #define EE_BFLOAT16 0

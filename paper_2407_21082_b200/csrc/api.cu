@@ -864,7 +864,7 @@ ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* la
 
 namespace {
 ee_status tensors_ok(const ee_tensor* tensors, int n_tensors) {
-    if (n_tensors < 0) return EE_ERR_SHAPE;
+    if (n_tensors < 0 || n_tensors > kMaxCount / 2) return EE_ERR_SHAPE;
     if (n_tensors > 0 && !tensors) return EE_ERR_NULL;
     long long bytes = 0;
     for (int i = 0; i < n_tensors; ++i) {
@@ -879,7 +879,7 @@ ee_status tensors_ok(const ee_tensor* tensors, int n_tensors) {
 }
 }  // namespace
 
-size_t ee_grad_norm_workspace_bytes(int n_tensors) { return n_tensors < 0 ? 0 : grad_norm_workspace_bytes(n_tensors); }
+size_t ee_grad_norm_workspace_bytes(int n_tensors) { return n_tensors < 0 || n_tensors > kMaxCount / 2 ? 0 : grad_norm_workspace_bytes(n_tensors); }
 
 ee_status ee_grad_norm(const ee_tensor* tensors, int n_tensors, float* norm, void* workspace, size_t workspace_bytes_, void* stream) {
     const ee_status ok = tensors_ok(tensors, n_tensors);
