@@ -941,7 +941,7 @@ _GRAD_TYPES = {torch.bfloat16: _lib.EE_BFLOAT16, torch.float16: _lib.EE_FLOAT16,
 
 
 class GradClip:
-    """The norm over a list of gradients (contiguous bf16, fp16 or fp32 tensors) and their scaling, with the list marshalled once: gradient
+    """The norm over a list of gradients (contiguous bf16, fp16 or fp32 tensors that do not overlap) and their scaling, with the list marshalled once: gradient
     buffers are the same from step to step (see ee_grad_norm and ee_grad_clip in include/eexit.h).  Calling it with max_norm computes the norm,
     scales the gradients, in place or into `out` (a list of tensors like them), and returns the norm, fp32 [1] on the device.  norm() and
     scale(max_norm) are its two halves, for a sum over several GPUs in between: scale reads self.value.  It launches on the
@@ -951,14 +951,13 @@ class GradClip:
         import ctypes as C
         grads = list(grads)
         dev = _device_of(grads[0], "grads[0]") if grads else torch.cuda.current_device()
-        seen = set()
+        spans = []
         self._tensors = (_lib.EETensor * max(1, len(grads)))()
         for i, g in enumerate(grads):
             self._one(g, f"grads[{i}]", dev)
-            if g.numel() and g.data_ptr() in seen:
-                raise ValueError(f"grads[{i}] is in the list twice")
-            seen.add(g.data_ptr())
-            self._tensors[i].data, self._tensors[i].n, self._tensors[i].type = g.data_ptr() or None, g.numel(), _GRAD_TYPES[g.dtype]
+            at, n = g.data_ptr(), g.numel()
+            spans.append((at, at + n * g.element_size(), "grads", i))
+            self._tensors[i].data, self._tensors[i].n, self._tensors[i].type = at or None, n, _GRAD_TYPES[g.dtype]
         self._out = None
         if out is not None:
             out = list(out)
@@ -969,7 +968,15 @@ class GradClip:
                 self._one(o, f"out[{i}]", dev)
                 if o.dtype is not g.dtype or o.numel() != g.numel():
                     raise ValueError(f"out[{i}] must be like grads[{i}]")
-                self._out[i] = o.data_ptr() or None
+                at = o.data_ptr()
+                self._out[i] = at or None
+                if at != spans[i][0]:                                    # (an out equal to its tensor is that tensor in place)
+                    spans.append((at, at + o.numel() * o.element_size(), "out", i))
+        # Tensors are read, scaled and written piece by piece in no order: one that lies in another would be scaled twice, or read after it was.
+        spans = sorted(s for s in spans if s[0] < s[1])
+        for a, b in zip(spans, spans[1:]):
+            if b[0] < a[1]:
+                raise ValueError(f"{a[2]}[{a[3]}] and {b[2]}[{b[3]}] overlap")
         self._n, self._dev, self._keep = len(grads), dev, grads
         self.out = grads if out is None else out
         self.value = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
