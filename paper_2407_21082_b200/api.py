@@ -945,7 +945,8 @@ class GradClip:
     buffers are the same from step to step (see ee_grad_norm and ee_grad_clip in include/eexit.h).  Calling it with max_norm computes the norm,
     scales the gradients, in place or into `out` (a list of tensors like them), and returns the norm, fp32 [1] on the device.  norm() and
     scale(max_norm) are its two halves, for a sum over several GPUs in between: scale reads self.value.  It launches on the
-    stream that is current when it is called; value and workspace are its own, so that its calls must not run at the same time."""
+    stream that is current when it is called, the first time behind what was queued where it was made; value and workspace are its own, so that its
+    calls must not run at the same time."""
 
     def __init__(self, grads, *, out=None, workspace=None):
         import ctypes as C
@@ -979,6 +980,8 @@ class GradClip:
                 raise ValueError(f"{a[2]}[{a[3]}] and {b[2]}[{b[3]}] overlap")
         self._n, self._dev, self._keep = len(grads), dev, grads
         self.out = grads if out is None else out
+        self._made_on = _stream()
+        self._ordered = {self._made_on}                                  # streams that are behind the making of value and workspace
         self.value = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
         self.workspace = new_grad_norm_workspace(grads, self.value.device) if workspace is None else _scratch(workspace, dev)
         lib, value = _lib.load(), C.c_void_p(self.value.data_ptr())
@@ -993,7 +996,17 @@ class GradClip:
     def _here(self):
         if torch._C._cuda_getDevice() != self._dev:
             raise ValueError(f"the gradients are on cuda:{self._dev}, the current device is cuda:{torch.cuda.current_device()}")
-        return _stream()
+        stream = _stream()
+        if stream not in self._ordered:
+            self._order(stream)
+        return stream
+
+    def _order(self, stream):
+        """The workspace is cleared, and the memory of both is free, only behind what is queued on the stream that the object was made on: the first
+        call on another one waits for that.  (A capture cannot wait for what is outside of it; torch synchronises before it begins one.)"""
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().wait_stream(torch.cuda.ExternalStream(self._made_on, device=self._dev))
+            self._ordered.add(stream)
 
     def norm(self) -> torch.Tensor:
         _check(self._norm_fn(*self._norm_args, self._here()), "ee_grad_norm")
