@@ -542,8 +542,8 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
  * are data of the stream (they may be written right before the call).  M up to 2^30; up to 64 rows are one pass over the packed weights.
  * V = 50304, single calls in a graph, bf16 head / 4-bit whole numbers in groups of 64 / this in groups of 16, us: 8 rows of 1024 24.7 / 17.8 / 11.4,
  * 64 of 1024 25.1 / 28.3 / 15.6, 256 of 1024 31.4 / 101.6 / 25.6, 64 of 2560 48.7 / 49.4 / 22.0, 16384 of 2560 2600 / - / 1100.
- * Workspace: ee_exit_head_fp4_workspace_bytes(M, d, V, group), 256-byte aligned, initialised once with ee_workspace_init; that of fewer
- * rows may be larger (other tiles).  M = 0 is a no-op.
+ * Workspace: ee_exit_head_fp4_workspace_bytes(M, d, V, group), 256-byte aligned, initialised once with ee_workspace_init; it serves fewer rows
+ * as well.  M = 0 is a no-op.
  */
 size_t    ee_head_fp4_bytes(int V, int d, int group);
 ee_status ee_head_fp4_pack(const void* W, int V, int d, int group, void* fp4, size_t fp4_bytes, void* stream);

@@ -816,7 +816,7 @@ def ee_exit_head_fp4_workspace_bytes(M: int, d: int, V: int, group: int) -> int:
 
 
 def new_exit_head_fp4_workspace(M: int, fp4: Fp4Weights) -> torch.Tensor:
-    """Allocates (through torch) and initialises a workspace for ee_exit_head_fp4 with these weights."""
+    """Allocates (through torch) and initialises a workspace for ee_exit_head_fp4 with these weights, for up to M rows."""
     return _workspace_of(ee_exit_head_fp4_workspace_bytes(M, fp4.d, fp4.V, fp4.group), "ee_exit_head_fp4_workspace_bytes", fp4.data.device)
 
 

@@ -602,9 +602,17 @@ ee_status launch_shape(GemmParams p, int device, cudaStream_t stream) {
 
 int fp4_gemm_act_tiles(int M) { return (fp4_tiles(M, kFp4Rows) + 1) / 2 * 2; }
 
-size_t fp4_gemm_parts_bytes(int M, int V) {      // for any number of pairs
+// For any number of pairs, and the most that any number of rows up to M takes: fewer rows have shorter runs, and more states to a row.  From
+// kMaxPairs pairs of row tiles on a run is a row tile at least, and the states grow with the rows.
+size_t fp4_gemm_parts_bytes(int M, int V) {
     const int m_pairs = fp4_gemm_act_tiles(M) / 2, n_tiles = fp4_tiles(V, kFp4Rows);
-    return (size_t)M * max_slots(m_pairs, n_tiles, pairs_of((long long)m_pairs * n_tiles, kMaxPairs)) * kParts * sizeof(RestState);
+    size_t most = 0;
+    for (int m = m_pairs; m > 0; m = m > kMaxPairs ? kMaxPairs : m - 1) {
+        const size_t rows = 2ll * m * kFp4Rows < M ? 2ll * m * kFp4Rows : M;
+        const size_t bytes = rows * max_slots(m, n_tiles, pairs_of((long long)m * n_tiles, kMaxPairs)) * kParts * sizeof(RestState);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 ee_status fp4_gemm_launch(const Fp4Head& q, int group, void* parts, int device, cudaStream_t stream) {

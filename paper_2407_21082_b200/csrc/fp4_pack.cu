@@ -246,7 +246,9 @@ HeadSpace head_space(int M, int d, int V, int group) {
     s.factor = kCtrlBytes;
     s.acts = align_up(s.factor + (size_t)M * sizeof(float), 1024);
     s.parts = align_up(s.acts + (size_t)tiles * fp4_blocks(d) * fp4_unit_bytes(group, rows), 256);
-    s.total = s.parts + (M <= kFp4StreamRows ? fp4_stream_parts_bytes(M) : fp4_gemm_parts_bytes(M, V));
+    // a workspace for M rows serves fewer as well: what lies in front of the states grows with M, and the states' part is the most of any
+    const size_t few = fp4_stream_parts_bytes(M <= kFp4StreamRows ? M : kFp4StreamRows), many = M <= kFp4StreamRows ? 0 : fp4_gemm_parts_bytes(M, V);
+    s.total = s.parts + (few > many ? few : many);
     return s;
 }
 

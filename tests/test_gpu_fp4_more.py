@@ -60,3 +60,16 @@ def test_packing_into_the_other_form_is_refused(ee):
         with pytest.raises(TypeError):
             pack(W, 32, out=out)
     assert ee.ee_head_fp4_pack(W, 32, out=floating) is floating and ee.ee_head_q4_pack(W, 32, out=whole) is whole
+
+
+def test_one_workspace_for_batches_of_all_sizes(ee):
+    d, V = 256, 20000
+    cfg = gen.make_config("c1", seed=6, planted=True, M=257, d=d, V=V, heads=1)
+    hd, h = head_to_dev(cfg["heads"][0]), dev_bf16(cfg["h"])
+    fp4 = ee.ee_head_fp4_pack(hd["W"], 16)
+    workspace = ee.new_exit_head_fp4_workspace(257, fp4)
+    for M in (257, 256, 1, 129, 64, 65, 9, 257):
+        got = ee.ee_exit_head_fp4(h[:M], hd["gamma"], hd["beta"], 1e-5, fp4, 1.0, workspace=workspace)
+        want = ee.ee_exit_head_fp4(h[:M], hd["gamma"], hd["beta"], 1e-5, fp4, 1.0)
+        for k in want:
+            assert torch.equal(got[k], want[k]), (M, k)
