@@ -6,10 +6,12 @@
 // sequence's own tokens, or a sequence's sum, is needed before any of its weights.  A unit (a sequence, a pair of sequences, or, where
 // all tokens count alike, a stretch of tokens) is therefore walked twice, the second time out of L1 or L2, by a warp where units are
 // short, by a CTA where they are long, and by a cluster of eight or sixteen CTAs, which exchange their sums through distributed shared memory,
-// where there are so few that the SMs would stand idle.
+// where they are long and few.
 //
 // What decides or cancels is done in fp64, which costs little here: the difference of two cross-entropies before the comparison with the
 // clip's border, and all sums, in a fixed order (a unit's by its threads, the units' by CTA, the CTAs' by the one that finishes last).
+// Powers and what is made of them are fp32: the ratio, the divergence and its slope to some 2^-21 of themselves (infinite where the power leaves fp32, from
+// an argument of 88.7 on), a pair's slope to 2^-22 of the larger of its two parts, which cancel where the margin is ln((1 - smoothing) / smoothing).
 //
 // Device times in a graph: policy loss of 512 tokens 3.0 us, of 65537 in 200 sequences 7.7 (a warp per sequence: 47); preference loss of 4001 tokens
 // in 8 pairs 5.8, of 300000 in 3 pairs 15 (1024 threads per CTA: 16; eight instead of sixteen CTAs: 17.5; loops that test for their end between two loads:
@@ -27,7 +29,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256, kClusterThreads = 512, kMaxWarps = kClusterThreads / 32;
-constexpr int kClusterCtas = 8, kWideClusterCtas = 16;  // the second where the device can run as many as there are units
+constexpr int kClusterCtas = 8, kWideClusterCtas = 16;
 constexpr int kMaxCtas = 2048;
 constexpr int kBatch = 8, kHalfBatch = 4;        // tokens whose loads a thread issues at once: a loop that tests for its end in between waits for each
 constexpr int kSums = 4;
@@ -359,15 +361,37 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
-// What walks a unit: a cluster where it has tokens for several turns of a CTA and there are few enough for all clusters to be there at once; a CTA
-// where it has tokens for half of its threads, or where there are hardly any units; a warp otherwise.  Policy loss of 65536 tokens, a warp /
-// a CTA / a cluster per sequence: 4096 sequences 7.5 / 18.7 / - us, 1024 7.9 / 10.3 / -, 512 12.6 / 7.2 / -, 64 75 / 12.5 / 17.0, 36 91 / 14.1 / 15.3,
-// 16 181 / 24.1 / 9.7; preference loss of 300000 tokens in 36 pairs 237 / 41.7 / 16.3.
-int span_of(int M, int units, int num_sms) {
-    const int each = M / units;
-    if (units <= num_sms && each >= 8 * kThreads) return kClusterSpan;
-    return each >= kThreads / 2 || units * 2 <= num_sms ? kCtaSpan : kWarpSpan;
+// What walks a unit, by the units' average length and their number.  A warp needs no exchange and starts soonest, but takes 10.7 ns for a token of
+// the policy loss and 4.1 of the preference loss, whose two sequences overlap; a CTA takes 1.3 and 0.8, and as more of them queue than SMs, it pays
+// the later the more units there are; a cluster of eight costs 3 us to start and 0.2 us more for every unit.  How far the longest is from the average
+// is on the device and decides as much: the borders are between those of equal units and of units cut at random places (the longest six times the average).
+// Device times, us, equal / random; policy loss:
+//   units of      8: 64 a warp 3.1 / 4.4, a CTA 4.5 / 4.5;  256 5.0 / 10.0, 4.5 / 4.9;   1024 a CTA 5.2 / 7.5, a cluster 7.4 / 7.3;  4096 9.1 / 17.6, 7.8 / 8.0
+//                36: 16 4.3 / 4.7, 4.7 / 4.7;  64 4.7 / 7.1, 4.7 / 4.9;                   2048 6.6 / 16.5, 15.4 / 14.7;  4096 9.3 / 28.8, 15.4 / 15.1
+//               148: 16 4.6 / 4.8, 4.8 / 4.9;  64 4.8 / 6.4, 4.9 / 4.8;                   8192 15 / 45, 41 / 41;  16384 25 / 85, 44 / 46
+//               600: 64 5.1 / 8.6, 8.4 / 8.6;  128 5.7 / 13.5, 8.7 / 9.3         2400: 128 7.9 / 16.3, 14.7 / 15.9;  256 10.7 / 28.1, 17.9 / 19.1
+// preference loss:
+//                 8: 128 3.9 / 3.8, 5.6 / 5.6;  512 4.5 / 7.2, 5.7 / 5.6;                 2048 6.2 / 7.6, 8.6 / 8.5;  4096 7.2 / 10.2, 8.8 / 8.7
+//                36: 128 5.5 / 6.2, 5.8 / 5.8;  256 5.5 / 7.3, 5.7 / 5.9;                 4096 7.6 / 15.8, 16.2 / 15.6;  8192 11.0 / 27.2, 16.5 / 16.3
+//               148: 128 5.6 / 6.3, 6.0 / 6.2;  512 6.2 / 10.8, 6.4 / 6.7;                8192 12 / 32, 39 / 38;  32768 54 / 163, 46 / 52
+//               600: 256 5.8 / 10.0, 10.9 / 10.9;  512 6.1 / 15.8, 11.3 / 11.5   2400: 512 8.6 / 16.4, 23.1 / 22.7;  1024 12.0 / 37.2, 24.0 / 25.7
+// One long sequence among very many short ones is walked by what suits the short ones: 2000 of 32 tokens take 6 us, with one of 4096 more 45 (policy)
+// and 21 us (preference), with one of 100000 1.0 and 0.13 ms.
+struct Borders {                                 // average lengths from which a CTA or a cluster walks a unit: so many, and so many more for 16 units
+    int cta, cta_more, cluster, cluster_more;
+};
+constexpr Borders kPolicyBorders{48, 1, 1024, 1024}, kPreferenceBorders{192, 6, 3072, 1536};
+
+int span_of(int M, int units, int num_sms, const Borders& b) {
+    const long long each = M / units, n = units;
+    if (units <= num_sms && each >= b.cluster + b.cluster_more * n / 16) return kClusterSpan;
+    return each >= b.cta + b.cta_more * n / 16 ? kCtaSpan : kWarpSpan;
 }
+
+// Clusters of sixteen CTAs instead of eight where units are long and few.  Sixteen and eight, equal / random, policy loss: 1 unit of 16384 7.8, 7.6,
+// of 131072 13.7, 20.6; 4 of 32768 9.6 / 12.5, 9.9 / 16.9; 8 of 32768 12.6 / 14.7, 10.5 / 16.1, of 131072 20.6 / 29.1, 23.0 / 43.5; 16 of 32768 18.9 / 20.6,
+// 13.8 / 20.5.  Preference loss: 2 of 32768 9.3 / 9.4, 9.4 / 11.0; 8 of 32768 14.6 / 14.7, 10.3 / 12.2, of 131072 17.1 / 19.4, 17.4 / 26.0.
+bool is_wide(int M, int units) { return M / units >= 8192ll * (units + 2); }
 
 // How many clusters of sixteen CTAs of this kernel (`kind`: which of the two it is) the device runs at once; 0 if it cannot.
 int wide_clusters(const void* kernel, int kind, int device) {
@@ -391,17 +415,18 @@ int wide_clusters(const void* kernel, int kind, int device) {
 }
 
 template <class Args>
-cudaError_t launch_spans(int kind, void (*warp)(Args), void (*cta)(Args), void (*cluster)(Args), const Args& p, int M, int units, int num_sms,
-                         int device, cudaStream_t stream) {
+cudaError_t launch_spans(int kind, void (*warp)(Args), void (*cta)(Args), void (*cluster)(Args), const Args& p, const Borders& borders, int M, int units,
+                         int num_sms, int device, cudaStream_t stream) {
     const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
-    switch (span_of(M, units, num_sms)) {
+    switch (span_of(M, units, num_sms, borders)) {
         case kWarpSpan: {
             const int grid = (units + kThreads / 32 - 1) / (kThreads / 32);
             return launch_pdl(warp, dim3(grid < most ? grid : most), kThreads, 0, stream, p);
         }
         case kCtaSpan: return launch_pdl(cta, dim3(units < most ? units : most), kThreads, 0, stream, p);
         default: {
-            const int ctas = units <= wide_clusters(reinterpret_cast<const void*>(cluster), kind, device) ? kWideClusterCtas : kClusterCtas;
+            const bool wide = is_wide(M, units) && units <= wide_clusters(reinterpret_cast<const void*>(cluster), kind, device);
+            const int ctas = wide ? kWideClusterCtas : kClusterCtas;
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
             pair_launch_config(cfg, attr, dim3(units * ctas), kClusterThreads, 0, stream);
@@ -419,7 +444,7 @@ ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, int device, cudaS
     cudaError_t e;
     if (p.seq_start) {
         e = launch_spans<PolicyArgs>(0, policy_sequences_kernel<kWarpSpan>, policy_sequences_kernel<kCtaSpan>, policy_sequences_kernel<kClusterSpan>, p,
-                                     p.M, p.S, num_sms, device, stream);
+                                     kPolicyBorders, p.M, p.S, num_sms, device, stream);
     } else {
         const long long need = ((long long)p.M + kThreads - 1) / kThreads;
         const int most = kMaxCtas < 8 * num_sms ? kMaxCtas : 8 * num_sms;
@@ -429,8 +454,8 @@ ee_status policy_loss_launch(const PolicyArgs& p, int num_sms, int device, cudaS
 }
 
 ee_status preference_loss_launch(const PreferenceArgs& p, int num_sms, int device, cudaStream_t stream) {
-    return launch_spans<PreferenceArgs>(1, preference_kernel<kWarpSpan>, preference_kernel<kCtaSpan>, preference_kernel<kClusterSpan>, p, p.M, p.P, num_sms,
-                                        device, stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
+    return launch_spans<PreferenceArgs>(1, preference_kernel<kWarpSpan>, preference_kernel<kCtaSpan>, preference_kernel<kClusterSpan>, p, kPreferenceBorders,
+                                        p.M, p.P, num_sms, device, stream) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
 }  // namespace ee

@@ -97,3 +97,51 @@ def test_sizes_beyond_32_bits_are_refused(ee):
         ee.ee_policy_loss(forward, many.view(torch.int32), 10, many, many, out=out)
     with pytest.raises(ee.EExitError):
         ee.ee_preference_loss(forward, many.view(torch.int32), 10, starts, out=out)
+
+
+# What walks a unit: a warp, a CTA, a cluster of eight or of sixteen, units of ordinary and of very unequal lengths.
+@pytest.mark.parametrize("M,S", [(140001, 2), (300001, 25), (20000, 100), (30000, 600), (30000, 300), (200000, 1), (60000, 7), (1000003, 148)])
+@pytest.mark.parametrize("skewed", [False, True])
+def test_policy_loss_whatever_walks_a_sequence(ee, M, S, skewed):
+    rng = np.random.default_rng(M + S)
+    V, ce, old, ref, labels, starts = _batch(rng, M, S, skewed)
+    adv = rng.normal(0, 1, S).astype(np.float32)
+    want = oracle.policy_loss(ce, old, adv, labels, V, ref, 0.1, (0.2, 0.2), starts)
+    workspace = ee.new_token_loss_workspace()
+    args = (_forward(ce, labels, V), dev(labels), V, dev(old), dev(adv))
+    got = [ee.ee_policy_loss(*args, ref_ce=dev(ref), kl_weight=0.1, seq_start=dev(starts), workspace=workspace) for _ in range(2)]
+    n = np.maximum(np.add.reduceat(np.append(labels >= 0, False), starts[:-1]) * (starts[1:] > starts[:-1]), 1)
+    size = np.repeat(np.abs(adv) * 5 + 0.5, np.diff(starts)) / (np.repeat(n, np.diff(starts)) * S)      # |a| e^x + the penalty's part, x below 1.6
+    assert (np.abs(_np(got[0]["dce"]) - want["dce"]) <= R * size).all()
+    assert np.abs(_np(got[0]["loss"]) - want["loss"]).max() <= R * 5 * (1 + np.abs(adv).mean())
+    assert torch.equal(got[0]["dce"], got[1]["dce"]) and torch.equal(got[0]["loss"], got[1]["loss"])
+
+
+@pytest.mark.parametrize("M,P", [(140001, 2), (130001, 12), (400001, 30), (50000, 40), (30000, 600), (60000, 600), (200000, 1), (2000003, 148)])
+@pytest.mark.parametrize("skewed", [False, True])
+def test_preference_loss_whatever_walks_a_pair(ee, M, P, skewed):
+    rng = np.random.default_rng(M + P)
+    V, ce, _, ref, labels, starts = _batch(rng, M, 2 * P, skewed)
+    want = oracle.preference_loss(ce, labels, V, starts, ref, 0.1, 0.1)
+    workspace = ee.new_token_loss_workspace()
+    args = (_forward(ce, labels, V), dev(labels), V, dev(starts))
+    got = [ee.ee_preference_loss(*args, ref_ce=dev(ref), smoothing=0.1, workspace=workspace) for _ in range(2)]
+    m = want["margin"]
+    assert (np.abs(_np(got[0]["margin"]) - m) <= 2.0 ** -23 * np.abs(m) + 1e-9).all()
+    assert (np.abs(_np(got[0]["dce"]) - want["dce"]) <= R * (1 + np.abs(m).max()) * np.abs(want["dce"]) + R * 0.1 * 0.1 / P).all()
+    assert np.abs(_np(got[0]["loss"]) - want["loss"]).max() <= R * (1 + np.abs(want["loss"]).max() + np.abs(m).max())
+    for k in got[0]:
+        assert torch.equal(got[0][k], got[1][k]), k
+
+
+def _batch(rng, M, n, skewed):
+    """Tokens, a third of them not counted, and boundaries: nearly equal lengths, or one sequence of half of all tokens and some empty ones."""
+    V = 100
+    ce = np.abs(rng.normal(0, 1.5, M)).astype(np.float32)
+    old, ref = (np.abs(ce + np.clip(rng.normal(0, 0.3, M), -0.8, 0.8)).astype(np.float32) for _ in range(2))
+    labels = np.where(rng.random(M) < 0.3, -1, rng.integers(0, V, M)).astype(np.int32)
+    starts = np.linspace(0, M, n + 1).astype(np.int32)
+    if skewed and n > 1:
+        starts = np.concatenate([[0], np.sort(rng.integers(M // 2, M + 1, n - 1)), [M]]).astype(np.int32)
+        starts[-2] = starts[-1]
+    return V, ce, old, ref, labels, starts
