@@ -223,17 +223,19 @@ __global__ void __launch_bounds__(kThreads) fp4_acts_kernel(const Fp4Acts a) {
 template <int kGroup>
 cudaError_t launch_acts(const Fp4Acts& a, cudaStream_t stream) {
     const int padded = fp4_blocks(a.d) * 16;                             // vectors of a row, zeros beyond d among them
-    // A CTA per row while there are too few rows to fill the SMs with warps, a warp per row above.
-    if (a.M <= 1024) {
+    // A CTA per row while there are too few rows to fill the SMs with warps, and where a row does not fit a warp's registers; a warp per row above.
+    // The whole call, us, a warp / a CTA per row (V = 50304): 256 rows of 2560 43 / 37, 1024 of 1024 52.9 / 50.7, 2048 of 512 71.0 / 70.6, of 1024 86.5 / 86.4,
+    // of 2560 146 / 143, 4096 of 512 124.5 / 125.1, of 1024 151 / 154, of 2560 265 / 264, 16384 of 512 438 / 441, of 1024 535 / 550, of 2560 969 / 1021;
+    // rows of 4096 (in a warp 128 registers): 1024 of them 139 / 112, 4096 478 / 426; 2048 of 8192 505 / 417.
+    if (a.M <= 2048 || padded > 320) {
         const int warps = (padded + 31) / 32;
         const int threads = 32 * (warps < kWarps ? warps : kWarps);
         return padded <= threads * 2 ? launch_pdl(fp4_acts_kernel<kGroup, kThreads, 2>, dim3(a.M), threads, 0, stream, a)
                                      : launch_pdl(fp4_acts_kernel<kGroup, kThreads, 4>, dim3(a.M), threads, 0, stream, a);
     }
     const dim3 grid((a.M + kWarps - 1) / kWarps);
-    return padded <= 128   ? launch_pdl(fp4_acts_kernel<kGroup, 32, 4>, grid, kThreads, 0, stream, a)
-           : padded <= 320 ? launch_pdl(fp4_acts_kernel<kGroup, 32, 10>, grid, kThreads, 0, stream, a)
-                           : launch_pdl(fp4_acts_kernel<kGroup, 32, 32>, grid, kThreads, 0, stream, a);
+    return padded <= 128 ? launch_pdl(fp4_acts_kernel<kGroup, 32, 4>, grid, kThreads, 0, stream, a)
+                         : launch_pdl(fp4_acts_kernel<kGroup, 32, 10>, grid, kThreads, 0, stream, a);
 }
 
 struct HeadSpace {

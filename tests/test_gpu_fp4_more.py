@@ -73,3 +73,14 @@ def test_one_workspace_for_batches_of_all_sizes(ee):
         want = ee.ee_exit_head_fp4(h[:M], hd["gamma"], hd["beta"], 1e-5, fp4, 1.0)
         for k in want:
             assert torch.equal(got[k], want[k]), (M, k)
+
+
+# Both forms of the activations' LayerNorm on both sides of the border between them, rows of all widths.
+@pytest.mark.parametrize("M,d,V", [(2048, 640, 200), (2049, 640, 200), (2300, 1056, 130), (2100, 2592, 130), (2500, 8192, 100), (2049, 2560, 260)])
+def test_activations_by_warps_and_by_ctas(ee, M, d, V):
+    cfg = gen.make_config("c1", seed=29, planted=True, M=M, d=d, V=V, heads=1)
+    head = cfg["heads"][0]
+    hd = head_to_dev(head)
+    for group in (16, 32):
+        out = ee.ee_exit_head_fp4(dev_bf16(cfg["h"]), hd["gamma"], hd["beta"], 1e-5, ee.ee_head_fp4_pack(hd["W"], group), 1.0)
+        assert_close(out, oracle.exit_head_fp4(cfg["h"], head, 1.0, group), d, V, f"{M} {d} {group}")
