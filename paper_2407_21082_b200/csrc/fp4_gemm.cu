@@ -2,7 +2,7 @@
 //
 // Persistent pairs of CTAs; the activations (256 rows to a pair, 128 to a CTA) are the M operand of the products, the weight tiles of 128 rows the
 // N operand, half of each staged by either CTA.  The tiles of the M x V plane are numbered row tile by row tile and every pair takes an equal run
-// of them, so that it stays with its rows: up to d = 2560 their elements stay in shared memory, and their scales in tensor memory, while the
+// of them, so that it stays with its rows: in long runs their elements (up to d = 2560) stay in shared memory, and their scales in tensor memory, while the
 // weights pass by (40 bytes per cycle and SM instead of 112; L2 gave 63), and the epilogue keeps the rows' softmax states in registers from
 // tile to tile.  A state leaves the chip only where a run or a row tile ends.
 //   warp 0 (one lane)  producer      warp 1 (one lane)  products      warps 2 .. 17  states      warp 18 (one lane)  scales to tensor memory
@@ -598,6 +598,23 @@ ee_status launch_shape(GemmParams p, int device, cudaStream_t stream) {
     return launch_pdl(fp4_merge_kernel, dim3((p.q.M + rows - 1) / rows), kMergeThreads, 0, stream, p, pairs) == cudaSuccess ? EE_OK : EE_ERR_CUDA;
 }
 
+// Whether a pair keeps the activations of its row tile.  It saves their loads, which the products of wide rows wait for, and power; it costs a start at
+// which a row tile arrives before anything else, and stages, of which three are left at d = 2560.  So: wide rows, long runs.
+// Kept / streamed, us, V = 50304, groups of 16; short runs: 300 rows of 1024 34.1 / 31.2, of 2560 51.1 / 43.9, 1000 of 2560 84 / 76, 4096 of 1024 150 / 142, of 1536
+// 192 / 187, of 2048 231 / 230, of 2560 273 / 275.  Long runs (medians of calls back to back, under the power cap): 16384 of 1024 568 / 539, of 1536
+// 733 / 746, of 2048 878 / 924, of 2560 1175 / 1126, and by themselves, at full clocks, 958 / 1040; 6144 of 2048 334 / 339, of 2560 449 / 426 and 408 / 401.
+// Groups of 32: 16384 of 1536 687 / 689, of 2048 817 / 857, of 2560 1084 / 1054 and 898 / 973.
+constexpr int kStreamedBlocks = 12;              // up to so many units of a row
+constexpr int kLongRun = 128;                    // tiles
+
+template <int kGroup>
+ee_status launch_group(const GemmParams& p, int device, cudaStream_t stream) {
+    const int blocks = fp4_blocks(p.q.d);
+    const bool keep = blocks > kStreamedBlocks && blocks <= kResidentBlocks &&
+                      (long long)p.m_pairs * p.n_tiles >= (long long)kLongRun * resident_pairs<kGroup, true>(device);
+    return keep ? launch_shape<kGroup, true>(p, device, stream) : launch_shape<kGroup, false>(p, device, stream);
+}
+
 }  // namespace
 
 int fp4_gemm_act_tiles(int M) { return (fp4_tiles(M, kFp4Rows) + 1) / 2 * 2; }
@@ -621,9 +638,7 @@ ee_status fp4_gemm_launch(const Fp4Head& q, int group, void* parts, int device, 
     p.parts = static_cast<RestState*>(parts);
     p.m_pairs = fp4_gemm_act_tiles(q.M) / 2;
     p.n_tiles = fp4_tiles(q.V, kFp4Rows);
-    const bool fits = fp4_blocks(q.d) <= kResidentBlocks;
-    if (group == 16) return fits ? launch_shape<16, true>(p, device, stream) : launch_shape<16, false>(p, device, stream);
-    return fits ? launch_shape<32, true>(p, device, stream) : launch_shape<32, false>(p, device, stream);
+    return group == 16 ? launch_group<16>(p, device, stream) : launch_group<32>(p, device, stream);
 }
 
 }  // namespace ee

@@ -36,7 +36,7 @@ def test_a_row_without_a_value_has_no_index_in_any_head(ee, M):
 
 # What a CTA or a pair of them carries from tile to tile, on some 148 SMs.  Up to 64 rows: 313 to 469 weight tiles, two to four to a CTA, of one to four
 # stages each, with the accumulators in turn.  Above: 5 to 21 tiles to a pair, of several units each; those of 1500 and 3000 rows cross from one row
-# tile to the next, where the activations and their scales are replaced.  2688 columns are more than a pair keeps of a row.
+# tile to the next.
 LONG_RUNS = [(12, 256, 60000), (32, 640, 40000), (64, 1024, 50304), (203, 1056, 50257), (1000, 128, 50304), (3000, 1024, 5000), (3000, 2560, 5000), (1500, 2688, 6000)]
 
 
@@ -84,3 +84,28 @@ def test_activations_by_warps_and_by_ctas(ee, M, d, V):
     for group in (16, 32):
         out = ee.ee_exit_head_fp4(dev_bf16(cfg["h"]), hd["gamma"], hd["beta"], 1e-5, ee.ee_head_fp4_pack(hd["W"], group), 1.0)
         assert_close(out, oracle.exit_head_fp4(cfg["h"], head, 1.0, group), d, V, f"{M} {d} {group}")
+
+
+# Runs in which a pair keeps its row tile's activations: 128 tiles and more to a pair, of 13 to 20 units; short row tiles, so that every run goes through
+# several, and long ones.  Rows are independent, so the oracle takes a sample of them.
+@pytest.mark.parametrize("group", [16, 32])
+@pytest.mark.parametrize("M,d,V", [(101200, 1664, 3000), (40000, 2048, 8000), (12300, 2560, 25200), (130000, 2528, 2400)])
+def test_runs_that_keep_their_activations_match_the_oracle(ee, M, d, V, group):
+    torch.manual_seed(M)
+    W = (0.05 * torch.randn(V, d, device="cuda")).bfloat16()
+    target = torch.randint(0, V, (M,), device="cuda")
+    lean = torch.rand(M, 1, device="cuda") * 0.25
+    h = (torch.randn(M, d, device="cuda") + lean * d ** 0.5 * torch.nn.functional.normalize(W[target].float(), dim=1)).bfloat16()
+    gamma, beta = 1 + 0.1 * torch.randn(d, device="cuda"), 0.02 * torch.randn(d, device="cuda")
+    fp4 = ee.ee_head_fp4_pack(W, group)
+    workspace = ee.new_exit_head_fp4_workspace(M, fp4)
+    out = ee.ee_exit_head_fp4(h, gamma, beta, 1e-5, fp4, 2.0, workspace=workspace)
+    assert ee.ee_query_async_error(workspace) == 0
+    rows = np.unique(np.concatenate([np.arange(20), np.arange(120, 136), np.arange(250, 262), np.arange(M - 20, M), np.random.default_rng(1).integers(0, M, 60)]))
+    at = torch.from_numpy(rows).cuda()
+    bits = lambda t: t.view(torch.int16).cpu().numpy().view(np.uint16)  # noqa: E731
+    head = dict(gamma=gamma.cpu().numpy(), beta=beta.cpu().numpy(), W=bits(W), ln_eps=1e-5)
+    assert_close({k: v[at] for k, v in out.items()}, oracle.exit_head_fp4(bits(h[at]), head, 2.0, group), d, V, f"{M} {d} {V} {group}")
+    again = ee.ee_exit_head_fp4(h, gamma, beta, 1e-5, fp4, 2.0, workspace=workspace)
+    for k in out:
+        assert torch.equal(out[k], again[k]), k
