@@ -165,9 +165,9 @@ struct Fp4Head {
     Control* ctrl;
 };
 
-// Few rows (fp4_stream.cu): weights as the M operand.  parts: [CTAs][rows padded] states.  A tile of 128 padded rows was built too and not kept: at
-// V = 50304 the kernel for many rows takes 21.2 us instead of 26.0 for 65 rows of 512, 24.8 instead of 27.1 for 100 of 1024, and 35.6 instead
-// of 32.5 for 128 of 2560.
+// Few rows (fp4_stream.cu): weights as the M operand.  parts: [CTAs][rows padded] states.  Whole calls at V = 50304, groups of 16, this kernel / the one for
+// many rows: 32 rows of 512 11.5 / 19.2 us, of 2560 18.5 / 28.6, 64 rows of 512 15.0 / 20.7, of 1024 15.8 / 22.6, of 2560 21.6 / 29.9, of 8192 50 / 65.  With a
+// tile of 128 padded rows, which was built too and not kept: 65 rows of 512 26.0 / 20.8, 100 of 1024 27.1 / 23.0, 128 of 2560 32.5 / 30.5.
 constexpr int kFp4StreamRows = 64;
 int fp4_stream_padded(int M);                    // rows of a tile of activations
 size_t fp4_stream_parts_bytes(int M);

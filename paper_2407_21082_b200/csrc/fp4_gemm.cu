@@ -12,7 +12,7 @@
 // instructions issued under elect.sync instead of lane == 0, 1.32 as pairs with resident activations and one unit per stage, 0.93 / 0.69 with four
 // (taking and giving a stage costs an issuing thread 250 cycles), 0.94 / 0.53 with sixteen epilogue warps instead of eight, each set with its own
 // accumulator (a warp alone needs 1500 cycles for 32 columns: the terms depend on one another; eight warps could not hide that).
-// 4096 x 512 takes 124 us, 203 x 1056 26 us.
+// Now 0.97 / 0.51 (narrow rows streamed); 4096 x 512 takes 124 us, 203 x 1056 24 us.
 //
 // What bounds it: at d = 2560 the products, some 200 cycles per 128 columns where 128 would be the tensor core's rate (with the loads left
 // out of a copy 0.80 instead of 0.95 ms): a product of 256 x 128 reads 6 KB of operands per SM for 64 cycles of work.  256 weight rows at a

@@ -8,7 +8,7 @@
 // The accumulators (lanes: the tile's rows, columns: the tokens) are double-buffered.  The eight epilogue warps move a tile of logits to
 // shared memory, token by token, and then a warp takes every eighth token: a lane four of the tile's rows, folded into states in its registers,
 // which it keeps from tile to tile.  The lanes' states are merged once, and the CTAs' by the CTA that finishes last (up to 8 rows, a warp
-// for each) or by a kernel of their own (64 rows in one CTA took longer than the head: 30 us of 512 instead of 16).
+// for each) or by a kernel of their own.
 //
 // The weights' first stages are requested before the wait for the kernel that writes the activations: at d = 1024 the ring of all SMs
 // together holds most of the head.
@@ -32,7 +32,10 @@ constexpr int kThreads = 320;
 constexpr int kFoldWarps = 8;
 constexpr int kUnits = 2;                        // units per stage
 constexpr int kMaxStages = 12;
-constexpr int kMergeHere = 8;                    // rows up to which the CTA that finishes last merges the states; more are a kernel of their own
+// Rows up to which the CTA that finishes last merges the states; more are a kernel of their own.  Device times at V = 50304, merged here / there: 4 rows of
+// 512 9.2 / 9.3 us, of 2560 16.5 / 16.7, 8 rows of 1024 11.5 / 11.0, of 2560 17.2 / 16.7, 16 rows of 512 11.8 / 9.7, of 1024 13.8 / 11.6, 64 of 512 24.4 / 14.8.
+// Up to 8 rows what the launch saves on the device it costs on the host, 2 us, which eager calls of this size wait for.
+constexpr int kMergeHere = 8;
 constexpr int kMergeThreads = 128;
 constexpr int kTmemCols = 512;
 constexpr size_t kSmemBudget = 226 * 1024;
