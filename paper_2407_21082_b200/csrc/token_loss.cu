@@ -58,20 +58,23 @@ __device__ __forceinline__ float expm1_minus(float g, float expm1_g) {
         s = fmaf(s, g, 0.5f);
         return g * g * s;
     }
-    return isinf(expm1_g) ? expm1_g : expm1_g - g;                       // (infinity - infinity otherwise)
+    return expm1_g - g;
 }
 
 __device__ __forceinline__ Term policy_term(const PolicyArgs& p, float ce, float old_ce, float ref_ce, float adv) {
     Term t;
     const double x = (double)old_ce - (double)ce;                        // ln of the ratio of the new to the old probability
     t.cut = adv > 0.f ? x > p.log_high : adv < 0.f && x < p.log_low;
-    float ratio = expf((float)x);
-    if (adv == 0.f && isinf(ratio)) ratio = 0.f;                         // a token that asks for nothing, however far its probability has come
+    float ln_ratio = (float)x;
+    if (adv == 0.f && ln_ratio > 0.f) ln_ratio = 0.f;                    // 0 times infinity: a token that asks for nothing, however far it has come
+    const float ratio = expf(ln_ratio);
     t.policy = -adv * (t.cut ? (adv > 0.f ? p.high : p.low) : ratio);
     t.grad = t.cut ? 0.f : adv * ratio;
     t.kl = 0.f;
     if (p.ref_ce) {
-        const float g = (float)((double)ce - (double)ref_ce), e = expm1f(g);
+        float g = (float)((double)ce - (double)ref_ce);
+        g = g > 1e30f ? 1e30f : g;                                       // infinity less infinity: its divergence is infinite
+        const float e = expm1f(g);
         t.kl = expm1_minus(g, e);
         if (p.kl_weight != 0.f) t.grad = fmaf(p.kl_weight, e, t.grad);   // 0 only watches the divergence, which may be infinite
     }
