@@ -13,8 +13,8 @@
 // Powers and what is made of them are fp32: the ratio, the divergence and its slope to some 2^-21 of themselves (infinite where the power leaves fp32, from
 // an argument of 88.7 on), a pair's slope to 2^-22 of the larger of its two parts, which cancel where the margin is ln((1 - smoothing) / smoothing).
 //
-// Device times in a graph: policy loss of 512 tokens 3.0 us, of 65537 in 200 sequences 7.7 (a warp per sequence: 47); preference loss of 4001 tokens
-// in 8 pairs 5.8, of 300000 in 3 pairs 15 (1024 threads per CTA: 16; eight instead of sixteen CTAs: 17.5; loops that test for their end between two loads:
+// Device times in a graph: policy loss of 512 tokens 3.1 us, of 65537 in 200 sequences 7.6; preference loss of 4001 tokens
+// in 8 pairs 5.3, of 300000 in 3 pairs 15 (1024 threads per CTA: 16; eight instead of sixteen CTAs: 17.5; loops that test for their end between two loads:
 // 19).  All of it is latency: reading and writing takes 0.8 us of the last one at the copy rate, the rest are start, two walks of some ten tokens
 // a thread on 48 SMs, the exchange within the cluster and the last sums.
 #include <cooperative_groups.h>
@@ -35,6 +35,9 @@ constexpr int kBatch = 8, kHalfBatch = 4;        // tokens whose loads a thread 
 constexpr int kSums = 4;
 
 enum Span { kWarpSpan, kCtaSpan, kClusterSpan };         // what walks a unit
+// Tokens of a unit above which a warp leaves it to its CTA, which takes 2 us for each.  Policy loss of 600 sequences of random lengths around 256, us: borders of
+// 256, 512, 1024, 2048 19, 18, 18, 22, of 2400 around 512 29, 29, 31, 33; preference loss of 600 pairs around 512 23, 24, 17, 13, of 4800 around 1024 52, 47, 38, 33.
+constexpr int kPolicyHandOver = 512, kPreferenceHandOver = 2048;
 
 struct LossSpace {
     Control ctrl;
@@ -197,6 +200,11 @@ __global__ void __launch_bounds__(kThreads) policy_tokens_kernel(const PolicyArg
     finish<kThreads / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
+template <int kValue>
+struct IntConstant {
+    static constexpr int value = kValue;
+};
+
 // Which units a thread has part in, and where in them it begins and how far it steps.
 template <int kSpan>
 constexpr int threads_of = kSpan == kClusterSpan ? kClusterThreads : kThreads;
@@ -204,7 +212,6 @@ template <int kSpan>
 struct Walk {
     static constexpr int kThreads = threads_of<kSpan>, kWarps = kThreads / 32;
     int unit, units_step, from, step;
-    bool leads;
     __device__ __forceinline__ Walk() {
         if (kSpan == kWarpSpan) {
             unit = blockIdx.x * kWarps + (threadIdx.x >> 5);
@@ -223,11 +230,86 @@ struct Walk {
             from = (blockIdx.x % ctas) * kThreads + threadIdx.x;
             step = ctas * kThreads;
         }
-        leads = from == 0;
     }
 };
 
-// Every sequence counts alike, and within a sequence every token.
+// Calls walk_unit(IntConstant<span>, unit, its rows (begin and end), from, step) for every unit that the thread has part in.  Among units that warps walk
+// one of more than `hand_over` rows is left to the whole CTA, after the warps' own.
+template <int kSpan, class Bounds, class WalkUnit>
+__device__ __forceinline__ void for_units(int units, int hand_over, const Bounds& bounds, const WalkUnit& walk_unit) {
+    const Walk<kSpan> walk;
+    if constexpr (kSpan == kWarpSpan) {
+        constexpr int kWarps = Walk<kSpan>::kWarps;
+        __shared__ int2 spans[kWarps];                                   // read once: what threads decide to walk together they decide alike
+        const int warp = threadIdx.x >> 5;
+        for (int first = blockIdx.x * kWarps; first < units; first += walk.units_step) {
+            const int unit = first + warp;
+            int2 b = unit < units ? bounds(unit) : make_int2(0, 0);
+            b.x = __shfl_sync(0xffffffffu, b.x, 0);
+            b.y = __shfl_sync(0xffffffffu, b.y, 0);
+            if (walk.from == 0) spans[warp] = b;
+            const bool is_long = b.y - b.x > hand_over;
+            if (unit < units && !is_long) walk_unit(IntConstant<kWarpSpan>{}, unit, b, walk.from, walk.step);
+            if (!__syncthreads_or(is_long ? 1 : 0)) continue;
+            for (int w = 0; w < kWarps; ++w) {
+                const int2 whole = spans[w];
+                if (whole.y - whole.x > hand_over) walk_unit(IntConstant<kCtaSpan>{}, first + w, whole, (int)threadIdx.x, kThreads);
+            }
+            __syncthreads();
+        }
+    } else {
+        for (int unit = walk.unit; unit < units; unit += walk.units_step) walk_unit(IntConstant<kSpan>{}, unit, bounds(unit), walk.from, walk.step);
+    }
+}
+
+// Every sequence counts alike, and within a sequence every token.  (Rows are at most 2^30, so that 32 bits hold every index here and below.)
+template <int kSpan>
+__device__ __forceinline__ void policy_unit(const PolicyArgs& p, int unit, int begin, int end, int from, int step, Slots (&slots)[2], int& turn,
+                                            double (&sums)[kSums]) {
+    const float adv = ld_dep(p.adv + unit);
+    int have = 0;
+    for (int i0 = begin + from; i0 < end; i0 += kBatch * step) {
+        bool in[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) in[u] = i0 + u * step < end && is_counted(p.labels, i0 + u * step, p.V);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) have += in[u] ? 1 : 0;
+    }
+    const double n = span_totals<kSpan>((double)have, 0.0, slots, turn).x;
+    const double w = n > 0.0 ? 1.0 / (n * (double)p.S) : 0.0;
+    const float wf = (float)w;
+    double policy = 0.0, kl = 0.0, cut = 0.0;
+    for (int i0 = begin + from; i0 < end; i0 += kHalfBatch * step) {
+        float ce[kHalfBatch], old_ce[kHalfBatch], ref[kHalfBatch];
+        bool in[kHalfBatch];
+#pragma unroll
+        for (int u = 0; u < kHalfBatch; ++u) {
+            const int i = i0 + u * step;
+            ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
+            old_ce[u] = i < end ? ld_dep(p.old_ce + i) : 0.f;
+            ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
+            in[u] = i < end && is_counted(p.labels, i, p.V);
+        }
+#pragma unroll
+        for (int u = 0; u < kHalfBatch; ++u) {
+            float d = 0.f;
+            if (in[u]) {
+                const Term t = policy_term(p, ce[u], old_ce[u], ref[u], adv);
+                d = wf * t.grad;
+                policy += (double)t.policy;
+                kl += (double)t.kl;
+                cut += t.cut ? 1.0 : 0.0;
+            }
+            if (i0 + u * step < end) p.dce[i0 + u * step] = d;
+        }
+    }
+    if (n > 0.0) {
+        sums[1] = fma(w, policy, sums[1]);
+        sums[2] = fma(w, kl, sums[2]);
+        sums[3] = fma(w, cut, sums[3]);
+    }
+}
+
 template <int kSpan>
 __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(const PolicyArgs p) {
     __shared__ Slots slots[2];
@@ -236,59 +318,16 @@ __global__ void __launch_bounds__(threads_of<kSpan>) policy_sequences_kernel(con
     clear_outside(p.seq_start, p.S, p.M, p.dce);
     double sums[kSums] = {};
     int turn = 0;
-    const Walk<kSpan> walk;
-    for (int unit = walk.unit; unit < p.S; unit += walk.units_step) {
-        const int begin = boundary(p.seq_start, unit, p.M), end = boundary(p.seq_start, unit + 1, p.M);
-        const float adv = ld_dep(p.adv + unit);
-        int have = 0;
-        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kBatch * walk.step) {
-            bool in[kBatch];
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) in[u] = i0 + u * walk.step < end && is_counted(p.labels, i0 + u * walk.step, p.V);
-#pragma unroll
-            for (int u = 0; u < kBatch; ++u) have += in[u] ? 1 : 0;
-        }
-        const double n = span_totals<kSpan>((double)have, 0.0, slots, turn).x;
-        const double w = n > 0.0 ? 1.0 / (n * (double)p.S) : 0.0;
-        const float wf = (float)w;
-        double policy = 0.0, kl = 0.0, cut = 0.0;
-        for (long long i0 = (long long)begin + walk.from; i0 < end; i0 += kHalfBatch * walk.step) {
-            float ce[kHalfBatch], old_ce[kHalfBatch], ref[kHalfBatch];
-            bool in[kHalfBatch];
-#pragma unroll
-            for (int u = 0; u < kHalfBatch; ++u) {
-                const long long i = i0 + u * walk.step;
-                ce[u] = i < end ? ld_dep(p.ce + i) : 0.f;
-                old_ce[u] = i < end ? ld_dep(p.old_ce + i) : 0.f;
-                ref[u] = i < end && p.ref_ce ? ld_dep(p.ref_ce + i) : 0.f;
-                in[u] = i < end && is_counted(p.labels, i, p.V);
-            }
-#pragma unroll
-            for (int u = 0; u < kHalfBatch; ++u) {
-                float d = 0.f;
-                if (in[u]) {
-                    const Term t = policy_term(p, ce[u], old_ce[u], ref[u], adv);
-                    d = wf * t.grad;
-                    policy += (double)t.policy;
-                    kl += (double)t.kl;
-                    cut += t.cut ? 1.0 : 0.0;
-                }
-                if (i0 + u * walk.step < end) p.dce[i0 + u * walk.step] = d;
-            }
-        }
-        if (n > 0.0) {
-            sums[1] = fma(w, policy, sums[1]);
-            sums[2] = fma(w, kl, sums[2]);
-            sums[3] = fma(w, cut, sums[3]);
-        }
-    }
+    for_units<kSpan>(
+        p.S, kPolicyHandOver, [&](int unit) { return make_int2(boundary(p.seq_start, unit, p.M), boundary(p.seq_start, unit + 1, p.M)); },
+        [&](auto span, int unit, int2 b, int from, int step) { policy_unit<decltype(span)::value>(p, unit, b.x, b.y, from, step, slots, turn, sums); });
     sums[0] = total_loss(p, sums[1], sums[2]);
     if (kSpan == kClusterSpan) cg::this_cluster().sync();                // nobody leaves while its sums may still be read
     finish<threads_of<kSpan> / 32>(sums, reinterpret_cast<LossSpace*>(p.workspace), p.loss);
 }
 
 // A thread's part of the sum of a sequence's gains, rows first, first + step, .. below end, and which of its first 64 tokens are counted, so that
-// their labels are read once.  (Rows are at most 2^30, so that 32 bits hold every index.)
+// their labels are read once.
 __device__ __forceinline__ double gains(const PreferenceArgs& p, int first, int end, int step, unsigned long long& counted) {
     double sum = 0.0;
     int k = 0;
@@ -327,6 +366,31 @@ __device__ __forceinline__ void put_weights(const PreferenceArgs& p, int first, 
 
 // Pairs of sequences 2u (preferred) and 2u + 1 (rejected).
 template <int kSpan>
+__device__ __forceinline__ void preference_unit(const PreferenceArgs& p, int unit, int begin, int end, int from, int step, Slots (&slots)[2], int& turn,
+                                                double (&sums)[kSums]) {
+    const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin);
+    unsigned long long counted[2];                                       // of the thread's first 64 tokens of each sequence
+    const double first = gains(p, begin + from, middle, step, counted[0]), second = gains(p, middle + from, end, step, counted[1]);
+    const double2 sum = span_totals<kSpan>(first, second, slots, turn);
+    const double good = (double)p.beta * sum.x, bad = (double)p.beta * sum.y;
+    // with t = e^-|m|: -ln sigma(m) = ln(1 + t) + max(-m, 0), and sigma(m) is 1 / (1 + t) or t / (1 + t)
+    const double margin = good - bad;
+    const float m = (float)margin, t = expf(-fabsf(m)), near = 1.f / (1.f + t), far = t * near;
+    const float up = log1pf(t) + fmaxf(-m, 0.f), down = log1pf(t) + fmaxf(m, 0.f);
+    const float slope = p.smoothing * (m >= 0.f ? near : far) - (1.f - p.smoothing) * (m >= 0.f ? far : near);
+    const float d = (float)((double)p.beta * (double)slope * p.share);
+    if (from == 0) {
+        p.margin[unit] = m;
+        sums[0] += (double)((1.f - p.smoothing) * up + (p.smoothing > 0.f ? p.smoothing * down : 0.f));
+        sums[1] += m > 0.f ? 1.0 : 0.0;
+        sums[2] += good;
+        sums[3] += bad;
+    }
+    put_weights(p, begin + from, middle, step, counted[0], -d);
+    put_weights(p, middle + from, end, step, counted[1], d);
+}
+
+template <int kSpan>
 __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const PreferenceArgs p) {
     __shared__ Slots slots[2];
     launch_dependents();
@@ -334,30 +398,13 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
     clear_outside(p.seq_start, 2 * p.P, p.M, p.dce);
     double sums[kSums] = {};
     int turn = 0;
-    const Walk<kSpan> walk;
-    for (int unit = walk.unit; unit < p.P; unit += walk.units_step) {
-        const int begin = boundary(p.seq_start, 2 * unit, p.M);
-        const int middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin), end = max(boundary(p.seq_start, 2 * unit + 2, p.M), middle);
-        unsigned long long counted[2];                                   // of the thread's first 64 tokens of each sequence
-        const double first = gains(p, begin + walk.from, middle, walk.step, counted[0]), second = gains(p, middle + walk.from, end, walk.step, counted[1]);
-        const double2 sum = span_totals<kSpan>(first, second, slots, turn);
-        const double good = (double)p.beta * sum.x, bad = (double)p.beta * sum.y;
-        // with t = e^-|m|: -ln sigma(m) = ln(1 + t) + max(-m, 0), and sigma(m) is 1 / (1 + t) or t / (1 + t)
-        const double margin = good - bad;
-        const float m = (float)margin, t = expf(-fabsf(m)), near = 1.f / (1.f + t), far = t * near;
-        const float up = log1pf(t) + fmaxf(-m, 0.f), down = log1pf(t) + fmaxf(m, 0.f);
-        const float slope = p.smoothing * (m >= 0.f ? near : far) - (1.f - p.smoothing) * (m >= 0.f ? far : near);
-        const float d = (float)((double)p.beta * (double)slope * p.share);
-        if (walk.leads) {
-            p.margin[unit] = m;
-            sums[0] += (double)((1.f - p.smoothing) * up + (p.smoothing > 0.f ? p.smoothing * down : 0.f));
-            sums[1] += m > 0.f ? 1.0 : 0.0;
-            sums[2] += good;
-            sums[3] += bad;
-        }
-        put_weights(p, begin + walk.from, middle, walk.step, counted[0], -d);
-        put_weights(p, middle + walk.from, end, walk.step, counted[1], d);
-    }
+    for_units<kSpan>(
+        p.P, kPreferenceHandOver,
+        [&](int unit) {
+            const int begin = boundary(p.seq_start, 2 * unit, p.M), middle = max(boundary(p.seq_start, 2 * unit + 1, p.M), begin);
+            return make_int2(begin, max(boundary(p.seq_start, 2 * unit + 2, p.M), middle));
+        },
+        [&](auto span, int unit, int2 b, int from, int step) { preference_unit<decltype(span)::value>(p, unit, b.x, b.y, from, step, slots, turn, sums); });
 #pragma unroll
     for (int k = 0; k < kSums; ++k) sums[k] *= p.share;
     if (kSpan == kClusterSpan) cg::this_cluster().sync();
@@ -365,25 +412,26 @@ __global__ void __launch_bounds__(threads_of<kSpan>) preference_kernel(const Pre
 }
 
 // What walks a unit, by the units' average length and their number.  A warp needs no exchange and starts soonest, but takes 10.7 ns for a token of
-// the policy loss and 4.1 of the preference loss, whose two sequences overlap; a CTA takes 1.3 and 0.8, and as more of them queue than SMs, it pays
+// the policy loss and 4.1 of the preference loss, whose two sequences overlap; a CTA takes 1.2 and 0.8, and as more of them queue than SMs, it pays
 // the later the more units there are; a cluster of eight costs 3 us to start and 0.2 us more for every unit.  How far the longest is from the average
 // is on the device and decides as much: the borders are between those of equal units and of units cut at random places (the longest six times the average).
 // Device times, us, equal / random; policy loss:
-//   units of      8: 64 a warp 3.1 / 4.4, a CTA 4.5 / 4.5;  256 5.0 / 10.0, 4.5 / 4.9;   1024 a CTA 5.2 / 7.5, a cluster 7.4 / 7.3;  4096 9.1 / 17.6, 7.8 / 8.0
-//                36: 16 4.3 / 4.7, 4.7 / 4.7;  64 4.7 / 7.1, 4.7 / 4.9;                   2048 6.6 / 16.5, 15.4 / 14.7;  4096 9.3 / 28.8, 15.4 / 15.1
-//               148: 16 4.6 / 4.8, 4.8 / 4.9;  64 4.8 / 6.4, 4.9 / 4.8;                   8192 15 / 45, 41 / 41;  16384 25 / 85, 44 / 46
-//               600: 64 5.1 / 8.6, 8.4 / 8.6;  128 5.7 / 13.5, 8.7 / 9.3         2400: 128 7.9 / 16.3, 14.7 / 15.9;  256 10.7 / 28.1, 17.9 / 19.1
+//   units of      8: 64 a warp 3.3 / 4.6, a CTA 4.3 / 4.5;  256 5.0 / 10.7, 4.5 / 4.7;   1024 a CTA 5.0 / 7.2, a cluster 7.4 / 7.2;  2048 6.1 / 10.2, 7.3 / 7.5
+//                36: 32 4.6 / 5.8, 4.5 / 4.8;  64 4.8 / 7.3, 4.7 / 4.9;                   2048 6.7 / 15.3, 15.2 / 14.8;  4096 8.8 / 26.7, 15.3 / 15.2
+//               148: 64 5.1 / 6.3, 5.0 / 5.2;  128 5.5 / 9.1, 5.1 / 5.3;                  8192 14 / 42, 40 / 40;  16384 24 / 79, 44 / 46
+//               600: 128 5.7 / 11.9, 8.5 / 9.3;  256 6.8 / 18.3, 9.0 / 10.3      2400: 256 10.6 / 20.1, 17.0 / 18.0;  512 15.8 / 27.8, 18.7 / 22.6
 // preference loss:
-//                 8: 128 3.9 / 3.8, 5.6 / 5.6;  512 4.5 / 7.2, 5.7 / 5.6;                 2048 6.2 / 7.6, 8.6 / 8.5;  4096 7.2 / 10.2, 8.8 / 8.7
-//                36: 128 5.5 / 6.2, 5.8 / 5.8;  256 5.5 / 7.3, 5.7 / 5.9;                 4096 7.6 / 15.8, 16.2 / 15.6;  8192 11.0 / 27.2, 16.5 / 16.3
-//               148: 128 5.6 / 6.3, 6.0 / 6.2;  512 6.2 / 10.8, 6.4 / 6.7;                8192 12 / 32, 39 / 38;  32768 54 / 163, 46 / 52
-//               600: 256 5.8 / 10.0, 10.9 / 10.9;  512 6.1 / 15.8, 11.3 / 11.5   2400: 512 8.6 / 16.4, 23.1 / 22.7;  1024 12.0 / 37.2, 24.0 / 25.7
-// One long sequence among very many short ones is walked by what suits the short ones: 2000 of 32 tokens take 6 us, with one of 4096 more 45 (policy)
-// and 21 us (preference), with one of 100000 1.0 and 0.13 ms.
+//                 8: 128 4.1 / 4.3, 5.1 / 5.1;  256 4.3 / 5.5, 5.1 / 5.3;                 2048 5.8 / 7.0, 8.6 / 8.6;  4096 6.6 / 9.2, 8.8 / 8.8
+//                36: 128 5.6 / 6.4, 5.5 / 5.5;  256 5.8 / 7.6, 5.5 / 5.7;                 4096 6.8 / 12.9, 16.0 / 15.2;  8192 9.6 / 21.2, 16.1 / 15.6
+//               148: 256 6.2 / 8.2, 5.8 / 6.0;  512 6.4 / 11.0, 5.9 / 6.2;                16384 15 / 55, 41 / 42;  32768 41 / 131, 47 / 53
+//               600: 512 6.4 / 12.7, 10.8 / 10.9;  1024 8.8 / 24.6, 11.3 / 11.7  2400: 1024 12.3 / 26.1, 23.5 / 24.6;  2048 21.8 / 46.1, 27.9 / 33.4
+// A long unit among many short ones goes from its warp to its CTA (kPolicyHandOver, kPreferenceHandOver): 600 sequences of random lengths around 256 take
+// 18 us instead of 22, 600 pairs around 1024 25 instead of 34, 2000 sequences of 32 tokens with one of 100000 135 instead of 1040 (without it 6).  From a CTA
+// nothing is handed on: 90 sequences of 300 and one of 300000 take 350 us.
 struct Borders {                                 // average lengths from which a CTA or a cluster walks a unit: so many, and so many more for 16 units
     int cta, cta_more, cluster, cluster_more;
 };
-constexpr Borders kPolicyBorders{48, 1, 1024, 1024}, kPreferenceBorders{192, 6, 3072, 1536};
+constexpr Borders kPolicyBorders{48, 3, 1024, 1024}, kPreferenceBorders{160, 12, 3072, 1536};
 
 int span_of(int M, int units, int num_sms, const Borders& b) {
     const long long each = M / units, n = units;
@@ -391,9 +439,9 @@ int span_of(int M, int units, int num_sms, const Borders& b) {
     return each >= b.cta + b.cta_more * n / 16 ? kCtaSpan : kWarpSpan;
 }
 
-// Clusters of sixteen CTAs instead of eight where units are long and few.  Sixteen and eight, equal / random, policy loss: 1 unit of 16384 7.8, 7.6,
-// of 131072 13.7, 20.6; 4 of 32768 9.6 / 12.5, 9.9 / 16.9; 8 of 32768 12.6 / 14.7, 10.5 / 16.1, of 131072 20.6 / 29.1, 23.0 / 43.5; 16 of 32768 18.9 / 20.6,
-// 13.8 / 20.5.  Preference loss: 2 of 32768 9.3 / 9.4, 9.4 / 11.0; 8 of 32768 14.6 / 14.7, 10.3 / 12.2, of 131072 17.1 / 19.4, 17.4 / 26.0.
+// Clusters of sixteen CTAs instead of eight where units are long and few.  Eight and sixteen, equal / random, policy loss: 1 unit of 16384 7.2, 7.4, of
+// 131072 18.6, 12.9; 4 of 32768 9.4 / 15.4, 9.2 / 12.3, of 131072 19 / 43, 14 / 26; 8 of 32768 9.6 / 15.0, 12.7 / 13.6, of 131072 19 / 39, 21 / 25; 12 of 131072
+// 27 / 61, 21 / 37.  Preference loss: 1 of 16384 8.0, 8.6; 4 of 65536 11.7 / 14.4, 10.7 / 12.2; 8 of 32768 10.2 / 12.0, 14.5 / 14.5, of 131072 17 / 26, 17 / 20.
 bool is_wide(int M, int units) { return M / units >= 8192ll * (units + 2); }
 
 // How many clusters of sixteen CTAs of this kernel (`kind`: which of the two it is) the device runs at once; 0 if it cannot.

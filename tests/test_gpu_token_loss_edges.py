@@ -145,3 +145,27 @@ def _batch(rng, M, n, skewed):
         starts = np.concatenate([[0], np.sort(rng.integers(M // 2, M + 1, n - 1)), [M]]).astype(np.int32)
         starts[-2] = starts[-1]
     return V, ce, old, ref, labels, starts
+
+
+@pytest.mark.parametrize("long", [513, 2049, 30000])
+def test_long_units_that_warps_leave_to_their_ctas(ee, long):
+    """Several to a CTA, the last unit of all among them, of ordinary ones of 20 tokens."""
+    rng = np.random.default_rng(long)
+    lengths = np.full(1000, 20)
+    lengths[[0, 3, 5, 6, 500, 999]] = long
+    lengths[[4, 501]] = 0
+    starts = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    V, ce, old, ref, labels, _ = _batch(rng, int(starts[-1]), 1, False)
+    adv = rng.normal(0, 1, 1000).astype(np.float32)
+    forward, lab, at = _forward(ce, labels, V), dev(labels), dev(starts)
+    out = ee.ee_policy_loss(forward, lab, V, dev(old), dev(adv), ref_ce=dev(ref), kl_weight=0.1, seq_start=at)
+    want = oracle.policy_loss(ce, old, adv, labels, V, ref, 0.1, (0.2, 0.2), starts)
+    n = np.maximum([(labels[a:b] >= 0).sum() for a, b in zip(starts[:-1], starts[1:])], 1)
+    size = np.repeat((np.abs(adv) * 5 + 0.5) / (n * 1000.0), lengths)
+    assert (np.abs(_np(out["dce"]) - want["dce"]) <= R * size).all() and np.abs(_np(out["loss"]) - want["loss"]).max() <= R * 10
+    out = ee.ee_preference_loss(forward, lab, V, at, ref_ce=dev(ref))
+    want = oracle.preference_loss(ce, labels, V, starts, ref)
+    m = want["margin"]
+    assert (np.abs(_np(out["margin"]) - m) <= 2.0 ** -23 * np.abs(m) + 1e-9).all()
+    assert (np.abs(_np(out["dce"]) - want["dce"]) <= R * (1 + np.abs(m).max()) * np.abs(want["dce"])).all()
+    assert np.abs(_np(out["loss"]) - want["loss"]).max() <= R * (1 + np.abs(want["loss"]).max() + np.abs(m).max())
