@@ -540,8 +540,8 @@ ee_status ee_exit_head_q4(const void* h, long long ld_h, const float* gamma, con
  * (sums in fp32), same outputs, strides, alignment and rules; a row whose y is not finite has an entropy that is not a number and, as
  * with the other heads where no logit is a number, the argmax 2^31 - 1, which is no index into the vocabulary.  The packed head, gamma and beta
  * are data of the stream (they may be written right before the call).  M up to 2^30; up to 64 rows are one pass over the packed weights.
- * V = 50304, single calls in a graph, bf16 head / 4-bit whole numbers in groups of 64 / this in groups of 16, us: 8 rows of 1024 24.7 / 17.8 / 11.4,
- * 64 of 1024 25.1 / 28.3 / 15.6, 256 of 1024 31.4 / 101.6 / 25.6, 64 of 2560 48.7 / 49.4 / 22.0, 16384 of 2560 2600 / - / 1100.
+ * V = 50304, single calls in a graph, bf16 head / 4-bit whole numbers in groups of 64 / this in groups of 16, us: 8 rows of 1024 23.8 / 17.5 / 11.6,
+ * 64 of 1024 24.7 / 28.0 / 15.6, 256 of 1024 30.2 / 100.8 / 23.3, 64 of 2560 48.8 / 49.3 / 21.3, 16384 of 2560 2630 / - / 960 to 1380.
  * Workspace: ee_exit_head_fp4_workspace_bytes(M, d, V, group), 256-byte aligned, initialised once with ee_workspace_init; it serves fewer rows
  * as well.  M = 0 is a no-op.
  */
@@ -573,8 +573,9 @@ ee_status ee_exit_head_fp4(const void* h, long long ld_h, const float* gamma, co
  *   loss fp32 [4]: means over the pairs of that, of whether m > 0, of the preferred and of the rejected sequences' rewards
  *   0 <= beta, 0 <= smoothing <= 1
  * ce, old_ce, ref_ce, dce fp32 [M], labels int32 [M].  Rows outside all sequences get dce = 0.  The means and sums are added up in fp64 in a
- * fixed order.  0 <= M <= 2^30, 1 <= S, P <= 2^29.  One launch.  Workspace: ee_token_loss_workspace_bytes(), 256-byte aligned, initialised once with
- * ee_workspace_init.
+ * fixed order; exponentials are fp32 and infinite from an argument of 88.7 on (r a is 0 for a = 0 all the same).  0 <= M <= 2^30, 1 <= S, P <= 2^29.
+ * One launch, made for lengths within some ten times of their average: one sequence of 300000 tokens among 90 of 300 takes it 350 us.
+ * Workspace: ee_token_loss_workspace_bytes(), 256-byte aligned, initialised once with ee_workspace_init.
  */
 size_t    ee_token_loss_workspace_bytes(void);
 ee_status ee_policy_loss(const float* ce, const float* old_ce, const float* ref_ce, const float* adv, const int* labels, int M, int V,
@@ -590,8 +591,8 @@ ee_status ee_preference_loss(const float* ce, const float* ref_ce, const int* la
  *   ee_grad_clip:  out = round(g * min(1, max_norm / (norm[0] + 1e-6))) in the tensor's type; `out` NULL: in place, where nothing is written if the
  *                  factor is 1.  A norm that is not a number makes everything that.
  * The tensors (a HOST array of at most 2^29; contiguous, n >= 0 elements of the type, aligned to it, at most 2^36 elements each) must not
- * overlap; norm is fp32 [1] on the device, so that a sum over several GPUs may be put in between.  out is a HOST array of pointers, one per tensor, aligned alike; an out equal to its
- * tensor is that tensor in place.  Tensors that begin on a 16-byte border are accessed by 16 bytes.  The arrays are read before the call
+ * overlap; norm is fp32 [1] on the device, so that a sum over several GPUs may be put in between.  out is a HOST array of pointers, one per
+ * tensor, aligned alike; an out equal to its tensor is that tensor in place, any other overlaps none of them.  Tensors that begin on a 16-byte border are accessed by 16 bytes.  The arrays are read before the call
  * returns; up to 512 tensors are one launch of each call.  Workspace of the norm: ee_grad_norm_workspace_bytes(n_tensors) (0 if that is out of range),
  * 256-byte aligned, initialised once with ee_workspace_init.
  */
